@@ -1,0 +1,634 @@
+"""The 4-bit KV cache and the eviction of tokens, as measured work.
+
+A case names one kind of call and its sizes:
+
+  append  kv4_append, then kv4_read of the same rows
+  attend  kv4_attention, with or without overlap branches
+  mass    attention_mass (bf16 keys) or kv4_attention_mass
+  evict   evict_tokens (bf16 cache), or kv4_evict_tokens and kv4_read of what is left
+
+The ragged structure of a batch (context lengths, rows, page table) follows
+from the case (its ``layout`` number), the tensors' values from the seed.
+
+4-bit cache.  A block holds 16 tokens of one KV head in 17 D bytes: K codes
+[16][D/2], K scales [16][D/32], V codes [16][D/2], V scales [16][D/32].  An
+element is sign and one of 0, .5, 1, 1.5, 2, 3, 4, 6 (even elements in the low
+four bits), times 2^(b - 127) with the scale byte b of its 32 elements: b is
+the biased exponent of the largest magnitude, one more from 1.75 of its power
+of two on, less 2, within 1 .. 252.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+PAGE = 16
+_POOL_SPARE = 8  # pool pages that no request owns
+_GRID = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def _case(name, kind, requests, ctx, heads, layout, *, cache="kv4", verify="0", draft="0", branches=False,
+          counted=False, decay=1.0, keep=0.0, sink=0, recent=0):
+    c = dict(kind=kind, requests=requests, ctx_min=ctx[0], ctx_max=ctx[1], q_heads=heads[0], kv_heads=heads[1],
+             head_dim=heads[2], cache=cache, layout=layout)
+    if kind == "evict":
+        c.update(keep=keep, sink=sink, recent=recent)
+    else:
+        c.update(verify=verify, draft=draft)
+    if kind == "attend":
+        c.update(branches=branches)
+    if kind == "mass":
+        c.update(counted=counted, decay=decay)
+    return dict(name=name, **c) if name else c
+
+
+_8B = (32, 8, 128)
+
+
+def listed():
+    return [
+        # The rows of one step at full concurrency, small blocks: a short call per layer.
+        _case("append_step_128", "append", 128, (512, 4096), _8B, 0, verify="2,2,2,2,4,4,4,8,8,16",
+              draft="2,2,2,2,4,4,4,8,8,16"),
+        # Prompts written at once, one of them behind a cached prefix that ends inside a page.
+        _case("append_prompts", "append", 4, (0, 1001), _8B, 0, verify="4096,8191,16384", draft="0"),
+        # One user, one token at a time: latency counts.
+        _case("attend_token", "attend", 1, (4096, 4096), _8B, 0, verify="1", draft="0"),
+        # A small server's draft-verify step with overlap branches.
+        _case("attend_overlap_16", "attend", 16, (1024, 8192), _8B, 0, verify="4,8,16", draft="4,8,16", branches=True),
+        # A smaller backbone at 48 requests, odd lengths and blocks.
+        _case("attend_d64", "attend", 48, (257, 6001), (16, 4, 64), 1, verify="1,3,7,13", draft="3,5,11,16"),
+        # Long documents, what a 4-bit cache is for: the largest case.
+        _case("attend_long", "attend", 40, (8192, 32768), _8B, 0, verify="4,8,16,32", draft="4,8,16,32"),
+        # After a step's verification: the accepted rows' weights on a bf16 cache, with decay.
+        _case("mass_step_16", "mass", 16, (1024, 8192), _8B, 0, cache="bf16", verify="4,8,16,32", draft="4,8,16",
+              counted=True, decay=0.98),
+        # The same on the 4-bit cache of long documents.
+        _case("mass_long", "mass", 40, (8192, 32768), _8B, 0, verify="4,8,16,32", draft="0", counted=True),
+        # A chunk of prompts: many rows a key, bound by the products.
+        _case("mass_prompt", "mass", 2, (1500, 3001), _8B, 0, cache="bf16", verify="2048,1555", draft="0", decay=0.0),
+        # One user whose cache is held at its budget, a block of tokens over it: latency counts.
+        _case("evict_block", "evict", 1, (4128, 4128), _8B, 0, cache="bf16", keep=0.9923, sink=4, recent=256),
+        # A small server frees a quarter of its cache.
+        _case("evict_16", "evict", 16, (1024, 8192), _8B, 0, cache="bf16", keep=0.75, sink=4, recent=128),
+        # Long documents in 4 bits cut to half, the rest read out.
+        _case("evict_long", "evict", 40, (8192, 32768), _8B, 0, keep=0.5, sink=16, recent=1024),
+    ]
+
+
+_HEADS = (_8B, _8B, (16, 4, 64), (8, 8, 64), (24, 8, 128), (14, 2, 64), (16, 1, 128))
+_ROWS = ("1", "1", "4,8,16,32", "2,2,2,2,4,4,4,8,8,16", "16", "1,3,7,13")
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(("append", "attend", "attend", "attend", "mass", "mass", "evict", "evict"))
+    heads, lay = rng.choice(_HEADS), rng.randrange(1 << 20)
+    hi = _log_int(rng, 64, 32768)
+    ctx = (max(1, int(hi * rng.uniform(0.1, 1.0))), hi)
+    R = _log_int(rng, 1, 160)
+    if kind == "append":
+        rows = rng.choice(_ROWS + ("%d" % _log_int(rng, 1, 8192),))
+        case = _case("", kind, R, (0, 3000), heads, lay, verify=rows, draft=rng.choice(_ROWS + ("0",)))
+    elif kind == "attend":
+        case = _case("", kind, R, ctx, heads, lay, verify=rng.choice(_ROWS), draft=rng.choice(_ROWS + ("0", "0")),
+                     branches=rng.random() < 0.3)
+    elif kind == "mass":
+        rows = rng.choice(_ROWS + ("%d" % _log_int(rng, 1, 2048),))
+        case = _case("", kind, R, ctx, heads, lay, cache=rng.choice(("bf16", "kv4")), verify=rows,
+                     draft=rng.choice(("0", "5", "16")), counted=rng.random() < 0.5, decay=rng.choice((1.0, 0.98, 0.0)))
+    else:
+        # sink and recent fit the smallest request's share
+        keep = rng.uniform(0.2, 0.99)
+        room = int(ctx[0] * keep)
+        sink = rng.randint(0, min(16, room))
+        case = _case("", kind, R, ctx, heads, lay, cache=rng.choice(("bf16", "kv4")), keep=round(keep, 3), sink=sink,
+                     recent=rng.randint(0, max(0, (room - sink) // 2)))
+    cap = [work(c) for c in listed() if c["kind"] == kind]
+    cap = {k: max(w[k] for w in cap) for k in ("bytes", "flops")}
+    while case["requests"] > 1:
+        w = work(case)
+        s = _structure(case)
+        padded = case["requests"] * case["q_heads"] * int(s["T"].max()) * int(max(1, s["n"].max()))
+        if w["bytes"] <= cap["bytes"] and w["flops"] <= cap["flops"] and (kind in ("append", "evict") or padded < 1.3e9):
+            break
+        case["requests"] = case["requests"] * 2 // 3
+    return case
+
+
+# ---------------------------------------------------------------------------
+# Structure of a case
+def _pick(rng, text, n):
+    return rng.choice(np.array([int(x) for x in text.split(",")]), size=n)
+
+
+def _prefix(x):
+    return np.concatenate([[0], np.cumsum(x)]).astype(np.int64)
+
+
+def _structure(case):
+    """Host arrays of the batch: ctx, nv, nd, n, T per request, the page
+    table, and per request its branches as (kept verify rows, lead, rows)."""
+    rng = np.random.default_rng([0x6B763431, case["layout"], case["requests"]])
+    R = case["requests"]
+    ctx = rng.integers(case["ctx_min"], case["ctx_max"] + 1, R)
+    nv = _pick(rng, case.get("verify", "0"), R)
+    nd = _pick(rng, case.get("draft", "0"), R)
+    br = None
+    if case.get("branches"):
+        # two corrections and a continuation, as an overlap round prepares them
+        br = []
+        for v, b in zip(nv, nd):
+            at = sorted(int(p) for p in rng.choice(int(v), size=min(2, int(v)), replace=False))
+            br.append([(p, 1, 1 + int(b)) for p in at] + ([(int(v), 0, int(b))] if b else []))
+        nd = np.array([sum(x[2] for x in one) for one in br])
+    n = nv + nd
+    T = ctx + n
+    pages = (T + PAGE - 1) // PAGE
+    indptr = _prefix(pages)
+    num_pages = int(indptr[-1]) + _POOL_SPARE
+    indices = rng.permutation(num_pages)[:int(indptr[-1])]
+    s = dict(ctx=ctx, nv=nv, nd=nd, n=n, T=T, q_indptr=_prefix(n), page_indptr=indptr, page_indices=indices,
+             num_pages=num_pages, branches=br)
+    if case["kind"] == "evict":
+        s["keep"] = np.maximum((ctx * case["keep"]).astype(np.int64), case["sink"] + case["recent"])
+        s["left"] = np.minimum(ctx, s["keep"])
+    return s
+
+
+def _sees(s):
+    """Per request and row: keys below lim, and keys lo .. hi - 1, are seen."""
+    out = []
+    for r in range(len(s["ctx"])):
+        L, V, n = int(s["ctx"][r]), int(s["nv"][r]), int(s["n"][r])
+        rows = [(L + i + 1, 0, 0) for i in range(V)]
+        at = L + V
+        for prefix, lead, m in (s["branches"][r] if s["branches"] else [(V, 0, n - V)]):
+            rows += [(L + prefix, at, at + (t + 1 if t < lead else m)) for t in range(m)]
+            at += m
+        out.append(np.array(rows, dtype=np.int64).reshape(n, 3))
+    return out
+
+
+def _token_bytes(case):
+    """Bytes of one token's K (or V) of one head."""
+    return case["head_dim"] * 2 if case["cache"] == "bf16" else case["head_dim"] * 17 // 32
+
+
+def work(case):
+    s = _structure(case)
+    hq, hkv, d = case["q_heads"], case["kv_heads"], case["head_dim"]
+    rows, table = int(s["n"].sum()), int(s["page_indptr"][-1]) * 4
+    if case["kind"] == "append":
+        # rows in as bf16 and out as bf16; codes and scales out and in
+        return dict(bytes=rows * hkv * 2 * (4 * d + 2 * d * 17 / 32) + 2 * table, flops=rows * hkv * d * 2 * 4)
+    if case["kind"] == "attend":
+        seen = sum(int((x[:, 0] + x[:, 2] - x[:, 1]).sum()) for x in _sees(s))
+        return dict(bytes=int(s["T"].sum()) * hkv * 2 * _token_bytes(case) + rows * hq * (4 * d + 4) + table,
+                    flops=4 * d * hq * seen)
+    if case["kind"] == "mass":
+        count = _counts(case, s)
+        keys = s["ctx"] + s["nv"]
+        seen = int((count * s["ctx"] + count * (count + 1) // 2).sum())
+        return dict(bytes=int(keys.sum()) * hkv * (_token_bytes(case) + 4) + int(count.sum()) * hq * (2 * d + 4) + table +
+                    (int(s["ctx"].sum()) * hkv * 4 if case["decay"] else 0), flops=2 * d * hq * seen)
+    L, left = s["ctx"], s["left"]
+    moved = float((left * (L - left) / L).sum()) * hkv  # as often as a place is evicted below what is left
+    bytes_ = float(L.sum()) * hkv * 4 + moved * (4 * _token_bytes(case) + 8) + float(left.sum()) * hkv * 4 + table
+    if case["cache"] == "kv4":
+        bytes_ += float(left.sum()) * hkv * 2 * (_token_bytes(case) + 2 * d)
+    return dict(bytes=bytes_, flops=float(L.sum()) * hkv * 4)
+
+
+def _counts(case, s):
+    """Rows of each request whose weights count: all, or the accepted ones."""
+    if not case.get("counted"):
+        return s["nv"].astype(np.int64)
+    rng = np.random.default_rng([case["layout"], 77])
+    return rng.integers(0, s["nv"] + 1)
+
+
+# ---------------------------------------------------------------------------
+# Inputs
+def _dev():
+    return torch.device("cuda")
+
+
+def _i64(a):
+    return torch.as_tensor(np.ascontiguousarray(a), dtype=torch.int64, device=_dev())
+
+
+def _i32(a):
+    return torch.as_tensor(np.ascontiguousarray(a), dtype=torch.int32, device=_dev())
+
+
+def _normal(gen, shape, std=1.0):
+    return (torch.randn(shape, generator=gen, device=_dev()) * std).to(torch.bfloat16)
+
+
+def _cache4(gen, pages, hkv, d):
+    """A 4-bit pool: any codes, scales that give values of about unit size."""
+    pool = torch.empty(pages, hkv, 17 * d, dtype=torch.uint8, device=_dev())
+    pool.random_(0, 256, generator=gen)
+    for at in (8 * d, 8 * d + d // 2 + 8 * d):
+        scale = pool[:, :, at:at + d // 2]
+        scale.copy_((scale & 1) + 125)  # 2^-2 or 2^-1
+    return pool
+
+
+def _inputs(case, seed):
+    """The tensors of a case that follow from the seed."""
+    s = _structure(case)
+    gen = torch.Generator(device=_dev()).manual_seed(seed)
+    hq, hkv, d = case["q_heads"], case["kv_heads"], case["head_dim"]
+    rows, pages = int(s["n"].sum()), s["num_pages"]
+    x = {}
+    if case["kind"] == "append":
+        # K with channels of different size, as models have them; rows of a fused projection
+        qkv = torch.randn(rows, hq + 2 * hkv, d, generator=gen, device=_dev())
+        qkv *= torch.exp(0.7 * torch.randn(1, hq + 2 * hkv, d, generator=gen, device=_dev()))
+        qkv = qkv.to(torch.bfloat16)
+        x["k"], x["v"] = qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+        x["cache"] = torch.zeros(pages, hkv, 17 * d, dtype=torch.uint8, device=_dev())
+        return s, x
+    if case["cache"] == "kv4":
+        x["cache"] = _cache4(gen, pages, hkv, d)
+    else:
+        x["k_cache"] = _normal(gen, (pages, hkv, PAGE, d))
+        if case["kind"] == "evict":
+            x["v_cache"] = _normal(gen, (pages, hkv, d, PAGE))
+    pool = (pages, hkv, PAGE)
+    if case["kind"] in ("attend", "mass"):
+        x["q"] = _normal(gen, (rows, hq, d))
+    if case["kind"] == "mass":
+        count = _counts(case, s)
+        x["row_count"] = _i32(count) if case["counted"] else None
+        # what the attention of such rows returns: about log(keys) + half the scores' variance
+        keys = np.concatenate([x_[:, 0] + x_[:, 2] - x_[:, 1] for x_ in _sees(s)])
+        var = 1.0 if case["cache"] == "bf16" else 1.25
+        x["lse"] = (torch.as_tensor(np.log(keys) + 0.5 * var, dtype=torch.float32, device=_dev())[:, None] +
+                    0.1 * torch.randn(rows, hq, generator=gen, device=_dev()))
+        x["mass"] = torch.rand(pool, generator=gen, device=_dev())
+    if case["kind"] == "evict":
+        # heavy-tailed weights, some of them zero
+        w = torch.exp(2.0 * torch.randn(pool, generator=gen, device=_dev()))
+        x["score"] = torch.where(torch.rand(pool, generator=gen, device=_dev()) < 0.1, 0.0, w)
+        x["mass"] = x["score"].clone()
+        x["positions"] = torch.zeros(pool, dtype=torch.int32, device=_dev())
+    return s, x
+
+
+def prepare(case, seed):
+    s, x = _inputs(case, seed)
+    st = dict(x, case=case, heads=(case["q_heads"], case["kv_heads"], case["head_dim"]))
+    if own:
+        _prepare_own(case, s, st)
+        return st
+    # the page table as rectangles, and the rows' and tokens' places in them
+    R, P = case["requests"], int(np.diff(s["page_indptr"]).max())
+    table = np.zeros((R, P), dtype=np.int64)
+    for r in range(R):
+        own_pages = s["page_indices"][s["page_indptr"][r]:s["page_indptr"][r + 1]]
+        table[r, :len(own_pages)] = own_pages
+    st["table"] = _i64(table)
+
+    def places(first, count):  # (request, place) of `count` places from `first` on
+        req = np.repeat(np.arange(R), count)
+        return _i64(req), _i64(np.arange(int(count.sum())) - np.repeat(_prefix(count)[:-1], count) + np.repeat(first, count))
+
+    zero = np.zeros(R, dtype=np.int64)
+    if case["kind"] == "append":
+        st["token"] = places(s["ctx"], s["n"])
+    elif case["kind"] == "attend":
+        st["row"] = places(zero, s["n"])
+        st["sees"] = _i64(np.concatenate(_sees(s)))
+        st["rows"] = int(s["n"].max())
+    elif case["kind"] == "mass":
+        count = _counts(case, s)
+        st["row"] = places(zero, count)
+        st["row_at"] = _i64(s["q_indptr"][:-1])
+        st["token"] = places(zero, s["ctx"] + s["nv"])
+        st["ctx"] = _i64(s["ctx"])
+        st["rows"] = int(max(1, count.max()))
+    else:
+        st["token"] = places(zero, s["left"])
+        st["ctx"], st["keep"] = _i64(s["ctx"]), _i64(s["left"])
+    return st
+
+
+def _prepare_own(case, s, st):
+    """What a serving program keeps for a batch: its layout, workspace and output buffers."""
+    from paper_2609_34388_amd import binding
+
+    hq, hkv, d = st["heads"]
+    pages = _i32(s["page_indices"])
+    if case["kind"] == "evict":
+        cache = st["cache"] if case["cache"] == "kv4" else st["k_cache"]
+        st["layout"] = binding.make_evict_layout(cache, s["ctx"], s["keep"], s["page_indptr"], pages,
+                                                 sink=case["sink"], recent=case["recent"])
+        st["workspace"] = binding.new_workspace(binding.evict_workspace_bytes(st["layout"]), _dev())
+        if case["cache"] == "bf16":
+            return
+        zero = np.zeros(case["requests"], dtype=np.int32)
+        st["kept"] = binding.make_kv4_layout(hq, cache, _prefix(s["left"]), zero, zero, s["page_indptr"], pages)
+        rows = int(s["left"].sum())
+    else:
+        args = (s["q_indptr"], s["nv"], s["ctx"], s["page_indptr"], pages)
+        if case["cache"] == "kv4":
+            st["layout"] = binding.make_kv4_layout(hq, st["cache"], *args)
+        else:
+            st["layout"] = binding.make_layout(st["q"], st["k_cache"], *args)
+        rows = int(s["n"].sum())
+    if case["kind"] == "attend":
+        st["branches"] = None
+        if s["branches"]:
+            flat = [b for one in s["branches"] for b in one]
+            st["branches"] = binding.make_branches(_prefix([len(one) for one in s["branches"]]),
+                                                   *([b[i] for b in flat] for i in range(3)))
+        need = binding.kv4_attention_workspace_bytes(st["layout"], st["branches"])
+        st["workspace"] = binding.new_workspace(need, _dev()) if need else None
+        st["out"] = torch.empty_like(st["q"])
+        st["lse"] = torch.empty(rows, hq, dtype=torch.float32, device=_dev())
+    if case["kind"] in ("append", "evict"):
+        st["k_out"] = torch.empty(rows, hkv, d, dtype=torch.bfloat16, device=_dev())
+        st["v_out"] = torch.empty_like(st["k_out"])
+
+
+# ---------------------------------------------------------------------------
+# One pass
+def run(state):
+    kind = state["case"]["kind"]
+    if own:
+        return _OWN[kind](state)
+    return _PLAIN[kind](state)
+
+
+def _own_append(st):
+    from paper_2609_34388_amd import binding
+
+    binding.kv4_append(st["k"], st["v"], st["cache"], st["layout"])
+    k, v = binding.kv4_read(st["cache"], st["layout"], k_out=st["k_out"], v_out=st["v_out"])
+    return dict(k=k, v=v)
+
+
+def _own_attend(st):
+    from paper_2609_34388_amd import binding
+
+    out, lse = binding.kv4_attention(st["q"], st["cache"], st["layout"], st["branches"], out=st["out"], lse=st["lse"],
+                                     workspace=st["workspace"])
+    return dict(out=out, lse=lse)
+
+
+def _own_mass(st):
+    from paper_2609_34388_amd import binding
+
+    c = st["case"]
+    if c["cache"] == "kv4":
+        binding.kv4_attention_mass(st["q"], st["cache"], st["lse"], st["mass"], st["layout"],
+                                   row_count=st["row_count"], decay=c["decay"])
+    else:
+        binding.attention_mass(st["q"], st["k_cache"], st["lse"], st["mass"], st["layout"],
+                               row_count=st["row_count"], decay=c["decay"])
+    return dict(mass=st["mass"])
+
+
+def _own_evict(st):
+    from paper_2609_34388_amd import binding
+
+    res = dict(mass=st["mass"], positions=st["positions"])
+    if st["case"]["cache"] == "kv4":
+        binding.kv4_evict_tokens(st["cache"], st["score"], st["positions"], st["layout"], mass=st["mass"],
+                                 workspace=st["workspace"])
+        k, v = binding.kv4_read(st["cache"], st["kept"], k_out=st["k_out"], v_out=st["v_out"])
+        return dict(res, k=k, v=v)
+    binding.evict_tokens(st["k_cache"], st["v_cache"], st["score"], st["positions"], st["layout"], mass=st["mass"],
+                         workspace=st["workspace"])
+    return dict(res, k_cache=st["k_cache"], v_cache=st["v_cache"])
+
+
+_OWN = dict(append=_own_append, attend=_own_attend, mass=_own_mass, evict=_own_evict)
+
+
+# ---------------------------------------------------------------------------
+# The same in elementary torch operations
+def _encode(x):
+    """Codes [.., D/2] and scale bytes [.., D/32] of bf16 rows."""
+    d = x.shape[-1]
+    g = x.float().reshape(*x.shape[:-1], d // 32, 32)
+    top = (g.abs().amax(-1).to(torch.bfloat16).view(torch.int16).to(torch.int32) + 0x20) >> 7
+    b = (top - 2).clamp(1, 252)
+    y = g.abs() / (b << 23).view(torch.float32)[..., None]
+    code = (y > 0.25).int() + (y >= 0.75) + (y > 1.25) + (y >= 1.75) + (y > 2.5) + (y >= 3.5) + (y > 5.0)
+    code = (code + 8 * torch.signbit(g)).reshape(*x.shape[:-1], d // 2, 2)
+    return (code[..., 0] + 16 * code[..., 1]).to(torch.uint8), b.to(torch.uint8)
+
+
+def _decode(code, scale):
+    grid = torch.tensor(_GRID, device=code.device)
+    grid = torch.cat([grid, -grid])
+    c = torch.stack([code & 15, code >> 4], -1).long()
+    x = grid[c].reshape(*scale.shape, 32)
+    return (x * (scale.to(torch.int32) << 23).view(torch.float32)[..., None]).reshape(*code.shape[:-1], -1)
+
+
+def _parts(pool, d):
+    """Views of a 4-bit pool: K codes, K scales, V codes, V scales, each [.., 16, bytes of a token]."""
+    cut, at, out = (8 * d, d // 2, 8 * d, d // 2), 0, []
+    for c in cut:
+        out.append(pool[..., at:at + c].unflatten(-1, (PAGE, c // PAGE)))
+        at += c
+    return out
+
+
+def _rect(pages):
+    """[R, pages, Hkv, 16, ..] as [R, Hkv, tokens, ..]."""
+    return pages.movedim(2, 1).flatten(2, 3)
+
+
+def _plain_append(st):
+    d = st["heads"][2]
+    req, tok = st["token"]
+    page, slot = st["table"][req, tok // PAGE], tok % PAGE
+    for part, data in zip(_parts(st["cache"], d), (*_encode(st["k"]), *_encode(st["v"]))):
+        part[page, :, slot] = data
+    kc, ks, vc, vs = (p[page, :, slot] for p in _parts(st["cache"], d))
+    return dict(k=_decode(kc, ks).to(torch.bfloat16), v=_decode(vc, vs).to(torch.bfloat16))
+
+
+def _scores(st, q, keys):
+    """Scaled scores [R, Hkv, rows, g, tokens] of padded rows q [R, rows, Hq, D]."""
+    hq, hkv, d = st["heads"]
+    R, n = q.shape[:2]
+    q = q.float().unflatten(2, (hkv, hq // hkv)).movedim(1, 2).reshape(R * hkv, n * (hq // hkv), d)
+    k = keys.flatten(0, 1).transpose(1, 2).contiguous()
+    return torch.bmm(q, k).mul_(1.0 / math.sqrt(d)).reshape(R, hkv, n, hq // hkv, -1)
+
+
+def _plain_attend(st):
+    hq, hkv, d = st["heads"]
+    req, row = st["row"]
+    R = st["table"].shape[0]
+    kc, ks, vc, vs = _parts(st["cache"][st["table"]], d)
+    keys, values = _rect(_decode(kc, ks)), _rect(_decode(vc, vs))
+    q = st["q"].new_zeros(R, st["rows"], hq, d)
+    q[req, row] = st["q"]
+    sees = torch.zeros(R, st["rows"], 3, dtype=torch.int64, device=q.device)
+    sees[req, row] = st["sees"]
+    j = torch.arange(keys.shape[2], device=q.device)
+    hide = ~((j < sees[..., :1]) | ((j >= sees[..., 1:2]) & (j < sees[..., 2:])))
+    s = _scores(st, q, keys).masked_fill_(hide[:, None, :, None], -math.inf)
+    top = s.amax(-1, keepdim=True).clamp(min=torch.finfo(torch.float32).min)
+    p = s.sub_(top).exp_()
+    z = p.sum(-1, keepdim=True)
+    out = torch.bmm(p.reshape(R * hkv, -1, p.shape[-1]), values.flatten(0, 1)).reshape(R, hkv, st["rows"], hq // hkv, d) / z
+    out = out.movedim(2, 1).flatten(2, 3)[req, row]
+    lse = (top + z.log())[..., 0].movedim(2, 1).flatten(2, 3)[req, row]
+    return dict(out=out.to(torch.bfloat16), lse=lse)
+
+
+def _plain_mass(st):
+    hq, hkv, d = st["heads"]
+    case = st["case"]
+    req, row = st["row"]
+    R = st["table"].shape[0]
+    if case["cache"] == "kv4":
+        kc, ks, _, _ = _parts(st["cache"][st["table"]], d)
+        keys = _rect(_decode(kc, ks))
+    else:
+        keys = _rect(st["k_cache"][st["table"]]).float()
+    at = st["row_at"][req] + row
+    q = st["q"].new_zeros(R, st["rows"], hq, d)
+    q[req, row] = st["q"][at]
+    lse = st["lse"].new_full((R, st["rows"], hq), math.inf)  # rows that do not count weigh nothing
+    lse[req, row] = st["lse"][at]
+    lse = lse.unflatten(2, (hkv, hq // hkv)).movedim(1, 2)
+    j = torch.arange(keys.shape[2], device=q.device)
+    last = st["ctx"][:, None] + torch.arange(st["rows"], device=q.device)
+    s = _scores(st, q, keys).masked_fill_((j > last[..., None])[:, None, :, None], -math.inf)
+    w = s.sub_(lse[..., None]).exp_().sum((2, 3))
+    req, tok = st["token"]
+    page, slot = st["table"][req, tok // PAGE], tok % PAGE
+    new = w[req, :, tok]
+    if case["decay"]:
+        new = new + torch.where((tok < st["ctx"][req])[:, None], case["decay"] * st["mass"][page, :, slot], 0.0)
+    st["mass"][page, :, slot] = new
+    return dict(mass=st["mass"])
+
+
+def _plain_evict(st):
+    hq, hkv, d = st["heads"]
+    case = st["case"]
+    score = _rect(st["score"][st["table"]])  # [R, Hkv, tokens]
+    j = torch.arange(score.shape[2], device=score.device)
+    L, keep = st["ctx"][:, None, None], st["keep"][:, None, None]
+    safe = (j < case["sink"]) | (j >= L - case["recent"])
+    key = torch.where(safe, math.inf, score).masked_fill(j >= L, -math.inf)
+    order = key.sort(dim=-1, descending=True, stable=True)[1]
+    kept = torch.zeros_like(key, dtype=torch.bool).scatter_(2, order, (j < keep).expand_as(order))
+    hole, mover = ~kept & (j < keep), kept & (j >= keep)
+    # the k-th hole takes the k-th token kept from behind
+    nth = torch.where(mover, mover.cumsum(-1) - 1, score.shape[2])
+    source = torch.zeros(*score.shape[:2], score.shape[2] + 1, dtype=torch.int64, device=score.device)
+    source.scatter_(2, nth, j.expand_as(nth))
+    source = torch.where(hole, source.gather(2, (hole.cumsum(-1) - 1).clamp(min=0)), j)
+    req, tok = st["token"]
+    src = source[req, :, tok]  # [kept tokens, Hkv]
+    head = torch.arange(hkv, device=src.device)
+    to_page, to_slot = st["table"][req, tok // PAGE], tok % PAGE
+    from_page, from_slot = st["table"][req[:, None], src // PAGE], src % PAGE
+    st["mass"][to_page, :, to_slot] = st["mass"][from_page, head, from_slot]
+    st["positions"][to_page, :, to_slot] = src.int()
+    res = dict(mass=st["mass"], positions=st["positions"])
+    if case["cache"] == "bf16":
+        st["k_cache"][to_page, :, to_slot] = st["k_cache"][from_page, head, from_slot]
+        st["v_cache"][to_page, :, :, to_slot] = st["v_cache"][from_page, head, :, from_slot]
+        return dict(res, k_cache=st["k_cache"], v_cache=st["v_cache"])
+    for part in _parts(st["cache"], d):
+        part[to_page, :, to_slot] = part[from_page, head, from_slot]
+    kc, ks, vc, vs = (p[to_page, :, to_slot] for p in _parts(st["cache"], d))
+    return dict(res, k=_decode(kc, ks).to(torch.bfloat16), v=_decode(vc, vs).to(torch.bfloat16))
+
+
+_PLAIN = dict(append=_plain_append, attend=_plain_attend, mass=_plain_mass, evict=_plain_evict)
+
+
+# ---------------------------------------------------------------------------
+# The same outputs in 64 bits
+def _exact_held(x):
+    """What the cache stands for after rows x went in."""
+    g = x.double().reshape(*x.shape[:-1], -1, 32)
+    frac, e = torch.frexp(g.abs().amax(-1, keepdim=True))  # 0.5 <= frac < 1
+    e = (e - 3 + (frac >= 0.875)).clamp(-126, 125)
+    y = torch.ldexp(g, -e)
+    a = y.abs()
+    a = torch.where(a < 2, (a * 2).round() / 2, torch.where(a < 4, a.round(), (a / 2).round() * 2)).clamp(max=6)
+    return torch.ldexp(a * y.sign(), e).reshape(x.shape)
+
+
+def _exact_tokens(block, d, which):
+    """K (which = 0) or V (1) of whole blocks [pages, 17 D] as [tokens, D]."""
+    half = 8 * d + d // 2
+    block = block[:, which * half:(which + 1) * half]
+    code = block[:, :8 * d].reshape(-1, d // 2).to(torch.int64)
+    nib = torch.empty(code.shape[0], d, dtype=torch.int64, device=code.device)
+    nib[:, 0::2], nib[:, 1::2] = code % 16, torch.div(code, 16, rounding_mode="floor")
+    mag, exp = nib % 2, torch.div(nib % 8, 2, rounding_mode="floor")
+    val = torch.where(exp == 0, mag * 0.5, (1 + 0.5 * mag) * torch.exp2((exp - 1).double()))
+    val = torch.where(nib >= 8, -val, val)
+    scale = torch.exp2(block[:, 8 * d:].reshape(-1, d // 32).double() - 127)
+    return (val.reshape(-1, d // 32, 32) * scale[..., None]).reshape(-1, d)
+
+
+def _exact_keys(case, x, pages, h, T):
+    d = case["head_dim"]
+    if case["cache"] == "bf16":
+        return x["k_cache"][pages, h].reshape(-1, d)[:T].double()
+    return _exact_tokens(x["cache"][pages, h], d, 0)[:T]
+
+
+def exact(case, seed):
+    kind = case["kind"]
+    if kind == "evict":
+        return None  # moves values, computes none
+    s, x = _inputs(case, seed)
+    if kind == "append":
+        return dict(k=_exact_held(x["k"]), v=_exact_held(x["v"]))
+    hq, hkv, d = case["q_heads"], case["kv_heads"], case["head_dim"]
+    g, dev, scale = hq // hkv, _dev(), 1.0 / math.sqrt(d)
+    if kind == "attend":
+        out = torch.empty(x["q"].shape, dtype=torch.float64, device=dev)
+        lse = torch.empty(x["q"].shape[:2], dtype=torch.float64, device=dev)
+    else:
+        mass, count = x["mass"].double(), _counts(case, s)
+    sees = _sees(s)
+    for r in range(case["requests"]):
+        q0, n = int(s["q_indptr"][r]), int(s["n"][r])
+        L, V, T = int(s["ctx"][r]), int(s["nv"][r]), int(s["T"][r])
+        pages = _i64(s["page_indices"][s["page_indptr"][r]:s["page_indptr"][r + 1]])
+        rows = n if kind == "attend" else int(count[r])
+        T = T if kind == "attend" else L + V
+        see = _i64(sees[r])[:rows, :, None]
+        j = torch.arange(T, device=dev)
+        hide = ~((j < see[:, 0]) | ((j >= see[:, 1]) & (j < see[:, 2])))
+        for h in range(hkv):
+            heads = slice(h * g, (h + 1) * g)
+            K = _exact_keys(case, x, pages, h, T)
+            w = (x["q"][q0:q0 + rows, heads].double().reshape(-1, d) @ K.T).reshape(rows, g, T) * scale
+            w.masked_fill_(hide[:, None], -math.inf)
+            if kind == "attend":
+                z = torch.logsumexp(w, -1, keepdim=True)
+                Vt = _exact_tokens(x["cache"][pages, h], d, 1)[:T]
+                out[q0:q0 + n, heads] = (torch.exp(w - z).reshape(-1, T) @ Vt).reshape(n, g, d)
+                lse[q0:q0 + n, heads] = z[..., 0]
+                continue
+            new = torch.exp(w - x["lse"][q0:q0 + rows, heads, None].double()).sum((0, 1))
+            page, slot = pages[torch.div(j, PAGE, rounding_mode="floor")], j % PAGE
+            if case["decay"]:
+                new = new + torch.where(j < L, case["decay"] * mass[page, h, slot], 0.0)
+            mass[page, h, slot] = new
+    return dict(out=out, lse=lse) if kind == "attend" else dict(mass=mass)
