@@ -10,12 +10,15 @@ A case names one kind of call and its sizes:
 The ragged structure of a batch (context lengths, rows, page table) follows
 from the case (its ``layout`` number), the tensors' values from the seed.
 
-4-bit cache.  A block holds 16 tokens of one KV head in 17 D bytes: K codes
-[16][D/2], K scales [16][D/32], V codes [16][D/2], V scales [16][D/32].  An
-element is sign and one of 0, .5, 1, 1.5, 2, 3, 4, 6 (even elements in the low
-four bits), times 2^(b - 127) with the scale byte b of its 32 elements: b is
-the biased exponent of the largest magnitude, one more from 1.75 of its power
-of two on, less 2, within 1 .. 252.
+4-bit cache.  A block holds 16 tokens of one KV head in 17 D bytes: a token's
+D/2 code bytes and D/32 scale bytes of K and of V, laid out as
+  K codes  [D/64][16 tokens][32]           V codes  [2][32][8 tokens][D/64]
+  K scales [16 tokens][D/32]               V scales [2][D/32][8 tokens]
+in the order K codes, K scales, V codes, V scales; the leading 2 of V is the
+token's place / 8.  An element is sign and one of 0, .5, 1, 1.5, 2, 3, 4, 6
+(even elements in the low four bits), times 2^(b - 127) with the scale byte b
+of its 32 elements: b is the biased exponent of the largest magnitude, one more
+from 1.75 of its power of two on, less 2, within 1 .. 252.
 """
 import math
 
@@ -436,13 +439,39 @@ def _decode(code, scale):
     return (x * (scale.to(torch.int32) << 23).view(torch.float32)[..., None]).reshape(*code.shape[:-1], -1)
 
 
-def _parts(pool, d):
-    """Views of a 4-bit pool: K codes, K scales, V codes, V scales, each [.., 16, bytes of a token]."""
-    cut, at, out = (8 * d, d // 2, 8 * d, d // 2), 0, []
-    for c in cut:
-        out.append(pool[..., at:at + c].unflatten(-1, (PAGE, c // PAGE)))
-        at += c
-    return out
+def _views(pool, d):
+    """A 4-bit pool's K codes [.., D/64, 16, 32], K scales [.., 16, D/32],
+    V codes [.., 2, 32, 8, D/64] and V scales [.., 2, D/32, 8]."""
+    kc, ks, vc, vs = pool.split((8 * d, d // 2, 8 * d, d // 2), -1)
+    return (kc.unflatten(-1, (d // 64, PAGE, 32)), ks.unflatten(-1, (PAGE, d // 32)),
+            vc.unflatten(-1, (2, 32, 8, d // 64)), vs.unflatten(-1, (2, d // 32, 8)))
+
+
+def _fetch(pool, d, page, slot, head=None):
+    """Codes and scales of K and V of tokens: page and slot [N], or with head [N, Hkv]."""
+    kc, ks, vc, vs = _views(pool, d)
+    h = slice(None) if head is None else head
+    return (kc[page, h, :, slot].flatten(-2), ks[page, h, slot], vc[page, h, slot // 8, :, slot % 8].flatten(-2),
+            vs[page, h, slot // 8, :, slot % 8])
+
+
+def _store(pool, d, page, slot, token):
+    kc, ks, vc, vs = _views(pool, d)
+    kc[page, :, :, slot] = token[0].unflatten(-1, (d // 64, 32))
+    ks[page, :, slot] = token[1]
+    vc[page, :, slot // 8, :, slot % 8] = token[2].unflatten(-1, (32, d // 64))
+    vs[page, :, slot // 8, :, slot % 8] = token[3]
+
+
+def _keys4(pages, d):
+    """Keys [R, Hkv, tokens, D] of whole pages [R, pages, Hkv, 17 D]."""
+    kc, ks, _, _ = _views(pages, d)
+    return _rect(_decode(kc.movedim(-3, -2).flatten(-2), ks))
+
+
+def _values4(pages, d):
+    _, _, vc, vs = _views(pages, d)
+    return _rect(_decode(vc.movedim(-2, -3).flatten(-2).flatten(-3, -2), vs.movedim(-1, -2).flatten(-3, -2)))
 
 
 def _rect(pages):
@@ -454,9 +483,8 @@ def _plain_append(st):
     d = st["heads"][2]
     req, tok = st["token"]
     page, slot = st["table"][req, tok // PAGE], tok % PAGE
-    for part, data in zip(_parts(st["cache"], d), (*_encode(st["k"]), *_encode(st["v"]))):
-        part[page, :, slot] = data
-    kc, ks, vc, vs = (p[page, :, slot] for p in _parts(st["cache"], d))
+    _store(st["cache"], d, page, slot, (*_encode(st["k"]), *_encode(st["v"])))
+    kc, ks, vc, vs = _fetch(st["cache"], d, page, slot)
     return dict(k=_decode(kc, ks).to(torch.bfloat16), v=_decode(vc, vs).to(torch.bfloat16))
 
 
@@ -473,8 +501,8 @@ def _plain_attend(st):
     hq, hkv, d = st["heads"]
     req, row = st["row"]
     R = st["table"].shape[0]
-    kc, ks, vc, vs = _parts(st["cache"][st["table"]], d)
-    keys, values = _rect(_decode(kc, ks)), _rect(_decode(vc, vs))
+    pages = st["cache"][st["table"]]
+    keys, values = _keys4(pages, d), _values4(pages, d)
     q = st["q"].new_zeros(R, st["rows"], hq, d)
     q[req, row] = st["q"]
     sees = torch.zeros(R, st["rows"], 3, dtype=torch.int64, device=q.device)
@@ -497,8 +525,7 @@ def _plain_mass(st):
     req, row = st["row"]
     R = st["table"].shape[0]
     if case["cache"] == "kv4":
-        kc, ks, _, _ = _parts(st["cache"][st["table"]], d)
-        keys = _rect(_decode(kc, ks))
+        keys = _keys4(st["cache"][st["table"]], d)
     else:
         keys = _rect(st["k_cache"][st["table"]]).float()
     at = st["row_at"][req] + row
@@ -548,9 +575,8 @@ def _plain_evict(st):
         st["k_cache"][to_page, :, to_slot] = st["k_cache"][from_page, head, from_slot]
         st["v_cache"][to_page, :, :, to_slot] = st["v_cache"][from_page, head, :, from_slot]
         return dict(res, k_cache=st["k_cache"], v_cache=st["v_cache"])
-    for part in _parts(st["cache"], d):
-        part[to_page, :, to_slot] = part[from_page, head, from_slot]
-    kc, ks, vc, vs = (p[to_page, :, to_slot] for p in _parts(st["cache"], d))
+    _store(st["cache"], d, to_page, to_slot, _fetch(st["cache"], d, from_page, from_slot, head))
+    kc, ks, vc, vs = _fetch(st["cache"], d, to_page, to_slot)
     return dict(res, k=_decode(kc, ks).to(torch.bfloat16), v=_decode(vc, vs).to(torch.bfloat16))
 
 
@@ -574,14 +600,20 @@ def _exact_tokens(block, d, which):
     """K (which = 0) or V (1) of whole blocks [pages, 17 D] as [tokens, D]."""
     half = 8 * d + d // 2
     block = block[:, which * half:(which + 1) * half]
-    code = block[:, :8 * d].reshape(-1, d // 2).to(torch.int64)
+    n = block.shape[0]
+    if which == 0:  # byte of token t, element pair e: [e / 32][t][e % 32]
+        code = block[:, :8 * d].reshape(n, d // 64, 16, 32).transpose(1, 2)
+        scale = block[:, 8 * d:].reshape(n * 16, d // 32)
+    else:  # [t / 8][e / (D/64)][t % 8][e % (D/64)]
+        code = block[:, :8 * d].reshape(n, 2, 32, 8, d // 64).transpose(2, 3)
+        scale = block[:, 8 * d:].reshape(n, 2, d // 32, 8).transpose(2, 3).reshape(n * 16, d // 32)
+    code = code.reshape(n * 16, d // 2).to(torch.int64)
     nib = torch.empty(code.shape[0], d, dtype=torch.int64, device=code.device)
     nib[:, 0::2], nib[:, 1::2] = code % 16, torch.div(code, 16, rounding_mode="floor")
     mag, exp = nib % 2, torch.div(nib % 8, 2, rounding_mode="floor")
     val = torch.where(exp == 0, mag * 0.5, (1 + 0.5 * mag) * torch.exp2((exp - 1).double()))
     val = torch.where(nib >= 8, -val, val)
-    scale = torch.exp2(block[:, 8 * d:].reshape(-1, d // 32).double() - 127)
-    return (val.reshape(-1, d // 32, 32) * scale[..., None]).reshape(-1, d)
+    return (val.reshape(-1, d // 32, 32) * torch.exp2(scale.double() - 127)[..., None]).reshape(-1, d)
 
 
 def _exact_keys(case, x, pages, h, T):
