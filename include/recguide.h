@@ -37,6 +37,17 @@
  *                              verification history, and the requests grouped
  *                              by that size
  *
+ * and, for long contexts, a cache in 4 bits and a cache of bounded length:
+ *
+ *   rg_kv4_append, rg_kv4_read the rows of a step into a 4-bit paged cache, and
+ *                              back out of it
+ *   rg_kv4_attention           the step's attention (with or without branches)
+ *                              over that cache
+ *   rg_attention_mass, rg_kv4_attention_mass
+ *                              the attention weight each cached key has received
+ *   rg_evict_tokens, rg_kv4_evict_tokens
+ *                              cut requests to their best-scored tokens, in place
+ *
  * Conventions shared by every entry point
  * ---------------------------------------
  * - bf16 tensors are passed as their raw 16-bit patterns (uint16_t).
@@ -75,7 +86,7 @@
 extern "C" {
 #endif
 
-#define RG_ABI_VERSION 7
+#define RG_ABI_VERSION 8
 
 typedef int32_t rg_status;
 #define RG_OK 0
@@ -490,6 +501,146 @@ rg_status rg_plan_block_sizes(const rg_block_policy* policy, const int32_t* acce
                               const float* accept_entropy, const int32_t* prev_block, float* entropy_hist,
                               int32_t num_requests, int32_t* next_block, int32_t* order,
                               int32_t* bucket_offsets, void* stream);
+
+/* ------------------------------------------------------------------------
+ * A paged KV cache in 4 bits
+ * ------------------------------------------------------------------------ */
+
+/*
+ * The cache is one pool [num_pages][num_kv_heads] of blocks of
+ * RG_KV4_BLOCK_BYTES(head_dim) bytes (16-byte aligned, contiguous), K and V of
+ * 16 tokens of one KV head each: 17/64 of the bf16 cache's bytes.  A token has
+ * D/2 code bytes and D/32 scale bytes of K, and as many of V, laid out in the
+ * order the attention's matrix instructions take them:
+ *
+ *   K codes  [D/64][16 tokens][32]       bytes of dims 64 i .. 64 i + 63
+ *   K scales [16 tokens][D/32]
+ *   V codes  [2][32][8 tokens][D/64]     token = 8 * first + third index; the
+ *                                        second and fourth make the code byte
+ *   V scales [2][D/32][8 tokens]
+ *
+ * Code byte i of a token holds element 2 i in its low four bits and 2 i + 1 in
+ * its high ones: a sign bit over 0, 0.5, 1, 1.5, 2, 3, 4, 6.  An element's
+ * value is that times 2^(b - 127), b the scale byte of its 32 elements, 1 to
+ * 252: the value is exact in bf16.
+ *
+ * Rows are rounded so: b is the biased exponent of the 32 elements' largest
+ * magnitude, plus one where it is at least 1.75 times its power of two, less
+ * 2, clamped to 1 .. 252 (so that magnitude / 2^(b - 127) lies in [3.5, 7)
+ * unless clamped); a code is the nearest of the grid, ties to the even code,
+ * magnitudes past 6 become 6, and the sign of an element is kept.
+ */
+#define RG_KV4_BLOCK_BYTES(head_dim) (17 * (head_dim))
+
+/*
+ * Rows into the 4-bit cache: row i of request r (rows q_indptr[r] ..
+ * q_indptr[r+1]-1) goes to token ctx_len[r] + i of the request's pages.  Those
+ * tokens are written and no others, whatever the pages hold.  A page that rows
+ * are written to must not be in another request's list.
+ *
+ *   k, v      DEVICE bf16 rows [Hkv][D], row j at k + j * k_stride and
+ *             v + j * v_stride (elements, at least Hkv * D, multiples of 8;
+ *             pointers 16-byte aligned)
+ *   cache     DEVICE pool
+ * The layout's n_verify, num_q_heads and sm_scale have no effect.
+ */
+rg_status rg_kv4_append(const rg_attn_layout* layout, const uint16_t* k, int64_t k_stride, const uint16_t* v,
+                        int64_t v_stride, uint8_t* cache, void* stream);
+
+/* The same tokens (ctx_len[r] .. ctx_len[r] + n_r - 1) out of the cache, as
+ * bf16 rows: the values they stand for.  A whole context is read with ctx_len
+ * 0 and q_indptr over its tokens (at most 65535 rows of a request a call). */
+rg_status rg_kv4_read(const rg_attn_layout* layout, const uint8_t* cache, uint16_t* k, int64_t k_stride, uint16_t* v,
+                      int64_t v_stride, void* stream);
+
+/*
+ * rg_draft_verify_attention (branches NULL) or rg_multibranch_attention over a
+ * 4-bit cache: layout, branches, q, out and lse as there, K and V the values
+ * the codes stand for.  Slots no request reads may hold anything.  The
+ * workspace needs no initialisation.
+ */
+rg_status rg_kv4_attention_workspace(const rg_attn_layout* layout, const rg_branch_layout* branches, size_t* bytes);
+rg_status rg_kv4_attention(const rg_attn_layout* layout, const rg_branch_layout* branches, const uint16_t* q,
+                           const uint8_t* cache, uint16_t* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Eviction of tokens by accumulated attention weight
+ * ------------------------------------------------------------------------ */
+
+/*
+ * The attention weight that the verify rows of a step give to each key, added
+ * to what the key has received.  Call it after the step's attention, with that
+ * call's layout, q and lse; with branches too, whose rows do not count.
+ *
+ *   row_count  DEVICE [R] or NULL: the first min(max(row_count[r], 0), V) verify
+ *              rows of request r count (e.g. those that verification accepted);
+ *              NULL: all V of them
+ *   decay      >= 0, finite: factor of what a key has received before
+ *   mass       DEVICE pool [num_pages][num_kv_heads][16] fp32 beside the cache
+ *
+ * For every request with query rows and its keys j < L + V, with w_j the sum
+ * of exp(scale * q.k_j - lse) over the KV head's query heads and the counted
+ * verify rows i with j <= L + i:
+ *   mass[j] = decay * mass[j] + w_j  for j < L (decay 0 does not read mass[j])
+ *   mass[j] = w_j                    for the step's own keys j >= L
+ * so that keys need no initialisation.  Pages must not be in two requests'
+ * lists.  The order of the sums is fixed: equal calls give equal bits.
+ */
+rg_status rg_attention_mass(const rg_attn_layout* layout, const uint16_t* q, const uint16_t* k_cache, const float* lse,
+                            const int32_t* row_count, float decay, float* mass, void* stream);
+rg_status rg_kv4_attention_mass(const rg_attn_layout* layout, const uint16_t* q, const uint8_t* cache, const float* lse,
+                                const int32_t* row_count, float decay, float* mass, void* stream);
+
+/*
+ * Requests to be cut, between steps (their cached tokens only).
+ *
+ * Request r has ctx_len[r] = L tokens in its pages, and min(keep[r], L) of them
+ * stay, for each KV head its own.  A token's position is its number in the
+ * request's whole sequence.  Slot j < tracked[r] holds the token of position
+ * positions[j] (as an earlier call left it); slot j >= tracked[r] that of
+ * position j + evicted[r], evicted[r] being the tokens evicted so far (of each
+ * head alike).  A new request has tracked = evicted = 0.
+ */
+typedef struct rg_evict_layout {
+  int32_t num_requests;        /* R >= 1                                        */
+  int32_t num_kv_heads;        /* >= 1                                          */
+  int32_t head_dim;            /* D: 64 or 128                                  */
+  int32_t page_size;           /* must be 16                                    */
+  int32_t num_pages;           /* pages in each pool                            */
+  int32_t sink;                /* >= 0: positions 0 .. sink - 1 always stay     */
+  int32_t recent;              /* >= 0: the latest `recent` positions always stay */
+  const int32_t* ctx_len;      /* host [R], >= 0                                */
+  const int32_t* keep;         /* host [R], >= 0; at least sink + recent where
+                                  below ctx_len                                 */
+  const int32_t* tracked;      /* host [R], 0 .. ctx_len                        */
+  const int32_t* evicted;      /* host [R], >= 0                                */
+  const int32_t* page_indptr;  /* host [R+1], as in rg_attn_layout              */
+  const int32_t* page_indices; /* DEVICE [page_indptr[R]], each < num_pages; no
+                                  page in two requests' lists                   */
+} rg_evict_layout;
+
+/* Workspace bytes of an eviction (no initialisation needed). */
+rg_status rg_evict_workspace(const rg_evict_layout* layout, size_t* bytes);
+
+/*
+ * Eviction in place.  Of a (request, KV head)'s L tokens the protected ones
+ * stay (see sink and recent), then those of the largest scores, ties going to
+ * the lowest slots.  The kept tokens of slots >= keep, in ascending order, move
+ * to the evicted ones' slots < keep, in ascending order, with their K, V, mass
+ * and position; every other slot keeps what it holds.  Afterwards the request
+ * has L' = min(keep, L) tokens in slots 0 .. L' - 1 and positions for all of
+ * them: continue with ctx_len = tracked = L', evicted + L - L', and free the
+ * pages past L'.  Attention does not depend on the order of cached tokens.
+ *
+ *   score      DEVICE pool [num_pages][num_kv_heads][16] fp32, not NaN; may be
+ *              the mass itself
+ *   mass       the same kind of pool, moved along, or NULL
+ *   positions  DEVICE pool [num_pages][num_kv_heads][16] int32
+ */
+rg_status rg_evict_tokens(const rg_evict_layout* layout, uint16_t* k_cache, uint16_t* v_cache, const float* score,
+                          float* mass, int32_t* positions, void* ws, size_t ws_bytes, void* stream);
+rg_status rg_kv4_evict_tokens(const rg_evict_layout* layout, uint8_t* cache, const float* score, float* mass,
+                              int32_t* positions, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -54,6 +54,14 @@ class BlockPolicy(ctypes.Structure):
                 ("rho", ctypes.c_float), ("value", ctypes.c_void_p)]
 
 
+class EvictLayout(ctypes.Structure):
+    _fields_ = [("num_requests", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("sink", ctypes.c_int32),
+                ("recent", ctypes.c_int32), ("ctx_len", ctypes.c_void_p), ("keep", ctypes.c_void_p),
+                ("tracked", ctypes.c_void_p), ("evicted", ctypes.c_void_p), ("page_indptr", ctypes.c_void_p),
+                ("page_indices", ctypes.c_void_p)]
+
+
 class AttnPlanInfo(ctypes.Structure):
     _fields_ = [("num_launches", ctypes.c_int32), ("chunk_keys", ctypes.c_int32),
                 ("work_items", ctypes.c_int64), ("split_requests", ctypes.c_int64),
@@ -75,7 +83,9 @@ EXPORTS = ("rg_abi_version", "rg_status_string", "rg_draft_verify_attention_work
            "rg_draft_confidence", "rg_verify_and_confidence_workspace", "rg_verify_and_confidence",
            "rg_verify_and_confidence_noalloc",
            "rg_multibranch_attention_workspace", "rg_multibranch_attention", "rg_plan_branches",
-           "rg_match_branches", "rg_plan_block_sizes")
+           "rg_match_branches", "rg_plan_block_sizes", "rg_kv4_append", "rg_kv4_read", "rg_kv4_attention_workspace",
+           "rg_kv4_attention", "rg_attention_mass", "rg_kv4_attention_mass", "rg_evict_workspace", "rg_evict_tokens",
+           "rg_kv4_evict_tokens")
 
 _LIB = None
 
@@ -113,6 +123,16 @@ def _lib():
         "rg_plan_branches": (I32, [P, P, P, I32, I32, ctypes.c_float, P, P, P, P, P, P]),
         "rg_match_branches": (I32, [P, P, P, P, P, P, P, P, I32, P, P]),
         "rg_plan_block_sizes": (I32, [ctypes.POINTER(BlockPolicy), P, P, P, P, I32, P, P, P, P]),
+        "rg_kv4_append": (I32, [ctypes.POINTER(AttnLayout), P, I64, P, I64, P, P]),
+        "rg_kv4_read": (I32, [ctypes.POINTER(AttnLayout), P, P, I64, P, I64, P]),
+        "rg_kv4_attention_workspace": (I32, [ctypes.POINTER(AttnLayout), ctypes.POINTER(BranchLayout),
+                                             ctypes.POINTER(SZ)]),
+        "rg_kv4_attention": (I32, [ctypes.POINTER(AttnLayout), ctypes.POINTER(BranchLayout), P, P, P, P, P, SZ, P]),
+        "rg_attention_mass": (I32, [ctypes.POINTER(AttnLayout), P, P, P, P, ctypes.c_float, P, P]),
+        "rg_kv4_attention_mass": (I32, [ctypes.POINTER(AttnLayout), P, P, P, P, ctypes.c_float, P, P]),
+        "rg_evict_workspace": (I32, [ctypes.POINTER(EvictLayout), ctypes.POINTER(SZ)]),
+        "rg_evict_tokens": (I32, [ctypes.POINTER(EvictLayout), P, P, P, P, P, P, SZ, P]),
+        "rg_kv4_evict_tokens": (I32, [ctypes.POINTER(EvictLayout), P, P, P, P, P, SZ, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -575,3 +595,248 @@ def verify_and_confidence(verify_logits: torch.Tensor, row_indptr: torch.Tensor,
     _check(st, "rg_verify_and_confidence")
     return ov, od
 
+
+
+# ---------------------------------------------------------------------------
+# A paged KV cache in 4 bits
+def kv4_block_bytes(head_dim: int) -> int:
+    """Bytes of K and V of 16 tokens of one KV head (RG_KV4_BLOCK_BYTES)."""
+    return 17 * head_dim
+
+
+def new_kv4_cache(num_pages: int, num_kv_heads: int, head_dim: int, device) -> torch.Tensor:
+    """A 4-bit cache pool, uint8 [pages, Hkv, 17 D] (contents undefined)."""
+    return torch.empty(num_pages, num_kv_heads, kv4_block_bytes(head_dim), dtype=torch.uint8, device=device)
+
+
+def _kv4(cache: torch.Tensor, head_dim: int, num_kv_heads: int, num_pages: int) -> torch.Tensor:
+    _dev(cache, "cache", torch.uint8)
+    if tuple(cache.shape) != (num_pages, num_kv_heads, kv4_block_bytes(head_dim)):
+        raise ValueError("cache must be [pages, Hkv, 17 D] of the layout's sizes")
+    return cache
+
+
+def make_kv4_layout(num_q_heads: int, cache: torch.Tensor, q_indptr, n_verify, ctx_len, page_indptr,
+                    page_indices: torch.Tensor, sm_scale: float = 0.0) -> _Layout:
+    """make_layout for a 4-bit cache (uint8 [pages, Hkv, 17 D])."""
+    num_pages, hkv, block = cache.shape
+    if block % 17:
+        raise ValueError("cache must be [pages, Hkv, 17 D]")
+    return _Layout(num_q_heads, hkv, block // 17, num_pages, q_indptr, n_verify, ctx_len, page_indptr, page_indices,
+                   sm_scale)
+
+
+def _check_layout(lay: _Layout, rows: int):
+    if int(lay.q_indptr[-1]) != rows:
+        raise ValueError("q_indptr[-1] must equal the number of rows")
+    if lay.page_indices.numel() < int(lay.page_indptr[-1]):
+        raise ValueError("page_indices is shorter than page_indptr[-1]")
+
+
+def _rows(t: torch.Tensor, name: str, lay: _Layout) -> int:
+    """Checks rows [rows, Hkv, D] (any row stride, heads contiguous) and returns the stride."""
+    hkv, d = lay.c.num_kv_heads, lay.c.head_dim
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.bfloat16:
+        raise TypeError(f"{name} must be a CUDA bf16 tensor")
+    if t.dim() != 3 or t.shape[1] != hkv or t.shape[2] != d or t.stride(2) != 1 or (hkv > 1 and t.stride(1) != d):
+        raise ValueError(f"{name} must be [rows, {hkv}, {d}], contiguous within a row")
+    _check_layout(lay, t.shape[0])
+    return t.stride(0) if t.shape[0] > 1 else hkv * d
+
+
+def kv4_append(k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor, layout: _Layout, *, stream=None) -> None:
+    """Rows k, v [rows, Hkv, D] (e.g. parts of one projection's output) into
+    the 4-bit cache, at the tokens behind each request's context
+    (rg_kv4_append)."""
+    ks, vs = _rows(k, "k", layout), _rows(v, "v", layout)
+    _kv4(cache, layout.c.head_dim, layout.c.num_kv_heads, layout.c.num_pages)
+    if k.shape[0] == 0:
+        return
+    _check(_lib().rg_kv4_append(ctypes.byref(layout.c), k.data_ptr(), ks, v.data_ptr(), vs, cache.data_ptr(),
+                                _stream(stream)), "rg_kv4_append")
+
+
+def kv4_read(cache: torch.Tensor, layout: _Layout, *, k_out: Optional[torch.Tensor] = None,
+             v_out: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The tokens kv4_append writes for this layout, as bf16 rows (rg_kv4_read)."""
+    _kv4(cache, layout.c.head_dim, layout.c.num_kv_heads, layout.c.num_pages)
+    shape = (int(layout.q_indptr[-1]), layout.c.num_kv_heads, layout.c.head_dim)
+    k = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if k_out is None else k_out
+    v = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if v_out is None else v_out
+    ks, vs = _rows(k, "k_out", layout), _rows(v, "v_out", layout)
+    if shape[0]:
+        _check(_lib().rg_kv4_read(ctypes.byref(layout.c), cache.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs,
+                                  _stream(stream)), "rg_kv4_read")
+    return k, v
+
+
+def kv4_attention_workspace_bytes(layout: _Layout, branches: Optional[_Branches] = None) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib().rg_kv4_attention_workspace(ctypes.byref(layout.c), ctypes.byref(branches.c) if branches else None,
+                                             ctypes.byref(n)), "rg_kv4_attention_workspace")
+    return int(n.value)
+
+
+def kv4_attention(q: torch.Tensor, cache: torch.Tensor, layout: _Layout, branches: Optional[_Branches] = None, *,
+                  out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = True,
+                  workspace: Optional[torch.Tensor] = None,
+                  stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """draft_verify_attention, or with branches multibranch_attention, over a
+    4-bit cache (rg_kv4_attention); the layout from make_kv4_layout."""
+    _dev(q, "q", torch.bfloat16)
+    if q.dim() != 3 or q.shape[1] != layout.c.num_q_heads or q.shape[2] != layout.c.head_dim:
+        raise ValueError("q must be [rows, Hq, D] of the layout's sizes")
+    _kv4(cache, layout.c.head_dim, layout.c.num_kv_heads, layout.c.num_pages)
+    _check_layout(layout, q.shape[0])
+    if branches is not None and branches.branch_indptr.shape[0] != layout.ctx_len.shape[0] + 1:
+        raise ValueError("branch_indptr must have num_requests + 1 entries")
+    if out is None:
+        out = torch.empty_like(q)
+    if _dev(out, "out", torch.bfloat16).shape != q.shape:
+        raise ValueError("out must have q's shape")
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[0], q.shape[1], dtype=torch.float32, device=q.device)
+    if lse is not None and _dev(lse, "lse", torch.float32).shape != q.shape[:2]:
+        raise ValueError("lse must be [rows, Hq]")
+    if q.shape[0] == 0:
+        return out, lse
+    if workspace is None:  # the call itself checks the size of one that is given
+        need = kv4_attention_workspace_bytes(layout, branches)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(_lib().rg_kv4_attention(ctypes.byref(layout.c), ctypes.byref(branches.c) if branches else None, q.data_ptr(),
+                                   cache.data_ptr(), out.data_ptr(), _ptr(lse), _ptr(workspace), ws_bytes,
+                                   _stream(stream)), "rg_kv4_attention")
+    return out, lse
+
+
+# ---------------------------------------------------------------------------
+# Eviction of tokens by accumulated attention weight
+def _slot_pool(t: torch.Tensor, name: str, dtype: torch.dtype, num_pages: int, num_kv_heads: int) -> torch.Tensor:
+    if tuple(_dev(t, name, dtype).shape) != (num_pages, num_kv_heads, 16):
+        raise ValueError(f"{name} must be [pages, Hkv, 16]")
+    return t
+
+
+def _mass_args(q, lse, mass, layout: _Layout, row_count, stream):
+    _dev(q, "q", torch.bfloat16)
+    if q.dim() != 3 or q.shape[1] != layout.c.num_q_heads or q.shape[2] != layout.c.head_dim:
+        raise ValueError("q must be [rows, Hq, D] of the layout's sizes")
+    _check_layout(layout, q.shape[0])
+    if _dev(lse, "lse", torch.float32).shape != q.shape[:2]:
+        raise ValueError("lse must be [rows, Hq]")
+    _slot_pool(mass, "mass", torch.float32, layout.c.num_pages, layout.c.num_kv_heads)
+    if row_count is not None and _dev(row_count, "row_count", torch.int32).numel() != layout.c.num_requests:
+        raise ValueError("row_count needs one entry per request")
+    return lse.data_ptr(), _ptr(row_count)
+
+
+def attention_mass(q: torch.Tensor, k_cache: torch.Tensor, lse: torch.Tensor, mass: torch.Tensor, layout: _Layout, *,
+                   row_count: Optional[torch.Tensor] = None, decay: float = 1.0, stream=None) -> torch.Tensor:
+    """Adds the verify rows' attention weights to the keys' mass (fp32
+    [pages, Hkv, 16], in place; rg_attention_mass).  q, lse and the layout are
+    those of the step's attention; row_count int32 [R]: the rows that count."""
+    _dev(k_cache, "k_cache", torch.bfloat16)
+    if tuple(k_cache.shape) != (layout.c.num_pages, layout.c.num_kv_heads, 16, layout.c.head_dim):
+        raise ValueError("k_cache must be [pages, Hkv, 16, D] of the layout's sizes")
+    lp, rp = _mass_args(q, lse, mass, layout, row_count, stream)
+    if q.shape[0]:
+        _check(_lib().rg_attention_mass(ctypes.byref(layout.c), q.data_ptr(), k_cache.data_ptr(), lp, rp, decay,
+                                        mass.data_ptr(), _stream(stream)), "rg_attention_mass")
+    return mass
+
+
+def kv4_attention_mass(q: torch.Tensor, cache: torch.Tensor, lse: torch.Tensor, mass: torch.Tensor, layout: _Layout, *,
+                       row_count: Optional[torch.Tensor] = None, decay: float = 1.0, stream=None) -> torch.Tensor:
+    """attention_mass over a 4-bit cache (rg_kv4_attention_mass)."""
+    _kv4(cache, layout.c.head_dim, layout.c.num_kv_heads, layout.c.num_pages)
+    lp, rp = _mass_args(q, lse, mass, layout, row_count, stream)
+    if q.shape[0]:
+        _check(_lib().rg_kv4_attention_mass(ctypes.byref(layout.c), q.data_ptr(), cache.data_ptr(), lp, rp, decay,
+                                            mass.data_ptr(), _stream(stream)), "rg_kv4_attention_mass")
+    return mass
+
+
+class _EvictLayout:
+    """Keeps the host arrays alive while the C struct points at them."""
+
+    def __init__(self, num_kv_heads, head_dim, num_pages, ctx_len, keep, tracked, evicted, page_indptr,
+                 page_indices, sink, recent):
+        self.ctx_len = _host_i32(ctx_len, "ctx_len")
+        R = self.ctx_len.shape[0]
+        zero = np.zeros(R, dtype=np.int32)
+        self.keep = _host_i32(keep, "keep")
+        self.tracked = zero if tracked is None else _host_i32(tracked, "tracked")
+        self.evicted = zero if evicted is None else _host_i32(evicted, "evicted")
+        self.page_indptr = _host_i32(page_indptr, "page_indptr")
+        self.page_indices = _dev(page_indices, "page_indices", torch.int32)
+        if any(a.shape != (R,) for a in (self.keep, self.tracked, self.evicted)) or self.page_indptr.shape != (R + 1,):
+            raise ValueError("per-request arrays disagree on the number of requests")
+        if self.page_indices.numel() < int(self.page_indptr[-1]):
+            raise ValueError("page_indices is shorter than page_indptr[-1]")
+        self.c = EvictLayout(R, num_kv_heads, head_dim, 16, num_pages, int(sink), int(recent), self.ctx_len.ctypes.data,
+                             self.keep.ctypes.data, self.tracked.ctypes.data, self.evicted.ctypes.data,
+                             self.page_indptr.ctypes.data, self.page_indices.data_ptr())
+
+
+def make_evict_layout(cache: torch.Tensor, ctx_len, keep, page_indptr, page_indices: torch.Tensor, *, tracked=None,
+                      evicted=None, sink: int = 0, recent: int = 0) -> _EvictLayout:
+    """Requests to cut to `keep` tokens; cache is the bf16 K pool [pages, Hkv,
+    16, D] or a 4-bit pool [pages, Hkv, 17 D].  tracked and evicted as an
+    earlier call left them (None: zero)."""
+    if cache.dim() == 3:
+        if cache.shape[2] % 17:
+            raise ValueError("cache must be [pages, Hkv, 17 D]")
+        d = cache.shape[2] // 17
+    elif cache.dim() == 4 and cache.shape[2] == 16:
+        d = cache.shape[3]
+    else:
+        raise ValueError("cache must be a K pool [pages, Hkv, 16, D] or a 4-bit pool [pages, Hkv, 17 D]")
+    return _EvictLayout(cache.shape[1], d, cache.shape[0], ctx_len, keep, tracked, evicted, page_indptr, page_indices,
+                        sink, recent)
+
+
+def evict_workspace_bytes(layout: _EvictLayout) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib().rg_evict_workspace(ctypes.byref(layout.c), ctypes.byref(n)), "rg_evict_workspace")
+    return int(n.value)
+
+
+def _evict_args(score, positions, layout: _EvictLayout, mass, workspace):
+    pool = (layout.c.num_pages, layout.c.num_kv_heads)
+    _slot_pool(score, "score", torch.float32, *pool)
+    _slot_pool(positions, "positions", torch.int32, *pool)
+    if mass is not None:
+        _slot_pool(mass, "mass", torch.float32, *pool)
+    if workspace is None:
+        workspace = torch.empty(evict_workspace_bytes(layout), dtype=torch.uint8, device=score.device)
+    return (score.data_ptr(), _ptr(mass), positions.data_ptr(), workspace.data_ptr(),
+            workspace.numel() * workspace.element_size())
+
+
+def evict_tokens(k_cache: torch.Tensor, v_cache: torch.Tensor, score: torch.Tensor, positions: torch.Tensor,
+                 layout: _EvictLayout, *, mass: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Cuts each request to its best-scored tokens, in place
+    (rg_evict_tokens): k_cache [pages, Hkv, 16, D], v_cache [pages, Hkv, D,
+    16], score and mass fp32 and positions int32 [pages, Hkv, 16]."""
+    c = layout.c
+    _dev(k_cache, "k_cache", torch.bfloat16)
+    _dev(v_cache, "v_cache", torch.bfloat16)
+    if tuple(k_cache.shape) != (c.num_pages, c.num_kv_heads, 16, c.head_dim) or \
+            tuple(v_cache.shape) != (c.num_pages, c.num_kv_heads, c.head_dim, 16):
+        raise ValueError("k_cache must be [pages, Hkv, 16, D] and v_cache [pages, Hkv, D, 16] of the layout's sizes")
+    args = _evict_args(score, positions, layout, mass, workspace)
+    _check(_lib().rg_evict_tokens(ctypes.byref(c), k_cache.data_ptr(), v_cache.data_ptr(), *args, _stream(stream)),
+           "rg_evict_tokens")
+
+
+def kv4_evict_tokens(cache: torch.Tensor, score: torch.Tensor, positions: torch.Tensor, layout: _EvictLayout, *,
+                     mass: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+    """evict_tokens on a 4-bit cache (rg_kv4_evict_tokens)."""
+    c = layout.c
+    _kv4(cache, c.head_dim, c.num_kv_heads, c.num_pages)
+    args = _evict_args(score, positions, layout, mass, workspace)
+    _check(_lib().rg_kv4_evict_tokens(ctypes.byref(c), cache.data_ptr(), *args, _stream(stream)), "rg_kv4_evict_tokens")

@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(HERE, "librecguide.so")
 BUILD_DIR = os.path.join(HERE, "_build")
-SOURCES = ("api.cpp", "attention.hip", "logits.hip", "branches.hip", "blocksize.hip")
+SOURCES = ("api.cpp", "cache_api.cpp", "attention.hip", "logits.hip", "branches.hip", "blocksize.hip", "kv4.hip",
+           "kv4_attention.hip", "mass.hip", "evict.hip")
 ARCH = "gfx950"
 
 # Packed fp32 VALU instructions are kept out of the generated code; MFMA

@@ -14,7 +14,7 @@
 #include <type_traits>
 #include <vector>
 
-#include "rg_internal.h"
+#include "plan_common.h"
 
 static_assert(RG_BLOCK_MAX_CANDIDATES == rg::kMaxBlockCandidates, "header and kernel limits agree");
 static_assert(RG_BLOCK_MAX_S_BINS == rg::kMaxSBins, "header and kernel limits agree");
@@ -22,13 +22,7 @@ static_assert(RG_BLOCK_MAX_REQUESTS == rg::kMaxBucketRequests, "header and kerne
 static_assert(RG_BRANCH_MAX_REQS_PER_LAUNCH == rg::kMaxReqPerLaunchBr, "header and kernel limits agree");
 static_assert(RG_NOALLOC_SCRATCH_BYTES == rg::kNoAllocScratchBytes, "header and scratch size agree");
 
-namespace {
-
-using namespace rg;
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+namespace rg {
 
 int env_int(const char* name, int fallback) {
   const char* v = std::getenv(name);
@@ -114,23 +108,6 @@ rg_status validate_branches(const rg_attn_layout* L, const rg_branch_layout* B) 
   return RG_OK;
 }
 
-template <typename Plan>
-struct FullPlanT {
-  std::vector<Plan> launches;
-  int chunk = 0;      // the finest split: it sizes the workspace and orders one-launch calls
-  int run = 0;        // keys per work item of the launches, >= chunk
-  bool narrow = false;  // narrow work groups
-  int cols_per_group = 256;
-  int64_t items = 0, split_requests = 0, max_partial_cols = 0, total_partial_cols = 0;
-  int64_t run_split_requests = 0, run_max_partial_cols = 0, run_partial_cols = 0;  // of the launches
-  int64_t max_comb = 0;
-  int persistent_launches = 0;
-  size_t ws_bytes = 0;
-  size_t o_offset = 0;
-  size_t ml_offset = 0;
-  size_t sync_offset = 0;
-};
-
 // Compute units of the current device: the rounds of the chunk rule and the
 // one-launch kernel's work groups (one per CU); 256 (MI355X) when the runtime
 // cannot say.  Every planning call (workspace query, plan query, the call
@@ -195,6 +172,29 @@ int choose_chunk(const std::vector<int64_t>& pair_keys, int hkv, int num_cus) {
   }
   return (int)(hi * kKeyTile);
 }
+
+}  // namespace rg
+
+namespace {
+
+using namespace rg;
+
+template <typename Plan>
+struct FullPlanT {
+  std::vector<Plan> launches;
+  int chunk = 0;      // the finest split: it sizes the workspace and orders one-launch calls
+  int run = 0;        // keys per work item of the launches, >= chunk
+  bool narrow = false;  // narrow work groups
+  int cols_per_group = 256;
+  int64_t items = 0, split_requests = 0, max_partial_cols = 0, total_partial_cols = 0;
+  int64_t run_split_requests = 0, run_max_partial_cols = 0, run_partial_cols = 0;  // of the launches
+  int64_t max_comb = 0;
+  int persistent_launches = 0;
+  size_t ws_bytes = 0;
+  size_t o_offset = 0;
+  size_t ml_offset = 0;
+  size_t sync_offset = 0;
+};
 
 // One (request, column group) of the batch; it stands for Hkv pairs.
 struct PairLoad {
@@ -295,9 +295,6 @@ bool narrow_items(const std::vector<PairLoad>& pairs, int hkv, int num_cus, int 
 }
 
 int item_threads(bool narrow) { return narrow ? kFullThreads / 2 : kFullThreads; }
-
-// Whether a grid of this many work groups, rounded up to 8, is one launch.
-bool fits_launch(int64_t groups, int threads) { return round_up(groups, 8) * threads <= kMaxLaunchThreads; }
 
 // Launches with a split request run as the main kernel plus the combine
 // kernel, or, with RG_ATTN_PERSIST=1, as one work-queue launch (main items,

@@ -1,0 +1,368 @@
+// C ABI of the 4-bit KV cache, the attention mass and the eviction of tokens:
+// argument validation, planning and launches.  As in api.cpp the plans travel
+// in the kernel arguments; nothing is uploaded or synchronised.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <numeric>
+
+#include "cache_internal.h"
+#include "plan_common.h"
+
+namespace {
+
+using namespace rg;
+
+// Calls launch(plan) for a layout's requests, in order, a plan's worth at a
+// time; items(r) is request r's number of work items (0: left out), fill(r, q)
+// completes its entry.  False from launch stops.
+template <typename Items, typename Launch>
+rg_status each_plan(const rg_attn_layout* L, int threads, Items items, Launch launch) {
+  AttnPlan p;
+  for (int pass = 0; pass < 2; ++pass) {  // check every plan, then launch
+    for (int r0 = 0; r0 < L->num_requests; r0 += kMaxReqPerLaunch) {
+      const int cnt = std::min(kMaxReqPerLaunch, L->num_requests - r0);
+      std::memset(&p, 0, sizeof(p));
+      p.num_req = cnt;
+      int64_t total = 0;
+      for (int k = 0; k < cnt; ++k) {
+        const int r = r0 + k;
+        AttnReq& q = p.req[k];
+        q.q_start = L->q_indptr[r];
+        q.ctx = L->ctx_len[r];
+        q.nv = (int32_t)((uint32_t)(L->q_indptr[r + 1] - L->q_indptr[r]) | ((uint32_t)L->n_verify[r] << 16));
+        q.page_start = L->page_indptr[r];
+        q.item_start = (int32_t)total;
+        q.part_start = r;
+        total += items(r);
+        if (total > INT32_MAX / 2 || !fits_launch(total, threads)) return RG_ERR_UNSUPPORTED;
+      }
+      p.req[cnt].item_start = p.total_items = (int32_t)total;
+      if (pass == 1 && total > 0 && launch(p) != hipSuccess) return RG_ERR_HIP;
+    }
+  }
+  return RG_OK;
+}
+
+// ---------------------------------------------------------------------------
+rg_status run_rows(const rg_attn_layout* L, const uint16_t* k, int64_t k_stride, const uint16_t* v, int64_t v_stride,
+                   const uint8_t* cache, bool append, void* stream) {
+  const rg_status st = validate_layout(L);
+  if (st != RG_OK) return st;
+  if (!k || !v || !cache) return RG_ERR_NULL;
+  const int64_t width = (int64_t)L->num_kv_heads * L->head_dim;
+  if (k_stride < width || v_stride < width) return RG_ERR_SHAPE;
+  if (k_stride % 8 || v_stride % 8 || !aligned(k, 16) || !aligned(v, 16) || !aligned(cache, 16) ||
+      !aligned(L->page_indices, 4))
+    return RG_ERR_UNSUPPORTED;
+  Kv4RowArgs a;
+  a.k = const_cast<uint16_t*>(k);
+  a.v = const_cast<uint16_t*>(v);
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.cache = const_cast<uint8_t*>(cache);
+  a.page_indices = L->page_indices;
+  a.hkv = L->num_kv_heads;
+  auto pages = [&](int r) -> int64_t {
+    const int64_t n = L->q_indptr[r + 1] - L->q_indptr[r];
+    return n == 0 ? 0 : (L->ctx_len[r] + n - 1) / kPageSize - L->ctx_len[r] / kPageSize + 1;
+  };
+  return each_plan(L, 256, pages, [&](const AttnPlan& p) {
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    return append ? launch_kv4_append(a, p, L->head_dim, s) : launch_kv4_read(a, p, L->head_dim, s);
+  });
+}
+
+// ---------------------------------------------------------------------------
+template <typename Plan>
+struct Kv4Plan {
+  std::vector<Plan> launches;
+  int64_t max_partial_cols = 0;
+  size_t ml_offset = 0, ws_bytes = 0;
+};
+
+template <typename Plan, int MaxReq>
+rg_status plan_kv4(const rg_attn_layout* L, const rg_branch_layout* B, Kv4Plan<Plan>& fp) {
+  const int R = L->num_requests, hkv = L->num_kv_heads, g = L->num_q_heads / hkv;
+  const int cus = device_cus();
+  std::vector<int64_t> pair_keys;
+  for (int r = 0; r < R; ++r) {
+    const int64_t n = L->q_indptr[r + 1] - L->q_indptr[r];
+    const int64_t ncg = (n * g + kKv4Cols - 1) / kKv4Cols;
+    for (int64_t cg = 0; cg < ncg; ++cg) pair_keys.push_back(L->ctx_len[r] + n);
+  }
+  const int chunk = choose_chunk(pair_keys, hkv, 2 * cus);
+  std::vector<int> order(R);
+  std::iota(order.begin(), order.end(), 0);
+  auto keys_of = [&](int r) {
+    const int64_t n = L->q_indptr[r + 1] - L->q_indptr[r];
+    return n == 0 ? int64_t(0) : L->ctx_len[r] + n;
+  };
+  std::stable_sort(order.begin(), order.end(), [&](int x, int y) {
+    return std::min<int64_t>(chunk, keys_of(x)) > std::min<int64_t>(chunk, keys_of(y));
+  });
+  for (int r0 = 0; r0 < R; r0 += MaxReq) {
+    const int cnt = std::min(MaxReq, R - r0);
+    Plan p;
+    std::memset(&p, 0, sizeof(p));
+    p.num_req = cnt;
+    p.chunk = chunk;
+    p.cols_per_group = kKv4Cols;
+    int64_t items = 0, part = 0, comb = 0;
+    for (int k = 0; k < cnt; ++k) {
+      const int r = order[r0 + k];
+      const int64_t n = L->q_indptr[r + 1] - L->q_indptr[r];
+      auto& q = p.req[k];
+      if constexpr (__is_same(Plan, AttnPlanBr)) pack_branches(B, r, q.br, q.rep);
+      q.q_start = L->q_indptr[r];
+      q.ctx = L->ctx_len[r];
+      q.nv = (int32_t)((uint32_t)n | ((uint32_t)L->n_verify[r] << 16));
+      q.page_start = L->page_indptr[r];
+      q.item_start = (int32_t)items;
+      q.part_start = (int32_t)part;
+      q.comb_start = (int32_t)comb;
+      if (n == 0) continue;
+      const int64_t M = n * g, nch = (L->ctx_len[r] + n + chunk - 1) / chunk;
+      items += hkv * ((M + kKv4Cols - 1) / kKv4Cols) * nch;
+      if (nch > 1) {
+        p.max_chunks = std::max<int32_t>(p.max_chunks, (int32_t)nch);
+        part += hkv * nch * round_up(M, 32);
+        comb += hkv * ((M + 31) / 32) * (L->head_dim / 8);
+      }
+      if (items > INT32_MAX / 2 || part > INT32_MAX / 2 || comb > INT32_MAX / 2) return RG_ERR_UNSUPPORTED;
+    }
+    p.req[cnt].item_start = (int32_t)items;
+    p.req[cnt].part_start = (int32_t)part;
+    p.req[cnt].comb_start = (int32_t)comb;
+    p.total_items = (int32_t)items;
+    p.total_comb = (int32_t)comb;
+    p.grid_items = (int32_t)round_up(items, 8);
+    p.grid_comb = (int32_t)round_up(comb, 8);
+    if (!fits_launch(items, 64 * kKv4Waves) || !fits_launch(comb, kKv4MergeRows * kKv4MergeParts))
+      return RG_ERR_UNSUPPORTED;
+    fp.max_partial_cols = std::max(fp.max_partial_cols, part);
+    if (items > 0) fp.launches.push_back(p);
+  }
+  fp.ml_offset = align256((size_t)fp.max_partial_cols * L->head_dim * sizeof(float));
+  fp.ws_bytes = fp.max_partial_cols ? fp.ml_offset + align256((size_t)fp.max_partial_cols * 2 * sizeof(float)) : 0;
+  return RG_OK;
+}
+
+// Calls f(plan) with the plan of a layout and its branches (or NULL).
+template <typename F>
+rg_status with_kv4_plan(const rg_attn_layout* L, const rg_branch_layout* B, F f) {
+  rg_status st = validate_layout(L);
+  if (st != RG_OK) return st;
+  if (B == nullptr) {
+    Kv4Plan<AttnPlan> fp;
+    st = plan_kv4<AttnPlan, kMaxReqPerLaunch>(L, nullptr, fp);
+    return st != RG_OK ? st : f(fp);
+  }
+  st = validate_branches(L, B);
+  if (st != RG_OK) return st;
+  Kv4Plan<AttnPlanBr> fp;
+  st = plan_kv4<AttnPlanBr, kMaxReqPerLaunchBr>(L, B, fp);
+  return st != RG_OK ? st : f(fp);
+}
+
+float softmax_scale(const rg_attn_layout* L) {
+  return L->sm_scale > 0.f ? L->sm_scale : 1.0f / std::sqrt((float)L->head_dim);
+}
+
+// ---------------------------------------------------------------------------
+rg_status run_mass(const rg_attn_layout* L, const uint16_t* q, const void* keys, bool kv4, const float* lse,
+                   const int32_t* row_count, float decay, float* mass, void* stream) {
+  const rg_status st = validate_layout(L);
+  if (st != RG_OK) return st;
+  if (!q || !keys || !lse || !mass) return RG_ERR_NULL;
+  if (!(decay >= 0.f) || std::isinf(decay)) return RG_ERR_SHAPE;
+  if (!aligned(q, 16) || !aligned(keys, 16) || !aligned(lse, 4) || !aligned(mass, 4) || !aligned(L->page_indices, 4) ||
+      (row_count && !aligned(row_count, 4)))
+    return RG_ERR_UNSUPPORTED;
+  MassArgs a;
+  a.q = q;
+  a.keys = keys;
+  a.lse = lse;
+  a.row_count = row_count;
+  a.mass = mass;
+  a.page_indices = L->page_indices;
+  a.hq = L->num_q_heads;
+  a.hkv = L->num_kv_heads;
+  a.g = a.hq / a.hkv;
+  a.scale_log2 = softmax_scale(L) * 1.4426950408889634f;
+  a.decay = decay;
+  auto items = [&](int r) -> int64_t {
+    // a request without query rows need not own pages for its context
+    if (L->q_indptr[r + 1] == L->q_indptr[r]) return 0;
+    return ((int64_t)L->ctx_len[r] + L->n_verify[r] + kMassKeys - 1) / kMassKeys * L->num_kv_heads;
+  };
+  return each_plan(L, 64 * kMassWaves, items, [&](const AttnPlan& p) {
+    return launch_mass(a, p, L->head_dim, kv4, static_cast<hipStream_t>(stream));
+  });
+}
+
+// ---------------------------------------------------------------------------
+rg_status validate_evict(const rg_evict_layout* L) {
+  if (L == nullptr) return RG_ERR_NULL;
+  if (!L->ctx_len || !L->keep || !L->tracked || !L->evicted || !L->page_indptr || !L->page_indices) return RG_ERR_NULL;
+  if (L->num_requests < 1 || L->num_kv_heads < 1 || L->num_pages < 1) return RG_ERR_SHAPE;
+  if (L->head_dim != 64 && L->head_dim != 128) return RG_ERR_UNSUPPORTED;
+  if (L->page_size != kPageSize) return RG_ERR_UNSUPPORTED;
+  if (L->sink < 0 || L->recent < 0 || L->page_indptr[0] != 0) return RG_ERR_SHAPE;
+  for (int r = 0; r < L->num_requests; ++r) {
+    const int64_t n = L->ctx_len[r], pages = (int64_t)L->page_indptr[r + 1] - L->page_indptr[r];
+    if (n < 0 || pages < 0 || L->keep[r] < 0 || L->evicted[r] < 0) return RG_ERR_SHAPE;
+    if (L->tracked[r] < 0 || L->tracked[r] > n) return RG_ERR_SHAPE;
+    if (n > (int64_t(1) << 30) || n + L->evicted[r] > INT32_MAX) return RG_ERR_UNSUPPORTED;
+    if (pages * kPageSize < n) return RG_ERR_SHAPE;
+    // every protected token has to fit
+    if (L->keep[r] < n && (int64_t)L->sink + L->recent > L->keep[r]) return RG_ERR_SHAPE;
+  }
+  return RG_OK;
+}
+
+// Calls f(plan) for the requests of a layout, a plan's worth at a time.  The
+// launches share the workspace one after another; `words` returns its size.
+template <typename F>
+rg_status each_evict_plan(const rg_evict_layout* L, int64_t& words, F f) {
+  words = 0;
+  for (int r0 = 0; r0 < L->num_requests; r0 += kMaxEvictReq) {
+    EvictPlan p;
+    std::memset(&p, 0, sizeof(p));
+    p.num_req = std::min(kMaxEvictReq, L->num_requests - r0);
+    int64_t ws = 0, moves = 0;
+    for (int k = 0; k < p.num_req; ++k) {
+      const int r = r0 + k;
+      EvictReq& q = p.req[k];
+      q.ctx = L->ctx_len[r];
+      q.keep = std::min(L->keep[r], L->ctx_len[r]);
+      q.tracked = L->tracked[r];
+      q.evicted = L->evicted[r];
+      q.page_start = L->page_indptr[r];
+      q.most = std::min(q.keep, q.ctx - q.keep);
+      q.ws_start = (int32_t)ws;
+      q.move_start = (int32_t)moves;
+      ws += (int64_t)L->num_kv_heads * (4 + 2 * (int64_t)q.most);
+      moves += (int64_t)L->num_kv_heads * ((q.most + kMoveTokens - 1) / kMoveTokens);
+      if (ws > INT32_MAX / 2 || !fits_launch(moves, kMoveThreads)) return RG_ERR_UNSUPPORTED;
+    }
+    if (!fits_launch((int64_t)p.num_req * L->num_kv_heads, kEvictThreads)) return RG_ERR_UNSUPPORTED;
+    p.move_items = (int32_t)moves;
+    p.req[p.num_req].move_start = (int32_t)moves;
+    words = std::max(words, ws);
+    const rg_status st = f(p);
+    if (st != RG_OK) return st;
+  }
+  return RG_OK;
+}
+
+rg_status run_evict(const rg_evict_layout* L, uint8_t* k_cache, uint8_t* v_cache, bool kv4, const float* score,
+                    float* mass, int32_t* positions, void* ws, size_t ws_bytes, void* stream) {
+  rg_status st = validate_evict(L);
+  if (st != RG_OK) return st;
+  if (!k_cache || !v_cache || !score || !positions) return RG_ERR_NULL;
+  if (!aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(score, 4) || !aligned(positions, 4) ||
+      (mass && !aligned(mass, 4)) || !aligned(L->page_indices, 4))
+    return RG_ERR_UNSUPPORTED;
+  int64_t words = 0;
+  st = each_evict_plan(L, words, [](const EvictPlan&) { return RG_OK; });
+  if (st != RG_OK) return st;
+  if (ws == nullptr || ws_bytes < (size_t)words * 4 || !aligned(ws, 16)) return RG_ERR_WORKSPACE;
+  EvictArgs a;
+  a.score = score;
+  a.mass = mass;
+  a.positions = positions;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.page_indices = L->page_indices;
+  a.ws = static_cast<int32_t*>(ws);
+  a.hkv = L->num_kv_heads;
+  a.sink = L->sink;
+  a.recent = L->recent;
+  return each_evict_plan(L, words, [&](const EvictPlan& p) {
+    return launch_evict(a, p, L->head_dim, kv4, static_cast<hipStream_t>(stream)) == hipSuccess ? RG_OK : RG_ERR_HIP;
+  });
+}
+
+}  // namespace
+
+extern "C" {
+
+rg_status rg_kv4_append(const rg_attn_layout* layout, const uint16_t* k, int64_t k_stride, const uint16_t* v,
+                        int64_t v_stride, uint8_t* cache, void* stream) {
+  return run_rows(layout, k, k_stride, v, v_stride, cache, true, stream);
+}
+
+rg_status rg_kv4_read(const rg_attn_layout* layout, const uint8_t* cache, uint16_t* k, int64_t k_stride, uint16_t* v,
+                      int64_t v_stride, void* stream) {
+  return run_rows(layout, k, k_stride, v, v_stride, cache, false, stream);
+}
+
+rg_status rg_kv4_attention_workspace(const rg_attn_layout* layout, const rg_branch_layout* branches, size_t* bytes) {
+  if (bytes == nullptr) return RG_ERR_NULL;
+  return with_kv4_plan(layout, branches, [&](const auto& fp) {
+    *bytes = fp.ws_bytes;
+    return RG_OK;
+  });
+}
+
+rg_status rg_kv4_attention(const rg_attn_layout* layout, const rg_branch_layout* branches, const uint16_t* q,
+                           const uint8_t* cache, uint16_t* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  return with_kv4_plan(layout, branches, [&](const auto& fp) -> rg_status {
+    if (!q || !cache || !out) return RG_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(cache, 16) || !aligned(out, 16) || (lse && !aligned(lse, 4)) ||
+        !aligned(layout->page_indices, 4))
+      return RG_ERR_UNSUPPORTED;
+    if (fp.ws_bytes > 0 && (ws == nullptr || ws_bytes < fp.ws_bytes || !aligned(ws, 16))) return RG_ERR_WORKSPACE;
+    Kv4AttnArgs a;
+    a.q = q;
+    a.cache = cache;
+    a.out = out;
+    a.lse = lse;
+    a.page_indices = layout->page_indices;
+    a.part_o = fp.ws_bytes ? static_cast<float*>(ws) : nullptr;
+    a.part_ml = fp.ws_bytes ? reinterpret_cast<float*>(static_cast<char*>(ws) + fp.ml_offset) : nullptr;
+    a.hq = layout->num_q_heads;
+    a.hkv = layout->num_kv_heads;
+    a.g = a.hq / a.hkv;
+    a.sm_scale = softmax_scale(layout);
+    a.scale_log2 = a.sm_scale * 1.4426950408889634f;
+    a.rescale_gap = 8.0f / a.scale_log2;
+    for (const auto& p : fp.launches)
+      if (launch_kv4_attention(a, p, layout->head_dim, static_cast<hipStream_t>(stream)) != hipSuccess) return RG_ERR_HIP;
+    return RG_OK;
+  });
+}
+
+rg_status rg_attention_mass(const rg_attn_layout* layout, const uint16_t* q, const uint16_t* k_cache, const float* lse,
+                            const int32_t* row_count, float decay, float* mass, void* stream) {
+  return run_mass(layout, q, k_cache, false, lse, row_count, decay, mass, stream);
+}
+
+rg_status rg_kv4_attention_mass(const rg_attn_layout* layout, const uint16_t* q, const uint8_t* cache, const float* lse,
+                                const int32_t* row_count, float decay, float* mass, void* stream) {
+  return run_mass(layout, q, cache, true, lse, row_count, decay, mass, stream);
+}
+
+rg_status rg_evict_workspace(const rg_evict_layout* layout, size_t* bytes) {
+  if (bytes == nullptr) return RG_ERR_NULL;
+  rg_status st = validate_evict(layout);
+  if (st != RG_OK) return st;
+  int64_t words = 0;
+  st = each_evict_plan(layout, words, [](const EvictPlan&) { return RG_OK; });
+  if (st == RG_OK) *bytes = (size_t)words * 4;
+  return st;
+}
+
+rg_status rg_evict_tokens(const rg_evict_layout* layout, uint16_t* k_cache, uint16_t* v_cache, const float* score,
+                          float* mass, int32_t* positions, void* ws, size_t ws_bytes, void* stream) {
+  return run_evict(layout, reinterpret_cast<uint8_t*>(k_cache), reinterpret_cast<uint8_t*>(v_cache), false, score, mass,
+                   positions, ws, ws_bytes, stream);
+}
+
+rg_status rg_kv4_evict_tokens(const rg_evict_layout* layout, uint8_t* cache, const float* score, float* mass,
+                              int32_t* positions, void* ws, size_t ws_bytes, void* stream) {
+  return run_evict(layout, cache, cache, true, score, mass, positions, ws, ws_bytes, stream);
+}
+
+}  // extern "C"

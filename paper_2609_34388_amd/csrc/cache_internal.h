@@ -1,0 +1,86 @@
+// Launch-side structures of the 4-bit KV cache, the attention mass and the
+// eviction of tokens, shared by cache_api.cpp and their kernels.
+#pragma once
+
+#include "rg_internal.h"
+
+namespace rg {
+
+// Rows into, or out of, the 4-bit cache.  Plans: AttnPlan with a work item
+// per page that a request's rows touch.
+struct Kv4RowArgs {
+  uint16_t* k;  // rows (appended: read, read back: written), or NULL
+  uint16_t* v;
+  int64_t k_stride, v_stride;  // elements
+  uint8_t* cache;
+  const int32_t* page_indices;
+  int32_t hkv;
+};
+hipError_t launch_kv4_append(const Kv4RowArgs& a, const AttnPlan& p, int head_dim, hipStream_t stream);
+hipError_t launch_kv4_read(const Kv4RowArgs& a, const AttnPlan& p, int head_dim, hipStream_t stream);
+
+// Attention over the 4-bit cache.
+constexpr int kKv4Waves = 4;                       // waves of a work group
+constexpr int kKv4Cols = 32 * kKv4Waves;           // query columns of a work group at most
+constexpr int kKv4MergeRows = 64;                  // 16-byte rows of a merge item
+constexpr int kKv4MergeParts = 4;                  // threads of a row where requests have many chunks
+struct Kv4AttnArgs {
+  const uint16_t* q;
+  const uint8_t* cache;
+  uint16_t* out;
+  float* lse;
+  const int32_t* page_indices;
+  float* part_o;   // per 32-column tile: 32 x D fp32 sums, 16-byte rows lane-interleaved
+  float* part_ml;  // [partial columns][2] (running maximum of raw scores, sum)
+  int32_t hq, hkv, g;
+  float sm_scale, scale_log2, rescale_gap;
+};
+hipError_t launch_kv4_attention(const Kv4AttnArgs& a, const AttnPlan& p, int head_dim, hipStream_t stream);
+hipError_t launch_kv4_attention(const Kv4AttnArgs& a, const AttnPlanBr& p, int head_dim, hipStream_t stream);
+
+// Attention mass.  Plans: AttnPlan with work items (KV head, kMassKeys keys).
+constexpr int kMassWaves = 4;
+constexpr int kMassSub = 2;                              // 32-key tiles of a wave
+constexpr int kMassKeys = 32 * kMassWaves * kMassSub;    // keys of a work item
+struct MassArgs {
+  const uint16_t* q;
+  const void* keys;  // bf16 K pool, or the 4-bit pool
+  const float* lse;
+  const int32_t* row_count;  // or NULL
+  float* mass;
+  const int32_t* page_indices;
+  int32_t hq, hkv, g;
+  float scale_log2, decay;
+};
+hipError_t launch_mass(const MassArgs& a, const AttnPlan& p, int head_dim, bool kv4, hipStream_t stream);
+
+// Eviction.
+constexpr int kEvictThreads = 1024;  // select: a work group per (request, KV head)
+constexpr int kMoveThreads = 256;
+constexpr int kMoveTokens = 16;      // move: tokens of a work group
+struct EvictReq {
+  int32_t ctx, keep, tracked, evicted;  // keep <= ctx
+  int32_t page_start;
+  int32_t ws_start;    // first word of the request's move lists in the workspace
+  int32_t most;        // moves of a head at most
+  int32_t move_start;  // first move item
+};
+constexpr int kMaxEvictReq = 96;
+struct EvictPlan {
+  int32_t num_req, move_items;
+  EvictReq req[kMaxEvictReq + 1];
+};
+static_assert(sizeof(EvictPlan) <= 3700, "plan must fit the kernel argument block");
+struct EvictArgs {
+  const float* score;
+  float* mass;  // or NULL
+  int32_t* positions;
+  uint8_t* k_cache;  // bf16 K pool, or the 4-bit pool
+  uint8_t* v_cache;  // bf16 V pool
+  const int32_t* page_indices;
+  int32_t* ws;       // per (request, head): count, 3 words free, then (to, from) pairs
+  int32_t hkv, sink, recent;
+};
+hipError_t launch_evict(const EvictArgs& a, const EvictPlan& p, int head_dim, bool kv4, hipStream_t stream);
+
+}  // namespace rg
