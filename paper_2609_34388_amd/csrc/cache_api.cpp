@@ -81,32 +81,80 @@ struct Kv4Plan {
   size_t ml_offset = 0, ws_bytes = 0;
 };
 
+// Column groups of a request: `full` of four tiles, then one of `rest` tiles
+// unless that is 0.
+struct Kv4Cols {
+  int64_t full;
+  int rest;
+};
+Kv4Cols kv4_cols(const rg_attn_layout* L, int r) {
+  const int64_t M = (int64_t)(L->q_indptr[r + 1] - L->q_indptr[r]) * (L->num_q_heads / L->num_kv_heads);
+  const int64_t tiles = (M + 31) / 32;
+  return {tiles / kKv4Waves, (int)(tiles % kKv4Waves)};
+}
+
+// Units (kv4_rate) of a work item at most: the least that gives one round of
+// items on the compute units (two work groups each, at head size 64 three), or
+// as many rounds as keep items below kKv4Long units: a long round ends unevenly.
+// Measured on 40 requests of 8k to 32k keys (GPU time of the call, merge
+// included): items of up to 4500 units, one round, 603 us, two rounds 580,
+// three 571, four 575; on 16 requests of 1k to 8k keys with branches one round
+// 85.4 us, two 92, three 122.
+constexpr int kKv4Least = 32, kKv4Long = 3072;
+int kv4_target(const rg_attn_layout* L, int cus) {
+  const int64_t slots = (int64_t)(L->head_dim == 64 ? 3 : 2) * cus;
+  struct Group {
+    int T, tiles;
+    int64_t count;
+  };
+  std::vector<Group> groups;
+  int64_t work = 0, least = 0;
+  for (int r = 0; r < L->num_requests; ++r) {
+    const Kv4Cols c = kv4_cols(L, r);
+    const int T = L->ctx_len[r] + (L->q_indptr[r + 1] - L->q_indptr[r]);
+    auto add = [&](int tiles, int64_t count) {
+      if (count == 0) return;
+      groups.push_back({T, tiles, count});
+      least += count;
+      work += count * ((T + 31) / 32) * kv4_rate(tiles);
+    };
+    add(kKv4Waves, c.full * L->num_kv_heads);
+    add(c.rest, c.rest ? L->num_kv_heads : 0);
+  }
+  auto fit = [&](int64_t rounds) {  // the least target whose items fit the rounds
+    for (int64_t t = std::max<int64_t>(env_int("KV4_MIN", kKv4Least), work / (rounds * slots));; t += 1 + t / 16) {
+      int64_t items = 0;
+      for (const Group& q : groups) items += q.count * kv4_runs(q.T, q.tiles, (int)std::min<int64_t>(t, INT32_MAX)).count;
+      if (items <= std::max(least, rounds * slots)) return t;
+    }
+  };
+  const int64_t one = fit(1), lim = env_int("KV4_LIM", kKv4Long);
+  return (int)std::min<int64_t>(INT32_MAX, one <= lim ? one : fit((one + lim - 1) / lim));
+}
+
 template <typename Plan, int MaxReq>
 rg_status plan_kv4(const rg_attn_layout* L, const rg_branch_layout* B, Kv4Plan<Plan>& fp) {
-  const int R = L->num_requests, hkv = L->num_kv_heads, g = L->num_q_heads / hkv;
-  const int cus = device_cus();
-  std::vector<int64_t> pair_keys;
-  for (int r = 0; r < R; ++r) {
-    const int64_t n = L->q_indptr[r + 1] - L->q_indptr[r];
-    const int64_t ncg = (n * g + kKv4Cols - 1) / kKv4Cols;
-    for (int64_t cg = 0; cg < ncg; ++cg) pair_keys.push_back(L->ctx_len[r] + n);
-  }
-  const int chunk = choose_chunk(pair_keys, hkv, 2 * cus);
+  const int R = L->num_requests, hkv = L->num_kv_heads;
+  const int target = kv4_target(L, device_cus());
+  auto runs_of = [&](int r, int tiles) {
+    return kv4_runs(L->ctx_len[r] + (L->q_indptr[r + 1] - L->q_indptr[r]), tiles, target);
+  };
+  // Costliest work items first.
   std::vector<int> order(R);
   std::iota(order.begin(), order.end(), 0);
-  auto keys_of = [&](int r) {
-    const int64_t n = L->q_indptr[r + 1] - L->q_indptr[r];
-    return n == 0 ? int64_t(0) : L->ctx_len[r] + n;
-  };
-  std::stable_sort(order.begin(), order.end(), [&](int x, int y) {
-    return std::min<int64_t>(chunk, keys_of(x)) > std::min<int64_t>(chunk, keys_of(y));
-  });
+  std::vector<int64_t> cost(R);
+  for (int r = 0; r < R; ++r) {
+    const Kv4Cols c = kv4_cols(L, r);
+    if (c.full) cost[r] = (int64_t)runs_of(r, kKv4Waves).keys * kv4_rate(kKv4Waves);
+    if (c.rest) cost[r] = std::max(cost[r], (int64_t)runs_of(r, c.rest).keys * kv4_rate(c.rest));
+  }
+  std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return cost[x] > cost[y]; });
   for (int r0 = 0; r0 < R; r0 += MaxReq) {
     const int cnt = std::min(MaxReq, R - r0);
     Plan p;
     std::memset(&p, 0, sizeof(p));
     p.num_req = cnt;
-    p.chunk = chunk;
+    p.chunk = target;
     p.cols_per_group = kKv4Cols;
     int64_t items = 0, part = 0, comb = 0;
     for (int k = 0; k < cnt; ++k) {
@@ -122,13 +170,17 @@ rg_status plan_kv4(const rg_attn_layout* L, const rg_branch_layout* B, Kv4Plan<P
       q.part_start = (int32_t)part;
       q.comb_start = (int32_t)comb;
       if (n == 0) continue;
-      const int64_t M = n * g, nch = (L->ctx_len[r] + n + chunk - 1) / chunk;
-      items += hkv * ((M + kKv4Cols - 1) / kKv4Cols) * nch;
-      if (nch > 1) {
+      const Kv4Cols c = kv4_cols(L, r);
+      auto add = [&](int tiles, int64_t groups) {
+        const int64_t nch = runs_of(r, tiles).count;
+        items += hkv * groups * nch;
+        if (nch == 1) return;
         p.max_chunks = std::max<int32_t>(p.max_chunks, (int32_t)nch);
-        part += hkv * nch * round_up(M, 32);
-        comb += hkv * ((M + 31) / 32) * (L->head_dim / 8);
-      }
+        part += hkv * groups * nch * 32 * tiles;
+        comb += hkv * groups * tiles * (L->head_dim / 8);
+      };
+      if (c.full) add(kKv4Waves, c.full);
+      if (c.rest) add(c.rest, 1);
       if (items > INT32_MAX / 2 || part > INT32_MAX / 2 || comb > INT32_MAX / 2) return RG_ERR_UNSUPPORTED;
     }
     p.req[cnt].item_start = (int32_t)items;

@@ -24,6 +24,22 @@ constexpr int kKv4Waves = 4;                       // waves of a work group
 constexpr int kKv4Cols = 32 * kKv4Waves;           // query columns of a work group at most
 constexpr int kKv4MergeRows = 64;                  // 16-byte rows of a merge item
 constexpr int kKv4MergeParts = 4;                  // threads of a row where requests have many chunks
+// A request's 32-column tiles form column groups of four, and a last one of
+// what remains.  Time of 32 keys in a group of 1 .. 4 tiles, in units of a
+// sixteenth of that of four: the vector instructions of a wave on one tile and
+// on two (which share the decoding) are as 5 to 8.
+__host__ __device__ inline int kv4_rate(int tiles) { return tiles == 1 ? 5 : tiles == 2 ? 8 : tiles == 3 ? 13 : 16; }
+// Runs that the T keys of such a group are cut into, for items of at most
+// `target` units, and the keys of each: all but the last alike.
+struct Kv4Runs {
+  int count, keys;
+};
+__host__ __device__ inline Kv4Runs kv4_runs(int T, int tiles, int target) {
+  const int steps = (T + 31) / 32;
+  const int most = target / kv4_rate(tiles) > 1 ? target / kv4_rate(tiles) : 1;  // steps of a run at most
+  const int n = (steps + most - 1) / most, each = (steps + n - 1) / n;
+  return {(steps + each - 1) / each, 32 * each};
+}
 struct Kv4AttnArgs {
   const uint16_t* q;
   const uint8_t* cache;

@@ -1,16 +1,20 @@
 // Hybrid-mask attention over the 4-bit paged cache (gfx950): the mask, the
 // columns and the split over keys of attention.hip, on a quarter of the bytes.
 //
-// A work item is (request, KV head, column group of up to 128 columns, run of
-// keys).  Its four waves are (32-column tiles) x (key groups): one tile gives
-// four key groups, two tiles two each, three or four tiles one.  A wave reads
-// its keys' codes straight from the pool into registers, as the block is laid
-// out for that: a lane's 16 bytes of K codes are the 32 dims of one scale
-// group of its key, and its 16 bytes of V codes are 8 tokens of its D / 32
-// dims, the operand rows of S^T = K Q^T and O^T += V^T P^T.  So the main loop
-// has no LDS and no barrier, and a decoded element costs half a conversion
-// (v_cvt_scalef32_pk_bf16_fp4, which multiplies by the group's scale), for V
-// plus half a byte permutation that pairs two tokens.
+// A work item is (request, KV head, column group of up to four 32-column tiles,
+// run of keys).  A wave holds one or two of the tiles (two share every decoded
+// element: decoding is more than half of a tile's vector instructions) and
+// takes every kg-th 32-key tile of the run: one pair of tiles gives the four
+// waves four key groups, two pairs two each.
+//
+// A wave reads its keys' codes straight from the pool into registers, as the
+// block is laid out for that: a lane's 16 bytes of K codes are the 32 dims of
+// one scale group of its key, and its 16 bytes of V codes are 8 tokens of its
+// D / 32 dims, the operand rows of S^T = K Q^T and O^T += V^T P^T.  So keys
+// need no LDS and the main loop no barrier, and a decoded element costs half a
+// conversion (v_cvt_scalef32_pk_bf16_fp4, which multiplies by the group's
+// scale), for V plus half a byte permutation that pairs two tokens.  Q is read
+// from LDS for each key tile; in registers it would leave one wave per SIMD.
 //
 // The dims go through the products in another order than in memory: K step ks
 // of S^T holds dims 64 (ks / 4) + 32 lh + 8 (ks % 4) .. + 7 of half-wave lh (Q
@@ -27,269 +31,396 @@ namespace {
 
 constexpr int kThreads = 64 * kKv4Waves;
 
-// A lane's codes of a 32-key tile: K of its key (scale groups lh, 2 + lh of
-// its token), V of tokens 8 lh .. 8 lh + 7 of both pages.
-template <int D>
-struct Tile4 {
-  u32x4 kc[D / 64];
-  uint32_t ks;
-  uint32_t vc[2][D / 32];
-  u32x2 vs[2];
+// Scale byte E of a word as a float whose exponent is the byte, all that the
+// conversion takes of its scale (the other bits are the word's other bytes).
+template <int E>
+__device__ __forceinline__ float scale_at(uint32_t word) {
+  return __uint_as_float(E < 3 ? word << (23 - 8 * E) : word >> 1);
+}
+
+// 16 bytes of every lane from base + off to LDS, byte `lds` + 16 * lane.  No
+// register waits for the data: they are there once s_waitcnt vmcnt says so.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const uint8_t* base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+
+// What a work group of a wave's tiles works on.
+struct Kv4Item {
+  int hk, kbeg, kend;  // KV head, keys of the run
+  int c, nch;          // the run, of how many
+  int n, L, M;         // rows, context, columns of the request
+  int tile0, nct;      // first tile, tiles of the column group
+  int part;            // first partial column of the item
 };
 
-template <int D, typename Plan>
-__global__ __launch_bounds__(kThreads, 2) void kv4_attn_kernel(Kv4AttnArgs a, Plan p) {
+template <int D>
+struct Kv4Shape {
+  static constexpr int DT = D / 32;
+  static constexpr int QROW = 2 * D + 16;             // bytes of a column of Q in LDS: 16 more, so that
+                                                      // a fragment read meets every bank once
+  static constexpr int STATE = 64 * 16 * DT + 128;    // floats of a wave's state of one tile
+  static constexpr int RING = 2;                      // key tiles of a wave in LDS
+  static constexpr int SLOT = 2 * Kv4<D>::BLOCK;      // bytes of one: two blocks
+  static constexpr int LOADS = 2 * ((Kv4<D>::BLOCK + 1023) / 1024);  // load instructions of one
+  // The rings come first: a load to LDS takes a 16-bit place.  Q behind them.
+  static constexpr int Q = kKv4Waves * RING * SLOT;
+  static constexpr int LDS = Q + kKv4Cols * QROW;
+  static_assert(Q <= 1 << 16, "places of loads to LDS");
+  static_assert((kKv4Waves - 1) * STATE * 4 <= LDS, "the states fit where Q and the codes were");
+};
+
+// The TILES column tiles of this wave: pair `pair` of `np`, key group `kgi`.
+template <int D, int TILES, typename Plan, typename Req>
+__device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, const Kv4Item& it, int pair, int np, int kgi,
+                                         char* lds) {
   using B = Kv4<D>;
+  using S = Kv4Shape<D>;
   constexpr bool BR = !__is_same(Plan, AttnPlan);
-  constexpr int DT = D / 32, KSTEPS = D / 16;
-  constexpr int SLOT = 64 * 16 * DT + 128;  // floats of a wave's state in LDS
-  __shared__ __attribute__((aligned(16))) float area[(kKv4Waves - 1) * SLOT];
-
-  const int item = p.num_req == 1 ? xcd_item(p.grid_items) : (int)blockIdx.x;
-  if (item >= p.total_items) return;
-  const int r = find_request(p, item, false);
-  const auto rq = request_of(p, r);
-  const int n = rq.nv & 0xffff, L = rq.ctx, T = L + n;
-  const int g = a.g;
-  const int M = n * g;
-  const int tiles = (M + 31) / 32, ncg = (M + kKv4Cols - 1) / kKv4Cols;
-  const int tpg = (tiles + ncg - 1) / ncg;  // tiles are dealt evenly to the column groups
-  const int nch = (T + p.chunk - 1) / p.chunk;
-  int local = item - rq.item_start;
-  const int c = local % nch;
-  local /= nch;
-  const int hk = local % a.hkv;
-  const int cg = local / a.hkv;
-  const int kbeg = c * p.chunk, kend = min(T, kbeg + p.chunk);
-
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lc = lane & 31, lh = lane >> 5;
-  const int nct = min(tpg, tiles - cg * tpg);
-  const int per = nct == 1 ? 1 : nct == 2 ? 2 : 4;  // waves of one key group
-  const int ct = wave % per, kg = kKv4Waves / per, kgi = wave / per;
-  if (ct >= nct) return;  // the fourth wave of three tiles; no merge waits for it
-
-  const int col = (cg * tpg + ct) * 32 + lc;
-  const bool valid = col < M;
-  const int tok = valid ? col / g : 0;
-  const int hh = col - tok * g;
-  int lim, slo, shi;
-  key_limits(rq, valid, tok, kend, lim, slo, shi);
-  int wave_min_lim = valid ? lim : kend;
-  for (int off = 32; off >= 1; off >>= 1) wave_min_lim = min(wave_min_lim, __shfl_xor(wave_min_lim, off));
-
-  bf16x8 qf[KSTEPS];
-  {
-    const uint16_t* qrow = a.q + ((size_t)(rq.q_start + tok) * a.hq + hk * g + hh) * D;
-#pragma unroll
-    for (int s = 0; s < KSTEPS; ++s) {
-      u32x4 w = {0u, 0u, 0u, 0u};
-      if (valid) w = *(const u32x4*)(qrow + 64 * (s / 4) + 32 * lh + 8 * (s % 4));
-      qf[s] = __builtin_bit_cast(bf16x8, w);
-    }
-  }
-
-  f32x16 acc[DT];
-  for (int dt = 0; dt < DT; ++dt)
-    for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
-  float m_run = kNegInf, l_run = 0.f;
+  constexpr int DT = D / 32;
+  const int lane = threadIdx.x & 63, lc = lane & 31, lh = lane >> 5;
+  const int kg = kKv4Waves / np, g = a.g;
+  const int kbeg = it.kbeg, kend = it.kend;
 
   typedef const int32_t __attribute__((address_space(4))) * cpage_ptr;
   const int pg0 = kbeg / kPageSize;
   const int npg = (kend + kPageSize - 1) / kPageSize - pg0;
   const cpage_ptr pages = (cpage_ptr)(a.page_indices + rq.page_start + pg0);
-  const uint8_t* pool = a.cache + (size_t)hk * B::BLOCK;
+  const uint8_t* pool = a.cache + (size_t)it.hk * B::BLOCK;
   const size_t page_bytes = (size_t)a.hkv * B::BLOCK;
   const int ktok = swap23(lc) & 15;
-  const uint32_t koff = (uint32_t)(ktok * 32 + 16 * lh), ksoff = (uint32_t)B::k_scale(ktok, 0);
-  const uint32_t voff = (uint32_t)B::v_unit(8 * lh, lc), vsoff = (uint32_t)B::v_scale(8 * lh, lc * DT / 32);
+  const char* qlane = lds + S::Q + (2 * pair * 32 + lc) * S::QROW + 64 * lh;
 
-  // Pages of tile j of the run; one past the run's last page is that page again.
-  auto load = [&](int j) {
-    Tile4<D> t;
-    const uint8_t* b0 = pool + (size_t)pages[2 * j] * page_bytes;
-    const uint8_t* b1 = pool + (size_t)pages[min(2 * j + 1, npg - 1)] * page_bytes;
-    const uint8_t* bk = lc < 16 ? b0 : b1;
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) t.kc[i] = *(const u32x4*)(bk + koff + 512 * i);
-    t.ks = D == 128 ? *(const uint32_t*)(bk + ksoff) : *(const uint16_t*)(bk + ksoff);
+  // The wave's ring of key tiles in LDS: both blocks as they lie in the pool.
+  // The loads of a tile go out two tiles ahead; a lane's share of a block is
+  // read from LDS when it is needed.
+  const int wave = kgi * np + pair;
+  char* ring = lds + wave * S::RING * S::SLOT;
+  const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
+  const int koff = (lc < 16 ? 0 : B::BLOCK) + ktok * 32 + 16 * lh;
+  const int ksoff = (lc < 16 ? 0 : B::BLOCK) + B::k_scale(ktok, 0);
+  const int voff = B::v_unit(8 * lh, lc), vsoff = B::v_scale(8 * lh, lc * DT / 32);
+  const int ntile = (kend - kbeg + 31) / 32;
+  // Pages of key tile j; past the run's last page that page again.
+  struct Pair {
+    int p0, p1;
+  };
+  auto pages_of = [&](int j) { return Pair{pages[min(2 * j, npg - 1)], pages[min(2 * j + 1, npg - 1)]}; };
+  auto load = [&](int slot, Pair x) {
 #pragma unroll
     for (int pp = 0; pp < 2; ++pp) {
-      const uint8_t* b = pp ? b1 : b0;
-      if constexpr (D == 128) {
-        const u32x4 w = *(const u32x4*)(b + voff);
-        for (int e = 0; e < 4; ++e) t.vc[pp][e] = w[e];
-      } else {
-        const u32x2 w = *(const u32x2*)(b + voff);
-        for (int e = 0; e < 2; ++e) t.vc[pp][e] = w[e];
-      }
-      t.vs[pp] = *(const u32x2*)(b + vsoff);
+      const uint8_t* b = pool + (size_t)(pp ? x.p1 : x.p0) * page_bytes;
+      const uint32_t to = ring_at + slot * S::SLOT + pp * B::BLOCK;
+#pragma unroll
+      for (int at = 0; at < B::BLOCK; at += 1024)
+        if (at + 1024 <= B::BLOCK || at + 16 * lane < B::BLOCK) load_to_lds(to + at, b + at, 16 * lane);
     }
-    return t;
   };
 
-  auto compute = [&](Tile4<D>& t, int kbase) {
-    f32x16 sc;
-    for (int i = 0; i < 16; ++i) sc[i] = 0.f;
-    const uint32_t kscale = t.ks >> (8 * lh);
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-      const float s = scale_of((kscale >> (16 * i)) & 0xff);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, decode8(t.kc[i][e], s)), qf[4 * i + e], sc,
-                                                     0, 0, 0);
+  Pair ahead{0, 0};
+  if (kgi < ntile) {
+    load(0, pages_of(kgi));
+    if (kgi + kg < ntile) load(1, pages_of(kgi + kg));
+    ahead = pages_of(kgi + 2 * kg);
+  }
+  // Q of the column group, by the whole work group, behind the first codes.
+  for (int u = threadIdx.x; u < it.nct * 32 * (D / 8); u += kThreads) {
+    const int row = u / (D / 8), ch = u % (D / 8), col = it.tile0 * 32 + row;
+    u32x4 x = {0u, 0u, 0u, 0u};
+    if (col < it.M) {
+      const int tok = col / g;
+      x = *(const u32x4*)(a.q + ((size_t)(rq.q_start + tok) * a.hq + it.hk * g + (col - tok * g)) * D + 8 * ch);
     }
-    if (kbase + 32 > wave_min_lim) {
+    *(u32x4*)(lds + S::Q + row * S::QROW + 16 * ch) = x;
+  }
+  int lim[TILES], slo[TILES], shi[TILES], min_lim[TILES];
+  bool open[TILES];  // some column that sees keys of the run has no reference yet
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = kbase + 16 * (i >> 3) + 8 * lh + 4 * ((i >> 2) & 1) + (i & 3);
-        if (key >= lim && (!BR || (uint32_t)(key - slo) >= (uint32_t)(shi - slo))) sc[i] = kNegInf;
+  for (int u = 0; u < TILES; ++u) {
+    const int col = (it.tile0 + 2 * pair + u) * 32 + lc;
+    key_limits(rq, col < it.M, col / g, kend, lim[u], slo[u], shi[u]);
+    int m = col < it.M ? lim[u] : kend;
+    for (int off = 32; off >= 1; off >>= 1) m = min(m, __shfl_xor(m, off));
+    min_lim[u] = __builtin_amdgcn_readfirstlane(m);
+    open[u] = true;
+  }
+
+  f32x16 acc[TILES][DT];
+  float m_run[TILES], l_run[TILES];
+#pragma unroll
+  for (int u = 0; u < TILES; ++u) {
+    for (int dt = 0; dt < DT; ++dt)
+      for (int i = 0; i < 16; ++i) acc[u][dt][i] = 0.f;
+    m_run[u] = kNegInf;
+    l_run[u] = 0.f;
+  }
+
+  lds_barrier();
+
+  int slot = 0;
+  for (int j = kgi; j < ntile; j += kg, slot ^= 1) {
+    const int kbase = kbeg + 32 * j;
+    if (j + kg < ntile) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(S::LOADS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const char* code = ring + slot * S::SLOT;
+    u32x4 kc[D / 64];
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) kc[i] = *(const u32x4*)(code + koff + 512 * i);
+    const uint32_t kscale = (D == 128 ? *(const uint32_t*)(code + ksoff) : *(const uint16_t*)(code + ksoff)) >> (8 * lh);
+    f32x16 sc[TILES];
+#pragma unroll
+    for (int u = 0; u < TILES; ++u)
+      for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
+    {
+      // Q fragments are read two K steps ahead
+      constexpr int N = D / 16, AHEAD = 2;
+      bf16x8 qf[AHEAD + 1][TILES];
+      auto read_q = [&](int s) {
+#pragma unroll
+        for (int u = 0; u < TILES; ++u)
+          qf[s % (AHEAD + 1)][u] = *(const bf16x8*)(qlane + u * 32 * S::QROW + 128 * (s / 4) + 16 * (s % 4));
+      };
+#pragma unroll
+      for (int s = 0; s < AHEAD; ++s) read_q(s);
+#pragma unroll
+      for (int s = 0; s < N; ++s) {
+        if (s + AHEAD < N) read_q(s + AHEAD);
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, decode8(kc[s / 4][s % 4], s < 4 ? scale_at<0>(kscale) : scale_at<2>(kscale)));
+#pragma unroll
+        for (int u = 0; u < TILES; ++u)
+          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s % (AHEAD + 1)][u], sc[u], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
       }
+    }
+    u32x4 pk[TILES][2];
+#pragma unroll
+    for (int u = 0; u < TILES; ++u) {
+      if (kbase + 32 > min_lim[u]) {
+        // key - kbase = 8 lh + place, place a constant of i
+        const int seen = lim[u] - kbase - 8 * lh, from = slo[u] - kbase - 8 * lh, to = shi[u] - kbase - 8 * lh;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int place = 16 * (i >> 3) + 4 * ((i >> 2) & 1) + (i & 3);
+          if (place >= seen && (!BR || place < from || place >= to)) sc[u][i] = kNegInf;
+        }
+      }
+      // P against the running reference, a maximum of earlier scores.  A sum
+      // of a lane's 16 past 2^12 (overflow included), or a column without a
+      // reference, moves the references to the maxima of this tile: P stays
+      // below 2^12, and no maximum is taken where nothing moves.
+      float sum;
+      auto weigh = [&]() {
+        const float mc = (m_run[u] == kNegInf) ? 0.f : m_run[u] * a.scale_log2;
+        sum = 0.f;
+#pragma unroll
+        for (int pp = 0; pp < 2; ++pp)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u][8 * pp + 2 * e], a.scale_log2, -mc));
+            const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u][8 * pp + 2 * e + 1], a.scale_log2, -mc));
+            sum += x + y;
+            pk[u][pp][e] = pack_bf16x2(x, y);
+          }
+      };
+      weigh();
+      if (open[u] || __any(!(sum <= 4096.f))) {
+        float mx = sc[u][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[u][i]);
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        const float m_new = fmaxf(m_run[u], fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
+        const float alpha = m_new == kNegInf ? 1.f : __builtin_amdgcn_exp2f((m_run[u] - m_new) * a.scale_log2);
+        l_run[u] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[u][dt][i] *= alpha;
+        m_run[u] = m_new;
+        open[u] = __any(m_new == kNegInf && (lim[u] > kbeg || (BR && shi[u] > max(slo[u], kbeg))));
+        weigh();
+      }
+      l_run[u] += sum;
+    }
+    uint32_t vc[2][DT];
+    u32x2 vs[2];
+#pragma unroll
+    for (int pp = 0; pp < 2; ++pp) {
+      if constexpr (D == 128) {
+        const u32x4 w = *(const u32x4*)(code + pp * B::BLOCK + voff);
+        for (int e = 0; e < 4; ++e) vc[pp][e] = w[e];
+      } else {
+        const u32x2 w = *(const u32x2*)(code + pp * B::BLOCK + voff);
+        for (int e = 0; e < 2; ++e) vc[pp][e] = w[e];
+      }
+      vs[pp] = *(const u32x2*)(code + pp * B::BLOCK + vsoff);
+    }
+    if (j + 2 * kg < ntile) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot is read
+      load(slot, ahead);
+      ahead = pages_of(j + 3 * kg);
     }
     if (kbase + 32 > kend) {
       // Slots past the last key may hold anything: scale bytes of infinity
       // become those of small numbers, which weigh zero.
 #pragma unroll
-      for (int pp = 0; pp < 2; ++pp)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (kbase + 16 * pp + 8 * lh + e >= kend) t.vs[pp][e >> 2] = (t.vs[pp][e >> 2] & ~(0xffu << (8 * (e & 3)))) | (1u << (8 * (e & 3)));
-    }
-    float mx = sc[0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
-    {
-      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-      mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-    }
-    // The reference maximum moves when a score exceeds it by 2^8 in
-    // probability: P stays below 256, and the sums are rescaled rarely.
-    const bool grew = mx > m_run + a.rescale_gap;
-    if (__any(grew)) {
-      const float m_new = grew ? mx : m_run;
-      const float alpha = grew ? __builtin_amdgcn_exp2f((m_run - m_new) * a.scale_log2) : 1.f;
-      l_run *= alpha;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
-      m_run = m_new;
-    }
-    const float mc = (m_run == kNegInf) ? 0.f : m_run * a.scale_log2;
-    u32x4 pk[2];
-#pragma unroll
-    for (int pp = 0; pp < 2; ++pp)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[8 * pp + 2 * e], a.scale_log2, -mc));
-        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[8 * pp + 2 * e + 1], a.scale_log2, -mc));
-        l_run += x + y;
-        pk[pp][e] = pack_bf16x2(x, y);
+      for (int pp = 0; pp < 2; ++pp) {
+        const int live = min(max(kend - kbase - 16 * pp - 8 * lh, 0), 8);
+        const uint64_t keep = live == 8 ? ~0ull : (1ull << (8 * live)) - 1;
+        const uint64_t w = (((uint64_t)vs[pp][1] << 32 | vs[pp][0]) & keep) | (0x0101010101010101ull & ~keep);
+        vs[pp] = u32x2{(uint32_t)w, (uint32_t)(w >> 32)};
       }
+    }
 #pragma unroll
     for (int pp = 0; pp < 2; ++pp) {
       u32x4 vf[DT];
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {  // tokens 2 w, 2 w + 1 of the lane's eight
-        const float s0 = scale_of((t.vs[pp][w >> 1] >> (16 * (w & 1))) & 0xff);
-        const float s1 = scale_of((t.vs[pp][w >> 1] >> (16 * (w & 1) + 8)) & 0xff);
-        auto pair = [&](int dt, uint32_t x, uint32_t y) {  // dims dt, dt + 1 of both tokens
+      // tokens 2 w, 2 w + 1 of the lane's eight
+      auto unit = [&](int w, uint32_t codes, float s0, float s1) {
+        auto both = [&](int dt, uint32_t x, uint32_t y) {  // dims dt, dt + 1 of both tokens
           vf[dt][w] = __builtin_amdgcn_perm(y, x, 0x05040100u);
           vf[dt + 1][w] = __builtin_amdgcn_perm(y, x, 0x07060302u);
         };
         if constexpr (D == 128) {
-          const uint32_t u = t.vc[pp][w];
-          pair(0, decode2<0>(u, s0), decode2<2>(u, s1));
-          pair(2, decode2<1>(u, s0), decode2<3>(u, s1));
+          both(0, decode2<0>(codes, s0), decode2<2>(codes, s1));
+          both(2, decode2<1>(codes, s0), decode2<3>(codes, s1));
+        } else if (w & 1) {
+          both(0, decode2<2>(codes, s0), decode2<3>(codes, s1));
         } else {
-          const uint32_t u = t.vc[pp][w >> 1];
-          if (w & 1) pair(0, decode2<2>(u, s0), decode2<3>(u, s1));
-          else pair(0, decode2<0>(u, s0), decode2<1>(u, s1));
+          both(0, decode2<0>(codes, s0), decode2<1>(codes, s1));
         }
+      };
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const uint32_t w = vs[pp][x];
+        unit(2 * x, vc[pp][D == 128 ? 2 * x : x], scale_at<0>(w), scale_at<1>(w));
+        unit(2 * x + 1, vc[pp][D == 128 ? 2 * x + 1 : x], scale_at<2>(w), scale_at<3>(w));
       }
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[dt]),
-                                                          __builtin_bit_cast(bf16x8, pk[pp]), acc[dt], 0, 0, 0);
-    }
-  };
-
-  const int ntile = (kend - kbeg + 31) / 32;
-  if (kgi < ntile) {
-    Tile4<D> cur = load(kgi);
-    for (int j = kgi; j < ntile; j += kg) {
-      Tile4<D> next = cur;
-      if (j + kg < ntile) next = load(j + kg);
-      compute(cur, kbeg + 32 * j);
-      cur = next;
+      for (int u = 0; u < TILES; ++u)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          acc[u][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[dt]),
+                                                               __builtin_bit_cast(bf16x8, pk[u][pp]), acc[u][dt], 0, 0, 0);
     }
   }
 
-  // Element f of run i4 of a lane: dim 8 DT i4 + 4 DT lh + f, f < 4 DT.
-  auto at = [&](int i4, int f) { return acc[f % DT][4 * i4 + f / DT]; };
-  float l_tot = l_run + __shfl_xor(l_run, 32);
-  if (kg > 1) {  // key groups meet in LDS (lane-wise: same columns, same dims)
-    if (kgi > 0) {
-      float* slot = area + (wave - 1) * SLOT;
+  // The key groups' states meet in LDS, one tile of a wave at a time
+  // (lane-wise: same columns, same dims), and key group 0 writes the result.
+  float* area = reinterpret_cast<float*>(lds);
 #pragma unroll
-      for (int v = 0; v < 4 * DT; ++v)
-        *(float4*)(slot + (v * 64 + lane) * 4) = make_float4(at(v / DT, 4 * (v % DT)), at(v / DT, 4 * (v % DT) + 1),
-                                                             at(v / DT, 4 * (v % DT) + 2), at(v / DT, 4 * (v % DT) + 3));
-      slot[64 * 16 * DT + lane] = m_run;
-      slot[64 * 16 * DT + 64 + lane] = l_tot;
+  for (int u = 0; u < 2; ++u) {
+    if (u == 1 && it.nct == 1) break;
+    lds_barrier();  // Q, or the states before, are no longer read
+    if (u < TILES && kgi > 0) {
+      float* slot = area + ((kgi - 1) * np + pair) * S::STATE;
+#pragma unroll
+      for (int v = 0; v < 4 * DT; ++v) {
+        const int i4 = v / DT, f = 4 * (v % DT);
+        *(float4*)(slot + (v * 64 + lane) * 4) =
+            make_float4(acc[u % TILES][f % DT][4 * i4 + f / DT], acc[u % TILES][(f + 1) % DT][4 * i4 + (f + 1) / DT],
+                        acc[u % TILES][(f + 2) % DT][4 * i4 + (f + 2) / DT], acc[u % TILES][(f + 3) % DT][4 * i4 + (f + 3) / DT]);
+      }
+      slot[64 * 16 * DT + lane] = m_run[u % TILES];
+      slot[64 * 16 * DT + 64 + lane] = l_run[u % TILES] + __shfl_xor(l_run[u % TILES], 32);
     }
-    __syncthreads();
-    if (kgi > 0) return;
+    lds_barrier();
+    if (u >= TILES || kgi > 0) continue;
+    f32x16(&o)[DT] = acc[u % TILES];
+    float m = m_run[u % TILES], l = l_run[u % TILES] + __shfl_xor(l_run[u % TILES], 32);
     for (int k = 1; k < kg; ++k) {
-      const float* slot = area + (wave + k * per - 1) * SLOT;
+      const float* slot = area + ((k - 1) * np + pair) * S::STATE;
       const float mk = slot[64 * 16 * DT + lane];
-      if (mk == kNegInf) continue;
       const float lk = slot[64 * 16 * DT + 64 + lane];
-      const float m_new = fmaxf(m_run, mk);
-      const float a0 = __builtin_amdgcn_exp2f((m_run - m_new) * a.scale_log2);
+      const float m_new = fmaxf(m, mk);
+      if (m_new == kNegInf) continue;  // neither group sees a key
+      const float a0 = __builtin_amdgcn_exp2f((m - m_new) * a.scale_log2);
       const float a1 = __builtin_amdgcn_exp2f((mk - m_new) * a.scale_log2);
 #pragma unroll
       for (int v = 0; v < 4 * DT; ++v) {
-        const float4 o = *(const float4*)(slot + (v * 64 + lane) * 4);
-        const float x[4] = {o.x, o.y, o.z, o.w};
+        const float4 x4 = *(const float4*)(slot + (v * 64 + lane) * 4);
+        const float x[4] = {x4.x, x4.y, x4.z, x4.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int f = 4 * (v % DT) + e;
-          acc[f % DT][4 * (v / DT) + f / DT] = at(v / DT, f) * a0 + x[e] * a1;
+          const int f = 4 * (v % DT) + e, i = 4 * (v / DT) + f / DT;
+          o[f % DT][i] = o[f % DT][i] * a0 + x[e] * a1;
         }
       }
-      l_tot = l_tot * a0 + lk * a1;
-      m_run = m_new;
+      l = l * a0 + lk * a1;
+      m = m_new;
+    }
+    const int col = (it.tile0 + 2 * pair + u) * 32 + lc;
+    if (col >= it.M) continue;
+    // Element f of run i4 of a lane: dim 8 DT i4 + 4 DT lh + f, f < 4 DT.
+    auto at = [&](int i4, int f) { return o[f % DT][4 * i4 + f / DT]; };
+    if (it.nch == 1) {
+      const int tok = col / g;
+      const size_t orow = (size_t)(rq.q_start + tok) * a.hq + it.hk * g + (col - tok * g);
+      const float inv = 1.f / l;
+      uint16_t* dst = a.out + orow * D + 4 * DT * lh;
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4)
+#pragma unroll
+        for (int f = 0; f < 4 * DT; f += 8) {
+          u32x4 w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(at(i4, f + 2 * e) * inv, at(i4, f + 2 * e + 1) * inv);
+          *(u32x4*)(dst + 8 * DT * i4 + f) = w;
+        }
+      if (a.lse != nullptr && lh == 0) a.lse[orow] = m * a.sm_scale + __logf(l);
+    } else {
+      const size_t tile = (size_t)it.part + (2 * pair + u) * 32;
+      float* dst = a.part_o + tile * D;
+#pragma unroll
+      for (int v = 0; v < 4 * DT; ++v)
+        *(float4*)(dst + (v * 64 + lane) * 4) = make_float4(at(v / DT, 4 * (v % DT)), at(v / DT, 4 * (v % DT) + 1),
+                                                            at(v / DT, 4 * (v % DT) + 2), at(v / DT, 4 * (v % DT) + 3));
+      if (lh == 0) *(float2*)(a.part_ml + 2 * (tile + lc)) = make_float2(m, l);
     }
   }
-  if (!valid) return;
+}
 
-  if (nch == 1) {
-    const size_t orow = (size_t)(rq.q_start + tok) * a.hq + hk * g + hh;
-    const float inv = 1.f / l_tot;
-    uint16_t* dst = a.out + orow * D + 4 * DT * lh;
-#pragma unroll
-    for (int i4 = 0; i4 < 4; ++i4)
-#pragma unroll
-      for (int f = 0; f < 4 * DT; f += 8) {
-        u32x4 w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(at(i4, f + 2 * e) * inv, at(i4, f + 2 * e + 1) * inv);
-        *(u32x4*)(dst + 8 * DT * i4 + f) = w;
-      }
-    if (a.lse != nullptr && lh == 0) a.lse[orow] = m_run * a.sm_scale + __logf(l_tot);
+template <int D, typename Plan>
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void kv4_attn_kernel(Kv4AttnArgs a, Plan p) {
+  using S = Kv4Shape<D>;
+  __shared__ __attribute__((aligned(16))) char lds[S::LDS];
+
+  const int item = p.num_req == 1 ? xcd_item(p.grid_items) : (int)blockIdx.x;
+  if (item >= p.total_items) return;
+  const int r = find_request(p, item, false);
+  const auto rq = request_of(p, r);
+  const int g = a.g;
+  Kv4Item it;
+  it.n = rq.nv & 0xffff;
+  it.L = rq.ctx;
+  it.M = it.n * g;
+  // Items of the full column groups (groups, then KV heads, then runs), then
+  // those of the last one; their partials lie in the same order.
+  const int T = it.L + it.n;
+  const int tiles = (it.M + 31) / 32, full = tiles / kKv4Waves;
+  int local = item - rq.item_start;
+  it.nct = kKv4Waves;
+  Kv4Runs runs = kv4_runs(T, it.nct, p.chunk);
+  it.part = rq.part_start;
+  if (local >= full * a.hkv * runs.count) {
+    local -= full * a.hkv * runs.count;
+    if (runs.count > 1) it.part += full * kKv4Cols * a.hkv * runs.count;
+    it.nct = tiles - full * kKv4Waves;
+    runs = kv4_runs(T, it.nct, p.chunk);
+    it.tile0 = full * kKv4Waves;
   } else {
-    const int M32 = (M + 31) & ~31;
-    const size_t tile0 = (size_t)rq.part_start + ((size_t)hk * nch + c) * M32 + (size_t)((cg * tpg + ct) * 32);
-    float* dst = a.part_o + tile0 * D;
-#pragma unroll
-    for (int v = 0; v < 4 * DT; ++v)
-      *(float4*)(dst + (v * 64 + lane) * 4) = make_float4(at(v / DT, 4 * (v % DT)), at(v / DT, 4 * (v % DT) + 1),
-                                                          at(v / DT, 4 * (v % DT) + 2), at(v / DT, 4 * (v % DT) + 3));
-    if (lh == 0) *(float2*)(a.part_ml + 2 * (tile0 + lc)) = make_float2(m_run, l_tot);
+    it.tile0 = local / (a.hkv * runs.count) * kKv4Waves;
+    local %= a.hkv * runs.count;
+    if (runs.count > 1) it.part += it.tile0 * 32 * a.hkv * runs.count;
   }
+  it.nch = runs.count;
+  it.hk = local / runs.count;
+  it.c = local % runs.count;
+  it.kbeg = it.c * runs.keys;
+  it.kend = min(T, it.kbeg + runs.keys);
+  it.part += local * it.nct * 32;
+
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int np = it.nct > 2 ? 2 : 1, pair = wave % np;
+  if (it.nct - 2 * pair >= 2) kv4_wave<D, 2, Plan>(a, rq, it, pair, np, wave / np, lds);
+  else kv4_wave<D, 1, Plan>(a, rq, it, pair, np, wave / np, lds);
 }
 
 // Merge of the runs of split requests.  A work item is (request, KV head,
@@ -304,16 +435,32 @@ __global__ __launch_bounds__(kKv4MergeRows * PARTS) void kv4_merge_kernel(Kv4Att
   const int r = find_request(p, item, true);
   const auto rq = p.req[r];
   const int n = rq.nv & 0xffff, T = rq.ctx + n;
-  const int g = a.g, M = n * g, M32 = (M + 31) & ~31;
-  const int nch = (T + p.chunk - 1) / p.chunk;
+  const int g = a.g, M = n * g, tiles = (M + 31) / 32, full = tiles / kKv4Waves;
+  // merge items: those of the full column groups' tiles where they are split, then the last one's
   int local = item - rq.comb_start;
   const int v = local % (4 * DT);
   local /= 4 * DT;
-  const int tile = local % (M32 / 32), hk = local / (M32 / 32);
+  const int split = kv4_runs(T, kKv4Waves, p.chunk).count > 1 ? full * kKv4Waves : 0;  // tiles of the former
+  int nct = kKv4Waves, tile, hk;
+  size_t base = rq.part_start;
+  if (local < split * a.hkv) {
+    tile = local / a.hkv;
+    hk = local % a.hkv;
+  } else {
+    local -= split * a.hkv;
+    nct = tiles - full * kKv4Waves;
+    tile = full * kKv4Waves + local / a.hkv;
+    hk = local % a.hkv;
+    if (split) base += (size_t)split * 32 * a.hkv * kv4_runs(T, kKv4Waves, p.chunk).count;
+  }
+  const int nch = kv4_runs(T, nct, p.chunk).count;
+  const int tile0 = tile / kKv4Waves * kKv4Waves;  // of its group
+  if (nct == kKv4Waves) base += (size_t)tile0 * 32 * a.hkv * nch;
+  base += (size_t)hk * nch * nct * 32 + (size_t)(tile - tile0) * 32;
+  const size_t stride = (size_t)nct * 32;  // partial columns from run to run
   const int lane = threadIdx.x & 63, lc = lane & 31, lh = lane >> 5;
   const int part = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int col = tile * 32 + lc;
-  const size_t base = (size_t)rq.part_start + (size_t)hk * nch * M32 + (size_t)tile * 32;
 
   float m = kNegInf, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
   auto absorb = [&](float mc, float lc_, const float (&oc)[4]) {
@@ -335,7 +482,7 @@ __global__ __launch_bounds__(kKv4MergeRows * PARTS) void kv4_merge_kernel(Kv4Att
         const int c = c0 + u * PARTS;
         ml[u] = make_float2(kNegInf, 0.f);
         if (c < nch) {
-          const size_t t0 = base + (size_t)c * M32;
+          const size_t t0 = base + (size_t)c * stride;
           ml[u] = *(const float2*)(a.part_ml + 2 * (t0 + lc));
           x[u] = *(const float4*)(a.part_o + t0 * D + (v * 64 + lane) * 4);
         }
@@ -377,7 +524,7 @@ hipError_t launch_impl(const Kv4AttnArgs& a, const Plan& p, hipStream_t stream) 
   hipLaunchKernelGGL((kv4_attn_kernel<D, Plan>), dim3(p.grid_items), dim3(kThreads), 0, stream, a, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.total_comb == 0) return e;
-  if (p.max_chunks > 8)
+  if (p.max_chunks > 8 && p.grid_comb <= 1024)  // many runs, and few enough items to be bound by latency
     hipLaunchKernelGGL((kv4_merge_kernel<D, kKv4MergeParts, Plan>), dim3(p.grid_comb),
                        dim3(kKv4MergeRows * kKv4MergeParts), 0, stream, a, p);
   else
