@@ -96,11 +96,12 @@ Kv4Cols kv4_cols(const rg_attn_layout* L, int r) {
 // Units (kv4_rate) of a work item at most: the least that gives one round of
 // items on the compute units (two work groups each, at head size 64 three), or
 // as many rounds as keep items below kKv4Long units: a long round ends unevenly.
-// Measured on 40 requests of 8k to 32k keys (GPU time of the call, merge
-// included): items of up to 4500 units, one round, 603 us, two rounds 580,
-// three 571, four 575; on 16 requests of 1k to 8k keys with branches one round
-// 85.4 us, two 92, three 122.
-constexpr int kKv4Least = 32, kKv4Long = 3072;
+// Measured (GPU time of the call, merge included): 40 requests of 8k to 32k
+// keys 565 us in one round, 560 in two to four, 585 in six; 16 requests of 1k
+// to 8k keys with branches 85 us in one round, 92 in two, 122 in three.
+// kKv4Least is two steps of a wave on one tile, or one on four: one token over
+// 4097 keys takes 14.4 us with it, 16.4 with half of it, 14.6 with twice.
+constexpr int kKv4Least = 32, kKv4Long = 4096;
 int kv4_target(const rg_attn_layout* L, int cus) {
   const int64_t slots = (int64_t)(L->head_dim == 64 ? 3 : 2) * cus;
   struct Group {
@@ -122,13 +123,13 @@ int kv4_target(const rg_attn_layout* L, int cus) {
     add(c.rest, c.rest ? L->num_kv_heads : 0);
   }
   auto fit = [&](int64_t rounds) {  // the least target whose items fit the rounds
-    for (int64_t t = std::max<int64_t>(env_int("KV4_MIN", kKv4Least), work / (rounds * slots));; t += 1 + t / 16) {
+    for (int64_t t = std::max<int64_t>(kKv4Least, work / (rounds * slots));; t += 1 + t / 16) {
       int64_t items = 0;
       for (const Group& q : groups) items += q.count * kv4_runs(q.T, q.tiles, (int)std::min<int64_t>(t, INT32_MAX)).count;
       if (items <= std::max(least, rounds * slots)) return t;
     }
   };
-  const int64_t one = fit(1), lim = env_int("KV4_LIM", kKv4Long);
+  const int64_t one = fit(1), lim = kKv4Long;
   return (int)std::min<int64_t>(INT32_MAX, one <= lim ? one : fit((one + lim - 1) / lim));
 }
 
