@@ -59,6 +59,20 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// 16 bytes of every lane from base + off to LDS, byte `lds` + 16 * lane (below
+// 64 KiB).  No register waits for the data: they are there once s_waitcnt vmcnt
+// says so.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const void* base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const void* lane_address) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(lane_address) : "memory", "m0");
+}
+// A pointer's byte of LDS.
+__device__ __forceinline__ uint32_t lds_place(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
+}
+
 // Request r of a plan.
 __device__ __forceinline__ AttnReq request_of(const AttnPlan& p, int r) { return p.req[r]; }
 __device__ __forceinline__ AttnReqBr request_of(const AttnPlanBr& p, int r) { return p.req[r]; }

@@ -65,7 +65,7 @@ rg_status run_rows(const rg_attn_layout* L, const uint16_t* k, int64_t k_stride,
   a.hkv = L->num_kv_heads;
   auto pages = [&](int r) -> int64_t {
     const int64_t n = L->q_indptr[r + 1] - L->q_indptr[r];
-    return n == 0 ? 0 : (L->ctx_len[r] + n - 1) / kPageSize - L->ctx_len[r] / kPageSize + 1;
+    return n == 0 ? 0 : ((L->ctx_len[r] + n - 1) / kPageSize - L->ctx_len[r] / kPageSize + 1) * L->num_kv_heads;
   };
   return each_plan(L, 256, pages, [&](const AttnPlan& p) {
     const hipStream_t s = static_cast<hipStream_t>(stream);
@@ -225,7 +225,7 @@ float softmax_scale(const rg_attn_layout* L) {
 // ---------------------------------------------------------------------------
 rg_status run_mass(const rg_attn_layout* L, const uint16_t* q, const void* keys, bool kv4, const float* lse,
                    const int32_t* row_count, float decay, float* mass, void* stream) {
-  const rg_status st = validate_layout(L);
+  rg_status st = validate_layout(L);
   if (st != RG_OK) return st;
   if (!q || !keys || !lse || !mass) return RG_ERR_NULL;
   if (!(decay >= 0.f) || std::isinf(decay)) return RG_ERR_SHAPE;
@@ -244,13 +244,26 @@ rg_status run_mass(const rg_attn_layout* L, const uint16_t* q, const void* keys,
   a.g = a.hq / a.hkv;
   a.scale_log2 = softmax_scale(L) * 1.4426950408889634f;
   a.decay = decay;
-  auto items = [&](int r) -> int64_t {
-    // a request without query rows need not own pages for its context
-    if (L->q_indptr[r + 1] == L->q_indptr[r]) return 0;
-    return ((int64_t)L->ctx_len[r] + L->n_verify[r] + kMassKeys - 1) / kMassKeys * L->num_kv_heads;
-  };
-  return each_plan(L, 64 * kMassWaves, items, [&](const AttnPlan& p) {
-    return launch_mass(a, p, L->head_dim, kv4, static_cast<hipStream_t>(stream));
+  // A request without query rows need not own pages for its context.
+  auto len = [&](int r) { return L->q_indptr[r + 1] == L->q_indptr[r] ? 0 : (int64_t)L->ctx_len[r] + L->n_verify[r]; };
+  auto many = [&](int r) { return (int64_t)L->n_verify[r] * a.g > kMassCols; };
+  auto runs = [&](int r, int64_t step) { return (len(r) + step - 1) / step * L->num_kv_heads; };
+  // 4-bit: the longest run that still gives every compute unit four work
+  // groups, so that a run's start is a small part of it.
+  int64_t all = 0;
+  for (int r = 0; r < L->num_requests; ++r)
+    if (!many(r)) all += len(r) * L->num_kv_heads;
+  const int64_t run = kv4 ? std::min<int64_t>(kMassRun, std::max<int64_t>(128, all / (4 * device_cus()) / 128 * 128)) : kMassKeys;
+  // rows of a request are addressed by 32-bit offsets
+  for (int r = 0; r < L->num_requests; ++r)
+    if (many(r) && (int64_t)L->n_verify[r] * a.hq * L->head_dim * 2 > INT32_MAX) return RG_ERR_UNSUPPORTED;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  st = each_plan(L, 64 * kMassWaves, [&](int r) { return many(r) ? runs(r, kMassRowKeys) : 0; },
+                 [&](const AttnPlan& p) { return launch_mass_rows(a, p, L->head_dim, kv4, s); });
+  if (st != RG_OK) return st;
+  return each_plan(L, 64 * kMassWaves, [&](int r) { return many(r) ? 0 : runs(r, run); }, [&](AttnPlan& p) {
+    p.chunk = (int32_t)run;
+    return launch_mass(a, p, L->head_dim, kv4, s);
   });
 }
 

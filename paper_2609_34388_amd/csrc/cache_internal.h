@@ -7,7 +7,7 @@
 namespace rg {
 
 // Rows into, or out of, the 4-bit cache.  Plans: AttnPlan with a work item
-// per page that a request's rows touch.
+// per page that a request's rows touch and KV head.
 struct Kv4RowArgs {
   uint16_t* k;  // rows (appended: read, read back: written), or NULL
   uint16_t* v;
@@ -54,10 +54,16 @@ struct Kv4AttnArgs {
 hipError_t launch_kv4_attention(const Kv4AttnArgs& a, const AttnPlan& p, int head_dim, hipStream_t stream);
 hipError_t launch_kv4_attention(const Kv4AttnArgs& a, const AttnPlanBr& p, int head_dim, hipStream_t stream);
 
-// Attention mass.  Plans: AttnPlan with work items (KV head, kMassKeys keys).
+// Attention mass.  Plans: AttnPlan, part_start the request's number.  Requests
+// of up to kMassCols query columns a KV head take launch_mass, with work items of
+// kMassKeys keys (bf16) or plan.chunk (4-bit) of a KV head; the others
+// launch_mass_rows, with items of kMassRowKeys keys.
 constexpr int kMassWaves = 4;
-constexpr int kMassSub = 2;                              // 32-key tiles of a wave
-constexpr int kMassKeys = 32 * kMassWaves * kMassSub;    // keys of a work item
+constexpr int kMassCols = 128;
+constexpr int kMassSub = 2;                            // 32-key tiles of a bf16 wave
+constexpr int kMassKeys = 32 * kMassWaves * kMassSub;
+constexpr int kMassRun = 2048;                         // plan.chunk at most
+constexpr int kMassRowKeys = 64;
 struct MassArgs {
   const uint16_t* q;
   const void* keys;  // bf16 K pool, or the 4-bit pool
@@ -69,6 +75,7 @@ struct MassArgs {
   float scale_log2, decay;
 };
 hipError_t launch_mass(const MassArgs& a, const AttnPlan& p, int head_dim, bool kv4, hipStream_t stream);
+hipError_t launch_mass_rows(const MassArgs& a, const AttnPlan& p, int head_dim, bool kv4, hipStream_t stream);
 
 // Eviction.
 constexpr int kEvictThreads = 1024;  // select: a work group per (request, KV head)

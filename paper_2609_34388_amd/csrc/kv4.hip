@@ -7,9 +7,11 @@
 // the scale is a power of two the quotient is exact and the result does not
 // depend on how it is computed.
 //
-// A work item is one page that a request's rows touch, for all KV heads: no
-// two work groups write the same block.  Four lanes hold a group, 8 elements
-// (16 bytes) each.
+// A work item is one page that a request's rows touch, of one KV head: no two
+// work groups write the same block, and a block goes through LDS, where its
+// codes change between the order of rows and that of the block.  A block whose
+// tokens are all new is written with 16-byte stores; of any other only the new
+// tokens' bytes are.  Bound by the bytes, at short calls by the launch.
 #include "cache_internal.h"
 #include "kv4_device.h"
 
@@ -18,78 +20,116 @@ namespace {
 
 constexpr int kRowThreads = 256;
 
-// Row units of a work item: calls f(slot, h, d0, kv, row) for every 8 elements.
-template <int D, typename F>
-__device__ __forceinline__ void each_unit(const Kv4RowArgs& a, const AttnPlan& p, F f) {
+// The tokens of a work item: slots s0 .. s1 - 1 of a block, rows row0 ...
+struct RowItem {
+  size_t block;  // of the pool
+  int s0, s1, h;
+  int64_t row0;  // row of slot 0 (may lie before the request's first)
+};
+__device__ __forceinline__ RowItem row_item(const Kv4RowArgs& a, const AttnPlan& p) {
   const int item = blockIdx.x;
   const int r = find_request(p, item, false);
   const AttnReq rq = p.req[r];
   const int n = rq.nv & 0xffff;
-  const int page = (rq.ctx >> 4) + (item - rq.item_start);
-  const int t0 = max(rq.ctx, page * 16), cnt = min(rq.ctx + n, page * 16 + 16) - t0;
-  const size_t block = (size_t)a.page_indices[rq.page_start + page] * a.hkv;
-  const int units = cnt * a.hkv * (D / 8) * 2;
-  for (int u = threadIdx.x; u < units; u += kRowThreads) {
-    const int c = u % (D / 8);
-    const int h = u / (D / 8) % a.hkv;
-    const int tok = u / (D / 8) / a.hkv;  // K rows of the page, then V rows
-    const int kv = tok >= cnt;
-    const int t = t0 + tok - kv * cnt;
-    f(a.cache + (block + h) * Kv4<D>::BLOCK, t & 15, h, 8 * c, kv, (int64_t)rq.q_start + (t - rq.ctx));
-  }
+  const int local = item - rq.item_start;
+  const int page = (rq.ctx >> 4) + local / a.hkv;
+  RowItem it;
+  it.h = local % a.hkv;
+  it.block = (size_t)a.page_indices[rq.page_start + page] * a.hkv + it.h;
+  it.s0 = max(rq.ctx - page * 16, 0);
+  it.s1 = min(rq.ctx + n - page * 16, 16);
+  it.row0 = (int64_t)rq.q_start + (page * 16 - rq.ctx);
+  return it;
 }
+
+// Units of 8 elements of a block: slot and first element of unit u.
+template <int D>
+constexpr int kUnits = 16 * D / 8;
 
 template <int D>
 __global__ __launch_bounds__(kRowThreads) void kv4_append_kernel(Kv4RowArgs a, AttnPlan p) {
   using B = Kv4<D>;
-  each_unit<D>(a, p, [&](uint8_t* block, int slot, int h, int d0, int kv, int64_t row) {
-    const uint16_t* src = kv ? a.v + row * a.v_stride : a.k + row * a.k_stride;
-    const u32x4 x = *(const u32x4*)(src + (size_t)h * D + d0);
+  __shared__ __attribute__((aligned(16))) uint8_t blk[B::BLOCK];
+  const RowItem it = row_item(a, p);
+  // K, then V: a thread takes a unit of each (D = 128) or of one (D = 64)
+  for (int u = threadIdx.x; u < 2 * kUnits<D>; u += kRowThreads) {
+    const int kv = u / kUnits<D>, slot = u % kUnits<D> / (D / 8), d0 = u % (D / 8) * 8;
+    u32x4 x = {0u, 0u, 0u, 0u};
+    if (slot >= it.s0 && slot < it.s1) {
+      const uint16_t* rows = kv ? a.v + (it.row0 + slot) * a.v_stride : a.k + (it.row0 + slot) * a.k_stride;
+      x = *(const u32x4*)(rows + (size_t)it.h * D + d0);
+    }
     uint32_t m = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) m = max(m, max(x[e] & 0x7fffu, (x[e] >> 16) & 0x7fffu));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 1));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 1));  // four lanes hold a group
     m = max(m, (uint32_t)__shfl_xor((int)m, 2));
     const uint32_t b = (uint32_t)min(max((int)((m + 0x20) >> 7) - 2, 1), 252);
     const uint32_t c = encode8(x, scale_of(b));
     if (kv == 0) {
-      *(uint32_t*)(block + B::k_code(slot, d0)) = c;
-      if ((d0 & 31) == 0) block[B::k_scale(slot, d0 >> 5)] = (uint8_t)b;
+      *(uint32_t*)(blk + B::k_code(slot, d0)) = c;
+      if ((d0 & 31) == 0) blk[B::k_scale(slot, d0 >> 5)] = (uint8_t)b;
     } else {
 #pragma unroll
       for (int e = 0; e < 8 / B::DT; ++e) {
-        uint8_t* at = block + B::v_unit(slot, d0 / B::DT + e);
+        uint8_t* at = blk + B::v_unit(slot, d0 / B::DT + e);
         if constexpr (D == 128) *(uint16_t*)at = (uint16_t)(c >> (16 * e));
         else *at = (uint8_t)(c >> (8 * e));
       }
-      if ((d0 & 31) == 0) block[B::v_scale(slot, d0 >> 5)] = (uint8_t)b;
+      if ((d0 & 31) == 0) blk[B::v_scale(slot, d0 >> 5)] = (uint8_t)b;
     }
-  });
+  }
+  __syncthreads();
+  uint8_t* dst = a.cache + it.block * B::BLOCK;
+  if (it.s0 == 0 && it.s1 == 16) {
+    for (int u = threadIdx.x; u < B::BLOCK / 16; u += kRowThreads) *(u32x4*)(dst + 16 * u) = *(const u32x4*)(blk + 16 * u);
+    return;
+  }
+  for (int u = threadIdx.x; u < kUnits<D>; u += kRowThreads) {
+    const int slot = u / (D / 8), c = u % (D / 8), d0 = 8 * c;
+    if (slot < it.s0 || slot >= it.s1) continue;
+    *(uint32_t*)(dst + B::k_code(slot, d0)) = *(const uint32_t*)(blk + B::k_code(slot, d0));
+#pragma unroll
+    for (int e = 0; e < 8 / B::DT; ++e) {
+      const int at = B::v_unit(slot, d0 / B::DT + e);
+      if constexpr (D == 128) *(uint16_t*)(dst + at) = *(const uint16_t*)(blk + at);
+      else dst[at] = blk[at];
+    }
+    if (c < B::DT) dst[B::k_scale(slot, c)] = blk[B::k_scale(slot, c)];
+    else if (c < 2 * B::DT) dst[B::v_scale(slot, c - B::DT)] = blk[B::v_scale(slot, c - B::DT)];
+  }
 }
 
 template <int D>
 __global__ __launch_bounds__(kRowThreads) void kv4_read_kernel(Kv4RowArgs a, AttnPlan p) {
   using B = Kv4<D>;
-  each_unit<D>(a, p, [&](const uint8_t* block, int slot, int h, int d0, int kv, int64_t row) {
+  __shared__ __attribute__((aligned(16))) uint8_t blk[B::BLOCK];
+  const RowItem it = row_item(a, p);
+  const uint8_t* src = a.cache + it.block * B::BLOCK;
+  for (int u = threadIdx.x; u < B::BLOCK / 16; u += kRowThreads) *(u32x4*)(blk + 16 * u) = *(const u32x4*)(src + 16 * u);
+  __syncthreads();
+  for (int u = threadIdx.x; u < 2 * kUnits<D>; u += kRowThreads) {
+    const int kv = u / kUnits<D>, slot = u % kUnits<D> / (D / 8), d0 = u % (D / 8) * 8;
+    if (slot < it.s0 || slot >= it.s1) continue;
     uint32_t c, b;
-    uint16_t* dst;
+    uint16_t* rows;
     if (kv == 0) {
-      c = *(const uint32_t*)(block + B::k_code(slot, d0));
-      b = block[B::k_scale(slot, d0 >> 5)];
-      dst = a.k + row * a.k_stride;
+      c = *(const uint32_t*)(blk + B::k_code(slot, d0));
+      b = blk[B::k_scale(slot, d0 >> 5)];
+      rows = a.k + (it.row0 + slot) * a.k_stride;
     } else {
       c = 0;
 #pragma unroll
       for (int e = 0; e < 8 / B::DT; ++e) {
-        const uint8_t* at = block + B::v_unit(slot, d0 / B::DT + e);
+        const uint8_t* at = blk + B::v_unit(slot, d0 / B::DT + e);
         if constexpr (D == 128) c |= (uint32_t)*(const uint16_t*)at << (16 * e);
         else c |= (uint32_t)*at << (8 * e);
       }
-      b = block[B::v_scale(slot, d0 >> 5)];
-      dst = a.v + row * a.v_stride;
+      b = blk[B::v_scale(slot, d0 >> 5)];
+      rows = a.v + (it.row0 + slot) * a.v_stride;
     }
-    *(u32x4*)(dst + (size_t)h * D + d0) = decode8(c, scale_of(b));
-  });
+    __builtin_nontemporal_store(decode8(c, scale_of(b)), (u32x4*)(rows + (size_t)it.h * D + d0));
+  }
 }
 
 }  // namespace

@@ -38,12 +38,6 @@ __device__ __forceinline__ float scale_at(uint32_t word) {
   return __uint_as_float(E < 3 ? word << (23 - 8 * E) : word >> 1);
 }
 
-// 16 bytes of every lane from base + off to LDS, byte `lds` + 16 * lane.  No
-// register waits for the data: they are there once s_waitcnt vmcnt says so.
-__device__ __forceinline__ void load_to_lds(uint32_t lds, const uint8_t* base, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
-}
-
 // What a work group of a wave's tiles works on.
 struct Kv4Item {
   int hk, kbeg, kend;  // KV head, keys of the run
@@ -61,7 +55,14 @@ struct Kv4Shape {
   static constexpr int STATE = 64 * 16 * DT + 128;    // floats of a wave's state of one tile
   static constexpr int RING = 2;                      // key tiles of a wave in LDS
   static constexpr int SLOT = 2 * Kv4<D>::BLOCK;      // bytes of one: two blocks
-  static constexpr int LOADS = 2 * ((Kv4<D>::BLOCK + 1023) / 1024);  // load instructions of one
+  // Loads of 16 bytes a lane that fill a slot: FULL of each block, and one of the
+  // REST bytes of both; the slot holds them in this order.
+  static constexpr int FULL = Kv4<D>::BLOCK / 1024, REST = Kv4<D>::BLOCK % 1024, LOADS = 2 * FULL + 1;
+  static_assert(2 * REST <= 1024, "one load");
+  // Place of byte x of block pp in a slot.
+  static __device__ __forceinline__ int place(int pp, int x) {
+    return x < 1024 * FULL ? 1024 * FULL * pp + x : 2 * 1024 * FULL + REST * pp + (x - 1024 * FULL);
+  }
   // The rings come first: a load to LDS takes a 16-bit place.  Q behind them.
   static constexpr int Q = kKv4Waves * RING * SLOT;
   static constexpr int LDS = Q + kKv4Cols * QROW;
@@ -95,10 +96,11 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
   // read from LDS when it is needed.
   const int wave = kgi * np + pair;
   char* ring = lds + wave * S::RING * S::SLOT;
-  const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
-  const int koff = (lc < 16 ? 0 : B::BLOCK) + ktok * 32 + 16 * lh;
-  const int ksoff = (lc < 16 ? 0 : B::BLOCK) + B::k_scale(ktok, 0);
-  const int voff = B::v_unit(8 * lh, lc), vsoff = B::v_scale(8 * lh, lc * DT / 32);
+  const uint32_t ring_at = lds_place(ring);
+  const int koff = S::place(lc >> 4, ktok * 32 + 16 * lh);  // K codes and scales lie in the full part
+  const int ksoff = S::place(lc >> 4, B::k_scale(ktok, 0));
+  const int voff[2] = {S::place(0, B::v_unit(8 * lh, lc)), S::place(1, B::v_unit(8 * lh, lc))};
+  const int vsoff[2] = {S::place(0, B::v_scale(8 * lh, lc * DT / 32)), S::place(1, B::v_scale(8 * lh, lc * DT / 32))};
   const int ntile = (kend - kbeg + 31) / 32;
   // Pages of key tile j; past the run's last page that page again.
   struct Pair {
@@ -106,14 +108,17 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
   };
   auto pages_of = [&](int j) { return Pair{pages[min(2 * j, npg - 1)], pages[min(2 * j + 1, npg - 1)]}; };
   auto load = [&](int slot, Pair x) {
+    const uint8_t* b0 = pool + (size_t)x.p0 * page_bytes;
+    const uint8_t* b1 = pool + (size_t)x.p1 * page_bytes;
+    const uint32_t to = ring_at + slot * S::SLOT;
 #pragma unroll
-    for (int pp = 0; pp < 2; ++pp) {
-      const uint8_t* b = pool + (size_t)(pp ? x.p1 : x.p0) * page_bytes;
-      const uint32_t to = ring_at + slot * S::SLOT + pp * B::BLOCK;
-#pragma unroll
-      for (int at = 0; at < B::BLOCK; at += 1024)
-        if (at + 1024 <= B::BLOCK || at + 16 * lane < B::BLOCK) load_to_lds(to + at, b + at, 16 * lane);
+    for (int i = 0; i < S::FULL; ++i) {
+      load_to_lds(to + 1024 * i, b0 + 1024 * i, 16 * lane);
+      load_to_lds(to + 1024 * (S::FULL + i), b1 + 1024 * i, 16 * lane);
     }
+    if (lane < 2 * S::REST / 16)  // from two places: the lanes' own addresses
+      load_to_lds(to + 1024 * 2 * S::FULL,
+                  (lane < S::REST / 16 ? b0 : b1 - S::REST) + 1024 * S::FULL + 16 * lane);
   };
 
   Pair ahead{0, 0};
@@ -245,13 +250,13 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
 #pragma unroll
     for (int pp = 0; pp < 2; ++pp) {
       if constexpr (D == 128) {
-        const u32x4 w = *(const u32x4*)(code + pp * B::BLOCK + voff);
+        const u32x4 w = *(const u32x4*)(code + voff[pp]);
         for (int e = 0; e < 4; ++e) vc[pp][e] = w[e];
       } else {
-        const u32x2 w = *(const u32x2*)(code + pp * B::BLOCK + voff);
+        const u32x2 w = *(const u32x2*)(code + voff[pp]);
         for (int e = 0; e < 2; ++e) vc[pp][e] = w[e];
       }
-      vs[pp] = *(const u32x2*)(code + pp * B::BLOCK + vsoff);
+      vs[pp] = *(const u32x2*)(code + vsoff[pp]);
     }
     if (j + 2 * kg < ntile) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot is read

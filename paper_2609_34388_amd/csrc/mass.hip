@@ -4,11 +4,18 @@
 // added to the key's history, mass_j = (j < L ? decay * mass_j : 0) + w_j.
 //
 // One pass over K after the attention (whose lse it needs): the products of
-// the scores once more, no V.  A work item is (request, KV head, 256 keys); a
-// wave holds two 32-key tiles of K in registers as the columns of S = Q K^T,
-// so a lane's 16 scores are 16 query columns of one key and the sum over
-// columns stays in the lane.  Query columns pass through LDS, 128 at a time.
-// No atomics: a key belongs to one lane pair, its sum to one order.
+// the scores once more, no V.  Keys are the columns of S = Q K^T, so a lane's
+// 16 scores of a 32 x 32 tile are 16 query columns of one key and the sum over
+// columns stays in the lane.  No atomics: a key's sum has one order.
+//
+// Up to 128 query columns a request (mass_kernel) the bytes of K bound it: Q
+// lies in LDS, waves take key tiles.  A bf16 wave holds two key tiles, read
+// straight from the pool; four times fewer bytes of a 4-bit key would leave a
+// work group that small waiting for its start, so it takes a longer run of keys
+// whose codes come through LDS, four key tiles ahead.  With more columns
+// (mass_rows_kernel, prompts) the products and exponentials bound it: a work
+// group takes 64 keys, held in registers by each of its waves, and the waves
+// share the column tiles, whose Q comes through a ring of LDS of the wave's own.
 #include "cache_internal.h"
 #include "kv4_device.h"
 
@@ -16,117 +23,275 @@ namespace rg {
 namespace {
 
 constexpr int kThreads = 64 * kMassWaves;
-constexpr int kCols = 128;  // query columns staged at a time
+constexpr float kLog2e = 1.4426950408889634f;
 
-template <int D, bool KV4>
-__global__ __launch_bounds__(kThreads, 2) void mass_kernel(MassArgs a, AttnPlan p) {
-  constexpr int NCH = D / 8, KSTEPS = D / 16;
-  __shared__ __attribute__((aligned(16))) uint16_t qs[kCols * D];
-  __shared__ float lse2[kCols];
+// Request and range of a work item.
+struct MassItem {
+  int V, L, T, M;  // verify rows, context, keys, counted columns
+  int hk, kbeg;
+  int q_start, page_start;
+};
+__device__ __forceinline__ MassItem mass_item(const MassArgs& a, const AttnPlan& p, int keys) {
   const int item = blockIdx.x;
   const int r = find_request(p, item, false);
   const AttnReq rq = p.req[r];
-  const int V = (int)((uint32_t)rq.nv >> 16), L = rq.ctx, T = L + V;
-  const int g = a.g;
-  const int nch = (T + kMassKeys - 1) / kMassKeys;
-  const int local = item - rq.item_start;
-  const int hk = local / nch, kbeg = local % nch * kMassKeys;
-  const int count = a.row_count ? min(max(a.row_count[rq.part_start], 0), V) : V;
-  const int M = count * g;
+  MassItem it;
+  it.V = (int)((uint32_t)rq.nv >> 16);
+  it.L = rq.ctx;
+  it.T = it.L + it.V;
+  it.M = (a.row_count ? min(max(a.row_count[rq.part_start], 0), it.V) : it.V) * a.g;
+  const int nch = (it.T + keys - 1) / keys, local = item - rq.item_start;
+  it.hk = local / nch;
+  it.kbeg = local % nch * keys;
+  it.q_start = rq.q_start;
+  it.page_start = rq.page_start;
+  return it;
+}
 
-  const int tid = threadIdx.x, lane = tid & 63, lc = lane & 31, lh = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+// Row of q and lse of a column.
+__device__ __forceinline__ size_t column_row(const MassArgs& a, const MassItem& it, int col) {
+  const int tok = col / a.g;
+  return (size_t)(it.q_start + tok) * a.hq + it.hk * a.g + (col - tok * a.g);
+}
 
-  // K of the wave's tiles: keys kbeg + 32 (wave + 4 s) + lc
-  bf16x8 kf[kMassSub][KSTEPS];
-  const int last_page = (T - 1) / kPageSize;
-  const int32_t* pages = a.page_indices + rq.page_start;
+// K of key tile `kb`'s lane key as the columns' operand, straight from the pool.
+template <int D, bool KV4>
+__device__ __forceinline__ void load_keys(const MassArgs& a, const MassItem& it, int kb, bf16x8 (&kf)[D / 16]) {
+  const int lane = threadIdx.x & 63, lc = lane & 31, lh = lane >> 5, key = kb + lc;
+  const size_t block = (size_t)a.page_indices[it.page_start + min(key >> 4, (it.T - 1) / kPageSize)] * a.hkv + it.hk;
+  if constexpr (KV4) {
+    using B = Kv4<D>;
+    const uint8_t* b = static_cast<const uint8_t*>(a.keys) + block * B::BLOCK;
 #pragma unroll
-  for (int s = 0; s < kMassSub; ++s) {
-    const int key = kbeg + 32 * (wave + kMassWaves * s) + lc;
-    const size_t block = (size_t)pages[min(key >> 4, last_page)] * a.hkv + hk;
-    if constexpr (KV4) {
-      using B = Kv4<D>;
-      const uint8_t* b = static_cast<const uint8_t*>(a.keys) + block * B::BLOCK;
+    for (int i = 0; i < D / 64; ++i) {
+      const u32x4 w = *(const u32x4*)(b + B::k_code(key & 15, 64 * i + 32 * lh));
+      const float sc = scale_of(b[B::k_scale(key & 15, 2 * i + lh)]);
 #pragma unroll
-      for (int i = 0; i < D / 64; ++i) {
-        const u32x4 w = *(const u32x4*)(b + B::k_code(key & 15, 64 * i + 32 * lh));
-        const float sc = scale_of(b[B::k_scale(key & 15, 2 * i + lh)]);
+      for (int e = 0; e < 4; ++e) kf[4 * i + e] = __builtin_bit_cast(bf16x8, decode8(w[e], sc));
+    }
+  } else {
+    const uint16_t* b = static_cast<const uint16_t*>(a.keys) + (block * kPageSize + (key & 15)) * D;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) kf[s][4 * i + e] = __builtin_bit_cast(bf16x8, decode8(w[e], sc));
-      }
-    } else {
-      const uint16_t* b = static_cast<const uint16_t*>(a.keys) + (block * kPageSize + (key & 15)) * D;
+    for (int ks = 0; ks < D / 16; ++ks) kf[ks] = *(const bf16x8*)(b + 16 * ks + 8 * lh);
+  }
+}
+
+// 16-byte chunk of a row of Q that K step ks takes (the 4-bit block's order of dims).
+template <bool KV4>
+__device__ __forceinline__ int q_chunk(int ks, int lh) {
+  return KV4 ? 8 * (ks / 4) + 4 * lh + ks % 4 : 2 * ks + lh;
+}
+
+// Adds a tile's weights: 32 columns from col0 on, keys kb + lc.
+__device__ __forceinline__ void add_weights(const MassArgs& a, const MassItem& it, f32x16 sc, const float (&ls)[16], int col0,
+                                            int kb, float& w) {
+  const int lane = threadIdx.x & 63, lc = lane & 31, lh = lane >> 5;
+  if (kb + 31 > it.L + col0 / a.g) {  // some row does not see every key
 #pragma unroll
-      for (int ks = 0; ks < KSTEPS; ++ks) kf[s][ks] = *(const bf16x8*)(b + 16 * ks + 8 * lh);
+    for (int i = 0; i < 16; ++i) {
+      const int col = col0 + 8 * (i >> 2) + 4 * lh + (i & 3);
+      if (kb + lc > it.L + col / a.g) sc[i] = kNegInf;
     }
   }
-
-  float w[kMassSub];
-  for (int s = 0; s < kMassSub; ++s) w[s] = 0.f;
-  // The first columns whose rows see a key of this item.
-  const int first = max(0, kbeg - L);
-  for (int c0 = (int)((int64_t)first * g / kCols) * kCols; c0 < M; c0 += kCols) {
-    __syncthreads();
-    for (int u = tid; u < kCols * NCH; u += kThreads) {
-      const int row = u / NCH, ch = u % NCH, col = c0 + row;
-      u32x4 x = {0u, 0u, 0u, 0u};
-      if (col < M) {
-        const int tok = col / g;
-        x = *(const u32x4*)(a.q + ((size_t)(rq.q_start + tok) * a.hq + hk * g + (col - tok * g)) * D + 8 * ch);
-      }
-      *(u32x4*)(qs + row * D + ((ch ^ (row & (NCH - 1))) * 8)) = x;
-    }
-    if (tid < kCols) {
-      const int col = c0 + tid, tok = col / g;
-      // a column that does not count weighs exp2(-inf) = 0
-      lse2[tid] = col < M ? a.lse[(size_t)(rq.q_start + tok) * a.hq + hk * g + (col - tok * g)] * 1.4426950408889634f
-                          : -kNegInf;
-    }
-    __syncthreads();
-    for (int t = 0; t < kCols / 32 && c0 + 32 * t < M; ++t) {
-      const int low = L + (c0 + 32 * t) / g;                      // last key the tile's first row sees
-      const int high = L + (min(c0 + 32 * t + 31, M - 1)) / g;    // ... its last row
-      bf16x8 qf[KSTEPS];
 #pragma unroll
-      for (int ks = 0; ks < KSTEPS; ++ks) {
-        const int ch = KV4 ? 8 * (ks / 4) + 4 * lh + ks % 4 : 2 * ks + lh;
-        qf[ks] = *(const bf16x8*)(qs + (32 * t + lc) * D + ((ch ^ (lc & (NCH - 1))) * 8));
-      }
+  for (int i = 0; i < 16; ++i) w += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.scale_log2, -ls[i]));
+}
+
+__device__ __forceinline__ void write_mass(const MassArgs& a, const MassItem& it, int key, float sum) {
+  float* at = a.mass + ((size_t)a.page_indices[it.page_start + (key >> 4)] * a.hkv + it.hk) * kPageSize + (key & 15);
+  *at = key < it.L && a.decay != 0.f ? a.decay * *at + sum : sum;
+}
+
+template <int D, bool KV4>
+__global__ __launch_bounds__(kThreads, 2) void mass_kernel(MassArgs a, AttnPlan p) {
+  constexpr int KSTEPS = D / 16, QROW = 2 * D + 16;  // 16 bytes more: a fragment read meets every bank once
+  constexpr int RING = 4, SLOT = KV4 ? 2 * 17 * D / 2 : 0;  // codes of K of two blocks
+  __shared__ __attribute__((aligned(16))) char lds[kMassWaves * RING * SLOT + kMassCols * QROW + kMassCols * 4 +
+                                                       (KV4 ? kMassRun * 4 : 0)];
+  char* qs = lds + kMassWaves * RING * SLOT;
+  float* lse2 = reinterpret_cast<float*>(qs + kMassCols * QROW);
+  float* sums = lse2 + kMassCols;  // 4-bit: of the run's keys
+  const int run = KV4 ? p.chunk : kMassKeys;
+  const MassItem it = mass_item(a, p, run);
+  const int tid = threadIdx.x, lane = tid & 63, lc = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tiles = (it.M + 31) / 32;
+
+  // 4-bit: the first tiles' codes go out first
+  typedef const int32_t __attribute__((address_space(4))) * cpage_ptr;
+  const cpage_ptr pages = (cpage_ptr)(a.page_indices + it.page_start);
+  const int last = (it.T - 1) / kPageSize;
+  char* ring = lds + wave * RING * SLOT;
+  const uint32_t ring_at = KV4 ? lds_place(ring) : 0;
+  constexpr int KPART = 17 * D / 2;
+  auto load = [&](int slot, int kb) {
+#pragma unroll
+    for (int pp = 0; pp < 2; ++pp) {
+      const uint8_t* b = static_cast<const uint8_t*>(a.keys) + ((size_t)pages[min((kb >> 4) + pp, last)] * a.hkv + it.hk) * (17 * D);
+#pragma unroll
+      for (int at = 0; at < KPART; at += 1024)
+        if (at + 1024 <= KPART || at + 16 * lane < KPART) load_to_lds(ring_at + slot * SLOT + pp * KPART + at, b + at, 16 * lane);
+    }
+  };
+  constexpr int LOADS = 2 * ((KPART + 1023) / 1024);
+  const int kend = min(it.T, it.kbeg + run);
+  if constexpr (KV4) {
+#pragma unroll
+    for (int s = 0; s < RING - 1; ++s)
+      if (it.kbeg + 32 * (wave + kMassWaves * s) < kend) load(s, it.kbeg + 32 * (wave + kMassWaves * s));
+  }
+  bf16x8 kf[KV4 ? 1 : kMassSub][KSTEPS];
+  if constexpr (!KV4) {
+#pragma unroll
+    for (int s = 0; s < kMassSub; ++s) load_keys<D, false>(a, it, it.kbeg + 32 * (wave + kMassWaves * s), kf[s]);
+  }
+
+  for (int u = tid; u < tiles * 32 * (D / 8); u += kThreads) {
+    const int row = u / (D / 8), ch = u % (D / 8);
+    u32x4 x = {0u, 0u, 0u, 0u};
+    if (row < it.M) x = *(const u32x4*)(a.q + column_row(a, it, row) * D + 8 * ch);
+    *(u32x4*)(qs + row * QROW + 16 * ch) = x;
+  }
+  // a column that does not count weighs exp2(-inf) = 0
+  if (tid < 32 * tiles) lse2[tid] = tid < it.M ? a.lse[column_row(a, it, tid)] * kLog2e : -kNegInf;
+  lds_barrier();
+
+  auto weigh = [&](const bf16x8 (&k)[KSTEPS], int kb, float& w) {
+    for (int t = 0; t < tiles; ++t) {
+      f32x16 sc;
+      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+      const char* row = qs + (32 * t + lc) * QROW;
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks)
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(row + 16 * q_chunk<KV4>(ks, lh)), k[ks], sc, 0, 0, 0);
       float ls[16];
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) {
         const float4 x = *(const float4*)(lse2 + 32 * t + 8 * i4 + 4 * lh);
         ls[4 * i4] = x.x, ls[4 * i4 + 1] = x.y, ls[4 * i4 + 2] = x.z, ls[4 * i4 + 3] = x.w;
       }
+      add_weights(a, it, sc, ls, 32 * t, kb, w);
+    }
+  };
+  if constexpr (KV4) {
+    using B = Kv4<D>;
+    const int koff = (lc < 16 ? 0 : KPART) + (lc & 15) * 32 + 16 * lh, ksoff = (lc < 16 ? 0 : KPART) + B::k_scale(lc & 15, 0);
+    int slot = 0;
+    for (int kb = it.kbeg + 32 * wave; kb < kend; kb += 32 * kMassWaves) {
+      // the loads of the tiles after this one may be in flight, its own not
+      const int ahead = min((kend - 1 - kb) / (32 * kMassWaves), RING - 2);
+      if (ahead == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
+      else if (ahead == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      static_assert(RING == 4, "the waits above");
+      const char* code = ring + slot * SLOT;
+      const uint32_t scale = (D == 128 ? *(const uint32_t*)(code + ksoff) : *(const uint16_t*)(code + ksoff)) >> (8 * lh);
+      bf16x8 k[KSTEPS];
 #pragma unroll
-      for (int s = 0; s < kMassSub; ++s) {
-        const int kb = kbeg + 32 * (wave + kMassWaves * s);
-        if (kb > high) continue;
-        f32x16 sc;
-        for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+      for (int i = 0; i < D / 64; ++i) {
+        const u32x4 c = *(const u32x4*)(code + koff + 512 * i);
+        const float s = scale_of((scale >> (16 * i)) & 0xff);
 #pragma unroll
-        for (int ks = 0; ks < KSTEPS; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[ks], kf[s][ks], sc, 0, 0, 0);
-        if (kb + 31 > low) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int col = c0 + 32 * t + 8 * (i >> 2) + 4 * lh + (i & 3);
-            if (kb + lc > L + col / g) sc[i] = kNegInf;
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) w[s] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.scale_log2, -ls[i]));
+        for (int e = 0; e < 4; ++e) k[4 * i + e] = __builtin_bit_cast(bf16x8, decode8(c[e], s));
       }
+      const int next = kb + 32 * kMassWaves * (RING - 1);
+      if (next < kend) load((slot + RING - 1) % RING, next);  // where the tile before this one was
+      float w = 0.f;
+      weigh(k, kb, w);
+      w += __shfl_xor(w, 32);
+      if (lh == 0) sums[kb - it.kbeg + lc] = w;
+      slot = (slot + 1) % RING;
+    }
+    // behind the loop: a load or store of the mass in it would wait for the codes
+    lds_barrier();
+    for (int key = it.kbeg + tid; key < kend; key += kThreads) write_mass(a, it, key, sums[key - it.kbeg]);
+  } else {
+#pragma unroll
+    for (int s = 0; s < kMassSub; ++s) {
+      const int kb = it.kbeg + 32 * (wave + kMassWaves * s);
+      float w = 0.f;
+      if (kb < it.T) weigh(kf[s], kb, w);
+      w += __shfl_xor(w, 32);
+      if (lh == 0 && kb + lc < it.T) write_mass(a, it, kb + lc, w);
     }
   }
+}
+
+template <int D, bool KV4>
+__global__ __launch_bounds__(kThreads, 2) void mass_rows_kernel(MassArgs a, AttnPlan p) {
+  constexpr int KSTEPS = D / 16, NCH = D / 8, TILE = 32 * D * 2;  // bytes of a column tile of Q
+  constexpr int LOADS = TILE / 1024;
+  __shared__ __attribute__((aligned(16))) char lds[kMassWaves * 2 * TILE + kMassWaves * 128 + kMassWaves * kMassRowKeys * 4];
+  const MassItem it = mass_item(a, p, kMassRowKeys);
+  const int tid = threadIdx.x, lane = tid & 63, lc = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  char* ring = lds + wave * 2 * TILE;
+  const uint32_t ring_at = lds_place(ring);
+  float* lse2 = reinterpret_cast<float*>(lds + kMassWaves * 2 * TILE) + wave * 32;
+  float* sums = reinterpret_cast<float*>(lds + kMassWaves * 2 * TILE + kMassWaves * 128);
+
+  // This wave's column tiles: every kMassWaves-th of those whose rows see a key.
+  const int tiles = (it.M + 31) / 32;
+  const int t0 = (int)((int64_t)max(0, it.kbeg - it.L) * a.g / 32) + wave;
+  // A tile of Q in LDS: rows of D, 16-byte chunks c of row r at place c ^ (r % NCH).
+  // Columns past the counted ones repeat the last: they weigh zero.
+  const uint16_t* base = a.q + (size_t)it.q_start * a.hq * D;
+  float ls_next = 0.f;
+  auto load = [&](int slot, int t) {
 #pragma unroll
-  for (int s = 0; s < kMassSub; ++s) {
-    const float sum = w[s] + __shfl_xor(w[s], 32);
-    const int key = kbeg + 32 * (wave + kMassWaves * s) + lc;
-    if (lh == 0 && key < T) {
-      float* at = a.mass + ((size_t)pages[key >> 4] * a.hkv + hk) * kPageSize + (key & 15);
-      *at = key < L && a.decay != 0.f ? a.decay * *at + sum : sum;
+    for (int i = 0; i < LOADS; ++i) {
+      const int row = (i * 64 + lane) / NCH, ch = (lane % NCH) ^ (row % NCH);
+      const int col = min(32 * t + row, it.M - 1);
+      // rows of a request lie within 2^31 bytes of its first (checked by the host)
+      load_to_lds(ring_at + slot * TILE + i * 1024, base,
+                  (uint32_t)((column_row(a, it, col) - (size_t)it.q_start * a.hq) * D + 8 * ch) * 2);
     }
+    const int col = 32 * t + lc;
+    ls_next = col < it.M ? a.lse[column_row(a, it, col)] : -kNegInf;
+  };
+  if (t0 < tiles) load(0, t0);
+
+  bf16x8 kf[2][KSTEPS];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) load_keys<D, KV4>(a, it, it.kbeg + 32 * s, kf[s]);
+
+  float w[2] = {0.f, 0.f};
+  int slot = 0;
+  for (int t = t0; t < tiles; t += kMassWaves, slot ^= 1) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (lh == 0) lse2[lc] = ls_next * kLog2e;  // the wave's own: no barrier
+    bf16x8 qf[KSTEPS];
+    const char* row = ring + slot * TILE + lc * (2 * D);
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = *(const bf16x8*)(row + 16 * (q_chunk<KV4>(ks, lh) ^ (lc % NCH)));
+    float ls[16];
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      const float4 x = *(const float4*)(lse2 + 8 * i4 + 4 * lh);
+      ls[4 * i4] = x.x, ls[4 * i4 + 1] = x.y, ls[4 * i4 + 2] = x.z, ls[4 * i4 + 3] = x.w;
+    }
+    if (t + kMassWaves < tiles) load(slot ^ 1, t + kMassWaves);
+    f32x16 sc[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+      for (int i = 0; i < 16; ++i) sc[s][i] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS; ++ks)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[ks], kf[s][ks], sc[s], 0, 0, 0);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) add_weights(a, it, sc[s], ls, 32 * t, it.kbeg + 32 * s, w[s]);
+  }
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    w[s] += __shfl_xor(w[s], 32);
+    if (lh == 0) sums[wave * kMassRowKeys + 32 * s + lc] = w[s];
+  }
+  lds_barrier();
+  if (tid < kMassRowKeys && it.kbeg + tid < it.T) {
+    float sum = sums[tid];
+    for (int k = 1; k < kMassWaves; ++k) sum += sums[k * kMassRowKeys + tid];
+    write_mass(a, it, it.kbeg + tid, sum);
   }
 }
 
@@ -138,6 +303,15 @@ hipError_t launch_mass(const MassArgs& a, const AttnPlan& p, int head_dim, bool 
   else if (head_dim == 128) hipLaunchKernelGGL((mass_kernel<128, false>), grid, block, 0, stream, a, p);
   else if (kv4) hipLaunchKernelGGL((mass_kernel<64, true>), grid, block, 0, stream, a, p);
   else hipLaunchKernelGGL((mass_kernel<64, false>), grid, block, 0, stream, a, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_mass_rows(const MassArgs& a, const AttnPlan& p, int head_dim, bool kv4, hipStream_t stream) {
+  const dim3 grid(p.total_items), block(kThreads);
+  if (head_dim == 128 && kv4) hipLaunchKernelGGL((mass_rows_kernel<128, true>), grid, block, 0, stream, a, p);
+  else if (head_dim == 128) hipLaunchKernelGGL((mass_rows_kernel<128, false>), grid, block, 0, stream, a, p);
+  else if (kv4) hipLaunchKernelGGL((mass_rows_kernel<64, true>), grid, block, 0, stream, a, p);
+  else hipLaunchKernelGGL((mass_rows_kernel<64, false>), grid, block, 0, stream, a, p);
   return hipGetLastError();
 }
 
