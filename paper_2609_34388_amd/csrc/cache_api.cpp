@@ -244,6 +244,12 @@ rg_status run_mass(const rg_attn_layout* L, const uint16_t* q, const void* keys,
   a.g = a.hq / a.hkv;
   a.scale_log2 = softmax_scale(L) * 1.4426950408889634f;
   a.decay = decay;
+  // With 2^l >= g, g_mul = ceil(2^(31 + l) / g) fits 32 bits and g_mul g exceeds
+  // 2^(31 + l) by e < g, so col g_mul / 2^(31 + l) exceeds col / g by
+  // col e / (g 2^(31 + l)) < 1 / g for every col below 2^31: the floors agree.
+  a.g_shift = 0;
+  while ((1ll << a.g_shift) < a.g) ++a.g_shift;
+  a.g_mul = (uint32_t)(((uint64_t(1) << (31 + a.g_shift)) + a.g - 1) / a.g);
   // A request without query rows need not own pages for its context.
   auto len = [&](int r) { return L->q_indptr[r + 1] == L->q_indptr[r] ? 0 : (int64_t)L->ctx_len[r] + L->n_verify[r]; };
   auto many = [&](int r) { return (int64_t)L->n_verify[r] * a.g > kMassCols; };
@@ -308,8 +314,10 @@ rg_status each_evict_plan(const rg_evict_layout* L, int64_t& words, F f) {
       q.most = std::min(q.keep, q.ctx - q.keep);
       q.ws_start = (int32_t)ws;
       q.move_start = (int32_t)moves;
-      ws += (int64_t)L->num_kv_heads * (4 + 2 * (int64_t)q.most);
-      moves += (int64_t)L->num_kv_heads * ((q.most + kMoveTokens - 1) / kMoveTokens);
+      if (q.most == 0) continue;
+      p.longest = std::max(p.longest, q.ctx);
+      ws += (int64_t)L->num_kv_heads * evict_words(q.keep, q.most);
+      moves += (int64_t)L->num_kv_heads * (((q.keep + 15) / 16 + kMoveWaves - 1) / kMoveWaves);
       if (ws > INT32_MAX / 2 || !fits_launch(moves, kMoveThreads)) return RG_ERR_UNSUPPORTED;
     }
     if (!fits_launch((int64_t)p.num_req * L->num_kv_heads, kEvictThreads)) return RG_ERR_UNSUPPORTED;
@@ -333,7 +341,7 @@ rg_status run_evict(const rg_evict_layout* L, uint8_t* k_cache, uint8_t* v_cache
   int64_t words = 0;
   st = each_evict_plan(L, words, [](const EvictPlan&) { return RG_OK; });
   if (st != RG_OK) return st;
-  if (ws == nullptr || ws_bytes < (size_t)words * 4 || !aligned(ws, 16)) return RG_ERR_WORKSPACE;
+  if (words > 0 && (ws == nullptr || ws_bytes < (size_t)words * 4 || !aligned(ws, 16))) return RG_ERR_WORKSPACE;
   EvictArgs a;
   a.score = score;
   a.mass = mass;

@@ -73,14 +73,19 @@ struct MassArgs {
   const int32_t* page_indices;
   int32_t hq, hkv, g;
   float scale_log2, decay;
+  uint32_t g_mul;  // col / g = umulhi(2 col, g_mul) >> g_shift
+  int32_t g_shift;
 };
 hipError_t launch_mass(const MassArgs& a, const AttnPlan& p, int head_dim, bool kv4, hipStream_t stream);
 hipError_t launch_mass_rows(const MassArgs& a, const AttnPlan& p, int head_dim, bool kv4, hipStream_t stream);
 
 // Eviction.
 constexpr int kEvictThreads = 1024;  // select: a work group per (request, KV head)
-constexpr int kMoveThreads = 256;
-constexpr int kMoveTokens = 16;      // move: tokens of a work group
+constexpr int kMoveWaves = 4;        // move: a page per wave
+constexpr int kMoveThreads = 64 * kMoveWaves;
+// Workspace words of a (request, head): two for every kept slot and for every
+// move at most.
+__host__ __device__ inline size_t evict_words(int keep, int most) { return (2 * (size_t)keep + 2 * (size_t)most + 3) / 4 * 4; }
 struct EvictReq {
   int32_t ctx, keep, tracked, evicted;  // keep <= ctx
   int32_t page_start;
@@ -91,6 +96,7 @@ struct EvictReq {
 constexpr int kMaxEvictReq = 96;
 struct EvictPlan {
   int32_t num_req, move_items;
+  int32_t longest;  // most tokens of a request that is cut
   EvictReq req[kMaxEvictReq + 1];
 };
 static_assert(sizeof(EvictPlan) <= 3700, "plan must fit the kernel argument block");
@@ -101,7 +107,7 @@ struct EvictArgs {
   uint8_t* k_cache;  // bf16 K pool, or the 4-bit pool
   uint8_t* v_cache;  // bf16 V pool
   const int32_t* page_indices;
-  int32_t* ws;       // per (request, head): count, 3 words free, then (to, from) pairs
+  int32_t* ws;       // per (request, head): evict_words
   int32_t hkv, sink, recent;
 };
 hipError_t launch_evict(const EvictArgs& a, const EvictPlan& p, int head_dim, bool kv4, hipStream_t stream);

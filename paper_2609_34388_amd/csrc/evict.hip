@@ -7,12 +7,20 @@
 // behind slot `keep` move: into the evicted slots before it, both in ascending
 // order.  No slot is both read and written, so moves run in any order.
 //
-// select: one work group per (request, KV head).  A radix selection over the
-// scores as ordered 32-bit words (protected tokens the largest word) finds the
-// word of the keep-th largest, then each wave walks a contiguous part of the
-// slots: ties are taken from the lowest slot on, holes and movers get their
-// ranks from wave ballots.  It writes the move list, the positions and the
-// mass.  move: copies K and V of 16 moves per work group.
+// select: one work group per (request, KV head), its slots' scores as ordered
+// 32-bit words (protected tokens the largest word) in registers.  A radix
+// selection of 11, 11 and 10 bits finds the word of the keep-th largest; then
+// each wave goes over a contiguous part of the slots: ties are taken from the
+// lowest slot on, holes and movers get their ranks from wave ballots.  It
+// writes for every kept slot which token it takes, if any.  Bound by latency:
+// its loads depend on the page list alone.
+//
+// move: a wave per page of the kept slots, which writes their positions and
+// fills the page's holes: mass and K rows as they are.  In V, where a 16-byte
+// unit holds eight tokens of few dims, a token is a 2-byte piece (1 byte, 4-bit
+// at head size 64) of every unit: the wave reads its sources' units whole, all
+// at once, and moves the pieces in registers.  Bound by the lines that the pieces
+// lie in, of which a page with any hole has most.
 #include "cache_internal.h"
 #include "kv4_device.h"
 
@@ -20,105 +28,145 @@ namespace rg {
 namespace {
 
 constexpr int kWaves = kEvictThreads / 64;
+constexpr int kBins = 2048;
+static_assert(kBins == 2 * kEvictThreads, "two bins a thread");
 
-__device__ __forceinline__ int evict_request(const EvictPlan& p, int item) {
-  const int lane = threadIdx.x & 63;
-  int r = 0;
-  for (int base = 1; base < p.num_req; base += 64) {
-    const int k = base + lane;
-    r += __popcll(__ballot(k < p.num_req && p.req[k].move_start <= item));
-  }
-  return __builtin_amdgcn_readfirstlane(r);
+// Workspace of a (request, head): for every kept slot the token that moves
+// there, as its slot (-1: none) and the page of the pool it is in; then the
+// slots of the holes and of the movers, in order.
+struct MoveList {
+  int2* take;
+  int32_t *hole, *mover;
+};
+__device__ __forceinline__ MoveList move_list(const EvictArgs& a, const EvictReq& q, int hk) {
+  int32_t* at = a.ws + q.ws_start + (size_t)hk * evict_words(q.keep, q.most);
+  return {reinterpret_cast<int2*>(at), at + 2 * (size_t)q.keep, at + 2 * (size_t)q.keep + q.most};
 }
 
-__device__ __forceinline__ int32_t* move_list(const EvictArgs& a, const EvictReq& q, int hk) {
-  return a.ws + q.ws_start + (size_t)hk * (4 + 2 * (size_t)q.most);
-}
-
-__global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a, EvictPlan p) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t s_digit, s_left;
+// KW: words of a thread in registers; slots past them are read again in each pass.
+template <int KW>
+__global__ __launch_bounds__(kEvictThreads, KW <= 8 ? 8 : 4) void evict_select_kernel(EvictArgs a, EvictPlan p) {
+  __shared__ uint32_t hist[kBins];
+  __shared__ uint32_t s_wave[kWaves], s_digit, s_left;
   __shared__ uint32_t s_count[kWaves][3];
   const int r = (int)blockIdx.x / a.hkv, hk = (int)blockIdx.x % a.hkv;
   const EvictReq q = p.req[r];
   const int L = q.ctx, keep = q.keep, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t* pages = a.page_indices + q.page_start;
-  const int recent_from = L + q.evicted - a.recent;  // positions from here on are protected
 
   auto place = [&](int j) { return ((size_t)pages[j >> 4] * a.hkv + hk) * kPageSize + (j & 15); };
   auto position = [&](int j, size_t at) { return j < q.tracked ? a.positions[at] : j + q.evicted; };
-  // A slot's score as a word of the same order: protected tokens the largest.
-  auto word = [&](int j) {
-    const size_t at = place(j);
-    const int pos = position(j, at);
-    if (pos < a.sink || pos >= recent_from) return 0xffffffffu;
-    const uint32_t u = __float_as_uint(a.score[at] + 0.f);  // -0 becomes 0
-    return (u & 0x80000000u) ? ~u : u | 0x80000000u;
-  };
-
-  if (keep == 0) {  // (also an empty request)
-    if (tid == 0) move_list(a, q, hk)[0] = 0;
+  if (q.most == 0) {  // nothing moves: every token stays, or none does
+    for (int j = q.tracked + tid; j < keep; j += kEvictThreads) a.positions[place(j)] = j + q.evicted;
     return;
   }
-  uint32_t prefix = 0, left = (uint32_t)keep;  // of the tokens whose words begin with the prefix, `left` are kept
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
-    __syncthreads();
-    const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
-    for (int j = tid; j < L; j += kEvictThreads) {
-      const uint32_t u = word(j);
-      if ((u & mask) == prefix) atomicAdd(&hist[(u >> shift) & 255], 1u);
+  const int recent_from = L + q.evicted - a.recent;  // positions from here on are protected
+  // Slots of this wave: 64 i + lane from j0 on.
+  const int steps = (L + kEvictThreads - 1) / kEvictThreads;
+  const int j0 = wave * steps * 64 + lane;
+  // A slot's score as a word of the same order: protected tokens the largest.
+  auto word = [&](float score, int pos) {
+    const uint32_t u = __float_as_uint(score + 0.f);  // -0 becomes 0
+    return pos < a.sink || pos >= recent_from ? 0xffffffffu : (u & 0x80000000u) ? ~u : u | 0x80000000u;
+  };
+  auto fetch = [&](int i) {
+    const int j = min(j0 + 64 * i, L - 1);
+    const size_t at = place(j);
+    return word(a.score[at], position(j, at));
+  };
+  // Page numbers of a batch, then its scores (and positions): two round trips.
+  // Slots past the last repeat it and are never asked for (see each()).
+  constexpr int kBatch = KW < 8 ? KW : 8;
+  uint32_t held[KW];
+#pragma unroll
+  for (int i0 = 0; i0 < KW; i0 += kBatch) {
+    if (i0 >= steps) break;
+    size_t at[kBatch];
+    float score[kBatch];
+    int pos[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int j = min(j0 + 64 * (i0 + i), L - 1);
+      at[i] = place(j);
+      pos[i] = j + q.evicted;
     }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) score[i] = a.score[at[i]];
+    if (q.tracked > 0) {
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (min(j0 + 64 * (i0 + i), L - 1) < q.tracked) pos[i] = a.positions[at[i]];
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) held[i0 + i] = word(score[i], pos[i]);
+  }
+  // Calls f(i, word, in range) over the wave's slots, in order.
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < KW; ++i)
+      if (i < steps) f(i, held[i], j0 + 64 * i < L);
+    for (int i = KW; i < steps; ++i) f(i, fetch(i), j0 + 64 * i < L);
+  };
+
+  uint32_t prefix = 0, left = (uint32_t)keep;  // of the tokens whose words begin with the prefix, `left` are kept
+#pragma unroll
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+    const uint32_t mask = pass == 0 ? 0u : pass == 1 ? ~0u << 21 : ~0u << 10;
+    const uint32_t bins = pass == 2 ? 1024u : 2048u;
+    hist[tid] = 0;
+    hist[tid + kEvictThreads] = 0;
     __syncthreads();
-    if (wave == 0) {  // lane l holds bins 255 - 4 l .. 252 - 4 l
-      uint32_t b[4], sum = 0;
-      for (int e = 0; e < 4; ++e) sum += b[e] = hist[255 - 4 * lane - e];
-      uint32_t upto = sum;
-      for (int off = 1; off < 64; off <<= 1) {
-        const uint32_t x = __shfl_up(upto, off);
-        if (lane >= off) upto += x;
-      }
-      uint32_t before = upto - sum;
-      if (before < left && left <= upto) {
-        int e = 0;
-        while (before + b[e] < left) before += b[e++];
-        s_digit = 255 - 4 * lane - e;
-        s_left = left - before;
-      }
+    each([&](int, uint32_t u, bool in) {
+      if (in && (u & mask) == prefix) atomicAdd(&hist[(u >> shift) & (bins - 1)], 1u);
+    });
+    __syncthreads();
+    // from the top bin down, two bins a thread
+    const uint32_t b0 = hist[kBins - 1 - 2 * tid], b1 = hist[kBins - 2 - 2 * tid];
+    uint32_t upto = b0 + b1;
+    for (int off = 1; off < 64; off <<= 1) {
+      const uint32_t x = __shfl_up(upto, off);
+      if (lane >= off) upto += x;
+    }
+    if (lane == 63) s_wave[wave] = upto;
+    __syncthreads();
+    uint32_t before = upto - b0 - b1;
+    for (int w = 0; w < wave; ++w) before += s_wave[w];
+    if (before < left && left <= before + b0 + b1) {
+      const bool second = left > before + b0;
+      s_digit = (uint32_t)(kBins - 1 - 2 * tid) - second;
+      s_left = left - before - (second ? b0 : 0u);
     }
     __syncthreads();
     prefix |= s_digit << shift;
     left = s_left;
   }
 
-  // Slots of this wave, a multiple of 64 from a multiple of 64 on.
-  const int seg = ((L + 64 * kWaves - 1) / (64 * kWaves)) * 64;
-  const int j0 = min(L, wave * seg), j1 = min(L, j0 + seg);
   const uint64_t below = (1ull << lane) - 1;
   uint32_t ties = 0;
-  for (int b = j0; b < j1; b += 64) ties += __popcll(__ballot(b + lane < j1 && word(b + lane) == prefix));
+  each([&](int, uint32_t u, bool in) { ties += __popcll(__ballot(in && u == prefix)); });
   if (lane == 0) s_count[wave][0] = ties;
   __syncthreads();
   uint32_t tie0 = 0;
   for (int w = 0; w < wave; ++w) tie0 += s_count[w][0];
 
-  auto walk = [&](auto visit) {  // visit(j, kept, rank of a hole or mover among the wave's)
+  // visit(j, kept, holes before j and movers before j among the wave's)
+  auto walk = [&](auto visit) {
     uint32_t tie = tie0, holes = 0, movers = 0;
-    for (int b = j0; b < j1; b += 64) {
-      const int j = b + lane;
-      const uint32_t u = j < j1 ? word(j) : 0;
-      const uint64_t eq = __ballot(j < j1 && u == prefix);
-      const bool kept = j < j1 && (u > prefix || (u == prefix && tie + __popcll(eq & below) < left));
-      const uint64_t hole = __ballot(j < j1 && j < keep && !kept), mover = __ballot(kept && j >= keep);
-      if (j < j1) visit(j, kept, j < keep ? holes + __popcll(hole & below) : movers + __popcll(mover & below));
+    each([&](int i, uint32_t u, bool in) {
+      const int j = j0 + 64 * i;
+      const uint64_t eq = __ballot(in && u == prefix);
+      const bool kept = in && (u > prefix || (u == prefix && tie + __popcll(eq & below) < left));
+      const uint64_t hole = __ballot(in && j < keep && !kept), mover = __ballot(kept && j >= keep);
+      if (in) visit(j, kept, holes + (uint32_t)__popcll(hole & below), movers + (uint32_t)__popcll(mover & below));
       tie += __popcll(eq);
       holes += __popcll(hole);
       movers += __popcll(mover);
-    }
+    });
     return make_uint2(holes, movers);
   };
-  const uint2 mine = walk([](int, bool, uint32_t) {});
+  const uint2 mine = walk([](int, bool, uint32_t, uint32_t) {});
   if (lane == 0) {
     s_count[wave][1] = mine.x;
     s_count[wave][2] = mine.y;
@@ -129,73 +177,221 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
     if (w < wave) hole0 += s_count[w][1], mover0 += s_count[w][2];
     count += s_count[w][2];
   }
-  int32_t* list = move_list(a, q, hk);
-  if (tid == 0) list[0] = (int32_t)count;
-  walk([&](int j, bool kept, uint32_t rank) {
-    if (j < keep && !kept) list[4 + 2 * (size_t)(hole0 + rank)] = j;
-    if (j >= keep && kept) list[5 + 2 * (size_t)(mover0 + rank)] = j;
+  const MoveList list = move_list(a, q, hk);
+  walk([&](int j, bool kept, uint32_t holes, uint32_t movers) {
+    if (j < keep) {
+      if (kept) list.take[j] = make_int2(-1, 0);
+      else list.hole[hole0 + holes] = j;
+    } else if (kept) {
+      list.mover[mover0 + movers] = j;
+    }
   });
   __syncthreads();
-  for (int j = max(q.tracked, 0) + tid; j < keep; j += kEvictThreads) a.positions[place(j)] = j + q.evicted;
-  __syncthreads();
-  for (uint32_t k = tid; k < count; k += kEvictThreads) {
-    const int to = list[4 + 2 * (size_t)k], from = list[5 + 2 * (size_t)k];
-    const size_t dst = place(to), src = place(from);
-    a.positions[dst] = position(from, src);
-    if (a.mass) a.mass[dst] = a.mass[src];
+  for (uint32_t k0 = tid; k0 < count; k0 += 4 * kEvictThreads) {  // four at a time in flight
+    int to[4], from[4], page[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const uint32_t k = min(k0 + u * kEvictThreads, count - 1);
+      to[u] = list.hole[k];
+      from[u] = list.mover[k];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) page[u] = pages[from[u] >> 4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (k0 + u * kEvictThreads < count) list.take[to[u]] = make_int2(from[u], page[u]);
   }
 }
 
+// Units of V of one lane: both formats hold eight tokens of a few dims in a
+// unit of E bytes a token; half h of a page's slots has its own units.
+template <int D, bool KV4>
+struct VUnits {
+  static constexpr int E = KV4 ? D / 64 : 2;          // bytes of a token
+  static constexpr int N = KV4 ? 1 : D / 32;          // units of a lane
+  static constexpr int WORDS = 2 * E;                 // 32-bit words of a unit
+  // Half that the lane's units belong to, and byte of its unit i for half h in a block.
+  static __device__ __forceinline__ int half(int lane) { return KV4 ? lane >> 5 : lane & 1; }
+  static __device__ __forceinline__ int at(int lane, int i, int h) {
+    if constexpr (KV4) return Kv4<D>::v_unit(8 * h, lane & 31);
+    else return (((lane >> 1) + 32 * i) * kPageSize + 8 * h) * 2;
+  }
+};
+
 template <int D, bool KV4>
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, EvictPlan p) {
+  using B = Kv4<D>;
+  using V = VUnits<D, KV4>;
   const int item = blockIdx.x;
-  const int r = evict_request(p, item);
-  const EvictReq q = p.req[r];
-  const int groups = (q.most + kMoveTokens - 1) / kMoveTokens;
-  const int local = item - q.move_start;
-  const int hk = local / groups;
-  const int32_t* list = move_list(a, q, hk);
-  const int k = local % groups * kMoveTokens + (int)threadIdx.x / 16, t = threadIdx.x % 16;
-  if (k >= list[0]) return;
-  const int to = list[4 + 2 * (size_t)k], from = list[5 + 2 * (size_t)k];
-  const int32_t* pages = a.page_indices + q.page_start;
-  const size_t dst = (size_t)pages[to >> 4] * a.hkv + hk, src = (size_t)pages[from >> 4] * a.hkv + hk;
-  const int ds = to & 15, ss = from & 15;
-  if constexpr (KV4) {
-    using B = Kv4<D>;
-    uint8_t* x = a.k_cache + dst * B::BLOCK;
-    const uint8_t* y = a.k_cache + src * B::BLOCK;
-    if constexpr (D == 128) {
-      *(uint32_t*)(x + B::k_code(ds, 8 * t)) = *(const uint32_t*)(y + B::k_code(ss, 8 * t));
-#pragma unroll
-      for (int e = 0; e < 2; ++e) *(uint16_t*)(x + B::v_unit(ds, t + 16 * e)) = *(const uint16_t*)(y + B::v_unit(ss, t + 16 * e));
-    } else {
-      *(uint16_t*)(x + B::k_code(ds, 4 * t)) = *(const uint16_t*)(y + B::k_code(ss, 4 * t));
-#pragma unroll
-      for (int e = 0; e < 2; ++e) x[B::v_unit(ds, t + 16 * e)] = y[B::v_unit(ss, t + 16 * e)];
+  int r = 0;
+  {
+    const int lane = threadIdx.x & 63;
+    for (int base = 1; base < p.num_req; base += 64) {
+      const int k = base + lane;
+      r += __popcll(__ballot(k < p.num_req && p.req[k].move_start <= item));
     }
-    if (t < B::DT) x[B::k_scale(ds, t)] = y[B::k_scale(ss, t)];
-    else if (t < 2 * B::DT) x[B::v_scale(ds, t - B::DT)] = y[B::v_scale(ss, t - B::DT)];
-  } else {
-    constexpr int E = D / 16;  // elements of a thread
-    uint16_t* k_cache = reinterpret_cast<uint16_t*>(a.k_cache);
-    uint16_t* v_cache = reinterpret_cast<uint16_t*>(a.v_cache);
-    uint16_t* kd = k_cache + (dst * kPageSize + ds) * D + E * t;
-    const uint16_t* ks = k_cache + (src * kPageSize + ss) * D + E * t;
-    if constexpr (D == 128) *(u32x4*)kd = *(const u32x4*)ks;
-    else *(u32x2*)kd = *(const u32x2*)ks;
-    uint16_t x[E];
+    r = __builtin_amdgcn_readfirstlane(r);
+  }
+  const EvictReq q = p.req[r];
+  const int npage = (q.keep + 15) / 16;
+  // heads fastest: with 8 of them a head's pages stay on one XCD, whose L2 then
+  // holds the sources that neighbouring pages share
+  const int local = item - q.move_start, hk = local % a.hkv;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int page = local / a.hkv * kMoveWaves + wave;
+  if (page >= npage) return;
+  if (q.most == 0) return;  // (its select wrote the positions)
+  const MoveList list = move_list(a, q, hk);
+  const int lane = threadIdx.x & 63;
+  const int32_t* pages = a.page_indices + q.page_start;
+  const size_t dst = (size_t)pages[page] * a.hkv + hk;
+  // lane l < 16: what slot l takes, its mass and position
+  const int j = page * 16 + lane;
+  const int2 take = lane < 16 && j < q.keep ? list.take[j] : make_int2(-1, 0);
+  const bool filled = take.x >= 0;
+  const uint64_t holes = __ballot(filled);
+  const int cnt = __popcll(holes);
+  if (filled) {
+    const size_t src = ((size_t)take.y * a.hkv + hk) * kPageSize + (take.x & 15);
+    a.positions[dst * kPageSize + lane] = take.x < q.tracked ? a.positions[src] : take.x + q.evicted;
+    if (a.mass) a.mass[dst * kPageSize + lane] = a.mass[src];
+  } else if (lane < 16 && j >= q.tracked && j < q.keep) {
+    a.positions[dst * kPageSize + lane] = j + q.evicted;
+  }
+  if (cnt == 0) return;
+  // lane k < cnt: the k-th hole (others of the wave send to a lane past the holes)
+  const int rank = filled ? __popcll(holes & ((1ull << lane) - 1)) : 32 + (lane & 31);
+  const int nth = __builtin_amdgcn_ds_permute(4 * rank, lane);
+  const int to = lane < cnt ? nth : 16;
+  const int from = __shfl(take.x, nth & 15), from_page = __shfl(take.y, nth & 15);
+  auto source = [&](int k) { return (size_t)__shfl(from_page, k) * a.hkv + hk; };
+
+  constexpr size_t KBLOCK = KV4 ? (size_t)B::BLOCK : (size_t)kPageSize * D * 2;  // bytes of a block of the K pool
+  constexpr size_t VBLOCK = KV4 ? (size_t)B::BLOCK : (size_t)kPageSize * D * 2;
+  uint8_t* vdst = (KV4 ? a.k_cache : a.v_cache) + dst * VBLOCK;
+  const uint8_t* vpool = KV4 ? a.k_cache : a.v_cache;
+  uint8_t* kdst = a.k_cache + dst * KBLOCK;
+
+  // K: 16 lanes a move, four moves at a time; the loads go out before the stores.
+  constexpr int KW = KV4 ? 1 : D / 32;  // 32-bit words of a lane (one of two or four bytes, 4-bit)
+  uint32_t kx[4][KW];
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = v_cache[(src * D + t + 16 * e) * kPageSize + ss];
+  for (int i = 0; i < 4; ++i) {
+    const int k = 4 * i + (lane >> 4), t = lane & 15, c = min(k, cnt - 1);
+    const int ss = __shfl(from, c) & 15;
+    const uint8_t* src = a.k_cache + source(c) * KBLOCK;
+    if (k >= cnt) continue;
+    if constexpr (KV4 && D == 128) kx[i][0] = *(const uint32_t*)(src + B::k_code(ss, 8 * t));
+    else if constexpr (KV4) kx[i][0] = *(const uint16_t*)(src + B::k_code(ss, 4 * t));
+    else
 #pragma unroll
-    for (int e = 0; e < E; ++e) v_cache[(dst * D + t + 16 * e) * kPageSize + ds] = x[e];
+      for (int e = 0; e < KW; ++e) kx[i][e] = *(const uint32_t*)(src + ss * 2 * D + 4 * KW * t + 4 * e);
+  }
+  uint8_t ks = 0, vs = 0;  // scales: a lane per (move, group)
+  if constexpr (KV4) {
+    const int k = lane / B::DT, c = min(k, cnt - 1), g = lane % B::DT;
+    const int ss = __shfl(from, c) & 15;
+    const uint8_t* src = a.k_cache + source(c) * KBLOCK;
+    if (k < cnt) {
+      ks = src[B::k_scale(ss, g)];
+      vs = src[B::v_scale(ss, g)];
+    }
+  }
+
+  // V: the lane's units of its half, patched by that half's moves, kBatch at a time.
+  constexpr int kBatch = KV4 ? 4 : 2;
+  const int h = V::half(lane);
+  const int n0 = __popcll(__ballot(to < 8)), mine0 = h ? n0 : 0, mine = h ? cnt - n0 : n0;
+  const int most = max(n0, cnt - n0);
+  uint32_t unit[V::N][V::WORDS];
+  auto read = [&](const uint8_t* block, int hh, uint32_t (&u)[V::N][V::WORDS]) {
+#pragma unroll
+    for (int i = 0; i < V::N; ++i) {
+      if constexpr (V::WORDS == 4) {
+        const u32x4 x = *(const u32x4*)(block + V::at(lane, i, hh));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[i][e] = x[e];
+      } else {
+        const u32x2 x = *(const u32x2*)(block + V::at(lane, i, hh));
+        u[i][0] = x[0], u[i][1] = x[1];
+      }
+    }
+  };
+  // A half that holds slots of `keep` and on, sources perhaps: its pieces are written alone.
+  const bool whole = page * 16 + 8 * h + 8 <= q.keep;
+  if (mine > 0 && whole) read(vdst, h, unit);
+  for (int i0 = 0; i0 < most; i0 += kBatch) {
+    uint32_t x[kBatch][V::N][V::WORDS];
+    int ds[kBatch], ss[kBatch];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const int c = min(mine0 + i0 + b, cnt - 1);  // shuffles are done by every lane
+      const int f = __shfl(from, c);
+      ds[b] = __shfl(to, c) & 7;
+      ss[b] = f & 7;
+      const size_t src = source(c);
+      if (i0 + b < mine) read(vpool + src * VBLOCK, (f >> 3) & 1, x[b]);
+    }
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      if (i0 + b >= mine) continue;
+      constexpr int PER = 4 / V::E;  // tokens of a word
+      const uint32_t mask = V::E == 2 ? 0xffffu : 0xffu;
+      const int sh = 8 * V::E * (ds[b] % PER);
+#pragma unroll
+      for (int n = 0; n < V::N; ++n) {
+        uint32_t w = x[b][n][0];
+#pragma unroll
+        for (int e = 1; e < V::WORDS; ++e) w = ss[b] / PER == e ? x[b][n][e] : w;
+        const uint32_t piece = (w >> (8 * V::E * (ss[b] % PER))) & mask;
+        if (whole) {
+#pragma unroll
+          for (int e = 0; e < V::WORDS; ++e)
+            if (ds[b] / PER == e) unit[n][e] = (unit[n][e] & ~(mask << sh)) | (piece << sh);
+        } else {
+          uint8_t* at = vdst + V::at(lane, n, h) + V::E * ds[b];
+          if constexpr (V::E == 2) *(uint16_t*)at = (uint16_t)piece;
+          else *at = (uint8_t)piece;
+        }
+      }
+    }
+  }
+  if (mine > 0 && whole) {
+#pragma unroll
+    for (int i = 0; i < V::N; ++i) {
+      if constexpr (V::WORDS == 4) *(u32x4*)(vdst + V::at(lane, i, h)) = u32x4{unit[i][0], unit[i][1], unit[i][2], unit[i][3]};
+      else *(u32x2*)(vdst + V::at(lane, i, h)) = u32x2{unit[i][0], unit[i][1]};
+    }
+  }
+
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int k = 4 * i + (lane >> 4), t = lane & 15, ds = __shfl(to, min(k, cnt - 1));
+    if (k >= cnt) continue;
+    if constexpr (KV4 && D == 128) *(uint32_t*)(kdst + B::k_code(ds, 8 * t)) = kx[i][0];
+    else if constexpr (KV4) *(uint16_t*)(kdst + B::k_code(ds, 4 * t)) = (uint16_t)kx[i][0];
+    else
+#pragma unroll
+      for (int e = 0; e < KW; ++e) *(uint32_t*)(kdst + ds * 2 * D + 4 * KW * t + 4 * e) = kx[i][e];
+  }
+  if constexpr (KV4) {
+    const int k = lane / B::DT, g = lane % B::DT, ds = __shfl(to, min(k, cnt - 1));
+    if (k < cnt) {
+      kdst[B::k_scale(ds, g)] = ks;
+      kdst[B::v_scale(ds, g)] = vs;
+    }
   }
 }
 
 }  // namespace
 
 hipError_t launch_evict(const EvictArgs& a, const EvictPlan& p, int head_dim, bool kv4, hipStream_t stream) {
-  hipLaunchKernelGGL(evict_select_kernel, dim3(p.num_req * a.hkv), dim3(kEvictThreads), 0, stream, a, p);
+  const dim3 heads(p.num_req * a.hkv), threads(kEvictThreads);
+  const int steps = (p.longest + kEvictThreads - 1) / kEvictThreads;
+  if (steps <= 4) hipLaunchKernelGGL((evict_select_kernel<4>), heads, threads, 0, stream, a, p);
+  else if (steps <= 8) hipLaunchKernelGGL((evict_select_kernel<8>), heads, threads, 0, stream, a, p);
+  else if (steps <= 16) hipLaunchKernelGGL((evict_select_kernel<16>), heads, threads, 0, stream, a, p);
+  else hipLaunchKernelGGL((evict_select_kernel<32>), heads, threads, 0, stream, a, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.move_items == 0) return e;
   const dim3 grid(p.move_items), block(kMoveThreads);

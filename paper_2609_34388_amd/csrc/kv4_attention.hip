@@ -128,14 +128,23 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
     ahead = pages_of(kgi + 2 * kg);
   }
   // Q of the column group, by the whole work group, behind the first codes.
-  for (int u = threadIdx.x; u < it.nct * 32 * (D / 8); u += kThreads) {
-    const int row = u / (D / 8), ch = u % (D / 8), col = it.tile0 * 32 + row;
-    u32x4 x = {0u, 0u, 0u, 0u};
-    if (col < it.M) {
-      const int tok = col / g;
-      x = *(const u32x4*)(a.q + ((size_t)(rq.q_start + tok) * a.hq + it.hk * g + (col - tok * g)) * D + 8 * ch);
+  {
+    constexpr int N = kKv4Cols * (D / 8) / kThreads;  // loads of a thread, all before the stores
+    u32x4 x[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const int u = threadIdx.x + e * kThreads, row = u / (D / 8), ch = u % (D / 8), col = it.tile0 * 32 + row;
+      x[e] = u32x4{0u, 0u, 0u, 0u};
+      if (row < 32 * it.nct && col < it.M) {
+        const int tok = col / g;
+        x[e] = *(const u32x4*)(a.q + ((size_t)(rq.q_start + tok) * a.hq + it.hk * g + (col - tok * g)) * D + 8 * ch);
+      }
     }
-    *(u32x4*)(lds + S::Q + row * S::QROW + 16 * ch) = x;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const int u = threadIdx.x + e * kThreads, row = u / (D / 8), ch = u % (D / 8);
+      if (row < 32 * it.nct) *(u32x4*)(lds + S::Q + row * S::QROW + 16 * ch) = x[e];
+    }
   }
   int lim[TILES], slo[TILES], shi[TILES], min_lim[TILES];
   bool open[TILES];  // some column that sees keys of the run has no reference yet

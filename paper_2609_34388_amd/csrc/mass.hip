@@ -11,11 +11,11 @@
 // Up to 128 query columns a request (mass_kernel) the bytes of K bound it: Q
 // lies in LDS, waves take key tiles.  A bf16 wave holds two key tiles, read
 // straight from the pool; four times fewer bytes of a 4-bit key would leave a
-// work group that small waiting for its start, so it takes a longer run of keys
-// whose codes come through LDS, four key tiles ahead.  With more columns
+// work group that small waiting for its start, so it takes a longer run of keys,
+// two tiles a step, with the next step's codes in flight.  With more columns
 // (mass_rows_kernel, prompts) the products and exponentials bound it: a work
 // group takes 64 keys, held in registers by each of its waves, and the waves
-// share the column tiles, whose Q comes through a ring of LDS of the wave's own.
+// share the column tiles, whose Q comes through LDS of the wave's own.
 #include "cache_internal.h"
 #include "kv4_device.h"
 
@@ -40,17 +40,21 @@ __device__ __forceinline__ MassItem mass_item(const MassArgs& a, const AttnPlan&
   it.L = rq.ctx;
   it.T = it.L + it.V;
   it.M = (a.row_count ? min(max(a.row_count[rq.part_start], 0), it.V) : it.V) * a.g;
-  const int nch = (it.T + keys - 1) / keys, local = item - rq.item_start;
-  it.hk = local / nch;
-  it.kbeg = local % nch * keys;
+  const int local = item - rq.item_start;  // heads fastest: a prompt's costliest keys, its first, come first
+  it.hk = local % a.hkv;
+  it.kbeg = local / a.hkv * keys;
   it.q_start = rq.q_start;
   it.page_start = rq.page_start;
   return it;
 }
 
+// Query row of a column: col / g, exact below 2^31 (cache_api.cpp).
+__device__ __forceinline__ int row_of(const MassArgs& a, int col) {
+  return (int)(__umulhi(2u * (uint32_t)col, a.g_mul) >> a.g_shift);
+}
 // Row of q and lse of a column.
 __device__ __forceinline__ size_t column_row(const MassArgs& a, const MassItem& it, int col) {
-  const int tok = col / a.g;
+  const int tok = row_of(a, col);
   return (size_t)(it.q_start + tok) * a.hq + it.hk * a.g + (col - tok * a.g);
 }
 
@@ -86,11 +90,11 @@ __device__ __forceinline__ int q_chunk(int ks, int lh) {
 __device__ __forceinline__ void add_weights(const MassArgs& a, const MassItem& it, f32x16 sc, const float (&ls)[16], int col0,
                                             int kb, float& w) {
   const int lane = threadIdx.x & 63, lc = lane & 31, lh = lane >> 5;
-  if (kb + 31 > it.L + col0 / a.g) {  // some row does not see every key
+  if (kb + 31 > it.L + row_of(a, col0)) {  // some row does not see every key
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int col = col0 + 8 * (i >> 2) + 4 * lh + (i & 3);
-      if (kb + lc > it.L + col / a.g) sc[i] = kNegInf;
+      if (kb + lc > it.L + row_of(a, col)) sc[i] = kNegInf;
     }
   }
 #pragma unroll
@@ -103,12 +107,10 @@ __device__ __forceinline__ void write_mass(const MassArgs& a, const MassItem& it
 }
 
 template <int D, bool KV4>
-__global__ __launch_bounds__(kThreads, 2) void mass_kernel(MassArgs a, AttnPlan p) {
+__global__ __launch_bounds__(kThreads, KV4 ? 3 : 2) void mass_kernel(MassArgs a, AttnPlan p) {
   constexpr int KSTEPS = D / 16, QROW = 2 * D + 16;  // 16 bytes more: a fragment read meets every bank once
-  constexpr int RING = 4, SLOT = KV4 ? 2 * 17 * D / 2 : 0;  // codes of K of two blocks
-  __shared__ __attribute__((aligned(16))) char lds[kMassWaves * RING * SLOT + kMassCols * QROW + kMassCols * 4 +
-                                                       (KV4 ? kMassRun * 4 : 0)];
-  char* qs = lds + kMassWaves * RING * SLOT;
+  __shared__ __attribute__((aligned(16))) char lds[kMassCols * QROW + kMassCols * 4 + (KV4 ? kMassRun * 4 : 0)];
+  char* qs = lds;
   float* lse2 = reinterpret_cast<float*>(qs + kMassCols * QROW);
   float* sums = lse2 + kMassCols;  // 4-bit: of the run's keys
   const int run = KV4 ? p.chunk : kMassKeys;
@@ -117,118 +119,125 @@ __global__ __launch_bounds__(kThreads, 2) void mass_kernel(MassArgs a, AttnPlan 
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int tiles = (it.M + 31) / 32;
 
-  // 4-bit: the first tiles' codes go out first
+  // 4-bit: codes and scales of two key tiles; their loads go out first
   typedef const int32_t __attribute__((address_space(4))) * cpage_ptr;
   const cpage_ptr pages = (cpage_ptr)(a.page_indices + it.page_start);
-  const int last = (it.T - 1) / kPageSize;
-  char* ring = lds + wave * RING * SLOT;
-  const uint32_t ring_at = KV4 ? lds_place(ring) : 0;
-  constexpr int KPART = 17 * D / 2;
-  auto load = [&](int slot, int kb) {
+  const int last = (it.T - 1) / kPageSize, kend = min(it.T, it.kbeg + run);
+  constexpr int STEP = 32 * kMassWaves;  // keys from a wave's tile to its next
+  u32x4 kc[2][D / 64];
+  uint32_t ksc[2];
+  auto load = [&](int kb) {
+    using B = Kv4<D>;
 #pragma unroll
-    for (int pp = 0; pp < 2; ++pp) {
-      const uint8_t* b = static_cast<const uint8_t*>(a.keys) + ((size_t)pages[min((kb >> 4) + pp, last)] * a.hkv + it.hk) * (17 * D);
+    for (int s = 0; s < 2; ++s) {
+      const int pg = (kb + STEP * s) >> 4;
+      const int p0 = pages[min(pg, last)], p1 = pages[min(pg + 1, last)];
+      const uint8_t* b = static_cast<const uint8_t*>(a.keys) + ((size_t)(lc < 16 ? p0 : p1) * a.hkv + it.hk) * B::BLOCK;
 #pragma unroll
-      for (int at = 0; at < KPART; at += 1024)
-        if (at + 1024 <= KPART || at + 16 * lane < KPART) load_to_lds(ring_at + slot * SLOT + pp * KPART + at, b + at, 16 * lane);
+      for (int i = 0; i < D / 64; ++i) kc[s][i] = *(const u32x4*)(b + B::k_code(lc & 15, 64 * i + 32 * lh));
+      const uint8_t* sc = b + B::k_scale(lc & 15, 0);
+      ksc[s] = D == 128 ? *(const uint32_t*)sc : *(const uint16_t*)sc;
     }
   };
-  constexpr int LOADS = 2 * ((KPART + 1023) / 1024);
-  const int kend = min(it.T, it.kbeg + run);
-  if constexpr (KV4) {
-#pragma unroll
-    for (int s = 0; s < RING - 1; ++s)
-      if (it.kbeg + 32 * (wave + kMassWaves * s) < kend) load(s, it.kbeg + 32 * (wave + kMassWaves * s));
-  }
+  if constexpr (KV4) load(it.kbeg + 32 * wave);
   bf16x8 kf[KV4 ? 1 : kMassSub][KSTEPS];
   if constexpr (!KV4) {
 #pragma unroll
     for (int s = 0; s < kMassSub; ++s) load_keys<D, false>(a, it, it.kbeg + 32 * (wave + kMassWaves * s), kf[s]);
+    asm volatile("" ::: "memory");  // these loads go out before those of Q
   }
 
-  for (int u = tid; u < tiles * 32 * (D / 8); u += kThreads) {
-    const int row = u / (D / 8), ch = u % (D / 8);
-    u32x4 x = {0u, 0u, 0u, 0u};
-    if (row < it.M) x = *(const u32x4*)(a.q + column_row(a, it, row) * D + 8 * ch);
-    *(u32x4*)(qs + row * QROW + 16 * ch) = x;
+  u32x4 qx[kMassCols * (D / 8) / kThreads];  // all loads, then all stores
+#pragma unroll
+  for (int e = 0; e < kMassCols * (D / 8) / kThreads; ++e) {
+    const int u = tid + e * kThreads, row = u / (D / 8), ch = u % (D / 8);
+    qx[e] = u32x4{0u, 0u, 0u, 0u};
+    if (row < it.M) qx[e] = *(const u32x4*)(a.q + column_row(a, it, row) * D + 8 * ch);
+  }
+#pragma unroll
+  for (int e = 0; e < kMassCols * (D / 8) / kThreads; ++e) {
+    const int u = tid + e * kThreads, row = u / (D / 8), ch = u % (D / 8);
+    if (row < 32 * tiles) *(u32x4*)(qs + row * QROW + 16 * ch) = qx[e];
   }
   // a column that does not count weighs exp2(-inf) = 0
   if (tid < 32 * tiles) lse2[tid] = tid < it.M ? a.lse[column_row(a, it, tid)] * kLog2e : -kNegInf;
   lds_barrier();
 
-  auto weigh = [&](const bf16x8 (&k)[KSTEPS], int kb, float& w) {
+  // Adds the weights of N key tiles, 32 * kMassWaves keys apart, over all columns.
+  auto weigh = [&](const auto& k, int kb, auto& w) {
+    constexpr int N = sizeof(w) / sizeof(w[0]);
     for (int t = 0; t < tiles; ++t) {
-      f32x16 sc;
-      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+      f32x16 sc[N];
+#pragma unroll
+      for (int s = 0; s < N; ++s)
+        for (int i = 0; i < 16; ++i) sc[s][i] = 0.f;
       const char* row = qs + (32 * t + lc) * QROW;
+      bf16x8 qf[KSTEPS];
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = *(const bf16x8*)(row + 16 * q_chunk<KV4>(ks, lh));
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks)
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(row + 16 * q_chunk<KV4>(ks, lh)), k[ks], sc, 0, 0, 0);
+#pragma unroll
+        for (int s = 0; s < N; ++s) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[ks], k[s][ks], sc[s], 0, 0, 0);
       float ls[16];
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) {
         const float4 x = *(const float4*)(lse2 + 32 * t + 8 * i4 + 4 * lh);
         ls[4 * i4] = x.x, ls[4 * i4 + 1] = x.y, ls[4 * i4 + 2] = x.z, ls[4 * i4 + 3] = x.w;
       }
-      add_weights(a, it, sc, ls, 32 * t, kb, w);
+#pragma unroll
+      for (int s = 0; s < N; ++s) add_weights(a, it, sc[s], ls, 32 * t, kb + 32 * kMassWaves * s, w[s]);
     }
   };
   if constexpr (KV4) {
-    using B = Kv4<D>;
-    const int koff = (lc < 16 ? 0 : KPART) + (lc & 15) * 32 + 16 * lh, ksoff = (lc < 16 ? 0 : KPART) + B::k_scale(lc & 15, 0);
-    int slot = 0;
-    for (int kb = it.kbeg + 32 * wave; kb < kend; kb += 32 * kMassWaves) {
-      // the loads of the tiles after this one may be in flight, its own not
-      const int ahead = min((kend - 1 - kb) / (32 * kMassWaves), RING - 2);
-      if (ahead == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
-      else if (ahead == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
-      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      static_assert(RING == 4, "the waits above");
-      const char* code = ring + slot * SLOT;
-      const uint32_t scale = (D == 128 ? *(const uint32_t*)(code + ksoff) : *(const uint16_t*)(code + ksoff)) >> (8 * lh);
-      bf16x8 k[KSTEPS];
+    // two key tiles a step: half the reads of Q, two chains of products
+    for (int kb = it.kbeg + 32 * wave; kb < kend; kb += 2 * STEP) {
+      bf16x8 k[2][KSTEPS];
 #pragma unroll
-      for (int i = 0; i < D / 64; ++i) {
-        const u32x4 c = *(const u32x4*)(code + koff + 512 * i);
-        const float s = scale_of((scale >> (16 * i)) & 0xff);
+      for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) k[4 * i + e] = __builtin_bit_cast(bf16x8, decode8(c[e], s));
-      }
-      const int next = kb + 32 * kMassWaves * (RING - 1);
-      if (next < kend) load((slot + RING - 1) % RING, next);  // where the tile before this one was
-      float w = 0.f;
+        for (int i = 0; i < D / 64; ++i) {
+          const float f = scale_of((ksc[s] >> (8 * lh + 16 * i)) & 0xff);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) k[s][4 * i + e] = __builtin_bit_cast(bf16x8, decode8(kc[s][i][e], f));
+        }
+      if (kb + 2 * STEP < kend) load(kb + 2 * STEP);
+      float w[2] = {0.f, 0.f};
       weigh(k, kb, w);
-      w += __shfl_xor(w, 32);
-      if (lh == 0) sums[kb - it.kbeg + lc] = w;
-      slot = (slot + 1) % RING;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const float sum = w[s] + __shfl_xor(w[s], 32);
+        if (lh == 0 && kb + STEP * s < kend) sums[kb + STEP * s - it.kbeg + lc] = sum;
+      }
     }
     // behind the loop: a load or store of the mass in it would wait for the codes
     lds_barrier();
     for (int key = it.kbeg + tid; key < kend; key += kThreads) write_mass(a, it, key, sums[key - it.kbeg]);
   } else {
+    const int kb = it.kbeg + 32 * wave;
+    float w[kMassSub] = {};
+    if (kb < it.T) weigh(kf, kb, w);
 #pragma unroll
     for (int s = 0; s < kMassSub; ++s) {
-      const int kb = it.kbeg + 32 * (wave + kMassWaves * s);
-      float w = 0.f;
-      if (kb < it.T) weigh(kf[s], kb, w);
-      w += __shfl_xor(w, 32);
-      if (lh == 0 && kb + lc < it.T) write_mass(a, it, kb + lc, w);
+      const float sum = w[s] + __shfl_xor(w[s], 32);
+      const int key = kb + 32 * kMassWaves * s + lc;
+      if (lh == 0 && key < it.T) write_mass(a, it, key, sum);
     }
   }
 }
 
 template <int D, bool KV4>
-__global__ __launch_bounds__(kThreads, 2) void mass_rows_kernel(MassArgs a, AttnPlan p) {
+__global__ __launch_bounds__(kThreads, 3) void mass_rows_kernel(MassArgs a, AttnPlan p) {
   constexpr int KSTEPS = D / 16, NCH = D / 8, TILE = 32 * D * 2;  // bytes of a column tile of Q
   constexpr int LOADS = TILE / 1024;
-  __shared__ __attribute__((aligned(16))) char lds[kMassWaves * 2 * TILE + kMassWaves * 128 + kMassWaves * kMassRowKeys * 4];
+  __shared__ __attribute__((aligned(16))) char lds[kMassWaves * TILE + kMassWaves * 128 + kMassWaves * kMassRowKeys * 4];
   const MassItem it = mass_item(a, p, kMassRowKeys);
   const int tid = threadIdx.x, lane = tid & 63, lc = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  char* ring = lds + wave * 2 * TILE;
-  const uint32_t ring_at = lds_place(ring);
-  float* lse2 = reinterpret_cast<float*>(lds + kMassWaves * 2 * TILE) + wave * 32;
-  float* sums = reinterpret_cast<float*>(lds + kMassWaves * 2 * TILE + kMassWaves * 128);
+  char* tile = lds + wave * TILE;
+  const uint32_t tile_at = lds_place(tile);
+  float* lse2 = reinterpret_cast<float*>(lds + kMassWaves * TILE) + wave * 32;
+  float* sums = reinterpret_cast<float*>(lds + kMassWaves * TILE + kMassWaves * 128);
 
   // This wave's column tiles: every kMassWaves-th of those whose rows see a key.
   const int tiles = (it.M + 31) / 32;
@@ -237,31 +246,31 @@ __global__ __launch_bounds__(kThreads, 2) void mass_rows_kernel(MassArgs a, Attn
   // Columns past the counted ones repeat the last: they weigh zero.
   const uint16_t* base = a.q + (size_t)it.q_start * a.hq * D;
   float ls_next = 0.f;
-  auto load = [&](int slot, int t) {
+  const uint32_t head = (uint32_t)(it.hk * a.g);
+  auto load = [&](int t) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int row = (i * 64 + lane) / NCH, ch = (lane % NCH) ^ (row % NCH);
-      const int col = min(32 * t + row, it.M - 1);
+      const int col = min(32 * t + row, it.M - 1), tok = row_of(a, col);
       // rows of a request lie within 2^31 bytes of its first (checked by the host)
-      load_to_lds(ring_at + slot * TILE + i * 1024, base,
-                  (uint32_t)((column_row(a, it, col) - (size_t)it.q_start * a.hq) * D + 8 * ch) * 2);
+      const uint32_t at = (uint32_t)(tok * a.hq + (col - tok * a.g)) + head;
+      load_to_lds(tile_at + i * 1024, base, (at * D + 8 * ch) * 2);
     }
     const int col = 32 * t + lc;
     ls_next = col < it.M ? a.lse[column_row(a, it, col)] : -kNegInf;
   };
-  if (t0 < tiles) load(0, t0);
+  if (t0 < tiles) load(t0);
 
   bf16x8 kf[2][KSTEPS];
 #pragma unroll
   for (int s = 0; s < 2; ++s) load_keys<D, KV4>(a, it, it.kbeg + 32 * s, kf[s]);
 
   float w[2] = {0.f, 0.f};
-  int slot = 0;
-  for (int t = t0; t < tiles; t += kMassWaves, slot ^= 1) {
+  for (int t = t0; t < tiles; t += kMassWaves) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (lh == 0) lse2[lc] = ls_next * kLog2e;  // the wave's own: no barrier
     bf16x8 qf[KSTEPS];
-    const char* row = ring + slot * TILE + lc * (2 * D);
+    const char* row = tile + lc * (2 * D);
 #pragma unroll
     for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = *(const bf16x8*)(row + 16 * (q_chunk<KV4>(ks, lh) ^ (lc % NCH)));
     float ls[16];
@@ -270,7 +279,10 @@ __global__ __launch_bounds__(kThreads, 2) void mass_rows_kernel(MassArgs a, Attn
       const float4 x = *(const float4*)(lse2 + 8 * i4 + 4 * lh);
       ls[4 * i4] = x.x, ls[4 * i4 + 1] = x.y, ls[4 * i4 + 2] = x.z, ls[4 * i4 + 3] = x.w;
     }
-    if (t + kMassWaves < tiles) load(slot ^ 1, t + kMassWaves);
+    if (t + kMassWaves < tiles) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile is in registers
+      load(t + kMassWaves);
+    }
     f32x16 sc[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s)
