@@ -611,7 +611,7 @@ def new_kv4_cache(num_pages: int, num_kv_heads: int, head_dim: int, device) -> t
 
 def _kv4(cache: torch.Tensor, head_dim: int, num_kv_heads: int, num_pages: int) -> torch.Tensor:
     _dev(cache, "cache", torch.uint8)
-    if tuple(cache.shape) != (num_pages, num_kv_heads, kv4_block_bytes(head_dim)):
+    if cache.shape != (num_pages, num_kv_heads, 17 * head_dim):
         raise ValueError("cache must be [pages, Hkv, 17 D] of the layout's sizes")
     return cache
 
@@ -626,11 +626,21 @@ def make_kv4_layout(num_q_heads: int, cache: torch.Tensor, q_indptr, n_verify, c
                    sm_scale)
 
 
-def _check_layout(lay: _Layout, rows: int):
-    if int(lay.q_indptr[-1]) != rows:
+def _check_layout(lay, rows: int, *tensors: torch.Tensor):
+    """The arrays' lengths, and that the call's tensors are all on the current
+    device, where its kernels run."""
+    if lay.q_indptr[-1] != rows:
         raise ValueError("q_indptr[-1] must equal the number of rows")
-    if lay.page_indices.numel() < int(lay.page_indptr[-1]):
+    if lay.page_indices.numel() < lay.page_indptr[-1]:
         raise ValueError("page_indices is shorter than page_indptr[-1]")
+    _here(lay.page_indices, *tensors)
+
+
+def _here(*tensors: Optional[torch.Tensor]):
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"a tensor is on device {t.get_device()}, the current device is {here}")
 
 
 def _rows(t: torch.Tensor, name: str, lay: _Layout) -> int:
@@ -638,10 +648,12 @@ def _rows(t: torch.Tensor, name: str, lay: _Layout) -> int:
     hkv, d = lay.c.num_kv_heads, lay.c.head_dim
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.bfloat16:
         raise TypeError(f"{name} must be a CUDA bf16 tensor")
-    if t.dim() != 3 or t.shape[1] != hkv or t.shape[2] != d or t.stride(2) != 1 or (hkv > 1 and t.stride(1) != d):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != hkv or shape[2] != d or stride[2] != 1 or (hkv > 1 and stride[1] != d):
         raise ValueError(f"{name} must be [rows, {hkv}, {d}], contiguous within a row")
-    _check_layout(lay, t.shape[0])
-    return t.stride(0) if t.shape[0] > 1 else hkv * d
+    if shape[0] != lay.q_indptr[-1]:
+        raise ValueError("q_indptr[-1] must equal the number of rows")
+    return stride[0] if shape[0] > 1 else hkv * d
 
 
 def kv4_append(k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor, layout: _Layout, *, stream=None) -> None:
@@ -650,6 +662,7 @@ def kv4_append(k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor, layout: _L
     (rg_kv4_append)."""
     ks, vs = _rows(k, "k", layout), _rows(v, "v", layout)
     _kv4(cache, layout.c.head_dim, layout.c.num_kv_heads, layout.c.num_pages)
+    _check_layout(layout, k.shape[0], k, v, cache)
     if k.shape[0] == 0:
         return
     _check(_lib().rg_kv4_append(ctypes.byref(layout.c), k.data_ptr(), ks, v.data_ptr(), vs, cache.data_ptr(),
@@ -664,6 +677,7 @@ def kv4_read(cache: torch.Tensor, layout: _Layout, *, k_out: Optional[torch.Tens
     k = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if k_out is None else k_out
     v = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if v_out is None else v_out
     ks, vs = _rows(k, "k_out", layout), _rows(v, "v_out", layout)
+    _check_layout(layout, shape[0], k, v, cache)
     if shape[0]:
         _check(_lib().rg_kv4_read(ctypes.byref(layout.c), cache.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs,
                                   _stream(stream)), "rg_kv4_read")
@@ -687,7 +701,7 @@ def kv4_attention(q: torch.Tensor, cache: torch.Tensor, layout: _Layout, branche
     if q.dim() != 3 or q.shape[1] != layout.c.num_q_heads or q.shape[2] != layout.c.head_dim:
         raise ValueError("q must be [rows, Hq, D] of the layout's sizes")
     _kv4(cache, layout.c.head_dim, layout.c.num_kv_heads, layout.c.num_pages)
-    _check_layout(layout, q.shape[0])
+    _check_layout(layout, q.shape[0], q, cache, workspace)
     if branches is not None and branches.branch_indptr.shape[0] != layout.ctx_len.shape[0] + 1:
         raise ValueError("branch_indptr must have num_requests + 1 entries")
     if out is None:
@@ -698,6 +712,7 @@ def kv4_attention(q: torch.Tensor, cache: torch.Tensor, layout: _Layout, branche
         lse = torch.empty(q.shape[0], q.shape[1], dtype=torch.float32, device=q.device)
     if lse is not None and _dev(lse, "lse", torch.float32).shape != q.shape[:2]:
         raise ValueError("lse must be [rows, Hq]")
+    _here(out, lse)
     if q.shape[0] == 0:
         return out, lse
     if workspace is None:  # the call itself checks the size of one that is given
@@ -719,16 +734,16 @@ def _slot_pool(t: torch.Tensor, name: str, dtype: torch.dtype, num_pages: int, n
     return t
 
 
-def _mass_args(q, lse, mass, layout: _Layout, row_count, stream):
+def _mass_args(q, keys, lse, mass, layout: _Layout, row_count):
     _dev(q, "q", torch.bfloat16)
     if q.dim() != 3 or q.shape[1] != layout.c.num_q_heads or q.shape[2] != layout.c.head_dim:
         raise ValueError("q must be [rows, Hq, D] of the layout's sizes")
-    _check_layout(layout, q.shape[0])
     if _dev(lse, "lse", torch.float32).shape != q.shape[:2]:
         raise ValueError("lse must be [rows, Hq]")
     _slot_pool(mass, "mass", torch.float32, layout.c.num_pages, layout.c.num_kv_heads)
     if row_count is not None and _dev(row_count, "row_count", torch.int32).numel() != layout.c.num_requests:
         raise ValueError("row_count needs one entry per request")
+    _check_layout(layout, q.shape[0], q, keys, lse, mass, row_count)
     return lse.data_ptr(), _ptr(row_count)
 
 
@@ -740,7 +755,7 @@ def attention_mass(q: torch.Tensor, k_cache: torch.Tensor, lse: torch.Tensor, ma
     _dev(k_cache, "k_cache", torch.bfloat16)
     if tuple(k_cache.shape) != (layout.c.num_pages, layout.c.num_kv_heads, 16, layout.c.head_dim):
         raise ValueError("k_cache must be [pages, Hkv, 16, D] of the layout's sizes")
-    lp, rp = _mass_args(q, lse, mass, layout, row_count, stream)
+    lp, rp = _mass_args(q, k_cache, lse, mass, layout, row_count)
     if q.shape[0]:
         _check(_lib().rg_attention_mass(ctypes.byref(layout.c), q.data_ptr(), k_cache.data_ptr(), lp, rp, decay,
                                         mass.data_ptr(), _stream(stream)), "rg_attention_mass")
@@ -751,7 +766,7 @@ def kv4_attention_mass(q: torch.Tensor, cache: torch.Tensor, lse: torch.Tensor, 
                        row_count: Optional[torch.Tensor] = None, decay: float = 1.0, stream=None) -> torch.Tensor:
     """attention_mass over a 4-bit cache (rg_kv4_attention_mass)."""
     _kv4(cache, layout.c.head_dim, layout.c.num_kv_heads, layout.c.num_pages)
-    lp, rp = _mass_args(q, lse, mass, layout, row_count, stream)
+    lp, rp = _mass_args(q, cache, lse, mass, layout, row_count)
     if q.shape[0]:
         _check(_lib().rg_kv4_attention_mass(ctypes.byref(layout.c), q.data_ptr(), cache.data_ptr(), lp, rp, decay,
                                             mass.data_ptr(), _stream(stream)), "rg_kv4_attention_mass")
@@ -809,6 +824,7 @@ def _evict_args(score, positions, layout: _EvictLayout, mass, workspace):
     _slot_pool(positions, "positions", torch.int32, *pool)
     if mass is not None:
         _slot_pool(mass, "mass", torch.float32, *pool)
+    _here(score, positions, mass, workspace, layout.page_indices)
     if workspace is None:
         workspace = torch.empty(evict_workspace_bytes(layout), dtype=torch.uint8, device=score.device)
     return (score.data_ptr(), _ptr(mass), positions.data_ptr(), workspace.data_ptr(),
@@ -827,6 +843,7 @@ def evict_tokens(k_cache: torch.Tensor, v_cache: torch.Tensor, score: torch.Tens
     if tuple(k_cache.shape) != (c.num_pages, c.num_kv_heads, 16, c.head_dim) or \
             tuple(v_cache.shape) != (c.num_pages, c.num_kv_heads, c.head_dim, 16):
         raise ValueError("k_cache must be [pages, Hkv, 16, D] and v_cache [pages, Hkv, D, 16] of the layout's sizes")
+    _here(k_cache, v_cache)
     args = _evict_args(score, positions, layout, mass, workspace)
     _check(_lib().rg_evict_tokens(ctypes.byref(c), k_cache.data_ptr(), v_cache.data_ptr(), *args, _stream(stream)),
            "rg_evict_tokens")
@@ -838,5 +855,6 @@ def kv4_evict_tokens(cache: torch.Tensor, score: torch.Tensor, positions: torch.
     """evict_tokens on a 4-bit cache (rg_kv4_evict_tokens)."""
     c = layout.c
     _kv4(cache, c.head_dim, c.num_kv_heads, c.num_pages)
+    _here(cache)
     args = _evict_args(score, positions, layout, mass, workspace)
     _check(_lib().rg_kv4_evict_tokens(ctypes.byref(c), cache.data_ptr(), *args, _stream(stream)), "rg_kv4_evict_tokens")

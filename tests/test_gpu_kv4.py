@@ -241,3 +241,48 @@ def test_argument_checks():
         binding.kv4_attention(q, pool, long.layout4(pool), workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
     with pytest.raises(ValueError):
         binding.make_kv4_layout(8, cache[:, :, :100], b.q_indptr, b.nv, b.ctx, b.page_indptr, b.device_pages(DEV))
+
+
+@pytest.mark.parametrize("heads", [(8, 1, 128), (16, 2, 64)])
+def test_attention_of_many_columns_split(heads):
+    """Full column groups and a last one, both cut into runs; with branches too."""
+    for requests in ([(3000, 20, 14)], [(2000, 3, [(1, 0, 16), (2, 0, 16), (3, 0, 16)]), (17, 1, 0)]):
+        b = Batch(requests, heads=heads)
+        q, pool = b.q(), b.pool4()
+        check_attention(*_attend(b, q, pool), *b.attention(q, pool), _score_size(b, q, pool))
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each, the same cache."""
+    b = Batch([(5000, 2, 2), (10, 1, 0)])
+    q, pool = b.q(), b.pool4()
+    cache, qd = dev(pool), q.to(DEV)
+    lay = b.layout4(cache)
+    need = binding.kv4_attention_workspace_bytes(lay)
+    ws = [torch.empty(need, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    torch.cuda.synchronize()
+    for s, w in zip(streams, ws):
+        got.append(binding.kv4_attention(qd, cache, lay, stream=s, workspace=w))
+    torch.cuda.synchronize()
+    want = b.attention(q, pool)
+    for out, lse in got:
+        check_attention(out, lse, *want, _score_size(b, q, pool))
+    assert torch.equal(got[0][0], got[1][0])
+
+
+def test_tensors_of_another_device(monkeypatch):
+    """Kernels run on the current device: tensors elsewhere are refused."""
+    b = Batch([(5, 1, 0)])
+    cache = torch.zeros(b.num_pages, b.hkv, 17 * b.d, dtype=torch.uint8, device=DEV)
+    lay, q, k = b.layout4(cache), b.q().to(DEV), b.normal(b.rows, b.hkv, b.d).to(DEV)
+    slots = torch.zeros(b.num_pages, b.hkv, PAGE, device=DEV)
+    el = binding.make_evict_layout(cache, [6], [3], b.page_indptr, b.device_pages(DEV))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in (lambda: binding.kv4_append(k, k, cache, lay), lambda: binding.kv4_read(cache, lay, k_out=k, v_out=k),
+                 lambda: binding.kv4_attention(q, cache, lay),
+                 lambda: binding.kv4_attention_mass(q, cache, torch.zeros(b.rows, b.hq, device=DEV), slots, lay),
+                 lambda: binding.kv4_evict_tokens(cache, slots, slots.int(), el)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
