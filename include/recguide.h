@@ -557,7 +557,8 @@ rg_status rg_kv4_read(const rg_attn_layout* layout, const uint8_t* cache, uint16
  * rg_draft_verify_attention (branches NULL) or rg_multibranch_attention over a
  * 4-bit cache: layout, branches, q, out and lse as there, K and V the values
  * the codes stand for.  Slots no request reads may hold anything.  The
- * workspace needs no initialisation.
+ * workspace needs no initialisation.  RG_ERR_WORKSPACE also where the host has
+ * no memory for the plan.
  */
 rg_status rg_kv4_attention_workspace(const rg_attn_layout* layout, const rg_branch_layout* branches, size_t* bytes);
 rg_status rg_kv4_attention(const rg_attn_layout* layout, const rg_branch_layout* branches, const uint16_t* q,
@@ -585,6 +586,7 @@ rg_status rg_kv4_attention(const rg_attn_layout* layout, const rg_branch_layout*
  *   mass[j] = w_j                    for the step's own keys j >= L
  * so that keys need no initialisation.  Pages must not be in two requests'
  * lists.  The order of the sums is fixed: equal calls give equal bits.
+ * RG_ERR_UNSUPPORTED where a request's verify rows of q span 2^31 bytes.
  */
 rg_status rg_attention_mass(const rg_attn_layout* layout, const uint16_t* q, const uint16_t* k_cache, const float* lse,
                             const int32_t* row_count, float decay, float* mass, void* stream);

@@ -24,7 +24,7 @@ static_assert(RG_NOALLOC_SCRATCH_BYTES == rg::kNoAllocScratchBytes, "header and 
 
 namespace rg {
 
-int env_int(const char* name, int fallback) {
+static int env_int(const char* name, int fallback) {
   const char* v = std::getenv(name);
   if (v == nullptr || *v == 0) return fallback;
   return std::atoi(v);
@@ -141,7 +141,7 @@ int device_cus() {
 // 24576-key chunks, a full chunk plus a short remainder per request, took
 // 1633 us against 1340 us whole), and finer chunks cost more than a dispatch
 // model with a fixed start-up predicts (merge work, partial traffic).
-int choose_chunk(const std::vector<int64_t>& pair_keys, int hkv, int num_cus) {
+static int choose_chunk(const std::vector<int64_t>& pair_keys, int hkv, int num_cus) {
   const int forced = env_int("RG_ATTN_CHUNK", 0);
   if (forced > 0) return (int)std::min<int64_t>(kMaxChunkKeys, round_up(forced, kKeyTile));
   const int64_t kCUs = std::max(1, num_cus);

@@ -4,7 +4,9 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <new>
 #include <numeric>
+#include <vector>
 
 #include "cache_internal.h"
 #include "plan_common.h"
@@ -14,34 +16,37 @@ namespace {
 using namespace rg;
 
 // Calls launch(plan) for a layout's requests, in order, a plan's worth at a
-// time; items(r) is request r's number of work items (0: left out), fill(r, q)
-// completes its entry.  False from launch stops.
+// time; items(r) is request r's number of work items (0: left out).
 template <typename Items, typename Launch>
 rg_status each_plan(const rg_attn_layout* L, int threads, Items items, Launch launch) {
   AttnPlan p;
-  for (int pass = 0; pass < 2; ++pass) {  // check every plan, then launch
-    for (int r0 = 0; r0 < L->num_requests; r0 += kMaxReqPerLaunch) {
-      const int cnt = std::min(kMaxReqPerLaunch, L->num_requests - r0);
-      std::memset(&p, 0, sizeof(p));
-      p.num_req = cnt;
-      int64_t total = 0;
-      for (int k = 0; k < cnt; ++k) {
-        const int r = r0 + k;
-        AttnReq& q = p.req[k];
-        q.q_start = L->q_indptr[r];
-        q.ctx = L->ctx_len[r];
-        q.nv = (int32_t)((uint32_t)(L->q_indptr[r + 1] - L->q_indptr[r]) | ((uint32_t)L->n_verify[r] << 16));
-        q.page_start = L->page_indptr[r];
-        q.item_start = (int32_t)total;
-        q.part_start = r;
-        total += items(r);
-        if (total > INT32_MAX / 2 || !fits_launch(total, threads)) return RG_ERR_UNSUPPORTED;
-      }
-      p.req[cnt].item_start = p.total_items = (int32_t)total;
-      if (pass == 1 && total > 0 && launch(p) != hipSuccess) return RG_ERR_HIP;
+  for (int r0 = 0; r0 < L->num_requests; r0 += kMaxReqPerLaunch) {
+    const int cnt = std::min(kMaxReqPerLaunch, L->num_requests - r0);
+    std::memset(&p, 0, sizeof(p));
+    p.num_req = cnt;
+    int64_t total = 0;
+    for (int k = 0; k < cnt; ++k) {
+      const int r = r0 + k;
+      AttnReq& q = p.req[k];
+      q.q_start = L->q_indptr[r];
+      q.ctx = L->ctx_len[r];
+      q.nv = (int32_t)((uint32_t)(L->q_indptr[r + 1] - L->q_indptr[r]) | ((uint32_t)L->n_verify[r] << 16));
+      q.page_start = L->page_indptr[r];
+      q.item_start = (int32_t)total;
+      q.part_start = r;
+      total += items(r);
+      if (total > INT32_MAX / 2 || !fits_launch(total, threads)) return RG_ERR_UNSUPPORTED;
     }
+    p.req[cnt].item_start = p.total_items = (int32_t)total;
+    if (total > 0 && launch(p) != hipSuccess) return RG_ERR_HIP;
   }
   return RG_OK;
+}
+// Whether every plan can be launched: asked before the first launch wherever a
+// later plan could refuse.
+template <typename Items>
+rg_status check_plans(const rg_attn_layout* L, int threads, Items items) {
+  return each_plan(L, threads, items, [](const AttnPlan&) { return hipSuccess; });
 }
 
 // ---------------------------------------------------------------------------
@@ -67,6 +72,10 @@ rg_status run_rows(const rg_attn_layout* L, const uint16_t* k, int64_t k_stride,
     const int64_t n = L->q_indptr[r + 1] - L->q_indptr[r];
     return n == 0 ? 0 : ((L->ctx_len[r] + n - 1) / kPageSize - L->ctx_len[r] / kPageSize + 1) * L->num_kv_heads;
   };
+  if (L->num_requests > kMaxReqPerLaunch) {
+    const rg_status fits = check_plans(L, 256, pages);
+    if (fits != RG_OK) return fits;
+  }
   return each_plan(L, 256, pages, [&](const AttnPlan& p) {
     const hipStream_t s = static_cast<hipStream_t>(stream);
     return append ? launch_kv4_append(a, p, L->head_dim, s) : launch_kv4_read(a, p, L->head_dim, s);
@@ -203,7 +212,7 @@ rg_status plan_kv4(const rg_attn_layout* L, const rg_branch_layout* B, Kv4Plan<P
 
 // Calls f(plan) with the plan of a layout and its branches (or NULL).
 template <typename F>
-rg_status with_kv4_plan(const rg_attn_layout* L, const rg_branch_layout* B, F f) {
+rg_status with_kv4_plan(const rg_attn_layout* L, const rg_branch_layout* B, F f) try {
   rg_status st = validate_layout(L);
   if (st != RG_OK) return st;
   if (B == nullptr) {
@@ -216,6 +225,8 @@ rg_status with_kv4_plan(const rg_attn_layout* L, const rg_branch_layout* B, F f)
   Kv4Plan<AttnPlanBr> fp;
   st = plan_kv4<AttnPlanBr, kMaxReqPerLaunchBr>(L, B, fp);
   return st != RG_OK ? st : f(fp);
+} catch (const std::bad_alloc&) {  // nothing is launched before a plan is whole
+  return RG_ERR_WORKSPACE;
 }
 
 float softmax_scale(const rg_attn_layout* L) {
@@ -263,11 +274,16 @@ rg_status run_mass(const rg_attn_layout* L, const uint16_t* q, const void* keys,
   // rows of a request are addressed by 32-bit offsets
   for (int r = 0; r < L->num_requests; ++r)
     if (many(r) && (int64_t)L->n_verify[r] * a.hq * L->head_dim * 2 > INT32_MAX) return RG_ERR_UNSUPPORTED;
-  const hipStream_t s = static_cast<hipStream_t>(stream);
-  st = each_plan(L, 64 * kMassWaves, [&](int r) { return many(r) ? runs(r, kMassRowKeys) : 0; },
-                 [&](const AttnPlan& p) { return launch_mass_rows(a, p, L->head_dim, kv4, s); });
+  const auto few_items = [&](int r) { return many(r) ? 0 : runs(r, run); };
+  const auto many_items = [&](int r) { return many(r) ? runs(r, kMassRowKeys) : 0; };
+  const int threads = 64 * kMassWaves;
+  st = check_plans(L, threads, few_items);
+  if (st == RG_OK) st = check_plans(L, threads, many_items);
   if (st != RG_OK) return st;
-  return each_plan(L, 64 * kMassWaves, [&](int r) { return many(r) ? 0 : runs(r, run); }, [&](AttnPlan& p) {
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  st = each_plan(L, threads, many_items, [&](const AttnPlan& p) { return launch_mass_rows(a, p, L->head_dim, kv4, s); });
+  if (st != RG_OK) return st;
+  return each_plan(L, threads, few_items, [&](AttnPlan& p) {
     p.chunk = (int32_t)run;
     return launch_mass(a, p, L->head_dim, kv4, s);
   });

@@ -429,7 +429,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void kv4_attn_kernel(Kv4
   it.c = local % runs.count;
   it.kbeg = it.c * runs.keys;
   it.kend = min(T, it.kbeg + runs.keys);
-  it.part += local * it.nct * 32;
+  if (it.nch > 1) it.part += local * it.nct * 32;
 
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int np = it.nct > 2 ? 2 : 1, pair = wave % np;

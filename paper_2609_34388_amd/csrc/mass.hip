@@ -27,7 +27,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 // Request and range of a work item.
 struct MassItem {
-  int V, L, T, M;  // verify rows, context, keys, counted columns
+  int L, T, M;  // context, keys, counted columns
+  int seen;     // keys that a counted row sees
   int hk, kbeg;
   int q_start, page_start;
 };
@@ -36,10 +37,12 @@ __device__ __forceinline__ MassItem mass_item(const MassArgs& a, const AttnPlan&
   const int r = find_request(p, item, false);
   const AttnReq rq = p.req[r];
   MassItem it;
-  it.V = (int)((uint32_t)rq.nv >> 16);
+  const int V = (int)((uint32_t)rq.nv >> 16);
+  const int rows = a.row_count ? min(max(a.row_count[rq.part_start], 0), V) : V;
   it.L = rq.ctx;
-  it.T = it.L + it.V;
-  it.M = (a.row_count ? min(max(a.row_count[rq.part_start], 0), it.V) : it.V) * a.g;
+  it.T = it.L + V;
+  it.M = rows * a.g;
+  it.seen = it.L + rows;
   const int local = item - rq.item_start;  // heads fastest: a prompt's costliest keys, its first, come first
   it.hk = local % a.hkv;
   it.kbeg = local / a.hkv * keys;
@@ -102,6 +105,7 @@ __device__ __forceinline__ void add_weights(const MassArgs& a, const MassItem& i
 }
 
 __device__ __forceinline__ void write_mass(const MassArgs& a, const MassItem& it, int key, float sum) {
+  if (key >= it.seen) sum = 0.f;  // whatever it holds: a column that does not count may see it
   float* at = a.mass + ((size_t)a.page_indices[it.page_start + (key >> 4)] * a.hkv + it.hk) * kPageSize + (key & 15);
   *at = key < it.L && a.decay != 0.f ? a.decay * *at + sum : sum;
 }

@@ -138,3 +138,23 @@ def test_evict_refusals():
 def test_keep_below_the_protected_is_fine_where_nothing_is_cut():
     n = ctypes.c_size_t()
     assert lib().rg_evict_workspace(E(ctx=(10, 64), keep=(11, 64)).ref, ctypes.byref(n)) == 0
+
+
+def test_mass_of_more_query_bytes_than_offsets_hold():
+    """A request's verify rows of q must span less than 2^31 bytes where the
+    kernel of many columns takes them."""
+    for hq, want in ((256, UNSUPPORTED), (128, None)):
+        l = L(ctx=(0,), nv=(65535,), n=(65535,), hq=hq, hkv=hq)
+        # group 1: more than 128 columns either way; the smaller one is refused for its alignment alone
+        assert mass(l, m=ctypes.c_void_p(0x1002)) == UNSUPPORTED
+        if want:
+            assert mass(l) == want
+
+
+def test_mass_refuses_before_it_launches():
+    """A batch of both kinds of requests one of whose launches is too large."""
+    n = 1 << 14
+    l = L(ctx=(1 << 29, 0), nv=(1, 200), n=(1, 200), hq=n, hkv=n)
+    assert mass(l) == UNSUPPORTED
+    l = L(ctx=(40, 1 << 29), nv=(1, 200), n=(1, 200), hq=n, hkv=n, D=64)
+    assert mass(l) == UNSUPPORTED

@@ -400,3 +400,62 @@ def test_captured_round():
         q2 = q * 0.5
         binding.kv4_attention(q2, cache, lay, workspace=ws)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("four", [False, True])
+def test_mass_of_keys_that_no_counted_row_sees(four):
+    """Such keys add nothing, whatever they hold (here NaN, in 4 bits 2^128 and more)."""
+    for heads, V in (((8, 2, 128), 8), ((16, 2, 64), 40)):  # few columns, and many
+        b = Batch([(75, V, 3), (0, V, 0)], heads=heads)
+        count = np.array([2, 0])
+        q, lse = b.q(), _lse(b, b.rng)
+        pool = b.pool4() if four else _pools16(b)
+        places = ref._scale_places(b.d, 0) if four else None
+        for r in range(b.R):
+            page, slot = b.places(r, V - int(count[r]), int(b.ctx[r] + count[r]))
+            for p, s in zip(page, slot):
+                if four:
+                    pool[p][:, places[s]] = 0xff
+                else:
+                    pool[0][int(p), :, s] = float("nan")
+        mass = torch.full((b.num_pages, b.hkv, PAGE), 0.25, device=DEV)
+        rc = torch.tensor(count, dtype=torch.int32, device=DEV)
+        if four:
+            cache = dev(pool)
+            binding.kv4_attention_mass(q.to(DEV), cache, dev(lse), mass, b.layout4(cache), row_count=rc)
+        else:
+            qd, kd = q.to(DEV), pool[0].to(DEV)
+            binding.attention_mass(qd, kd, dev(lse), mass, b.layout16(qd, kd), row_count=rc)
+        got = mass.cpu().numpy()
+        assert np.isfinite(got).all()
+        for r in range(b.R):
+            page, slot = b.places(r, V - int(count[r]), int(b.ctx[r] + count[r]))
+            assert (got[page, :, slot] == 0).all()
+
+
+def test_mass_of_long_runs():
+    """Work items of several steps of 4-bit keys, the last of them incomplete."""
+    b = Batch([(13009, 2, 0)], heads=(32, 32, 64))
+    q, pool, lse = b.q(), b.pool4(), None
+    lse = _lse(b, b.rng)
+    old = b.rng.random((b.num_pages, b.hkv, PAGE)).astype(np.float32)
+    cache, mass = dev(pool), dev(old)
+    binding.kv4_attention_mass(q.to(DEV), cache, dev(lse), mass, b.layout4(cache), decay=0.5)
+    want = b.mass(old, q, pool, lse, None, 0.5)
+    page, slot = b.places(0, int(b.T[0]))
+    _check_mass(mass.cpu()[page, :, slot], want[page, :, slot], old, b, None, _score_size(b, q, pool))
+
+
+@pytest.mark.parametrize("L", [4096, 4097, 8192, 8193, 16384, 16385, 32769])
+def test_evict_lengths(L):
+    """Around the lengths at which a thread holds more slots."""
+    _evict_case([L, 60], [L - 700, 54], (1, 1, 64), True, score=_ties, tracked=[L // 2, 0], evicted=[77, 0], sink=3, recent=50)
+    _evict_case([L], [L // 3], (1, 1, 64), False, score=_signed, mass=False)
+
+
+@pytest.mark.parametrize("four", [False, True])
+def test_evict_one_page_partly_kept(four):
+    """The page that holds slots on both sides of `keep`, token counts around it."""
+    for L, keep in ((32, 17), (31, 23), (30, 24), (40, 25), (16, 9), (9, 8), (17, 15)):
+        for heads in ((2, 2, 128), (2, 2, 64)):
+            _evict_case([L, L], [keep, keep - 1], heads, four, seed=L)

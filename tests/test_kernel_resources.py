@@ -50,3 +50,18 @@ def test_default_attention_kernels_do_not_spill(tmp_path):
     for name, k in kernels.items():
         assert int(k["vgpr_spill_count"]) == 0 and int(k["private_segment_fixed_size"]) == 0, name
         assert int(k["vgpr_count"]) <= 168, name  # three waves per SIMD
+
+
+@pytest.mark.parametrize("part, count, vgprs", [
+    ("kv4_append_kernel", 2, 64), ("kv4_read_kernel", 2, 64),  # head sizes
+    ("kv4_attn_kernel", 2 * 2, 256),                           # x plan forms; two waves per SIMD
+    ("kv4_merge_kernel", 2 * 2 * 2, 128),                      # x threads of a row
+    ("mass_kernel", 2 * 2, 168), ("mass_rows_kernel", 2 * 2, 168),  # x caches; three waves per SIMD
+    ("evict_select_kernel", 4, 128),                           # slots of a thread; a work group of 1024 needs four
+    ("evict_move_kernel", 2 * 2, 128)])
+def test_cache_kernels_do_not_spill(tmp_path, part, count, vgprs):
+    kernels = {k: v for k, v in _kernels(tmp_path).items() if part in k}
+    assert len(kernels) == count
+    for name, k in kernels.items():
+        assert int(k["vgpr_spill_count"]) == 0 and int(k["private_segment_fixed_size"]) == 0, name
+        assert int(k["vgpr_count"]) <= vgprs, name
