@@ -26,9 +26,9 @@ constexpr int kKv4MergeRows = 64;                  // 16-byte rows of a merge it
 constexpr int kKv4MergeParts = 4;                  // threads of a row where requests have many chunks
 // A request's 32-column tiles form column groups of four, and a last one of
 // what remains.  Time of 32 keys in a group of 1 .. 4 tiles, in units of a
-// sixteenth of that of four: the vector instructions of a wave on one tile and
-// on two (which share the decoding) are as 5 to 8.
-__host__ __device__ inline int kv4_rate(int tiles) { return tiles == 1 ? 5 : tiles == 2 ? 8 : tiles == 3 ? 13 : 16; }
+// sixteenth of that of four, as work groups' own clocks gave it (three tiles: of
+// the two wave pairs one has a single tile and waits for the other).
+__host__ __device__ inline int kv4_rate(int tiles) { return tiles == 1 ? 6 : tiles == 2 ? 9 : tiles == 3 ? 15 : 16; }
 // Runs that the T keys of such a group are cut into, for items of at most
 // `target` units, and the keys of each: all but the last alike.
 struct Kv4Runs {

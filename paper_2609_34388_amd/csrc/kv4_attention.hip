@@ -184,6 +184,9 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
 #pragma unroll
     for (int u = 0; u < TILES; ++u)
       for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
+    // Products before the other wave's softmax: a product occupies the matrix core
+    // for longer than its issue takes, the softmax fills what is between.
+    __builtin_amdgcn_s_setprio(1);
     {
       // Q fragments are read two K steps ahead
       constexpr int N = D / 16, AHEAD = 2;
@@ -205,6 +208,7 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     u32x4 pk[TILES][2];
 #pragma unroll
     for (int u = 0; u < TILES; ++u) {
@@ -283,6 +287,7 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
         vs[pp] = u32x2{(uint32_t)w, (uint32_t)(w >> 32)};
       }
     }
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int pp = 0; pp < 2; ++pp) {
       u32x4 vf[DT];
@@ -314,6 +319,7 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
           acc[u][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[dt]),
                                                                __builtin_bit_cast(bf16x8, pk[u][pp]), acc[u][dt], 0, 0, 0);
     }
+    __builtin_amdgcn_s_setprio(0);
   }
 
   // The key groups' states meet in LDS, one tile of a wave at a time
