@@ -229,6 +229,18 @@ rg_status with_kv4_plan(const rg_attn_layout* L, const rg_branch_layout* B, F f)
   return RG_ERR_WORKSPACE;
 }
 
+// Query heads a KV head, and the factor and shift that divide by them: with
+// 2^l >= g, g_mul = ceil(2^(31 + l) / g) fits 32 bits and g_mul g exceeds
+// 2^(31 + l) by e < g, so col g_mul / 2^(31 + l) exceeds col / g by
+// col e / (g 2^(31 + l)) < 1 / g for every col below 2^31: the floors agree.
+template <typename Args>
+void set_group(Args& a) {
+  a.g = a.hq / a.hkv;
+  a.g_shift = 0;
+  while ((1ll << a.g_shift) < a.g) ++a.g_shift;
+  a.g_mul = (uint32_t)(((uint64_t(1) << (31 + a.g_shift)) + a.g - 1) / a.g);
+}
+
 float softmax_scale(const rg_attn_layout* L) {
   return L->sm_scale > 0.f ? L->sm_scale : 1.0f / std::sqrt((float)L->head_dim);
 }
@@ -252,15 +264,9 @@ rg_status run_mass(const rg_attn_layout* L, const uint16_t* q, const void* keys,
   a.page_indices = L->page_indices;
   a.hq = L->num_q_heads;
   a.hkv = L->num_kv_heads;
-  a.g = a.hq / a.hkv;
+  set_group(a);
   a.scale_log2 = softmax_scale(L) * 1.4426950408889634f;
   a.decay = decay;
-  // With 2^l >= g, g_mul = ceil(2^(31 + l) / g) fits 32 bits and g_mul g exceeds
-  // 2^(31 + l) by e < g, so col g_mul / 2^(31 + l) exceeds col / g by
-  // col e / (g 2^(31 + l)) < 1 / g for every col below 2^31: the floors agree.
-  a.g_shift = 0;
-  while ((1ll << a.g_shift) < a.g) ++a.g_shift;
-  a.g_mul = (uint32_t)(((uint64_t(1) << (31 + a.g_shift)) + a.g - 1) / a.g);
   // A request without query rows need not own pages for its context.
   auto len = [&](int r) { return L->q_indptr[r + 1] == L->q_indptr[r] ? 0 : (int64_t)L->ctx_len[r] + L->n_verify[r]; };
   auto many = [&](int r) { return (int64_t)L->n_verify[r] * a.g > kMassCols; };
@@ -414,7 +420,7 @@ rg_status rg_kv4_attention(const rg_attn_layout* layout, const rg_branch_layout*
     a.part_ml = fp.ws_bytes ? reinterpret_cast<float*>(static_cast<char*>(ws) + fp.ml_offset) : nullptr;
     a.hq = layout->num_q_heads;
     a.hkv = layout->num_kv_heads;
-    a.g = a.hq / a.hkv;
+    set_group(a);
     a.sm_scale = softmax_scale(layout);
     a.scale_log2 = a.sm_scale * 1.4426950408889634f;
     a.rescale_gap = 8.0f / a.scale_log2;

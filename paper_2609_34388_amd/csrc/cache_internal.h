@@ -49,6 +49,8 @@ struct Kv4AttnArgs {
   float* part_o;   // per 32-column tile: 32 x D fp32 sums, 16-byte rows lane-interleaved
   float* part_ml;  // [partial columns][2] (running maximum of raw scores, sum)
   int32_t hq, hkv, g;
+  uint32_t g_mul;  // row_of
+  int32_t g_shift;
   float sm_scale, scale_log2, rescale_gap;
 };
 hipError_t launch_kv4_attention(const Kv4AttnArgs& a, const AttnPlan& p, int head_dim, hipStream_t stream);
@@ -73,7 +75,7 @@ struct MassArgs {
   const int32_t* page_indices;
   int32_t hq, hkv, g;
   float scale_log2, decay;
-  uint32_t g_mul;  // col / g = umulhi(2 col, g_mul) >> g_shift
+  uint32_t g_mul;  // row_of
   int32_t g_shift;
 };
 hipError_t launch_mass(const MassArgs& a, const AttnPlan& p, int head_dim, bool kv4, hipStream_t stream);

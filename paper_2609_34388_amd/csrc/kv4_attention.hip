@@ -67,7 +67,7 @@ struct Kv4Shape {
   static constexpr int Q = kKv4Waves * RING * SLOT;
   static constexpr int LDS = Q + kKv4Cols * QROW;
   static_assert(Q <= 1 << 16, "places of loads to LDS");
-  static_assert((kKv4Waves - 1) * STATE * 4 <= LDS, "the states fit where Q and the codes were");
+  static_assert(kKv4Waves * STATE * 4 <= LDS, "the states fit where Q and the codes were");
 };
 
 // The TILES column tiles of this wave: pair `pair` of `np`, key group `kgi`.
@@ -136,7 +136,7 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
       const int u = threadIdx.x + e * kThreads, row = u / (D / 8), ch = u % (D / 8), col = it.tile0 * 32 + row;
       x[e] = u32x4{0u, 0u, 0u, 0u};
       if (row < 32 * it.nct && col < it.M) {
-        const int tok = col / g;
+        const int tok = row_of(a, col);
         x[e] = *(const u32x4*)(a.q + ((size_t)(rq.q_start + tok) * a.hq + it.hk * g + (col - tok * g)) * D + 8 * ch);
       }
     }
@@ -151,7 +151,7 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
 #pragma unroll
   for (int u = 0; u < TILES; ++u) {
     const int col = (it.tile0 + 2 * pair + u) * 32 + lc;
-    key_limits(rq, col < it.M, col / g, kend, lim[u], slo[u], shi[u]);
+    key_limits(rq, col < it.M, row_of(a, col), kend, lim[u], slo[u], shi[u]);
     int m = col < it.M ? lim[u] : kend;
     for (int off = 32; off >= 1; off >>= 1) m = min(m, __shfl_xor(m, off));
     min_lim[u] = __builtin_amdgcn_readfirstlane(m);
@@ -322,77 +322,68 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
     __builtin_amdgcn_s_setprio(0);
   }
 
-  // The key groups' states meet in LDS, one tile of a wave at a time
-  // (lane-wise: same columns, same dims), and key group 0 writes the result.
+  // The key groups' states meet in LDS, one tile of a wave at a time (lane-wise:
+  // same columns, same dims), and each group's wave joins a share of the rows.
+  // In loops: this code runs once an item, so its fetch is what it costs.
   float* area = reinterpret_cast<float*>(lds);
+  const float* states = area + pair * S::STATE;  // of the pair, np apart
+  const int step = np * S::STATE, share = 4 * DT / kg;
+  auto put = [&](const f32x16(&o)[DT], float m, float l) {
+    float* state = area + wave * S::STATE;
 #pragma unroll
+    for (int v = 0; v < 4 * DT; ++v) {
+      const int i4 = v / DT, f = 4 * (v % DT);
+      *(float4*)(state + (v * 64 + lane) * 4) =
+          make_float4(o[f % DT][4 * i4 + f / DT], o[(f + 1) % DT][4 * i4 + (f + 1) / DT],
+                      o[(f + 2) % DT][4 * i4 + (f + 2) / DT], o[(f + 3) % DT][4 * i4 + (f + 3) / DT]);
+    }
+    state[64 * 16 * DT + lane] = m;
+    state[64 * 16 * DT + 64 + lane] = l + __shfl_xor(l, 32);
+  };
+#pragma unroll 1
   for (int u = 0; u < 2; ++u) {
     if (u == 1 && it.nct == 1) break;
-    lds_barrier();  // Q, or the states before, are no longer read
-    if (u < TILES && kgi > 0) {
-      float* slot = area + ((kgi - 1) * np + pair) * S::STATE;
-#pragma unroll
-      for (int v = 0; v < 4 * DT; ++v) {
-        const int i4 = v / DT, f = 4 * (v % DT);
-        *(float4*)(slot + (v * 64 + lane) * 4) =
-            make_float4(acc[u % TILES][f % DT][4 * i4 + f / DT], acc[u % TILES][(f + 1) % DT][4 * i4 + (f + 1) / DT],
-                        acc[u % TILES][(f + 2) % DT][4 * i4 + (f + 2) / DT], acc[u % TILES][(f + 3) % DT][4 * i4 + (f + 3) / DT]);
-      }
-      slot[64 * 16 * DT + lane] = m_run[u % TILES];
-      slot[64 * 16 * DT + 64 + lane] = l_run[u % TILES] + __shfl_xor(l_run[u % TILES], 32);
-    }
+    lds_barrier();  // Q and the codes, or the states before, are no longer read
+    if (u == 0) put(acc[0], m_run[0], l_run[0]);
+    else if (TILES == 2) put(acc[TILES - 1], m_run[TILES - 1], l_run[TILES - 1]);
     lds_barrier();
-    if (u >= TILES || kgi > 0) continue;
-    f32x16(&o)[DT] = acc[u % TILES];
-    float m = m_run[u % TILES], l = l_run[u % TILES] + __shfl_xor(l_run[u % TILES], 32);
-    for (int k = 1; k < kg; ++k) {
-      const float* slot = area + ((k - 1) * np + pair) * S::STATE;
-      const float mk = slot[64 * 16 * DT + lane];
-      const float lk = slot[64 * 16 * DT + 64 + lane];
-      const float m_new = fmaxf(m, mk);
-      if (m_new == kNegInf) continue;  // neither group sees a key
-      const float a0 = __builtin_amdgcn_exp2f((m - m_new) * a.scale_log2);
-      const float a1 = __builtin_amdgcn_exp2f((mk - m_new) * a.scale_log2);
-#pragma unroll
-      for (int v = 0; v < 4 * DT; ++v) {
-        const float4 x4 = *(const float4*)(slot + (v * 64 + lane) * 4);
-        const float x[4] = {x4.x, x4.y, x4.z, x4.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int f = 4 * (v % DT) + e, i = 4 * (v / DT) + f / DT;
-          o[f % DT][i] = o[f % DT][i] * a0 + x[e] * a1;
-        }
-      }
-      l = l * a0 + lk * a1;
-      m = m_new;
-    }
     const int col = (it.tile0 + 2 * pair + u) * 32 + lc;
-    if (col >= it.M) continue;
-    // Element f of run i4 of a lane: dim 8 DT i4 + 4 DT lh + f, f < 4 DT.
-    auto at = [&](int i4, int f) { return o[f % DT][4 * i4 + f / DT]; };
-    if (it.nch == 1) {
-      const int tok = col / g;
-      const size_t orow = (size_t)(rq.q_start + tok) * a.hq + it.hk * g + (col - tok * g);
-      const float inv = 1.f / l;
-      uint16_t* dst = a.out + orow * D + 4 * DT * lh;
+    if (u >= TILES || col >= it.M) continue;
+    float m = kNegInf, l = 0.f, w[kKv4Waves];
 #pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4)
+    for (int k = 0; k < kKv4Waves; ++k) {
+      w[k] = k < kg ? states[k * step + 64 * 16 * DT + lane] : kNegInf;
+      m = fmaxf(m, w[k]);
+    }
 #pragma unroll
-        for (int f = 0; f < 4 * DT; f += 8) {
-          u32x4 w;
+    for (int k = 0; k < kKv4Waves; ++k) {
+      // a group none of whose keys the column sees weighs nothing
+      w[k] = w[k] == kNegInf ? 0.f : __builtin_amdgcn_exp2f((w[k] - m) * a.scale_log2);
+      if (k < kg) l += w[k] * states[k * step + 64 * 16 * DT + 64 + lane];
+    }
+    const int tok = row_of(a, col);
+    const size_t orow = (size_t)(rq.q_start + tok) * a.hq + it.hk * g + (col - tok * g);
+    const size_t tile = (size_t)it.part + (2 * pair + u) * 32;
+    const float inv = 1.f / l;
+    // Element e of row v of a lane: dim 8 DT (v / DT) + 4 DT lh + 4 (v % DT) + e.
+#pragma unroll 1
+    for (int v = kgi * share; v < kgi * share + share; ++v) {
+      float4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(at(i4, f + 2 * e) * inv, at(i4, f + 2 * e + 1) * inv);
-          *(u32x4*)(dst + 8 * DT * i4 + f) = w;
-        }
-      if (a.lse != nullptr && lh == 0) a.lse[orow] = m * a.sm_scale + __logf(l);
-    } else {
-      const size_t tile = (size_t)it.part + (2 * pair + u) * 32;
-      float* dst = a.part_o + tile * D;
-#pragma unroll
-      for (int v = 0; v < 4 * DT; ++v)
-        *(float4*)(dst + (v * 64 + lane) * 4) = make_float4(at(v / DT, 4 * (v % DT)), at(v / DT, 4 * (v % DT) + 1),
-                                                            at(v / DT, 4 * (v % DT) + 2), at(v / DT, 4 * (v % DT) + 3));
-      if (lh == 0) *(float2*)(a.part_ml + 2 * (tile + lc)) = make_float2(m, l);
+      for (int k = 0; k < kKv4Waves; ++k) {
+        const float4 x = *(const float4*)(states + (k < kg ? k : 0) * step + (v * 64 + lane) * 4);
+        o.x += w[k] * x.x, o.y += w[k] * x.y, o.z += w[k] * x.z, o.w += w[k] * x.w;
+      }
+      if (it.nch == 1) {
+        const u32x2 x = {pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv)};
+        *(u32x2*)(a.out + orow * D + 8 * DT * (v / DT) + 4 * DT * lh + 4 * (v % DT)) = x;
+      } else {
+        *(float4*)(a.part_o + tile * D + (v * 64 + lane) * 4) = o;
+      }
+    }
+    if (kgi == 0 && lh == 0) {
+      if (it.nch > 1) *(float2*)(a.part_ml + 2 * (tile + lc)) = make_float2(m, l);
+      else if (a.lse != nullptr) a.lse[orow] = m * a.sm_scale + __logf(l);
     }
   }
 }
@@ -529,7 +520,7 @@ __global__ __launch_bounds__(kKv4MergeRows * PARTS) void kv4_merge_kernel(Kv4Att
     }
   }
   if (col >= M) return;
-  const int tok = col / g, hh = col - tok * g;
+  const int tok = row_of(a, col), hh = col - tok * g;
   const size_t orow = (size_t)(rq.q_start + tok) * a.hq + hk * g + hh;
   const float inv = 1.f / l;
   u32x2 w;

@@ -47,5 +47,11 @@ __device__ __forceinline__ uint32_t encode8(u32x4 x, float scale) {
   return c;
 }
 
+// Query row of a column, col / g: exact below 2^31 (set_group in cache_api.cpp).
+template <typename Args>
+__device__ __forceinline__ int row_of(const Args& a, int col) {
+  return (int)(__umulhi(2u * (uint32_t)col, a.g_mul) >> a.g_shift);
+}
+
 }  // namespace
 }  // namespace rg

@@ -51,10 +51,6 @@ __device__ __forceinline__ MassItem mass_item(const MassArgs& a, const AttnPlan&
   return it;
 }
 
-// Query row of a column: col / g, exact below 2^31 (cache_api.cpp).
-__device__ __forceinline__ int row_of(const MassArgs& a, int col) {
-  return (int)(__umulhi(2u * (uint32_t)col, a.g_mul) >> a.g_shift);
-}
 // Row of q and lse of a column.
 __device__ __forceinline__ size_t column_row(const MassArgs& a, const MassItem& it, int col) {
   const int tok = row_of(a, col);

@@ -286,3 +286,15 @@ def test_tensors_of_another_device(monkeypatch):
                  lambda: binding.kv4_evict_tokens(cache, slots, slots.int(), el)):
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+@pytest.mark.parametrize("heads, most", [((32, 8, 128), 6000), ((16, 16, 64), 9000), ((16, 16, 128), 6000)])
+def test_attention_of_larger_batches(heads, most):
+    """Larger batches of unlike requests: runs of every kind side by side."""
+    rng = np.random.default_rng(11)
+    plain = [(int(rng.integers(300, most)), int(rng.integers(1, 30)), int(rng.integers(0, 40))) for _ in range(9)]
+    branched = [(c, 4, [(1, 1, 19), (3, 0, 19), (4, 0, 19)] if i % 2 else 3) for i, (c, _, _) in enumerate(plain)]
+    for requests in (plain + [(5, 1, 0), (0, 0, 0), (0, 1, 0)], branched + [(0, 2, [(1, 0, 3)])]):
+        b = Batch(requests, heads=heads)
+        q, pool = b.q(), b.pool4()
+        check_attention(*_attend(b, q, pool), *b.attention(q, pool), _score_size(b, q, pool))
