@@ -325,8 +325,13 @@ rg_status each_evict_plan(const rg_evict_layout* L, int64_t& words, F f) {
     std::memset(&p, 0, sizeof(p));
     p.num_req = std::min(kMaxEvictReq, L->num_requests - r0);
     int64_t ws = 0, moves = 0;
+    // The longest requests first: a choice takes as long as its request, and one
+    // of more than 8192 tokens fills a compute unit.
+    int order[kMaxEvictReq];
+    std::iota(order, order + p.num_req, r0);
+    std::stable_sort(order, order + p.num_req, [&](int x, int y) { return L->ctx_len[x] > L->ctx_len[y]; });
     for (int k = 0; k < p.num_req; ++k) {
-      const int r = r0 + k;
+      const int r = order[k];
       EvictReq& q = p.req[k];
       q.ctx = L->ctx_len[r];
       q.keep = std::min(L->keep[r], L->ctx_len[r]);

@@ -35,10 +35,10 @@ struct Kv4Runs {
   int count, keys;
 };
 __host__ __device__ inline Kv4Runs kv4_runs(int T, int tiles, int target) {
-  const int steps = (T + 31) / 32;
-  const int most = target / kv4_rate(tiles) > 1 ? target / kv4_rate(tiles) : 1;  // steps of a run at most
-  const int n = (steps + most - 1) / most, each = (steps + n - 1) / n;
-  return {(steps + each - 1) / each, 32 * each};
+  const uint32_t steps = ((uint32_t)T + 31) / 32, rate = kv4_rate(tiles);
+  const uint32_t most = (uint32_t)target > rate ? (uint32_t)target / rate : 1;  // steps of a run at most
+  const uint32_t n = (steps + most - 1) / most, each = (steps + n - 1) / n;
+  return {(int)((steps + each - 1) / each), (int)(32 * each)};
 }
 struct Kv4AttnArgs {
   const uint16_t* q;

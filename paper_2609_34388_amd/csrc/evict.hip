@@ -21,6 +21,8 @@
 // at head size 64) of every unit: the wave reads its sources' units whole, all
 // at once, and moves the pieces in registers.  Bound by the lines that the pieces
 // lie in, of which a page with any hole has most.
+#include <type_traits>
+
 #include "cache_internal.h"
 #include "kv4_device.h"
 
@@ -43,11 +45,27 @@ __device__ __forceinline__ MoveList move_list(const EvictArgs& a, const EvictReq
   return {reinterpret_cast<int2*>(at), at + 2 * (size_t)q.keep, at + 2 * (size_t)q.keep + q.most};
 }
 
+// Sum over this lane and those before it (data moves within the vector unit).
+__device__ __forceinline__ uint32_t scan64(uint32_t x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1, 2, 4, 8: rows of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15: row 0 to 1, 2 to 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31: both to 2 and 3
+  return x;
+}
+
+// Lanes of a mask before this one, added to `x`.
+__device__ __forceinline__ uint32_t count_below(uint64_t mask, uint32_t x) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, x));
+}
+
 // KW: words of a thread in registers; slots past them are read again in each pass.
 template <int KW>
 __global__ __launch_bounds__(kEvictThreads, KW <= 8 ? 8 : 4) void evict_select_kernel(EvictArgs a, EvictPlan p) {
-  __shared__ uint32_t hist[kBins];
-  __shared__ uint32_t s_wave[kWaves], s_digit, s_left;
+  __shared__ uint32_t hist[kBins];  // later the lists of holes and movers, where they fit
+  __shared__ uint32_t s_wave[kWaves], s_word, s_left, s_in;
   __shared__ uint32_t s_count[kWaves][3];
   const int r = (int)blockIdx.x / a.hkv, hk = (int)blockIdx.x % a.hkv;
   const EvictReq q = p.req[r];
@@ -62,13 +80,14 @@ __global__ __launch_bounds__(kEvictThreads, KW <= 8 ? 8 : 4) void evict_select_k
     return;
   }
   const int recent_from = L + q.evicted - a.recent;  // positions from here on are protected
-  // Slots of this wave: 64 i + lane from j0 on.
+  // Slots of this wave: 64 i + lane from first on.
   const int steps = (L + kEvictThreads - 1) / kEvictThreads;
-  const int j0 = wave * steps * 64 + lane;
+  const int first = wave * steps * 64, j0 = first + lane;
   // A slot's score as a word of the same order: protected tokens the largest.
+  constexpr uint32_t kProtected = 0xffffffffu;
   auto word = [&](float score, int pos) {
     const uint32_t u = __float_as_uint(score + 0.f);  // -0 becomes 0
-    return pos < a.sink || pos >= recent_from ? 0xffffffffu : (u & 0x80000000u) ? ~u : u | 0x80000000u;
+    return pos < a.sink || pos >= recent_from ? kProtected : (u & 0x80000000u) ? ~u : u | 0x80000000u;
   };
   auto fetch = [&](int i) {
     const int j = min(j0 + 64 * i, L - 1);
@@ -109,67 +128,91 @@ __global__ __launch_bounds__(kEvictThreads, KW <= 8 ? 8 : 4) void evict_select_k
     for (int i = KW; i < steps; ++i) f(i, fetch(i), j0 + 64 * i < L);
   };
 
-  uint32_t prefix = 0, left = (uint32_t)keep;  // of the tokens whose words begin with the prefix, `left` are kept
-#pragma unroll
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-    const uint32_t mask = pass == 0 ? 0u : pass == 1 ? ~0u << 21 : ~0u << 10;
-    const uint32_t bins = pass == 2 ? 1024u : 2048u;
+  // Of the tokens whose words begin with the prefix (under the mask) `left` are
+  // kept; where that is all `in` of them the other bits need not be looked at.
+  uint32_t prefix = 0, mask = 0, left = (uint32_t)keep, in_prefix = 0;
+  auto pass = [&](auto shift_of) {  // true: the next bits have to be looked at
+    constexpr int shift = decltype(shift_of)::value;
+    constexpr uint32_t bins = shift == 0 ? 1024u : 2048u;
     hist[tid] = 0;
     hist[tid + kEvictThreads] = 0;
     __syncthreads();
-    each([&](int, uint32_t u, bool in) {
-      if (in && (u & mask) == prefix) atomicAdd(&hist[(u >> shift) & (bins - 1)], 1u);
-    });
+    if constexpr (shift == 21) {  // protected tokens, one word for all, are counted by the wave
+      uint32_t safe = 0;
+      each([&](int, uint32_t u, bool in) {
+        safe += __popcll(__ballot(in && u == kProtected));
+        if (in && u != kProtected) atomicAdd(&hist[u >> shift], 1u);
+      });
+      if (lane == 0 && safe > 0) atomicAdd(&hist[bins - 1], safe);
+    } else {
+      each([&](int, uint32_t u, bool in) {
+        if (in && (u & mask) == prefix) atomicAdd(&hist[(u >> shift) & (bins - 1)], 1u);
+      });
+    }
     __syncthreads();
     // from the top bin down, two bins a thread
     const uint32_t b0 = hist[kBins - 1 - 2 * tid], b1 = hist[kBins - 2 - 2 * tid];
-    uint32_t upto = b0 + b1;
-    for (int off = 1; off < 64; off <<= 1) {
-      const uint32_t x = __shfl_up(upto, off);
-      if (lane >= off) upto += x;
-    }
+    const uint32_t upto = scan64(b0 + b1);
     if (lane == 63) s_wave[wave] = upto;
     __syncthreads();
     uint32_t before = upto - b0 - b1;
     for (int w = 0; w < wave; ++w) before += s_wave[w];
     if (before < left && left <= before + b0 + b1) {
       const bool second = left > before + b0;
-      s_digit = (uint32_t)(kBins - 1 - 2 * tid) - second;
+      s_word = (uint32_t)(kBins - 1 - 2 * tid) - second;
       s_left = left - before - (second ? b0 : 0u);
+      s_in = second ? b1 : b0;
     }
     __syncthreads();
-    prefix |= s_digit << shift;
+    prefix |= s_word << shift;
+    mask = ~0u << shift;
     left = s_left;
-  }
-
-  const uint64_t below = (1ull << lane) - 1;
-  uint32_t ties = 0;
-  each([&](int, uint32_t u, bool in) { ties += __popcll(__ballot(in && u == prefix)); });
-  if (lane == 0) s_count[wave][0] = ties;
-  __syncthreads();
-  uint32_t tie0 = 0;
-  for (int w = 0; w < wave; ++w) tie0 += s_count[w][0];
-
-  // visit(j, kept, holes before j and movers before j among the wave's)
-  auto walk = [&](auto visit) {
-    uint32_t tie = tie0, holes = 0, movers = 0;
-    each([&](int i, uint32_t u, bool in) {
-      const int j = j0 + 64 * i;
-      const uint64_t eq = __ballot(in && u == prefix);
-      const bool kept = in && (u > prefix || (u == prefix && tie + __popcll(eq & below) < left));
-      const uint64_t hole = __ballot(in && j < keep && !kept), mover = __ballot(kept && j >= keep);
-      if (in) visit(j, kept, holes + (uint32_t)__popcll(hole & below), movers + (uint32_t)__popcll(mover & below));
-      tie += __popcll(eq);
-      holes += __popcll(hole);
-      movers += __popcll(mover);
-    });
-    return make_uint2(holes, movers);
+    in_prefix = s_in;
+    return left != in_prefix;
   };
-  const uint2 mine = walk([](int, bool, uint32_t, uint32_t) {});
+  if (pass(std::integral_constant<int, 21>()) && pass(std::integral_constant<int, 10>()))
+    pass(std::integral_constant<int, 0>());
+
+  // Ties: those that share the prefix and lie in waves before this one.
+  uint32_t tie0 = 0;
+  if (left < in_prefix) {
+    uint32_t ties = 0;
+    each([&](int, uint32_t u, bool in) { ties += __popcll(__ballot(in && (u & mask) == prefix)); });
+    if (lane == 0) s_count[wave][0] = ties;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) tie0 += s_count[w][0];
+  }
+  // Lanes whose slot is kept; `tie` counts the ties so far.
+  auto kept_lanes = [&](uint32_t u, bool in, uint32_t& tie) -> uint64_t {
+    uint64_t kept = __ballot(in && (u & mask) > prefix);
+    const uint64_t eq = __ballot(in && (u & mask) == prefix);
+    if (eq != 0) {
+      const uint32_t n = (uint32_t)__popcll(eq);
+      if (tie + n <= left) kept |= eq;
+      else if (tie < left) kept |= eq & __ballot(count_below(eq, tie) < left);
+      tie += n;
+    }
+    return kept;
+  };
+  // Lanes of step i whose slot lies before `keep`.
+  auto low_lanes = [&](int i) -> uint64_t {
+    const int n = keep - first - 64 * i;
+    return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
+  };
+
+  constexpr int kMasks = KW < 16 ? KW : 16;  // masks held (in scalar registers); the others are made again
+  uint64_t kept[kMasks];
+  uint32_t tie = tie0, holes = 0, movers = 0, tie_past = 0;  // tie_past: at the first of those
+  each([&](int i, uint32_t u, bool in) {
+    if (i == kMasks) tie_past = tie;
+    const uint64_t m = kept_lanes(u, in, tie), low = low_lanes(i);
+    if (i < kMasks) kept[i < kMasks ? i : 0] = m;
+    holes += (uint32_t)__popcll(low & ~m);
+    movers += (uint32_t)__popcll(m & ~low);
+  });
   if (lane == 0) {
-    s_count[wave][1] = mine.x;
-    s_count[wave][2] = mine.y;
+    s_count[wave][1] = holes;
+    s_count[wave][2] = movers;
   }
   __syncthreads();
   uint32_t hole0 = 0, mover0 = 0, count = 0;
@@ -178,22 +221,39 @@ __global__ __launch_bounds__(kEvictThreads, KW <= 8 ? 8 : 4) void evict_select_k
     count += s_count[w][2];
   }
   const MoveList list = move_list(a, q, hk);
-  walk([&](int j, bool kept, uint32_t holes, uint32_t movers) {
-    if (j < keep) {
-      if (kept) list.take[j] = make_int2(-1, 0);
-      else list.hole[hole0 + holes] = j;
-    } else if (kept) {
-      list.mover[mover0 + movers] = j;
+  const bool near = count <= kBins / 2;  // the lists fit LDS: no trip to memory and back
+  auto visit = [&](int i, uint64_t m) {
+    const int j = j0 + 64 * i;
+    const uint64_t low = low_lanes(i), hole = low & ~m, mover = m & ~low;
+    if (low >> lane & 1) {
+      if (m >> lane & 1) {
+        list.take[j] = make_int2(-1, 0);
+      } else {
+        const uint32_t k = count_below(hole, hole0);
+        if (near) hist[k] = j;
+        else list.hole[k] = j;
+      }
+    } else if (m >> lane & 1) {
+      const uint32_t k = count_below(mover, mover0);
+      if (near) hist[kBins / 2 + k] = j;
+      else list.mover[k] = j;
     }
-  });
-  __syncthreads();
+    hole0 += (uint32_t)__popcll(hole);
+    mover0 += (uint32_t)__popcll(mover);
+  };
+#pragma unroll
+  for (int i = 0; i < KW; ++i)
+    if (i < steps) visit(i, i < kMasks ? kept[i < kMasks ? i : 0] : kept_lanes(held[i], j0 + 64 * i < L, tie_past));
+  for (int i = KW; i < steps; ++i) visit(i, kept_lanes(fetch(i), j0 + 64 * i < L, tie_past));
+  if (near) lds_barrier();  // not for what went to memory, which no one reads here
+  else __syncthreads();
   for (uint32_t k0 = tid; k0 < count; k0 += 4 * kEvictThreads) {  // four at a time in flight
     int to[4], from[4], page[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const uint32_t k = min(k0 + u * kEvictThreads, count - 1);
-      to[u] = list.hole[k];
-      from[u] = list.mover[k];
+      to[u] = near ? (int)hist[k] : list.hole[k];
+      from[u] = near ? (int)hist[kBins / 2 + k] : list.mover[k];
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) page[u] = pages[from[u] >> 4];

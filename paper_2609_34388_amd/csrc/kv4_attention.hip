@@ -41,7 +41,7 @@ __device__ __forceinline__ float scale_at(uint32_t word) {
 // What a work group of a wave's tiles works on.
 struct Kv4Item {
   int hk, kbeg, kend;  // KV head, keys of the run
-  int c, nch;          // the run, of how many
+  int nch;             // runs that the column group's keys are cut into
   int n, L, M;         // rows, context, columns of the request
   int tile0, nct;      // first tile, tiles of the column group
   int part;            // first partial column of the item
@@ -406,25 +406,26 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void kv4_attn_kernel(Kv4
   // those of the last one; their partials lie in the same order.
   const int T = it.L + it.n;
   const int tiles = (it.M + 31) / 32, full = tiles / kKv4Waves;
-  int local = item - rq.item_start;
+  uint32_t local = item - rq.item_start;
   it.nct = kKv4Waves;
-  Kv4Runs runs = kv4_runs(T, it.nct, p.chunk);
+  it.tile0 = 0;
   it.part = rq.part_start;
-  if (local >= full * a.hkv * runs.count) {
-    local -= full * a.hkv * runs.count;
-    if (runs.count > 1) it.part += full * kKv4Cols * a.hkv * runs.count;
-    it.nct = tiles - full * kKv4Waves;
+  Kv4Runs runs = {0, 0};
+  if (full > 0) {
     runs = kv4_runs(T, it.nct, p.chunk);
-    it.tile0 = full * kKv4Waves;
-  } else {
-    it.tile0 = local / (a.hkv * runs.count) * kKv4Waves;
-    local %= a.hkv * runs.count;
-    if (runs.count > 1) it.part += it.tile0 * 32 * a.hkv * runs.count;
+    const uint32_t group = (uint32_t)a.hkv * runs.count;  // items of a column group
+    const uint32_t group0 = min(local / group, (uint32_t)full);
+    local -= group0 * group;
+    it.tile0 = group0 * kKv4Waves;
+    if (runs.count > 1) it.part += it.tile0 * 32 * group;
+  }
+  if (it.tile0 == full * kKv4Waves) {
+    it.nct = tiles - it.tile0;
+    runs = kv4_runs(T, it.nct, p.chunk);
   }
   it.nch = runs.count;
-  it.hk = local / runs.count;
-  it.c = local % runs.count;
-  it.kbeg = it.c * runs.keys;
+  it.hk = local / (uint32_t)runs.count;
+  it.kbeg = (local - it.hk * runs.count) * runs.keys;
   it.kend = min(T, it.kbeg + runs.keys);
   if (it.nch > 1) it.part += local * it.nct * 32;
 
