@@ -50,6 +50,8 @@ rg_status check_plans(const rg_attn_layout* L, int threads, Items items) {
 }
 
 // ---------------------------------------------------------------------------
+// Blocks from which on a work item takes kRowHeads of them.
+constexpr int64_t kRowBlocks = 4096;
 rg_status run_rows(const rg_attn_layout* L, const uint16_t* k, int64_t k_stride, const uint16_t* v, int64_t v_stride,
                    const uint8_t* cache, bool append, void* stream) {
   const rg_status st = validate_layout(L);
@@ -70,13 +72,18 @@ rg_status run_rows(const rg_attn_layout* L, const uint16_t* k, int64_t k_stride,
   a.hkv = L->num_kv_heads;
   auto pages = [&](int r) -> int64_t {
     const int64_t n = L->q_indptr[r + 1] - L->q_indptr[r];
-    return n == 0 ? 0 : ((L->ctx_len[r] + n - 1) / kPageSize - L->ctx_len[r] / kPageSize + 1) * L->num_kv_heads;
+    return n == 0 ? 0 : (L->ctx_len[r] + n - 1) / kPageSize - L->ctx_len[r] / kPageSize + 1;
   };
+  int64_t blocks = 0;
+  for (int r = 0; r < L->num_requests; ++r) blocks += pages(r) * L->num_kv_heads;
+  const int heads = blocks > kRowBlocks ? kRowHeads : 1;
+  auto items = [&](int r) { return pages(r) * ((L->num_kv_heads + heads - 1) / heads); };
   if (L->num_requests > kMaxReqPerLaunch) {
-    const rg_status fits = check_plans(L, 256, pages);
+    const rg_status fits = check_plans(L, 256, items);
     if (fits != RG_OK) return fits;
   }
-  return each_plan(L, 256, pages, [&](const AttnPlan& p) {
+  return each_plan(L, 256, items, [&](AttnPlan& p) {
+    p.chunk = heads;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     return append ? launch_kv4_append(a, p, L->head_dim, s) : launch_kv4_read(a, p, L->head_dim, s);
   });

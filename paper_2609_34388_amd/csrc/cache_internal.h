@@ -6,8 +6,9 @@
 
 namespace rg {
 
-// Rows into, or out of, the 4-bit cache.  Plans: AttnPlan with a work item
-// per page that a request's rows touch and KV head.
+// Rows into, or out of, the 4-bit cache.  Plans: AttnPlan with a work item per
+// page that a request's rows touch and plan.chunk KV heads (1 .. kRowHeads).
+constexpr int kRowHeads = 4;
 struct Kv4RowArgs {
   uint16_t* k;  // rows (appended: read, read back: written), or NULL
   uint16_t* v;

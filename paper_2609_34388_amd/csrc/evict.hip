@@ -63,7 +63,7 @@ __device__ __forceinline__ uint32_t count_below(uint64_t mask, uint32_t x) {
 
 // KW: words of a thread in registers; slots past them are read again in each pass.
 template <int KW>
-__global__ __launch_bounds__(kEvictThreads, KW <= 8 ? 8 : 4) void evict_select_kernel(EvictArgs a, EvictPlan p) {
+__global__ __launch_bounds__(kEvictThreads, 8) void evict_select_kernel(EvictArgs a, EvictPlan p) {
   __shared__ uint32_t hist[kBins];  // later the lists of holes and movers, where they fit
   __shared__ uint32_t s_wave[kWaves], s_word, s_left, s_in;
   __shared__ uint32_t s_count[kWaves][3];
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(kEvictThreads, KW <= 8 ? 8 : 4) void evict_select_k
   };
   // Page numbers of a batch, then its scores (and positions): two round trips.
   // Slots past the last repeat it and are never asked for (see each()).
-  constexpr int kBatch = KW < 8 ? KW : 8;
+  constexpr int kBatch = KW < 32 ? (KW < 8 ? KW : 8) : 4;
   uint32_t held[KW];
 #pragma unroll
   for (int i0 = 0; i0 < KW; i0 += kBatch) {

@@ -298,3 +298,30 @@ def test_attention_of_larger_batches(heads, most):
         b = Batch(requests, heads=heads)
         q, pool = b.q(), b.pool4()
         check_attention(*_attend(b, q, pool), *b.attention(q, pool), _score_size(b, q, pool))
+
+
+@pytest.mark.parametrize("heads", [(6, 6, 64), (7, 7, 128)])
+def test_append_and_read_of_many_blocks(heads):
+    """So many that a work item takes several heads: as request by request,
+    whose bytes test_append_and_read pins."""
+    requests = [(5, 4000, 0), (16, 4096, 0), (0, 3333, 0), (31, 1, 0), (0, 0, 0), (100, 30, 0)]
+    b = Batch(requests, heads=heads)
+    k, v = (b.normal(b.rows, b.hkv, b.d).to(DEV) for _ in range(2))
+    both = [torch.full((b.num_pages, b.hkv, 17 * b.d), 0xff, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    lay = b.layout4(both[0])
+    binding.kv4_append(k, v, both[0], lay)
+    pages = b.device_pages(DEV)
+    rows = [slice(int(b.q_indptr[r]), int(b.q_indptr[r + 1])) for r in range(b.R)]
+    one = []
+    for r, (at, ctx) in enumerate(zip(rows, b.ctx)):
+        n = at.stop - at.start
+        half = n // 2  # two calls, the second behind the first
+        for first, count in ((0, half), (half, n - half)):
+            mine = torch.as_tensor(b.pages(r), device=DEV)
+            l1 = binding.make_kv4_layout(b.hq, both[1], [0, count], [0], [int(ctx) + first], [0, len(mine)], mine)
+            part = slice(at.start + first, at.start + first + count)
+            binding.kv4_append(k[part], v[part], both[1], l1)
+            one.append(binding.kv4_read(both[1], l1))
+    assert torch.equal(both[0], both[1])
+    kr, vr = binding.kv4_read(both[0], lay)
+    assert torch.equal(kr, torch.cat([x for x, _ in one])) and torch.equal(vr, torch.cat([x for _, x in one]))
