@@ -50,7 +50,9 @@ rg_status check_plans(const rg_attn_layout* L, int threads, Items items) {
 }
 
 // ---------------------------------------------------------------------------
-// Blocks from which on a work item takes kRowHeads of them.
+// Blocks from which on a work item takes kRowHeads of them: 1400 blocks take
+// 6.6 us in and 5.1 out one by one, 7.4 and 4.7 in fours; 217 thousand take 483 us
+// out one by one, 409 in fours, 413 in eights.
 constexpr int64_t kRowBlocks = 4096;
 rg_status run_rows(const rg_attn_layout* L, const uint16_t* k, int64_t k_stride, const uint16_t* v, int64_t v_stride,
                    const uint8_t* cache, bool append, void* stream) {
@@ -114,7 +116,10 @@ Kv4Cols kv4_cols(const rg_attn_layout* L, int r) {
 // as many rounds as keep items below kKv4Long units: a long round ends unevenly.
 // Measured (GPU time of the call, merge included): 40 requests of 8k to 32k
 // keys 565 us in one round, 560 in two to four, 585 in six; 16 requests of 1k
-// to 8k keys with branches 85 us in one round, 92 in two, 122 in three.
+// to 8k keys with branches 85 us in one round, 92 in two, 122 in three.  Equal
+// shares of a request's segments, a work group ending one and beginning the
+// next, took 73 us where these runs take 67: a second start costs more than even
+// lengths give.
 // kKv4Least is two steps of a wave on one tile, or one on four: one token over
 // 4097 keys takes 14.4 us with it, 16.4 with half of it, 14.6 with twice.
 constexpr int kKv4Least = 32, kKv4Long = 4096;

@@ -9,18 +9,24 @@
 //
 // select: one work group per (request, KV head), its slots' scores as ordered
 // 32-bit words (protected tokens the largest word) in registers.  A radix
-// selection of 11, 11 and 10 bits finds the word of the keep-th largest; then
-// each wave goes over a contiguous part of the slots: ties are taken from the
-// lowest slot on, holes and movers get their ranks from wave ballots.  It
-// writes for every kept slot which token it takes, if any.  Bound by latency:
-// its loads depend on the page list alone.
+// selection of 11, 11 and 10 bits finds the word of the keep-th largest, ending
+// where all tokens of a prefix are kept; then each wave goes over a contiguous
+// part of the slots: ties are taken from the lowest slot on, holes and movers get
+// their ranks from wave ballots.  It writes for every kept slot which token it
+// takes, if any.  Bound by latency: a few thousand tokens give one compute unit
+// work that 255 others cannot share.  One request of 4128 tokens 12.5 us, 16 of 1k
+// to 8k 14.5, 40 of 8k to 32k 51 (8 heads each; the start 1.3 us, the first bits 2.3,
+// each later pass 1.3 to 1.6, ranks and lists 3).  Comparing the last few hundred
+// candidates each with all, instead of further bits, took 2.0 us.
 //
 // move: a wave per page of the kept slots, which writes their positions and
 // fills the page's holes: mass and K rows as they are.  In V, where a 16-byte
 // unit holds eight tokens of few dims, a token is a 2-byte piece (1 byte, 4-bit
 // at head size 64) of every unit: the wave reads its sources' units whole, all
 // at once, and moves the pieces in registers.  Bound by the lines that the pieces
-// lie in, of which a page with any hole has most.
+// lie in, of which a page with any hole has most: 16 requests cut to 3/4, bf16,
+// 320 MB of lines in 68 us; 40 long ones cut to half, 4-bit, 1.2 GB in 342 us.
+// Pieces written one by one, without reading the page's units: 67 and 353 us.
 #include <type_traits>
 
 #include "cache_internal.h"
@@ -62,6 +68,8 @@ __device__ __forceinline__ uint32_t count_below(uint64_t mask, uint32_t x) {
 }
 
 // KW: words of a thread in registers; slots past them are read again in each pass.
+// 64 registers let two work groups share a compute unit (40 long requests: 59 us
+// where they do not, 51).
 template <int KW>
 __global__ __launch_bounds__(kEvictThreads, 8) void evict_select_kernel(EvictArgs a, EvictPlan p) {
   __shared__ uint32_t hist[kBins];  // later the lists of holes and movers, where they fit
@@ -96,7 +104,7 @@ __global__ __launch_bounds__(kEvictThreads, 8) void evict_select_kernel(EvictArg
   };
   // Page numbers of a batch, then its scores (and positions): two round trips.
   // Slots past the last repeat it and are never asked for (see each()).
-  constexpr int kBatch = KW < 32 ? (KW < 8 ? KW : 8) : 4;
+  constexpr int kBatch = KW < 8 ? KW : KW < 32 ? 8 : 4;  // 32 held words leave registers for four
   uint32_t held[KW];
 #pragma unroll
   for (int i0 = 0; i0 < KW; i0 += kBatch) {

@@ -5,16 +5,17 @@
 // run of keys).  A wave holds one or two of the tiles (two share every decoded
 // element: decoding is more than half of a tile's vector instructions) and
 // takes every kg-th 32-key tile of the run: one pair of tiles gives the four
-// waves four key groups, two pairs two each.
+// waves four key groups, two pairs two each.  The main loop has no barrier.
 //
-// A wave reads its keys' codes straight from the pool into registers, as the
-// block is laid out for that: a lane's 16 bytes of K codes are the 32 dims of
-// one scale group of its key, and its 16 bytes of V codes are 8 tokens of its
-// D / 32 dims, the operand rows of S^T = K Q^T and O^T += V^T P^T.  So keys
-// need no LDS and the main loop no barrier, and a decoded element costs half a
-// conversion (v_cvt_scalef32_pk_bf16_fp4, which multiplies by the group's
-// scale), for V plus half a byte permutation that pairs two tokens.  Q is read
-// from LDS for each key tile; in registers it would leave one wave per SIMD.
+// A wave copies both blocks of a key tile as they lie in the pool into its own
+// ring of two in LDS, by loads that need no register, two tiles ahead; the block
+// is laid out for what the lanes take from there: 16 bytes of K codes are the 32
+// dims of one scale group of the lane's key, 16 bytes of V codes 8 tokens of its
+// D / 32 dims, the operand rows of S^T = K Q^T and O^T += V^T P^T.  A decoded
+// element costs half a conversion (v_cvt_scalef32_pk_bf16_fp4, which multiplies
+// by the group's scale), for V plus half a byte permutation that pairs two
+// tokens.  Q is read from LDS for each key tile; in registers it would leave one
+// wave per SIMD.
 //
 // The dims go through the products in another order than in memory: K step ks
 // of S^T holds dims 64 (ks / 4) + 32 lh + 8 (ks % 4) .. + 7 of half-wave lh (Q
@@ -22,7 +23,17 @@
 //
 // Softmax online in base 2; the running sum adds P in fp32, the product takes
 // it rounded to bf16 (off by at most 2^-8 of each term, as the output's own
-// rounding).  Runs of a request's keys meet in fp32 in the workspace.
+// rounding).  No maximum is taken where the running reference holds (below).
+// Runs of a request's keys meet in fp32 in the workspace.
+//
+// Measured (query heads / KV heads / head size 32/8/128 unless said):
+// one token over 4097 keys 8.4 us + 4.8 of the merge, bound by the chain of its
+// start, one key tile a wave, and its end; 16 requests of 1k to 8k keys with
+// branches 67 + 12 us; 48 of up to 6k keys, heads 16/4/64, 30 + 7 us; 40 of 8k to
+// 32k keys 525 + 25 us, 685 TFLOP/s of bf16 products at 2.0 GHz, to which the
+// chip's power limit takes the clock: vector instructions fill 52 % of the
+// cycles, products 38 %.  Codes read straight into registers measured the same
+// within 2 % at head size 128 and leave no registers for a second wave at 64.
 #include "cache_internal.h"
 #include "kv4_device.h"
 
@@ -435,14 +446,17 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void kv4_attn_kernel(Kv4
   else kv4_wave<D, 1, Plan>(a, rq, it, pair, np, wave / np, lds);
 }
 
-// Merge of the runs of split requests.  A work item is (request, KV head,
-// 32-column tile, row v): 64 rows of 16 bytes, 4 dims of a column each.  PARTS
-// threads share a row, part j taking runs j, j + PARTS, ..., and meet in LDS.
+// Merge of the runs of split requests.  An item is (request, KV head, 32-column
+// tile, row v): 64 rows of 16 bytes, 4 dims of a column each.  PARTS 1: a wave an
+// item, four of the same tile a work group (of one wave they were bound by the
+// rate at which work groups start: 13.0 -> 11.6 us for 6700 items).  Else the
+// four waves share an item, wave j taking runs j, j + PARTS, ..., and meet in LDS.
 template <int D, int PARTS, typename Plan>
-__global__ __launch_bounds__(kKv4MergeRows * PARTS) void kv4_merge_kernel(Kv4AttnArgs a, Plan p) {
+__global__ __launch_bounds__(kKv4MergeRows * kKv4MergeParts) void kv4_merge_kernel(Kv4AttnArgs a, Plan p) {
   constexpr int DT = D / 32;
   __shared__ float st[PARTS > 1 ? (PARTS - 1) * 6 * 64 : 1];
-  const int item = xcd_item(p.grid_comb);
+  const int part = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int item = PARTS > 1 ? xcd_item(gridDim.x) : xcd_item(gridDim.x) * kKv4MergeParts + part;
   if (item >= p.total_comb) return;
   const int r = find_request(p, item, true);
   const auto rq = p.req[r];
@@ -471,7 +485,6 @@ __global__ __launch_bounds__(kKv4MergeRows * PARTS) void kv4_merge_kernel(Kv4Att
   base += (size_t)hk * nch * nct * 32 + (size_t)(tile - tile0) * 32;
   const size_t stride = (size_t)nct * 32;  // partial columns from run to run
   const int lane = threadIdx.x & 63, lc = lane & 31, lh = lane >> 5;
-  const int part = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int col = tile * 32 + lc;
 
   float m = kNegInf, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
@@ -486,7 +499,7 @@ __global__ __launch_bounds__(kKv4MergeRows * PARTS) void kv4_merge_kernel(Kv4Att
     m = m_new;
   };
   if (col < M) {
-    for (int c0 = part; c0 < nch; c0 += 8 * PARTS) {
+    for (int c0 = PARTS > 1 ? part : 0; c0 < nch; c0 += 8 * PARTS) {
       float2 ml[8];
       float4 x[8];
 #pragma unroll
@@ -540,7 +553,8 @@ hipError_t launch_impl(const Kv4AttnArgs& a, const Plan& p, hipStream_t stream) 
     hipLaunchKernelGGL((kv4_merge_kernel<D, kKv4MergeParts, Plan>), dim3(p.grid_comb),
                        dim3(kKv4MergeRows * kKv4MergeParts), 0, stream, a, p);
   else
-    hipLaunchKernelGGL((kv4_merge_kernel<D, 1, Plan>), dim3(p.grid_comb), dim3(kKv4MergeRows), 0, stream, a, p);
+    hipLaunchKernelGGL((kv4_merge_kernel<D, 1, Plan>), dim3((p.total_comb / kKv4MergeParts + 7) / 8 * 8),
+                       dim3(kKv4MergeRows * kKv4MergeParts), 0, stream, a, p);
   return hipGetLastError();
 }
 

@@ -16,6 +16,12 @@
 // (mass_rows_kernel, prompts) the products and exponentials bound it: a work
 // group takes 64 keys, held in registers by each of its waves, and the waves
 // share the column tiles, whose Q comes through LDS of the wave's own.
+//
+// Measured (heads 32/8/128): 16 requests' steps over 1k to 8k bf16 keys 32 to 36 us
+// (146 MB); 40 over 8k to 32k 4-bit keys 150 us; two prompts of 2048 and 1555 rows
+// 125 to 138 us, 77 of products at the matrix product's rate and 56 of exponentials
+// and sums, which overlap little.  A prompt's 128 columns and more through mass_kernel, Q read from LDS by
+// each key tile anew, took 406 us.
 #include "cache_internal.h"
 #include "kv4_device.h"
 
