@@ -17,11 +17,13 @@
 // group takes 64 keys, held in registers by each of its waves, and the waves
 // share the column tiles, whose Q comes through LDS of the wave's own.
 //
-// Measured (heads 32/8/128): 16 requests' steps over 1k to 8k bf16 keys 32 to 36 us
-// (146 MB); 40 over 8k to 32k 4-bit keys 150 us; two prompts of 2048 and 1555 rows
-// 125 to 138 us, 77 of products at the matrix product's rate and 56 of exponentials
-// and sums, which overlap little.  A prompt's 128 columns and more through mass_kernel, Q read from LDS by
-// each key tile anew, took 406 us.
+// Measured (heads 32/8/128): 16 requests' steps over 1k to 8k bf16 keys 34 us (144 MB,
+// 4.2 TB/s); 40 over 8k to 32k 4-bit keys 150 us (532 MB, 3.6 TB/s, where a kernel
+// that only reads reaches 4.0); two prompts of 2048 and 1555 rows 109 us, 77 of
+// products at a large product's rate and 56 of exponentials and sums, which overlap
+// little.  Prompts through mass_kernel, Q read from LDS by each key tile anew, took
+// 406 us; the next tile's products placed between a wave's exponentials, at two
+// waves a SIMD, took 157 where the plain order then took 135.
 #include "cache_internal.h"
 #include "kv4_device.h"
 
@@ -96,11 +98,11 @@ __device__ __forceinline__ void add_weights(const MassArgs& a, const MassItem& i
                                             int kb, float& w) {
   const int lane = threadIdx.x & 63, lc = lane & 31, lh = lane >> 5;
   if (kb + 31 > it.L + row_of(a, col0)) {  // some row does not see every key
+    int first = col0 + 4 * lh;
+    asm volatile("" : "+v"(first));  // or the rows are found, 96 instructions, for every tile
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int col = col0 + 8 * (i >> 2) + 4 * lh + (i & 3);
-      if (kb + lc > it.L + row_of(a, col)) sc[i] = kNegInf;
-    }
+    for (int i = 0; i < 16; ++i)
+      if (kb + lc > it.L + row_of(a, first + 8 * (i >> 2) + (i & 3))) sc[i] = kNegInf;
   }
 #pragma unroll
   for (int i = 0; i < 16; ++i) w += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.scale_log2, -ls[i]));
@@ -252,18 +254,38 @@ __global__ __launch_bounds__(kThreads, 3) void mass_rows_kernel(MassArgs a, Attn
   // Columns past the counted ones repeat the last: they weigh zero.
   const uint16_t* base = a.q + (size_t)it.q_start * a.hq * D;
   float ls_next = 0.f;
-  const uint32_t head = (uint32_t)(it.hk * a.g);
-  auto load = [&](int t) {
+  // Byte of chunk i of the lane's in q, past the request's first row, its column
+  // `col` of the tile's: rows of a request span less than 2^31 (host check).
+  auto byte_at = [&](int i, int col) {
+    const int row = (i * 64 + lane) / NCH, ch = (lane % NCH) ^ (row % NCH), tok = row_of(a, col);
+    return ((uint32_t)(tok * a.hq + (col - tok * a.g) + it.hk * a.g) * D + 8 * ch) * 2;
+  };
+  // Where 16 columns are whole rows, the second half of a tile and a wave's next
+  // tile, 32 kMassWaves columns on, lie at constant distances: only the base moves.
+  const bool whole = 16 % a.g == 0;
+  const size_t half = (size_t)(16 / a.g) * a.hq, stride = 2 * kMassWaves * half;
+  const uint16_t* qt = base;
+  const float* lt = a.lse + (size_t)it.q_start * a.hq;
+  uint32_t at[LOADS / 2];
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int row = (i * 64 + lane) / NCH, ch = (lane % NCH) ^ (row % NCH);
-      const int col = min(32 * t + row, it.M - 1), tok = row_of(a, col);
-      // rows of a request lie within 2^31 bytes of its first (checked by the host)
-      const uint32_t at = (uint32_t)(tok * a.hq + (col - tok * a.g)) + head;
-      load_to_lds(tile_at + i * 1024, base, (at * D + 8 * ch) * 2);
+  for (int i = 0; i < LOADS / 2; ++i) at[i] = byte_at(i, 32 * t0 + (i * 64 + lane) / NCH);
+  const uint32_t lse_at = (uint32_t)(column_row(a, it, 32 * t0 + lc) - (size_t)it.q_start * a.hq);
+  auto load = [&](int t) {
+    if (whole && 32 * t + 32 <= it.M) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+        load_to_lds(tile_at + i * 1024, qt + (i < LOADS / 2 ? 0 : half * D), at[i % (LOADS / 2)]);
+      ls_next = lt[lse_at];
+    } else {
+      int first = 32 * t;
+      asm volatile("" : "+v"(first));  // not for every tile
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+        load_to_lds(tile_at + i * 1024, base, byte_at(i, min(first + (i * 64 + lane) / NCH, it.M - 1)));
+      ls_next = first + lc < it.M ? a.lse[column_row(a, it, first + lc)] : -kNegInf;
     }
-    const int col = 32 * t + lc;
-    ls_next = col < it.M ? a.lse[column_row(a, it, col)] : -kNegInf;
+    qt += stride * D;
+    lt += stride;
   };
   if (t0 < tiles) load(t0);
 
@@ -279,12 +301,6 @@ __global__ __launch_bounds__(kThreads, 3) void mass_rows_kernel(MassArgs a, Attn
     const char* row = tile + lc * (2 * D);
 #pragma unroll
     for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = *(const bf16x8*)(row + 16 * (q_chunk<KV4>(ks, lh) ^ (lc % NCH)));
-    float ls[16];
-#pragma unroll
-    for (int i4 = 0; i4 < 4; ++i4) {
-      const float4 x = *(const float4*)(lse2 + 8 * i4 + 4 * lh);
-      ls[4 * i4] = x.x, ls[4 * i4 + 1] = x.y, ls[4 * i4 + 2] = x.z, ls[4 * i4 + 3] = x.w;
-    }
     if (t + kMassWaves < tiles) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile is in registers
       load(t + kMassWaves);
@@ -297,6 +313,12 @@ __global__ __launch_bounds__(kThreads, 3) void mass_rows_kernel(MassArgs a, Attn
     for (int ks = 0; ks < KSTEPS; ++ks)
 #pragma unroll
       for (int s = 0; s < 2; ++s) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[ks], kf[s][ks], sc[s], 0, 0, 0);
+    float ls[16];
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      const float4 x = *(const float4*)(lse2 + 8 * i4 + 4 * lh);
+      ls[4 * i4] = x.x, ls[4 * i4 + 1] = x.y, ls[4 * i4 + 2] = x.z, ls[4 * i4 + 3] = x.w;
+    }
 #pragma unroll
     for (int s = 0; s < 2; ++s) add_weights(a, it, sc[s], ls, 32 * t, it.kbeg + 32 * s, w[s]);
   }
