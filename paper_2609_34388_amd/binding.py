@@ -636,8 +636,13 @@ def _check_layout(lay, rows: int, *tensors: torch.Tensor):
     _here(lay.page_indices, *tensors)
 
 
+# The current device without torch.cuda's own checks (0.6 us a call): tensors of
+# a device are there, so it is initialised.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _here(*tensors: Optional[torch.Tensor]):
-    here = torch.cuda.current_device()
+    here = _current_device()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"a tensor is on device {t.get_device()}, the current device is {here}")
@@ -645,15 +650,17 @@ def _here(*tensors: Optional[torch.Tensor]):
 
 def _rows(t: torch.Tensor, name: str, lay: _Layout) -> int:
     """Checks rows [rows, Hkv, D] (any row stride, heads contiguous) and returns the stride."""
-    hkv, d = lay.c.num_kv_heads, lay.c.head_dim
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.bfloat16:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not torch.bfloat16:
         raise TypeError(f"{name} must be a CUDA bf16 tensor")
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[1] != hkv or shape[2] != d or stride[2] != 1 or (hkv > 1 and stride[1] != d):
+    if t.dim() != 3:
+        raise ValueError(f"{name} must have three dimensions")
+    (rows, heads, width), (ahead, apart, next_to) = t.shape, t.stride()
+    hkv, d = lay.c.num_kv_heads, lay.c.head_dim
+    if heads != hkv or width != d or next_to != 1 or (hkv > 1 and apart != d):
         raise ValueError(f"{name} must be [rows, {hkv}, {d}], contiguous within a row")
-    if shape[0] != lay.q_indptr[-1]:
+    if rows != lay.q_indptr[-1]:
         raise ValueError("q_indptr[-1] must equal the number of rows")
-    return stride[0] if shape[0] > 1 else hkv * d
+    return ahead if rows > 1 else hkv * d
 
 
 def kv4_append(k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor, layout: _Layout, *, stream=None) -> None:

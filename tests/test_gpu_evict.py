@@ -459,3 +459,66 @@ def test_evict_one_page_partly_kept(four):
     for L, keep in ((32, 17), (31, 23), (30, 24), (40, 25), (16, 9), (9, 8), (17, 15)):
         for heads in ((2, 2, 128), (2, 2, 64)):
             _evict_case([L, L], [keep, keep - 1], heads, four, seed=L)
+
+
+@pytest.mark.parametrize("heads", [(32, 1, 64), (40, 2, 128), (10, 2, 64)])
+def test_mass_of_other_groups(heads):
+    """Query heads a KV head that do not divide 16 columns, or not 128."""
+    for four in (False, True):
+        b = Batch([(37, 77, 3), (0, 150, 0), (600, 2, 0)], heads=heads)
+        q, lse = b.q(), _lse(b, b.rng)
+        pool = b.pool4() if four else _pools16(b)
+        old = b.rng.random((b.num_pages, b.hkv, PAGE)).astype(np.float32)
+        mass, qd = dev(old), q.to(DEV)
+        count = np.array([70, 150, 1])
+        rc = torch.as_tensor(count, dtype=torch.int32, device=DEV)
+        if four:
+            cache = dev(pool)
+            binding.kv4_attention_mass(qd, cache, dev(lse), mass, b.layout4(cache), row_count=rc)
+        else:
+            kd = pool[0].to(DEV)
+            binding.attention_mass(qd, kd, dev(lse), mass, b.layout16(qd, kd), row_count=rc)
+        want = b.mass(old, q, pool, lse, count, 1.0)
+        for r in range(b.R):
+            page, slot = b.places(r, int(b.ctx[r] + b.nv[r]))
+            _check_mass(mass.cpu()[page, :, slot], want[page, :, slot], old, b, count, _score_size(b, q, pool))
+
+
+def test_pools_past_32_bits():
+    """The same pages at the far end of pools of more than 2^32 bytes."""
+    hkv, d, far = 8, 128, 270000
+    b = Batch([(300, 4, 3), (90, 2, 0), (517, 1, 0)], heads=(16, hkv, d), spare=0)
+    n = b.num_pages
+    q = b.q().to(DEV)
+    k, v = (b.normal(b.rows, hkv, d).to(DEV) for _ in range(2))
+    pool, (k16, v16) = dev(b.pool4()), (x.to(DEV) for x in _pools16(b, poison=0.0))
+    lse, score = dev(_lse(b, b.rng)), dev(b.rng.random((n, hkv, PAGE)).astype(np.float32))
+    keep = [200, 60, 400]
+
+    def call(pages, cache, kc, vc, mass, mass16, pos, pos16):
+        args = (b.q_indptr, b.nv, b.ctx, b.page_indptr, pages)
+        lay, lay16 = binding.make_kv4_layout(16, cache, *args), binding.make_layout(q, kc, *args)
+        binding.kv4_append(k, v, cache, lay)
+        out = [*binding.kv4_read(cache, lay), *binding.kv4_attention(q, cache, lay)]
+        binding.kv4_attention_mass(q, cache, lse, mass, lay)
+        binding.attention_mass(q, kc, lse, mass16, lay16)
+        out += [mass[-n:].clone(), mass16[-n:].clone()]
+        for c, extra in ((cache, ()), (kc, (vc,))):
+            el = binding.make_evict_layout(c, b.T, keep, b.page_indptr, pages, sink=2, recent=9)
+            if extra:
+                binding.evict_tokens(c, *extra, mass16, pos16, el, mass=mass16)
+            else:
+                binding.kv4_evict_tokens(c, mass, pos, el, mass=mass)
+        return out + [x[-n:].clone() for x in (cache, kc, vc, mass, mass16, pos, pos16)]
+
+    pages = b.device_pages(DEV)
+    pos = torch.zeros(n, hkv, PAGE, dtype=torch.int32, device=DEV)
+    near = [pool, k16, v16, score, score, pos, pos]
+    want = call(pages, *(x.clone() for x in near))
+    big = [torch.empty(far + n, *x.shape[1:], dtype=x.dtype, device=DEV) for x in near]
+    for x, y in zip(big, near):
+        x[far:] = y
+    assert all(x.numel() * x.element_size() > 1 << 32 for x in big[:3])
+    for got, w in zip(call(pages + far, *big), want):
+        assert torch.equal(got.view(torch.int16) if got.dtype == torch.bfloat16 else got,
+                           w.view(torch.int16) if w.dtype == torch.bfloat16 else w)

@@ -279,7 +279,7 @@ def test_tensors_of_another_device(monkeypatch):
     lay, q, k = b.layout4(cache), b.q().to(DEV), b.normal(b.rows, b.hkv, b.d).to(DEV)
     slots = torch.zeros(b.num_pages, b.hkv, PAGE, device=DEV)
     el = binding.make_evict_layout(cache, [6], [3], b.page_indptr, b.device_pages(DEV))
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(binding, "_current_device", lambda: 1)
     for call in (lambda: binding.kv4_append(k, k, cache, lay), lambda: binding.kv4_read(cache, lay, k_out=k, v_out=k),
                  lambda: binding.kv4_attention(q, cache, lay),
                  lambda: binding.kv4_attention_mass(q, cache, torch.zeros(b.rows, b.hq, device=DEV), slots, lay),
@@ -325,3 +325,10 @@ def test_append_and_read_of_many_blocks(heads):
     assert torch.equal(both[0], both[1])
     kr, vr = binding.kv4_read(both[0], lay)
     assert torch.equal(kr, torch.cat([x for x, _ in one])) and torch.equal(vr, torch.cat([x for _, x in one]))
+
+
+@pytest.mark.parametrize("heads", [(32, 1, 64), (5, 1, 128)])
+def test_attention_of_other_groups(heads):
+    b = Batch([(700, 2, 5), (31, 1, 0), (0, 9, 0)], heads=heads)
+    q, pool = b.q(), b.pool4()
+    check_attention(*_attend(b, q, pool), *b.attention(q, pool), _score_size(b, q, pool))
