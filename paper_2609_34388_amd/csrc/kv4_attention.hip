@@ -27,10 +27,10 @@
 // Runs of a request's keys meet in fp32 in the workspace.
 //
 // Measured (query heads / KV heads / head size 32/8/128 unless said):
-// one token over 4097 keys 8.4 us + 4.8 of the merge, bound by the chain of its
+// one token over 4097 keys 8.3 us + 4.3 of the merge, bound by the chain of its
 // start, one key tile a wave, and its end; 16 requests of 1k to 8k keys with
-// branches 67 + 12 us; 48 of up to 6k keys, heads 16/4/64, 30 + 7 us; 40 of 8k to
-// 32k keys 525 + 25 us, 685 TFLOP/s of bf16 products at 2.0 GHz, to which the
+// branches 67 + 10 us; 48 of up to 6k keys, heads 16/4/64, 30 + 7 us; 40 of 8k to
+// 32k keys 530 + 22 us, 700 TFLOP/s of bf16 products at 2.0 GHz, to which the
 // chip's power limit takes the clock: vector instructions fill 52 % of the
 // cycles, products 38 %.  Codes read straight into registers measured the same
 // within 2 % at head size 128 and leave no registers for a second wave at 64.
@@ -446,17 +446,20 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void kv4_attn_kernel(Kv4
   else kv4_wave<D, 1, Plan>(a, rq, it, pair, np, wave / np, lds);
 }
 
-// Merge of the runs of split requests.  An item is (request, KV head, 32-column
-// tile, row v): 64 rows of 16 bytes, 4 dims of a column each.  PARTS 1: a wave an
-// item, four of the same tile a work group (of one wave they were bound by the
-// rate at which work groups start: 13.0 -> 11.6 us for 6700 items).  Else the
-// four waves share an item, wave j taking runs j, j + PARTS, ..., and meet in LDS.
+// Merge of the runs of split requests.  Rows of 16 bytes, 4 dims of a column
+// each, are counted by (request, KV head, 32-column tile, v); a wave has the 32
+// columns of a v, one half of the dims in each half-wave.  PARTS 1: a wave takes
+// kKv4MergeRows of a tile's v, in work groups of four waves (for 6700 of them 9.6 us;
+// with one v a wave, bound by the rate at which waves start, 11.6, in work groups
+// of one wave 13.0, with four v 10.5).  Else four waves share a v, wave j taking
+// runs j, j + PARTS, ..., and meet in LDS.
 template <int D, int PARTS, typename Plan>
-__global__ __launch_bounds__(kKv4MergeRows * kKv4MergeParts) void kv4_merge_kernel(Kv4AttnArgs a, Plan p) {
+__global__ __launch_bounds__(64 * kKv4MergeParts) void kv4_merge_kernel(Kv4AttnArgs a, Plan p) {
   constexpr int DT = D / 32;
   __shared__ float st[PARTS > 1 ? (PARTS - 1) * 6 * 64 : 1];
   const int part = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int item = PARTS > 1 ? xcd_item(gridDim.x) : xcd_item(gridDim.x) * kKv4MergeParts + part;
+  constexpr int ROWS = PARTS > 1 ? 1 : kKv4MergeRows;  // row numbers of a wave
+  const int item = PARTS > 1 ? xcd_item(gridDim.x) : (xcd_item(gridDim.x) * kKv4MergeParts + part) * ROWS;
   if (item >= p.total_comb) return;
   const int r = find_request(p, item, true);
   const auto rq = p.req[r];
@@ -487,34 +490,48 @@ __global__ __launch_bounds__(kKv4MergeRows * kKv4MergeParts) void kv4_merge_kern
   const int lane = threadIdx.x & 63, lc = lane & 31, lh = lane >> 5;
   const int col = tile * 32 + lc;
 
-  float m = kNegInf, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  auto absorb = [&](float mc, float lc_, const float (&oc)[4]) {
-    if (mc == kNegInf) return;  // no key of that run is visible to the column
-    const float m_new = fmaxf(m, mc);
-    const float a0 = __builtin_amdgcn_exp2f((m - m_new) * a.scale_log2);
-    const float a1 = __builtin_amdgcn_exp2f((mc - m_new) * a.scale_log2);
-    l = l * a0 + lc_ * a1;
+  float m = kNegInf, l = 0.f, o[ROWS][4] = {};
+  // Joins N states; those of runs that the column sees no key of weigh nothing.
+  auto absorb = [&](const auto& mc, const auto& lc_, const auto& oc) {
+    constexpr int N = sizeof(lc_) / sizeof(lc_[0]);
+    float m_new = m, w[N];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = o[e] * a0 + oc[e] * a1;
+    for (int u = 0; u < N; ++u) m_new = fmaxf(m_new, mc[u]);
+    const float a0 = m == kNegInf ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * a.scale_log2);
+    l *= a0;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      w[u] = mc[u] == kNegInf ? 0.f : __builtin_amdgcn_exp2f((mc[u] - m_new) * a.scale_log2);
+      l += w[u] * lc_[u];
+    }
+#pragma unroll
+    for (int r4 = 0; r4 < ROWS; ++r4)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        o[r4][e] *= a0;
+#pragma unroll
+        for (int u = 0; u < N; ++u) o[r4][e] += w[u] * oc[u][r4][e];
+      }
     m = m_new;
   };
   if (col < M) {
-    for (int c0 = PARTS > 1 ? part : 0; c0 < nch; c0 += 8 * PARTS) {
-      float2 ml[8];
-      float4 x[8];
+    constexpr int N = 8;  // runs in flight
+    for (int c0 = PARTS > 1 ? part : 0; c0 < nch; c0 += N * PARTS) {
+      float mc[N], lc_[N], x[N][ROWS][4];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int c = c0 + u * PARTS;
-        ml[u] = make_float2(kNegInf, 0.f);
-        if (c < nch) {
-          const size_t t0 = base + (size_t)c * stride;
-          ml[u] = *(const float2*)(a.part_ml + 2 * (t0 + lc));
-          x[u] = *(const float4*)(a.part_o + t0 * D + (v * 64 + lane) * 4);
+      for (int u = 0; u < N; ++u) {
+        const int c = min(c0 + u * PARTS, nch - 1);  // past the last: that one again, for nothing
+        const size_t t0 = base + (size_t)c * stride;
+        const float2 ml = *(const float2*)(a.part_ml + 2 * (t0 + lc));
+        mc[u] = c0 + u * PARTS < nch ? ml.x : kNegInf;
+        lc_[u] = ml.y;
+#pragma unroll
+        for (int r4 = 0; r4 < ROWS; ++r4) {
+          const float4 y = *(const float4*)(a.part_o + t0 * D + ((v + r4) * 64 + lane) * 4);
+          x[u][r4][0] = y.x, x[u][r4][1] = y.y, x[u][r4][2] = y.z, x[u][r4][3] = y.w;
         }
       }
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (c0 + u * PARTS < nch) absorb(ml[u].x, ml[u].y, {x[u].x, x[u].y, x[u].z, x[u].w});
+      absorb(mc, lc_, x);
     }
   }
   if (PARTS > 1) {
@@ -523,24 +540,26 @@ __global__ __launch_bounds__(kKv4MergeRows * kKv4MergeParts) void kv4_merge_kern
       s[0] = m;
       s[64] = l;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[(2 + e) * 64] = o[e];
+      for (int e = 0; e < 4; ++e) s[(2 + e) * 64] = o[0][e];
     }
     __syncthreads();
     if (part > 0) return;
 #pragma unroll
     for (int j = 0; j < PARTS - 1; ++j) {
       const float* s = st + j * 6 * 64 + lane;
-      absorb(s[0], s[64], {s[2 * 64], s[3 * 64], s[4 * 64], s[5 * 64]});
+      const float mc[1] = {s[0]}, lc_[1] = {s[64]}, x[1][1][4] = {{{s[2 * 64], s[3 * 64], s[4 * 64], s[5 * 64]}}};
+      if constexpr (PARTS > 1) absorb(mc, lc_, x);
     }
   }
   if (col >= M) return;
   const int tok = row_of(a, col), hh = col - tok * g;
   const size_t orow = (size_t)(rq.q_start + tok) * a.hq + hk * g + hh;
   const float inv = 1.f / l;
-  u32x2 w;
-  w[0] = pack_bf16x2(o[0] * inv, o[1] * inv);
-  w[1] = pack_bf16x2(o[2] * inv, o[3] * inv);
-  *(u32x2*)(a.out + orow * D + 8 * DT * (v / DT) + 4 * DT * lh + 4 * (v % DT)) = w;
+#pragma unroll
+  for (int r4 = 0; r4 < ROWS; ++r4) {
+    const u32x2 w = {pack_bf16x2(o[r4][0] * inv, o[r4][1] * inv), pack_bf16x2(o[r4][2] * inv, o[r4][3] * inv)};
+    *(u32x2*)(a.out + orow * D + 8 * DT * ((v + r4) / DT) + 4 * DT * lh + 4 * ((v + r4) % DT)) = w;
+  }
   if (a.lse != nullptr && v == 0 && lh == 0) a.lse[orow] = m * a.sm_scale + __logf(l);
 }
 
@@ -549,12 +568,14 @@ hipError_t launch_impl(const Kv4AttnArgs& a, const Plan& p, hipStream_t stream) 
   hipLaunchKernelGGL((kv4_attn_kernel<D, Plan>), dim3(p.grid_items), dim3(kThreads), 0, stream, a, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.total_comb == 0) return e;
-  if (p.max_chunks > 8 && p.grid_comb <= 1024)  // many runs, and few enough items to be bound by latency
+  // Many runs, and few enough rows to be bound by latency: one token over 26 runs
+  // takes 4.3 us so, 10.7 with a wave for each row; 40 long requests 75 and 22.
+  if (p.max_chunks > 8 && p.grid_comb <= 1024)
     hipLaunchKernelGGL((kv4_merge_kernel<D, kKv4MergeParts, Plan>), dim3(p.grid_comb),
-                       dim3(kKv4MergeRows * kKv4MergeParts), 0, stream, a, p);
+                       dim3(64 * kKv4MergeParts), 0, stream, a, p);
   else
-    hipLaunchKernelGGL((kv4_merge_kernel<D, 1, Plan>), dim3((p.total_comb / kKv4MergeParts + 7) / 8 * 8),
-                       dim3(kKv4MergeRows * kKv4MergeParts), 0, stream, a, p);
+    hipLaunchKernelGGL((kv4_merge_kernel<D, 1, Plan>), dim3((p.total_comb / (kKv4MergeRows * kKv4MergeParts) + 8) / 8 * 8),
+                       dim3(64 * kKv4MergeParts), 0, stream, a, p);
   return hipGetLastError();
 }
 
