@@ -31,8 +31,8 @@
 // start, one key tile a wave, and its end; 16 requests of 1k to 8k keys with
 // branches 67 + 10 us; 48 of up to 6k keys, heads 16/4/64, 30 + 7 us; 40 of 8k to
 // 32k keys 530 + 22 us, 700 TFLOP/s of bf16 products at 2.0 GHz, to which the
-// chip's power limit takes the clock: vector instructions fill 52 % of the
-// cycles, products 38 %.  Codes read straight into registers measured the same
+// chip's power limit takes the clock: vector instructions fill 56 % of the
+// cycles, products 41 %.  Codes read straight into registers measured the same
 // within 2 % at head size 128 and leave no registers for a second wave at 64.
 #include "cache_internal.h"
 #include "kv4_device.h"
