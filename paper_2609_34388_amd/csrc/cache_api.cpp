@@ -121,7 +121,8 @@ Kv4Cols kv4_cols(const rg_attn_layout* L, int r) {
 // next, took 73 us where these runs take 67: a second start costs more than even
 // lengths give.
 // kKv4Least is two steps of a wave on one tile, or one on four: one token over
-// 4097 keys takes 14.4 us with it, 16.4 with half of it, 14.6 with twice.
+// 4097 keys takes 12.5 us with it, 13.3 with three quarters of it, 12.6 with one
+// and a half.
 constexpr int kKv4Least = 32, kKv4Long = 4096;
 int kv4_target(const rg_attn_layout* L, int cus) {
   const int64_t slots = (int64_t)(L->head_dim == 64 ? 3 : 2) * cus;
@@ -177,7 +178,6 @@ rg_status plan_kv4(const rg_attn_layout* L, const rg_branch_layout* B, Kv4Plan<P
     std::memset(&p, 0, sizeof(p));
     p.num_req = cnt;
     p.chunk = target;
-    p.cols_per_group = kKv4Cols;
     int64_t items = 0, part = 0, comb = 0;
     for (int k = 0; k < cnt; ++k) {
       const int r = order[r0 + k];

@@ -10,7 +10,7 @@ namespace rg {
 // page that a request's rows touch and plan.chunk KV heads (1 .. kRowHeads).
 constexpr int kRowHeads = 4;
 struct Kv4RowArgs {
-  uint16_t* k;  // rows (appended: read, read back: written), or NULL
+  uint16_t* k;  // rows (appended: read, read back: written)
   uint16_t* v;
   int64_t k_stride, v_stride;  // elements
   uint8_t* cache;
