@@ -332,3 +332,26 @@ def test_attention_of_other_groups(heads):
     b = Batch([(700, 2, 5), (31, 1, 0), (0, 9, 0)], heads=heads)
     q, pool = b.q(), b.pool4()
     check_attention(*_attend(b, q, pool), *b.attention(q, pool), _score_size(b, q, pool))
+
+
+def test_append_and_read_of_many_requests():
+    """More requests than a launch takes, some without rows."""
+    b = Batch([(i % 37, i % 4, i % 3) for i in range(300)], heads=(2, 2, 64))
+    k, v = (b.normal(b.rows, b.hkv, b.d) for _ in range(2))
+    pool = np.full((b.num_pages, b.hkv, 17 * b.d), 0xff, dtype=np.uint8)
+    cache = dev(pool)
+    lay = b.layout4(cache)
+    binding.kv4_append(k.to(DEV), v.to(DEV), cache, lay)
+    assert (cache.cpu().numpy() == _append_reference(b, pool.copy(), k, v)).all()
+    kr, _ = binding.kv4_read(cache, lay)
+    code, s = ref.encode(ref.bf16_values(W.bf16_bits(k)))
+    assert (kr.double().cpu().numpy() == ref.decode(code, s)).all()
+
+
+@pytest.mark.parametrize("heads", [(8, 1, 64), (4, 2, 128)])
+def test_attention_of_a_prompt(heads):
+    """Many column groups: a prompt behind a short prefix, whole and in a batch."""
+    for requests in ([(100, 700, 0)], [(0, 333, 0), (50, 3, 2), (17, 400, 16)]):
+        b = Batch(requests, heads=heads)
+        q, pool = b.q(), b.pool4()
+        check_attention(*_attend(b, q, pool), *b.attention(q, pool), _score_size(b, q, pool))
