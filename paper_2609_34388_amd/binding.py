@@ -12,6 +12,7 @@ synchronising.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Dict, Optional, Tuple
@@ -648,6 +649,15 @@ def _here(*tensors: Optional[torch.Tensor]):
             raise ValueError(f"a tensor is on device {t.get_device()}, the current device is {here}")
 
 
+def _pool_of(stream):
+    """Where a call's own tensors come from: the memory pool of the stream that
+    uses them, not of one that may still have work on the same memory, or give it
+    away before the call has run."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
+
+
 def _rows(t: torch.Tensor, name: str, lay: _Layout) -> int:
     """Checks rows [rows, Hkv, D] (any row stride, heads contiguous) and returns the stride."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not torch.bfloat16:
@@ -681,8 +691,11 @@ def kv4_read(cache: torch.Tensor, layout: _Layout, *, k_out: Optional[torch.Tens
     """The tokens kv4_append writes for this layout, as bf16 rows (rg_kv4_read)."""
     _kv4(cache, layout.c.head_dim, layout.c.num_kv_heads, layout.c.num_pages)
     shape = (int(layout.q_indptr[-1]), layout.c.num_kv_heads, layout.c.head_dim)
-    k = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if k_out is None else k_out
-    v = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if v_out is None else v_out
+    k, v = k_out, v_out
+    if k is None or v is None:
+        with _pool_of(stream):
+            k = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if k is None else k
+            v = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if v is None else v
     ks, vs = _rows(k, "k_out", layout), _rows(v, "v_out", layout)
     _check_layout(layout, shape[0], k, v, cache)
     if shape[0]:
@@ -711,12 +724,13 @@ def kv4_attention(q: torch.Tensor, cache: torch.Tensor, layout: _Layout, branche
     _check_layout(layout, q.shape[0], q, cache, workspace)
     if branches is not None and branches.branch_indptr.shape[0] != layout.ctx_len.shape[0] + 1:
         raise ValueError("branch_indptr must have num_requests + 1 entries")
-    if out is None:
-        out = torch.empty_like(q)
+    if out is None or (lse is None and want_lse):
+        with _pool_of(stream):
+            out = torch.empty_like(q) if out is None else out
+            if lse is None and want_lse:
+                lse = torch.empty(q.shape[0], q.shape[1], dtype=torch.float32, device=q.device)
     if _dev(out, "out", torch.bfloat16).shape != q.shape:
         raise ValueError("out must have q's shape")
-    if lse is None and want_lse:
-        lse = torch.empty(q.shape[0], q.shape[1], dtype=torch.float32, device=q.device)
     if lse is not None and _dev(lse, "lse", torch.float32).shape != q.shape[:2]:
         raise ValueError("lse must be [rows, Hq]")
     _here(out, lse)
@@ -725,7 +739,8 @@ def kv4_attention(q: torch.Tensor, cache: torch.Tensor, layout: _Layout, branche
     if workspace is None:  # the call itself checks the size of one that is given
         need = kv4_attention_workspace_bytes(layout, branches)
         if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            with _pool_of(stream):
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(_lib().rg_kv4_attention(ctypes.byref(layout.c), ctypes.byref(branches.c) if branches else None, q.data_ptr(),
                                    cache.data_ptr(), out.data_ptr(), _ptr(lse), _ptr(workspace), ws_bytes,
@@ -825,7 +840,8 @@ def evict_workspace_bytes(layout: _EvictLayout) -> int:
     return int(n.value)
 
 
-def _evict_args(score, positions, layout: _EvictLayout, mass, workspace):
+def _evict_args(score, positions, layout: _EvictLayout, mass, workspace, stream):
+    """The arguments behind the caches', and the workspace, which has to live until the call is made."""
     pool = (layout.c.num_pages, layout.c.num_kv_heads)
     _slot_pool(score, "score", torch.float32, *pool)
     _slot_pool(positions, "positions", torch.int32, *pool)
@@ -833,9 +849,10 @@ def _evict_args(score, positions, layout: _EvictLayout, mass, workspace):
         _slot_pool(mass, "mass", torch.float32, *pool)
     _here(score, positions, mass, workspace, layout.page_indices)
     if workspace is None:
-        workspace = torch.empty(evict_workspace_bytes(layout), dtype=torch.uint8, device=score.device)
+        with _pool_of(stream):
+            workspace = torch.empty(evict_workspace_bytes(layout), dtype=torch.uint8, device=score.device)
     return (score.data_ptr(), _ptr(mass), positions.data_ptr(), workspace.data_ptr(),
-            workspace.numel() * workspace.element_size())
+            workspace.numel() * workspace.element_size()), workspace
 
 
 def evict_tokens(k_cache: torch.Tensor, v_cache: torch.Tensor, score: torch.Tensor, positions: torch.Tensor,
@@ -851,7 +868,7 @@ def evict_tokens(k_cache: torch.Tensor, v_cache: torch.Tensor, score: torch.Tens
             tuple(v_cache.shape) != (c.num_pages, c.num_kv_heads, c.head_dim, 16):
         raise ValueError("k_cache must be [pages, Hkv, 16, D] and v_cache [pages, Hkv, D, 16] of the layout's sizes")
     _here(k_cache, v_cache)
-    args = _evict_args(score, positions, layout, mass, workspace)
+    args, workspace = _evict_args(score, positions, layout, mass, workspace, stream)
     _check(_lib().rg_evict_tokens(ctypes.byref(c), k_cache.data_ptr(), v_cache.data_ptr(), *args, _stream(stream)),
            "rg_evict_tokens")
 
@@ -863,5 +880,5 @@ def kv4_evict_tokens(cache: torch.Tensor, score: torch.Tensor, positions: torch.
     c = layout.c
     _kv4(cache, c.head_dim, c.num_kv_heads, c.num_pages)
     _here(cache)
-    args = _evict_args(score, positions, layout, mass, workspace)
+    args, workspace = _evict_args(score, positions, layout, mass, workspace, stream)
     _check(_lib().rg_kv4_evict_tokens(ctypes.byref(c), cache.data_ptr(), *args, _stream(stream)), "rg_kv4_evict_tokens")

@@ -522,3 +522,36 @@ def test_pools_past_32_bits():
     for got, w in zip(call(pages + far, *big), want):
         assert torch.equal(got.view(torch.int16) if got.dtype == torch.bfloat16 else got,
                            w.view(torch.int16) if w.dtype == torch.bfloat16 else w)
+
+
+def test_own_tensors_on_another_stream():
+    """Calls on a stream of their own that make their outputs and workspaces,
+    while the current stream takes and fills memory."""
+    b = Batch([(6000, 4, 3), (40, 1, 0)], heads=(8, 2, 128))
+    q, pool0 = b.q().to(DEV), dev(b.pool4())
+    L, keep = b.T, [4000, 20]
+
+    def calls(stream):
+        cache = pool0.clone()
+        mass = torch.zeros(b.num_pages, b.hkv, PAGE, device=DEV)
+        pos = torch.zeros(b.num_pages, b.hkv, PAGE, dtype=torch.int32, device=DEV)
+        lay = b.layout4(cache)
+        el = binding.make_evict_layout(cache, L, keep, b.page_indptr, b.device_pages(DEV), recent=8)
+        if stream is not None:
+            torch.cuda.synchronize()
+        out, lse = binding.kv4_attention(q, cache, lay, stream=stream)
+        noise = [torch.full((n,), 0x5a, dtype=torch.uint8, device=DEV) for n in (1 << 20, 1 << 22, 1 << 24, 1 << 25)]
+        binding.kv4_attention_mass(q, cache, lse, mass, lay, stream=stream)
+        del noise
+        binding.kv4_evict_tokens(cache, mass, pos, el, mass=mass, stream=stream)
+        noise = [torch.full((n,), 0x5a, dtype=torch.uint8, device=DEV) for n in (1 << 16, 1 << 18, 1 << 20, 1 << 22)]
+        k, v = binding.kv4_read(cache, lay, stream=stream)
+        torch.cuda.synchronize()
+        return out, lse, mass, pos, cache, k, v
+
+    want = calls(None)
+    s = torch.cuda.Stream()
+    for stream in (s, s.cuda_stream, s, s):
+        for got, w in zip(calls(stream), want):
+            assert torch.equal(got.view(torch.int16) if got.dtype == torch.bfloat16 else got,
+                               w.view(torch.int16) if w.dtype == torch.bfloat16 else w)
