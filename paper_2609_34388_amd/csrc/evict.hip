@@ -62,6 +62,15 @@ __device__ __forceinline__ uint32_t scan64(uint32_t x) {
   return x;
 }
 
+// Sum of the counts of the waves before `wave`, and of all: one read and a scan,
+// where a loop over the waves would wait for each of its reads.
+__device__ __forceinline__ uint2 before_wave(const uint32_t (&counts)[kWaves], int wave) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t upto = scan64(lane < kWaves ? counts[lane] : 0u);
+  const uint32_t before = __builtin_amdgcn_readlane(upto, wave > 0 ? wave - 1 : 0);
+  return make_uint2(wave > 0 ? before : 0u, __builtin_amdgcn_readlane(upto, kWaves - 1));
+}
+
 // Lanes of a mask before this one, added to `x`.
 __device__ __forceinline__ uint32_t count_below(uint64_t mask, uint32_t x) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, x));
@@ -75,7 +84,7 @@ template <int KW>
 __global__ __launch_bounds__(kEvictThreads, 8) void evict_select_kernel(EvictArgs a, EvictPlan p) {
   __shared__ uint32_t hist[kBins];  // later the lists of holes and movers, where they fit
   __shared__ uint32_t s_wave[kWaves], s_word, s_left, s_in;
-  __shared__ uint32_t s_count[kWaves][3];
+  __shared__ uint32_t s_count[3][kWaves];
   const int r = (int)blockIdx.x / a.hkv, hk = (int)blockIdx.x % a.hkv;
   const EvictReq q = p.req[r];
   const int L = q.ctx, keep = q.keep, tid = threadIdx.x, lane = tid & 63;
@@ -164,8 +173,7 @@ __global__ __launch_bounds__(kEvictThreads, 8) void evict_select_kernel(EvictArg
     const uint32_t upto = scan64(b0 + b1);
     if (lane == 63) s_wave[wave] = upto;
     __syncthreads();
-    uint32_t before = upto - b0 - b1;
-    for (int w = 0; w < wave; ++w) before += s_wave[w];
+    const uint32_t before = upto - b0 - b1 + before_wave(s_wave, wave).x;
     if (before < left && left <= before + b0 + b1) {
       const bool second = left > before + b0;
       s_word = (uint32_t)(kBins - 1 - 2 * tid) - second;
@@ -187,9 +195,9 @@ __global__ __launch_bounds__(kEvictThreads, 8) void evict_select_kernel(EvictArg
   if (left < in_prefix) {
     uint32_t ties = 0;
     each([&](int, uint32_t u, bool in) { ties += __popcll(__ballot(in && (u & mask) == prefix)); });
-    if (lane == 0) s_count[wave][0] = ties;
+    if (lane == 0) s_count[0][wave] = ties;
     __syncthreads();
-    for (int w = 0; w < wave; ++w) tie0 += s_count[w][0];
+    tie0 = before_wave(s_count[0], wave).x;
   }
   // Lanes whose slot is kept; `tie` counts the ties so far.
   auto kept_lanes = [&](uint32_t u, bool in, uint32_t& tie) -> uint64_t {
@@ -220,15 +228,14 @@ __global__ __launch_bounds__(kEvictThreads, 8) void evict_select_kernel(EvictArg
     movers += (uint32_t)__popcll(m & ~low);
   });
   if (lane == 0) {
-    s_count[wave][1] = holes;
-    s_count[wave][2] = movers;
+    s_count[1][wave] = holes;
+    s_count[2][wave] = movers;
   }
   __syncthreads();
-  uint32_t hole0 = 0, mover0 = 0, count = 0;
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) hole0 += s_count[w][1], mover0 += s_count[w][2];
-    count += s_count[w][2];
-  }
+  uint32_t hole0 = before_wave(s_count[1], wave).x;
+  const uint2 moves = before_wave(s_count[2], wave);
+  uint32_t mover0 = moves.x;
+  const uint32_t count = moves.y;
   const MoveList list = move_list(a, q, hk);
   const bool near = count <= kBins / 2;  // the lists fit LDS: no trip to memory and back
   auto visit = [&](int i, uint64_t m) {
