@@ -14,10 +14,11 @@
 // part of the slots: ties are taken from the lowest slot on, holes and movers get
 // their ranks from wave ballots.  It writes for every kept slot which token it
 // takes, if any.  Bound by latency: a few thousand tokens give one compute unit
-// work that 255 others cannot share.  One request of 4128 tokens 12.5 us, 16 of 1k
-// to 8k 14.5, 40 of 8k to 32k 51 (8 heads each; the start 1.3 us, the first bits 2.3,
-// each later pass 1.3 to 1.6, ranks and lists 3).  Comparing the last few hundred
-// candidates each with all, instead of further bits, took 2.0 us.
+// work that 255 others cannot share.  One request of 4128 tokens 11.0 us, 16 of 1k
+// to 8k 13.5, 40 of 8k to 32k 51 (8 heads each; the start 1.2 us, the first bits 1.8,
+// each later pass 1.1, ranks and lists 4).  Comparing the last few hundred
+// candidates each with all, instead of further bits, took 2.0 us; copies of the
+// bins, so that fewer lanes meet in one, changed nothing.
 //
 // move: a wave per page of the kept slots, which writes their positions and
 // fills the page's holes: mass and K rows as they are.  In V, where a 16-byte
@@ -79,7 +80,7 @@ __device__ __forceinline__ uint32_t count_below(uint64_t mask, uint32_t x) {
 // KW: words of a thread in registers; slots past them are read again in each pass.
 // 64 registers let two work groups share a compute unit (40 long requests: 59 us
 // where they do not, 51).  As few words as the longest request needs: every step
-// is in the code as often as there are words (4128 tokens: 12.5 us with 8, 16.5 with 32).
+// is in the code as often as there are words (4128 tokens: 12.3 us with 8, 16.5 with 32).
 template <int KW>
 __global__ __launch_bounds__(kEvictThreads, 8) void evict_select_kernel(EvictArgs a, EvictPlan p) {
   __shared__ uint32_t hist[kBins];  // later the lists of holes and movers, where they fit

@@ -19,11 +19,12 @@
 //
 // Measured (heads 32/8/128): 16 requests' steps over 1k to 8k bf16 keys 34 us (144 MB,
 // 4.2 TB/s); 40 over 8k to 32k 4-bit keys 150 us (532 MB, 3.6 TB/s, where a kernel
-// that only reads reaches 4.0); two prompts of 2048 and 1555 rows 109 us, 77 of
+// that only reads reaches 4.0); two prompts of 2048 and 1555 rows 106 us, 77 of
 // products at a large product's rate and 56 of exponentials and sums, which overlap
 // little.  Prompts through mass_kernel, Q read from LDS by each key tile anew, took
 // 406 us; the next tile's products placed between a wave's exponentials, at two
-// waves a SIMD, took 157 where the plain order then took 135.
+// waves a SIMD, took 157 where the plain order then took 135; 32, 96 or 128 keys a
+// work group take 146, 106 and 110.
 #include "cache_internal.h"
 #include "kv4_device.h"
 
@@ -319,8 +320,14 @@ __global__ __launch_bounds__(kThreads, 3) void mass_rows_kernel(MassArgs a, Attn
       const float4 x = *(const float4*)(lse2 + 8 * i4 + 4 * lh);
       ls[4 * i4] = x.x, ls[4 * i4 + 1] = x.y, ls[4 * i4 + 2] = x.z, ls[4 * i4 + 3] = x.w;
     }
+    // A tile's sum by itself: thousands of rows one by one would each round at the
+    // size of the whole.
 #pragma unroll
-    for (int s = 0; s < 2; ++s) add_weights(a, it, sc[s], ls, 32 * t, it.kbeg + 32 * s, w[s]);
+    for (int s = 0; s < 2; ++s) {
+      float sum = 0.f;
+      add_weights(a, it, sc[s], ls, 32 * t, it.kbeg + 32 * s, sum);
+      w[s] += sum;
+    }
   }
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
