@@ -147,7 +147,7 @@ int kv4_target(const rg_attn_layout* L, int cus) {
   auto fit = [&](int64_t rounds) {  // the least target whose items fit the rounds
     for (int64_t t = std::max<int64_t>(kKv4Least, work / (rounds * slots));; t += 1 + t / 16) {
       int64_t items = 0;
-      for (const Group& q : groups) items += q.count * kv4_runs(q.T, q.tiles, (int)std::min<int64_t>(t, INT32_MAX)).count;
+      for (const Group& q : groups) items += q.count * kv4_run_count(q.T, q.tiles, (int)std::min<int64_t>(t, INT32_MAX));
       if (items <= std::max(least, rounds * slots)) return t;
     }
   };
@@ -159,17 +159,16 @@ template <typename Plan, int MaxReq>
 rg_status plan_kv4(const rg_attn_layout* L, const rg_branch_layout* B, Kv4Plan<Plan>& fp) {
   const int R = L->num_requests, hkv = L->num_kv_heads;
   const int target = kv4_target(L, device_cus());
-  auto runs_of = [&](int r, int tiles) {
-    return kv4_runs(L->ctx_len[r] + (L->q_indptr[r + 1] - L->q_indptr[r]), tiles, target);
-  };
+  auto keys_of = [&](int r) { return L->ctx_len[r] + (L->q_indptr[r + 1] - L->q_indptr[r]); };
+  auto runs_of = [&](int r, int tiles) { return kv4_run_count(keys_of(r), tiles, target); };
   // Costliest work items first.
   std::vector<int> order(R);
   std::iota(order.begin(), order.end(), 0);
   std::vector<int64_t> cost(R);
   for (int r = 0; r < R; ++r) {
     const Kv4Cols c = kv4_cols(L, r);
-    if (c.full) cost[r] = (int64_t)runs_of(r, kKv4Waves).keys * kv4_rate(kKv4Waves);
-    if (c.rest) cost[r] = std::max(cost[r], (int64_t)runs_of(r, c.rest).keys * kv4_rate(c.rest));
+    if (c.full) cost[r] = (int64_t)kv4_run_keys(keys_of(r), runs_of(r, kKv4Waves)) * kv4_rate(kKv4Waves);
+    if (c.rest) cost[r] = std::max(cost[r], (int64_t)kv4_run_keys(keys_of(r), runs_of(r, c.rest)) * kv4_rate(c.rest));
   }
   std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return cost[x] > cost[y]; });
   for (int r0 = 0; r0 < R; r0 += MaxReq) {
@@ -194,7 +193,7 @@ rg_status plan_kv4(const rg_attn_layout* L, const rg_branch_layout* B, Kv4Plan<P
       if (n == 0) continue;
       const Kv4Cols c = kv4_cols(L, r);
       auto add = [&](int tiles, int64_t groups) {
-        const int64_t nch = runs_of(r, tiles).count;
+        const int64_t nch = runs_of(r, tiles);
         items += hkv * groups * nch;
         if (nch == 1) return;
         p.max_chunks = std::max<int32_t>(p.max_chunks, (int32_t)nch);
@@ -241,16 +240,14 @@ rg_status with_kv4_plan(const rg_attn_layout* L, const rg_branch_layout* B, F f)
   return RG_ERR_WORKSPACE;
 }
 
-// Query heads a KV head, and the factor and shift that divide by them: with
-// 2^l >= g, g_mul = ceil(2^(31 + l) / g) fits 32 bits and g_mul g exceeds
-// 2^(31 + l) by e < g, so col g_mul / 2^(31 + l) exceeds col / g by
-// col e / (g 2^(31 + l)) < 1 / g for every col below 2^31: the floors agree.
-template <typename Args>
-void set_group(Args& a) {
-  a.g = a.hq / a.hkv;
-  a.g_shift = 0;
-  while ((1ll << a.g_shift) < a.g) ++a.g_shift;
-  a.g_mul = (uint32_t)(((uint64_t(1) << (31 + a.g_shift)) + a.g - 1) / a.g);
+// The factor and shift that divide by d (quotient in kv4_device.h): with 2^l >= d,
+// mul = ceil(2^(31 + l) / d) fits 32 bits and mul d exceeds 2^(31 + l) by e < d, so
+// x mul / 2^(31 + l) exceeds x / d by x e / (d 2^(31 + l)) < 1 / d for every x below
+// 2^31: the floors agree.
+void set_divisor(int32_t d, uint32_t& mul, int32_t& shift) {
+  shift = 0;
+  while ((1ll << shift) < d) ++shift;
+  mul = (uint32_t)(((uint64_t(1) << (31 + shift)) + d - 1) / d);
 }
 
 float softmax_scale(const rg_attn_layout* L) {
@@ -276,7 +273,8 @@ rg_status run_mass(const rg_attn_layout* L, const uint16_t* q, const void* keys,
   a.page_indices = L->page_indices;
   a.hq = L->num_q_heads;
   a.hkv = L->num_kv_heads;
-  set_group(a);
+  a.g = a.hq / a.hkv;
+  set_divisor(a.g, a.g_mul, a.g_shift);
   a.scale_log2 = softmax_scale(L) * 1.4426950408889634f;
   a.decay = decay;
   // A request without query rows need not own pages for its context.
@@ -438,7 +436,9 @@ rg_status rg_kv4_attention(const rg_attn_layout* layout, const rg_branch_layout*
     a.part_ml = fp.ws_bytes ? reinterpret_cast<float*>(static_cast<char*>(ws) + fp.ml_offset) : nullptr;
     a.hq = layout->num_q_heads;
     a.hkv = layout->num_kv_heads;
-    set_group(a);
+    a.g = a.hq / a.hkv;
+    set_divisor(a.g, a.g_mul, a.g_shift);
+    set_divisor(a.hkv, a.hkv_mul, a.hkv_shift);
     a.sm_scale = softmax_scale(layout);
     a.scale_log2 = a.sm_scale * 1.4426950408889634f;
     for (const auto& p : fp.launches)

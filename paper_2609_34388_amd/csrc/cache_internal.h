@@ -31,15 +31,16 @@ constexpr int kKv4MergeParts = 4;                  // waves of a work group of t
 // the two wave pairs one has a single tile and waits for the other).
 __host__ __device__ inline int kv4_rate(int tiles) { return tiles == 1 ? 6 : tiles == 2 ? 9 : tiles == 3 ? 15 : 16; }
 // Runs that the T keys of such a group are cut into, for items of at most
-// `target` units, and the keys of each: all but the last alike.
-struct Kv4Runs {
-  int count, keys;
-};
-__host__ __device__ inline Kv4Runs kv4_runs(int T, int tiles, int target) {
+// `target` units, and the keys of a run: all but the last alike.
+__host__ __device__ inline int kv4_run_count(int T, int tiles, int target) {
   const uint32_t steps = ((uint32_t)T + 31) / 32, rate = kv4_rate(tiles);
   const uint32_t most = (uint32_t)target > rate ? (uint32_t)target / rate : 1;  // steps of a run at most
   const uint32_t n = (steps + most - 1) / most, each = (steps + n - 1) / n;
-  return {(int)((steps + each - 1) / each), (int)(32 * each)};
+  return (int)((steps + each - 1) / each);
+}
+__host__ __device__ inline int kv4_run_keys(int T, int count) {
+  const uint32_t steps = ((uint32_t)T + 31) / 32;
+  return (int)(32 * ((steps + count - 1) / count));
 }
 struct Kv4AttnArgs {
   const uint16_t* q;
@@ -50,8 +51,8 @@ struct Kv4AttnArgs {
   float* part_o;   // per 32-column tile: 32 x D fp32 sums, 16-byte rows lane-interleaved
   float* part_ml;  // [partial columns][2] (running maximum of raw scores, sum)
   int32_t hq, hkv, g;
-  uint32_t g_mul;  // row_of
-  int32_t g_shift;
+  uint32_t g_mul, hkv_mul;  // quotient by g, by hkv
+  int32_t g_shift, hkv_shift;
   float sm_scale, scale_log2;
 };
 hipError_t launch_kv4_attention(const Kv4AttnArgs& a, const AttnPlan& p, int head_dim, hipStream_t stream);
@@ -78,7 +79,7 @@ struct MassArgs {
   const int32_t* page_indices;
   int32_t hq, hkv, g;
   float scale_log2, decay;
-  uint32_t g_mul;  // row_of
+  uint32_t g_mul;  // quotient by g
   int32_t g_shift;
 };
 hipError_t launch_mass(const MassArgs& a, const AttnPlan& p, int head_dim, bool kv4, hipStream_t stream);

@@ -413,31 +413,33 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void kv4_attn_kernel(Kv4
   it.n = rq.nv & 0xffff;
   it.L = rq.ctx;
   it.M = it.n * g;
-  // Items of the full column groups (groups, then KV heads, then runs), then
-  // those of the last one; their partials lie in the same order.
+  // Items of the full column groups (groups, then runs, then KV heads), then those
+  // of the last one; their partials lie in the same order.  The last one's runs
+  // follow from the number of items: an integer division here costs 0.16 us, and an
+  // item of one token's batch lasts 7.
   const int T = it.L + it.n;
   const int tiles = (it.M + 31) / 32, full = tiles / kKv4Waves;
-  uint32_t local = item - rq.item_start;
+  int local = item - rq.item_start;
   it.nct = kKv4Waves;
   it.tile0 = 0;
+  it.nch = 0;
   it.part = rq.part_start;
-  Kv4Runs runs = {0, 0};
   if (full > 0) {
-    runs = kv4_runs(T, it.nct, p.chunk);
-    const uint32_t group = (uint32_t)a.hkv * runs.count;  // items of a column group
-    const uint32_t group0 = min(local / group, (uint32_t)full);
+    it.nch = kv4_run_count(T, kKv4Waves, p.chunk);
+    const int group = a.hkv * it.nch;  // items of a column group
+    const int group0 = min((int)((uint32_t)local / (uint32_t)group), full);
     local -= group0 * group;
     it.tile0 = group0 * kKv4Waves;
-    if (runs.count > 1) it.part += it.tile0 * 32 * group;
+    if (it.nch > 1) it.part += it.tile0 * 32 * group;
   }
   if (it.tile0 == full * kKv4Waves) {
     it.nct = tiles - it.tile0;
-    runs = kv4_runs(T, it.nct, p.chunk);
+    it.nch = quotient(p.req[r + 1].item_start - rq.item_start, a.hkv_mul, a.hkv_shift) - full * it.nch;
   }
-  it.nch = runs.count;
-  it.hk = local / (uint32_t)runs.count;
-  it.kbeg = (local - it.hk * runs.count) * runs.keys;
-  it.kend = min(T, it.kbeg + runs.keys);
+  const int run = quotient(local, a.hkv_mul, a.hkv_shift), keys = kv4_run_keys(T, it.nch);
+  it.hk = local - run * a.hkv;
+  it.kbeg = run * keys;
+  it.kend = min(T, it.kbeg + keys);
   if (it.nch > 1) it.part += local * it.nct * 32;
 
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -469,24 +471,26 @@ __global__ __launch_bounds__(64 * kKv4MergeParts) void kv4_merge_kernel(Kv4AttnA
   int local = item - rq.comb_start;
   const int v = local % (4 * DT);
   local /= 4 * DT;
-  const int split = kv4_runs(T, kKv4Waves, p.chunk).count > 1 ? full * kKv4Waves : 0;  // tiles of the former
+  int nch = full > 0 ? kv4_run_count(T, kKv4Waves, p.chunk) : 0;
+  const int split = nch > 1 ? full * kKv4Waves : 0;  // tiles of the former
   int nct = kKv4Waves, tile, hk;
   size_t base = rq.part_start;
   if (local < split * a.hkv) {
-    tile = local / a.hkv;
-    hk = local % a.hkv;
+    tile = quotient(local, a.hkv_mul, a.hkv_shift);
+    hk = local - tile * a.hkv;
   } else {
     local -= split * a.hkv;
     nct = tiles - full * kKv4Waves;
-    tile = full * kKv4Waves + local / a.hkv;
-    hk = local % a.hkv;
-    if (split) base += (size_t)split * 32 * a.hkv * kv4_runs(T, kKv4Waves, p.chunk).count;
+    tile = quotient(local, a.hkv_mul, a.hkv_shift);
+    hk = local - tile * a.hkv;
+    tile += full * kKv4Waves;
+    if (split) base += (size_t)split * 32 * a.hkv * nch;
+    nch = quotient(p.req[r + 1].item_start - rq.item_start, a.hkv_mul, a.hkv_shift) - full * nch;
   }
-  const int nch = kv4_runs(T, nct, p.chunk).count;
   const int tile0 = tile / kKv4Waves * kKv4Waves;  // of its group
   if (nct == kKv4Waves) base += (size_t)tile0 * 32 * a.hkv * nch;
-  base += (size_t)hk * nch * nct * 32 + (size_t)(tile - tile0) * 32;
-  const size_t stride = (size_t)nct * 32;  // partial columns from run to run
+  base += (size_t)hk * nct * 32 + (size_t)(tile - tile0) * 32;
+  const size_t stride = (size_t)a.hkv * nct * 32;  // partial columns from run to run
   const int lane = threadIdx.x & 63, lc = lane & 31, lh = lane >> 5;
   const int col = tile * 32 + lc;
 

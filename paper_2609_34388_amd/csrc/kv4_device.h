@@ -47,10 +47,15 @@ __device__ __forceinline__ uint32_t encode8(u32x4 x, float scale) {
   return c;
 }
 
-// Query row of a column, col / g: exact below 2^31 (set_group in cache_api.cpp).
+// x over the divisor that the factor and shift stand for: exact below 2^31
+// (set_divisor in cache_api.cpp).
+__device__ __forceinline__ int quotient(int x, uint32_t mul, int shift) {
+  return (int)(__umulhi(2u * (uint32_t)x, mul) >> shift);
+}
+// Query row of a column.
 template <typename Args>
 __device__ __forceinline__ int row_of(const Args& a, int col) {
-  return (int)(__umulhi(2u * (uint32_t)col, a.g_mul) >> a.g_shift);
+  return quotient(col, a.g_mul, a.g_shift);
 }
 
 }  // namespace
