@@ -627,26 +627,27 @@ def make_kv4_layout(num_q_heads: int, cache: torch.Tensor, q_indptr, n_verify, c
                    sm_scale)
 
 
-def _check_layout(lay, rows: int, *tensors: torch.Tensor):
-    """The arrays' lengths, and that the call's tensors are all on the current
-    device, where its kernels run."""
-    if lay.q_indptr[-1] != rows:
-        raise ValueError("q_indptr[-1] must equal the number of rows")
-    if lay.page_indices.numel() < lay.page_indptr[-1]:
-        raise ValueError("page_indices is shorter than page_indptr[-1]")
-    _here(lay.page_indices, *tensors)
-
-
 # The current device without torch.cuda's own checks (0.6 us a call): tensors of
 # a device are there, so it is initialised.
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _here(*tensors: Optional[torch.Tensor]):
+def _here(*tensors: Optional[torch.Tensor]) -> int:
+    """The current device, where a call's kernels run and its tensors have to be."""
     here = _current_device()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"a tensor is on device {t.get_device()}, the current device is {here}")
+    return here
+
+
+def _check_layout(lay, rows: int, *tensors: Optional[torch.Tensor]) -> int:
+    """Checks the arrays' lengths and the tensors' device; returns the device."""
+    if lay.q_indptr.item(-1) != rows:
+        raise ValueError("q_indptr[-1] must equal the number of rows")
+    if lay.page_indices.numel() < lay.page_indptr.item(-1):
+        raise ValueError("page_indices is shorter than page_indptr[-1]")
+    return _here(lay.page_indices, *tensors)
 
 
 def _pool_of(stream):
@@ -658,49 +659,57 @@ def _pool_of(stream):
     return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
 
 
-def _rows(t: torch.Tensor, name: str, lay: _Layout) -> int:
+def _rows(t: torch.Tensor, name: str, hkv: int, d: int) -> int:
     """Checks rows [rows, Hkv, D] (any row stride, heads contiguous) and returns the stride."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not torch.bfloat16:
         raise TypeError(f"{name} must be a CUDA bf16 tensor")
     if t.dim() != 3:
         raise ValueError(f"{name} must have three dimensions")
     (rows, heads, width), (ahead, apart, next_to) = t.shape, t.stride()
-    hkv, d = lay.c.num_kv_heads, lay.c.head_dim
     if heads != hkv or width != d or next_to != 1 or (hkv > 1 and apart != d):
         raise ValueError(f"{name} must be [rows, {hkv}, {d}], contiguous within a row")
-    if rows != lay.q_indptr[-1]:
-        raise ValueError("q_indptr[-1] must equal the number of rows")
     return ahead if rows > 1 else hkv * d
+
+
+def _rows_call(name: str, k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor, layout: _Layout, stream, out: str):
+    """Checks and calls rg_kv4_append or rg_kv4_read."""
+    c = layout.c
+    hkv, d = c.num_kv_heads, c.head_dim
+    ks, vs = _rows(k, "k" + out, hkv, d), _rows(v, "v" + out, hkv, d)
+    _kv4(cache, d, hkv, c.num_pages)
+    rows = k.shape[0]
+    if v.shape[0] != rows:
+        raise ValueError("k and v must have as many rows")
+    here = _check_layout(layout, rows, k, v, cache)
+    if rows == 0:
+        return
+    on = _raw_stream(here) if stream is None and _raw_stream is not None else _stream(stream)
+    ref, kp, vp, cp = ctypes.byref(c), k.data_ptr(), v.data_ptr(), cache.data_ptr()
+    if out:
+        status = _lib().rg_kv4_read(ref, cp, kp, ks, vp, vs, on)
+    else:
+        status = _lib().rg_kv4_append(ref, kp, ks, vp, vs, cp, on)
+    _check(status, name)
 
 
 def kv4_append(k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor, layout: _Layout, *, stream=None) -> None:
     """Rows k, v [rows, Hkv, D] (e.g. parts of one projection's output) into
     the 4-bit cache, at the tokens behind each request's context
     (rg_kv4_append)."""
-    ks, vs = _rows(k, "k", layout), _rows(v, "v", layout)
-    _kv4(cache, layout.c.head_dim, layout.c.num_kv_heads, layout.c.num_pages)
-    _check_layout(layout, k.shape[0], k, v, cache)
-    if k.shape[0] == 0:
-        return
-    _check(_lib().rg_kv4_append(ctypes.byref(layout.c), k.data_ptr(), ks, v.data_ptr(), vs, cache.data_ptr(),
-                                _stream(stream)), "rg_kv4_append")
+    _rows_call("rg_kv4_append", k, v, cache, layout, stream, "")
 
 
 def kv4_read(cache: torch.Tensor, layout: _Layout, *, k_out: Optional[torch.Tensor] = None,
              v_out: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The tokens kv4_append writes for this layout, as bf16 rows (rg_kv4_read)."""
-    _kv4(cache, layout.c.head_dim, layout.c.num_kv_heads, layout.c.num_pages)
-    shape = (int(layout.q_indptr[-1]), layout.c.num_kv_heads, layout.c.head_dim)
     k, v = k_out, v_out
     if k is None or v is None:
+        _dev(cache, "cache", torch.uint8)
+        shape = (int(layout.q_indptr[-1]), layout.c.num_kv_heads, layout.c.head_dim)
         with _pool_of(stream):
             k = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if k is None else k
             v = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if v is None else v
-    ks, vs = _rows(k, "k_out", layout), _rows(v, "v_out", layout)
-    _check_layout(layout, shape[0], k, v, cache)
-    if shape[0]:
-        _check(_lib().rg_kv4_read(ctypes.byref(layout.c), cache.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs,
-                                  _stream(stream)), "rg_kv4_read")
+    _rows_call("rg_kv4_read", k, v, cache, layout, stream, "_out")
     return k, v
 
 
