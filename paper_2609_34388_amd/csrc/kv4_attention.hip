@@ -21,9 +21,13 @@
 // of S^T holds dims 64 (ks / 4) + 32 lh + 8 (ks % 4) .. + 7 of half-wave lh (Q
 // is read alike), and row l of output tile dt is dim DT l + dt, DT = D / 32.
 //
-// Softmax online in base 2; the running sum adds P in fp32, the product takes
-// it rounded to bf16 (off by at most 2^-8 of each term, as the output's own
-// rounding).  No maximum is taken where the running reference holds (below).
+// Softmax online in base 2; the product takes P rounded to bf16 (off by at most
+// 2^-8 of each term, as the output's own rounding).  Two sums run in fp32: of P,
+// for the lse, and of the rounded P, by which the product is divided, so that the
+// weights add up to one (a dominant key's V comes out as it is; over the exact
+// sum it would be off by up to 2^-8).  The second sum costs 1.5 % of a call at head
+// size 128, 5 % at 64, by v_dot2 (by unpacking and adding 4 and 9 %).  No maximum is
+// taken where the running reference holds (below).
 // Runs of a request's keys meet in fp32 in the workspace.
 //
 // Measured (query heads / KV heads / head size 32/8/128 unless said):
@@ -63,7 +67,7 @@ struct Kv4Shape {
   static constexpr int DT = D / 32;
   static constexpr int QROW = 2 * D + 16;             // bytes of a column of Q in LDS: 16 more, so that
                                                       // a fragment read meets every bank once
-  static constexpr int STATE = 64 * 16 * DT + 128;    // floats of a wave's state of one tile
+  static constexpr int STATE = 64 * 16 * DT + 192;    // floats of a wave's state of one tile
   static constexpr int RING = 2;                      // key tiles of a wave in LDS
   static constexpr int SLOT = 2 * Kv4<D>::BLOCK;      // bytes of one: two blocks
   // Loads of 16 bytes a lane that fill a slot: FULL of each block, and one of the
@@ -170,13 +174,13 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
   }
 
   f32x16 acc[TILES][DT];
-  float m_run[TILES], l_run[TILES];
+  float m_run[TILES], l_run[TILES], r_run[TILES];  // reference, sum of P, of the rounded P
 #pragma unroll
   for (int u = 0; u < TILES; ++u) {
     for (int dt = 0; dt < DT; ++dt)
       for (int i = 0; i < 16; ++i) acc[u][dt][i] = 0.f;
     m_run[u] = kNegInf;
-    l_run[u] = 0.f;
+    l_run[u] = r_run[u] = 0.f;
   }
 
   lds_barrier();
@@ -221,6 +225,7 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
     }
     __builtin_amdgcn_s_setprio(0);
     u32x4 pk[TILES][2];
+    const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
 #pragma unroll
     for (int u = 0; u < TILES; ++u) {
       if (kbase + 32 > min_lim[u]) {
@@ -236,10 +241,10 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
       // of a lane's 16 past 2^12 (overflow included), or a column without a
       // reference, moves the references to the maxima of this tile: P stays
       // below 2^12, and no maximum is taken where nothing moves.
-      float sum;
+      float sum, rsum;
       auto weigh = [&]() {
         const float mc = (m_run[u] == kNegInf) ? 0.f : m_run[u] * a.scale_log2;
-        sum = 0.f;
+        sum = rsum = 0.f;
 #pragma unroll
         for (int pp = 0; pp < 2; ++pp)
 #pragma unroll
@@ -247,7 +252,9 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
             const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u][8 * pp + 2 * e], a.scale_log2, -mc));
             const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u][8 * pp + 2 * e + 1], a.scale_log2, -mc));
             sum += x + y;
-            pk[u][pp][e] = pack_bf16x2(x, y);
+            const uint32_t xy = pack_bf16x2(x, y);
+            rsum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, xy), ones, rsum, false);
+            pk[u][pp][e] = xy;
           }
       };
       weigh();
@@ -259,6 +266,7 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
         const float m_new = fmaxf(m_run[u], fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
         const float alpha = m_new == kNegInf ? 1.f : __builtin_amdgcn_exp2f((m_run[u] - m_new) * a.scale_log2);
         l_run[u] *= alpha;
+        r_run[u] *= alpha;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -268,6 +276,7 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
         weigh();
       }
       l_run[u] += sum;
+      r_run[u] += rsum;
     }
     uint32_t vc[2][DT];
     u32x2 vs[2];
@@ -339,7 +348,7 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
   float* area = reinterpret_cast<float*>(lds);
   const float* states = area + pair * S::STATE;  // of the pair, np apart
   const int step = np * S::STATE, share = 4 * DT / kg;
-  auto put = [&](const f32x16(&o)[DT], float m, float l) {
+  auto put = [&](const f32x16(&o)[DT], float m, float l, float rounded) {
     float* state = area + wave * S::STATE;
 #pragma unroll
     for (int v = 0; v < 4 * DT; ++v) {
@@ -349,14 +358,18 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
                       o[(f + 2) % DT][4 * i4 + (f + 2) / DT], o[(f + 3) % DT][4 * i4 + (f + 3) / DT]);
     }
     state[64 * 16 * DT + lane] = m;
-    state[64 * 16 * DT + 64 + lane] = l + __shfl_xor(l, 32);
+    l += __shfl_xor(l, 32);
+    rounded += __shfl_xor(rounded, 32);
+    state[64 * 16 * DT + 64 + lane] = l;
+    // what makes the products sums of weights l; one where nothing was added
+    state[64 * 16 * DT + 128 + lane] = rounded > 0.f ? l / rounded : 1.f;
   };
 #pragma unroll 1
   for (int u = 0; u < 2; ++u) {
     if (u == 1 && it.nct == 1) break;
     lds_barrier();  // Q and the codes, or the states before, are no longer read
-    if (u == 0) put(acc[0], m_run[0], l_run[0]);
-    else if (TILES == 2) put(acc[TILES - 1], m_run[TILES - 1], l_run[TILES - 1]);
+    if (u == 0) put(acc[0], m_run[0], l_run[0], r_run[0]);
+    else if (TILES == 2) put(acc[TILES - 1], m_run[TILES - 1], l_run[TILES - 1], r_run[TILES - 1]);
     lds_barrier();
     const int col = (it.tile0 + 2 * pair + u) * 32 + lc;
     if (u >= TILES || col >= it.M) continue;
@@ -370,7 +383,10 @@ __device__ __forceinline__ void kv4_wave(const Kv4AttnArgs& a, const Req& rq, co
     for (int k = 0; k < kKv4Waves; ++k) {
       // a group none of whose keys the column sees weighs nothing
       w[k] = w[k] == kNegInf ? 0.f : __builtin_amdgcn_exp2f((w[k] - m) * a.scale_log2);
-      if (k < kg) l += w[k] * states[k * step + 64 * 16 * DT + 64 + lane];
+      if (k < kg) {
+        l += w[k] * states[k * step + 64 * 16 * DT + 64 + lane];
+        w[k] *= states[k * step + 64 * 16 * DT + 128 + lane];
+      }
     }
     const int tok = row_of(a, col);
     const size_t orow = (size_t)(rq.q_start + tok) * a.hq + it.hk * g + (col - tok * g);
