@@ -656,7 +656,10 @@ def _pool_of(stream):
     away before the call has run."""
     if stream is None:
         return contextlib.nullcontext()
-    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
+    if not isinstance(stream, torch.cuda.Stream):
+        # 0 is the default stream's handle; ExternalStream(0) would be some other stream
+        stream = torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
 
 
 def _rows(t: torch.Tensor, name: str, hkv: int, d: int) -> int:
