@@ -522,13 +522,16 @@ rg_status rg_plan_block_sizes(const rg_block_policy* policy, const int32_t* acce
  * Code byte i of a token holds element 2 i in its low four bits and 2 i + 1 in
  * its high ones: a sign bit over 0, 0.5, 1, 1.5, 2, 3, 4, 6.  An element's
  * value is that times 2^(b - 127), b the scale byte of its 32 elements, 1 to
- * 252: the value is exact in bf16.
+ * 252: the value is exact in bf16.  With b = 255 all 32 are NaN.
  *
  * Rows are rounded so: b is the biased exponent of the 32 elements' largest
  * magnitude, plus one where it is at least 1.75 times its power of two, less
  * 2, clamped to 1 .. 252 (so that magnitude / 2^(b - 127) lies in [3.5, 7)
  * unless clamped); a code is the nearest of the grid, ties to the even code,
- * magnitudes past 6 become 6, and the sign of an element is kept.
+ * magnitudes past 6 become 6, and the sign of an element is kept.  32 elements
+ * with an infinity or a NaN among them get b = 255: attention over such a token
+ * comes out as NaN, as with NaN in a bf16 cache (from K in the rows that see
+ * the token, from V in any of the request's).
  */
 #define RG_KV4_BLOCK_BYTES(head_dim) (17 * (head_dim))
 

@@ -17,8 +17,11 @@ def bf16_values(bits: np.ndarray) -> np.ndarray:
 
 
 def encode(x: np.ndarray) -> Tuple[np.ndarray, np.ndarray]:
-    """4-bit codes [.., D] and scale bytes [.., D/32] of rows x [.., D] in float64."""
+    """4-bit codes [.., D] and scale bytes [.., D/32] of rows x [.., D] in float64.
+    Groups with an infinity or a NaN get scale byte 255; their codes say nothing."""
     groups = x.reshape(*x.shape[:-1], -1, 32)
+    finite = np.isfinite(groups).all(axis=-1)
+    groups = np.where(finite[..., None], groups, 0.0)
     top = np.abs(groups).max(axis=-1)
     frac, e = np.frexp(top)  # top = frac 2^e, 0.5 <= frac < 1: power of two 2^(e-1), mantissa 2 frac
     b = np.clip(np.where(top > 0, e - 1 + 127 + (2 * frac >= 1.75) - 2, 1), 1, 252).astype(np.int64)
@@ -30,12 +33,12 @@ def encode(x: np.ndarray) -> Tuple[np.ndarray, np.ndarray]:
     even = near & (np.arange(8) % 2 == 0)
     code = np.where(even.any(axis=-1), even.argmax(axis=-1), near.argmax(axis=-1))
     code = code + 8 * np.signbit(groups)
-    return code.reshape(x.shape).astype(np.int64), b
+    return code.reshape(x.shape).astype(np.int64), np.where(finite, b, 255)
 
 
 def decode(code: np.ndarray, b: np.ndarray) -> np.ndarray:
     v = GRID[code & 7] * np.where(code >= 8, -1.0, 1.0)
-    v = v.reshape(*b.shape, 32) * np.exp2(b.astype(np.float64) - 127)[..., None]
+    v = v.reshape(*b.shape, 32) * np.where(b == 255, np.nan, np.exp2(b.astype(np.float64) - 127))[..., None]
     return v.reshape(code.shape)
 
 

@@ -698,7 +698,8 @@ def _rows_call(name: str, k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor,
 def kv4_append(k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor, layout: _Layout, *, stream=None) -> None:
     """Rows k, v [rows, Hkv, D] (e.g. parts of one projection's output) into
     the 4-bit cache, at the tokens behind each request's context
-    (rg_kv4_append)."""
+    (rg_kv4_append).  32 elements with an infinity or a NaN among them read as
+    NaN."""
     _rows_call("rg_kv4_append", k, v, cache, layout, stream, "")
 
 

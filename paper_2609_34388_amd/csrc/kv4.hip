@@ -5,7 +5,8 @@
 // a step of the grid (a tie to 8 cannot occur, 6 saturates only what rounds to
 // it); the codes are the nearest elements of 0, .5, 1, 1.5, 2, 3, 4, 6.  As
 // the scale is a power of two the quotient is exact and the result does not
-// depend on how it is computed.
+// depend on how it is computed.  A group with an infinity or a NaN, which the
+// grid has no element for, gets the scale byte that makes every element a NaN.
 //
 // A work item is one page that a request's rows touch, of plan.chunk neighbouring
 // KV heads (blocks that lie together): no two work groups write the same block,
@@ -93,8 +94,8 @@ __global__ __launch_bounds__(kRowThreads) void kv4_append_kernel(Kv4RowArgs a, A
       for (int e = 0; e < 4; ++e) m = max(m, max(w[e] & 0x7fffu, (w[e] >> 16) & 0x7fffu));
       m = max(m, (uint32_t)__shfl_xor((int)m, 1));  // four lanes hold a group
       m = max(m, (uint32_t)__shfl_xor((int)m, 2));
-      const uint32_t b = (uint32_t)min(max((int)((m + 0x20) >> 7) - 2, 1), 252);
-      const uint32_t c = encode8(w, scale_of(b));
+      const uint32_t scale = (uint32_t)min(max((int)((m + 0x20) >> 7) - 2, 1), 252);
+      const uint32_t c = encode8(w, scale_of(scale)), b = m >= 0x7f80u ? kNanScale : scale;
       if (u.kv == 0) {
         *(uint32_t*)(blk + B::k_code(u.slot, u.d0)) = c;
         if ((u.d0 & 31) == 0) blk[B::k_scale(u.slot, u.d0 >> 5)] = (uint8_t)b;

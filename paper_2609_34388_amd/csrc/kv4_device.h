@@ -22,7 +22,10 @@ struct Kv4 {
   static __device__ __forceinline__ int v_scale(int slot, int g) { return VS + ((slot >> 3) * DT + g) * 8 + (slot & 7); }
 };
 
-// Scale byte (1 .. 252) as its power of two.
+// Scale byte (1 .. 252) as its power of two.  Of kNanScale, and of any float with
+// its exponent, the conversions make NaN whatever the code (all codes of both kinds
+// measured), zero included.
+constexpr uint32_t kNanScale = 255;
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // Elements 2 SEL and 2 SEL + 1 of eight 4-bit codes, as bf16 (exact: two

@@ -62,3 +62,12 @@ def test_evict_keeps_protected_then_best_then_lowest():
     assert ref.evict(score, pos, 8, 1, 1, 8) == []
     assert ref.evict(score, pos, 0, 0, 0, 8) == []
     assert ref.evict(np.zeros(5), np.arange(5), 2, 0, 0, 5) == []
+
+
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+def test_a_group_without_a_value_reads_as_nan(bad):
+    x = np.concatenate([_group(1.0, bad, 2.0), _group(1.0, 4.0)])
+    code, b = ref.encode(x)
+    assert b.tolist() == [255, 127]
+    got = ref.decode(code, b)
+    assert np.isnan(got[:32]).all() and got[32:34].tolist() == [1.0, 4.0]
