@@ -279,15 +279,38 @@ rg_status run_mass(const rg_attn_layout* L, const uint16_t* q, const void* keys,
   a.decay = decay;
   // A request without query rows need not own pages for its context.
   auto len = [&](int r) { return L->q_indptr[r + 1] == L->q_indptr[r] ? 0 : (int64_t)L->ctx_len[r] + L->n_verify[r]; };
-  auto many = [&](int r) { return (int64_t)L->n_verify[r] * a.g > kMassCols; };
   auto runs = [&](int r, int64_t step) { return (len(r) + step - 1) / step * L->num_kv_heads; };
+  // launch_mass goes over a key's columns kMassCols at a time, in one work group;
+  // launch_mass_rows shares them among a work group's waves, with fewer keys each.  The
+  // latter is the faster of the two where there are few keys (it has more work groups,
+  // each done sooner) or many columns; the former, which decodes and reads a key and
+  // starts a work group for more of them at once, else.  So up to `most` times kMassCols
+  // columns go to the former, by the work groups of kMassKeys keys that the batch gives
+  // a compute unit.  us, former / latter, heads 32/8/128, by columns (* not taken):
+  //                             132          256          512          1024
+  //   40 of 8k-32k keys, bf16   482 / 1081   613 / 1164   1059 / 1496  1957 / 2320
+  //                      4-bit  341 / 637    474 / 711    883 / 1107   *1763 / 1851
+  //   16 of 1k-8k keys, bf16    51 / 100     66 / 107     114 / 140    218 / 224
+  //                     4-bit   41 / 61      56 / 67      *109 / 106   *224 / 178
+  //   one of 4096 keys, bf16    *10 / 11     *13 / 12     *22 / 14     *37 / 20
+  //                     4-bit   *13 / 9      *18 / 9      *30 / 11     *57 / 16
+  const int cus = device_cus();
+  auto chunks = [&](int r) { return ((int64_t)L->n_verify[r] * a.g + kMassCols - 1) / kMassCols; };
+  const int64_t limit = kv4 ? 4 : 8;
+  int64_t groups = 0;
+  for (int r = 0; r < L->num_requests; ++r)
+    if (chunks(r) <= limit) groups += runs(r, kMassKeys);
+  const int64_t most = std::min(limit, std::max<int64_t>(1, groups / (kv4 ? 4 * cus : cus)));
+  auto many = [&](int r) { return chunks(r) > most; };
+  bool wide = false;
+  for (int r = 0; r < L->num_requests; ++r) wide = wide || (!many(r) && chunks(r) > 1);
   // 4-bit: the longest run that still gives every compute unit four work
   // groups, so that a run's start is a small part of it (40 long requests take 150
   // us so, 151 with eight, 153 with two, 310 with as many as bf16 keys give).
   int64_t all = 0;
   for (int r = 0; r < L->num_requests; ++r)
     if (!many(r)) all += len(r) * L->num_kv_heads;
-  const int64_t run = kv4 ? std::min<int64_t>(kMassRun, std::max<int64_t>(128, all / (4 * device_cus()) / 128 * 128)) : kMassKeys;
+  const int64_t run = kv4 ? std::min<int64_t>(kMassRun, std::max<int64_t>(128, all / (4 * cus) / 128 * 128)) : kMassKeys;
   // rows of a request are addressed by 32-bit offsets
   for (int r = 0; r < L->num_requests; ++r)
     if (many(r) && (int64_t)L->n_verify[r] * a.hq * L->head_dim * 2 > INT32_MAX) return RG_ERR_UNSUPPORTED;
@@ -302,7 +325,7 @@ rg_status run_mass(const rg_attn_layout* L, const uint16_t* q, const void* keys,
   if (st != RG_OK) return st;
   return each_plan(L, threads, few_items, [&](AttnPlan& p) {
     p.chunk = (int32_t)run;
-    return launch_mass(a, p, L->head_dim, kv4, s);
+    return launch_mass(a, p, L->head_dim, kv4, wide, s);
   });
 }
 

@@ -59,11 +59,10 @@ hipError_t launch_kv4_attention(const Kv4AttnArgs& a, const AttnPlan& p, int hea
 hipError_t launch_kv4_attention(const Kv4AttnArgs& a, const AttnPlanBr& p, int head_dim, hipStream_t stream);
 
 // Attention mass.  Plans: AttnPlan, part_start the request's number.  Requests
-// of up to kMassCols query columns a KV head take launch_mass, with work items of
-// kMassKeys keys (bf16) or plan.chunk (4-bit) of a KV head; the others
-// launch_mass_rows, with items of kMassRowKeys keys.  (16 requests' steps take 34 us
-// by the first, 44 by the second, 40 long ones in 4 bits 150 and 499; two prompts 406
-// and, before its later steps, 138.)
+// of few query columns a KV head take launch_mass (`wide` where one has more than
+// kMassCols), with work items of kMassKeys keys (bf16) or plan.chunk (4-bit) of a KV
+// head; the others launch_mass_rows, with items of kMassRowKeys keys.  Where the line
+// lies: run_mass in cache_api.cpp.
 constexpr int kMassWaves = 4;
 constexpr int kMassCols = 128;
 constexpr int kMassSub = 2;                            // 32-key tiles of a bf16 wave
@@ -82,7 +81,7 @@ struct MassArgs {
   uint32_t g_mul;  // quotient by g
   int32_t g_shift;
 };
-hipError_t launch_mass(const MassArgs& a, const AttnPlan& p, int head_dim, bool kv4, hipStream_t stream);
+hipError_t launch_mass(const MassArgs& a, const AttnPlan& p, int head_dim, bool kv4, bool wide, hipStream_t stream);
 hipError_t launch_mass_rows(const MassArgs& a, const AttnPlan& p, int head_dim, bool kv4, hipStream_t stream);
 
 // Eviction.

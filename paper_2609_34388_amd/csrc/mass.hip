@@ -8,11 +8,11 @@
 // 16 scores of a 32 x 32 tile are 16 query columns of one key and the sum over
 // columns stays in the lane.  No atomics: a key's sum has one order.
 //
-// Up to 128 query columns a request (mass_kernel) the bytes of K bound it: Q
-// lies in LDS, waves take key tiles.  A bf16 wave holds two key tiles, read
+// With few query columns (mass_kernel) the bytes of K bound it: up to 128 of them
+// lie in LDS, waves take key tiles; mass_wide_kernel takes more, 128 after 128.  A bf16 wave holds two key tiles, read
 // straight from the pool; four times fewer bytes of a 4-bit key would leave a
 // work group that small waiting for its start, so it takes a longer run of keys,
-// two tiles a step, with the next step's codes in flight.  With more columns
+// two tiles a step, with the next step's codes in flight.  With many columns
 // (mass_rows_kernel, prompts) the products and exponentials bound it: a work
 // group takes 64 keys, held in registers by each of its waves, and the waves
 // share the column tiles, whose Q comes through LDS of the wave's own.
@@ -115,8 +115,11 @@ __device__ __forceinline__ void write_mass(const MassArgs& a, const MassItem& it
   *at = key < it.L && a.decay != 0.f ? a.decay * *at + sum : sum;
 }
 
-template <int D, bool KV4>
-__global__ __launch_bounds__(kThreads, KV4 ? 3 : 2) void mass_kernel(MassArgs a, AttnPlan p) {
+// A run of keys over up to kMassCols columns, or with WIDE over any number of
+// them, kMassCols at a time: bf16 keys stay in registers, 4-bit ones are read
+// again (from a cache, as a run's codes are 160 KB at most) and their sums stay in LDS.
+template <int D, bool KV4, bool WIDE>
+__device__ __forceinline__ void mass_run(const MassArgs& a, const AttnPlan& p) {
   constexpr int KSTEPS = D / 16, QROW = 2 * D + 16;  // 16 bytes more: a fragment read meets every bank once
   __shared__ __attribute__((aligned(16))) char lds[kMassCols * QROW + kMassCols * 4 + (KV4 ? kMassRun * 4 : 0)];
   char* qs = lds;
@@ -126,7 +129,8 @@ __global__ __launch_bounds__(kThreads, KV4 ? 3 : 2) void mass_kernel(MassArgs a,
   const MassItem it = mass_item(a, p, run);
   const int tid = threadIdx.x, lane = tid & 63, lc = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int tiles = (it.M + 31) / 32;
+  int c0 = 0;                                           // first column in LDS
+  int tiles = (WIDE ? min(it.M, kMassCols) + 31 : it.M + 31) / 32;  // column tiles there
 
   // 4-bit: codes and scales of two key tiles; their loads go out first
   typedef const int32_t __attribute__((address_space(4))) * cpage_ptr;
@@ -156,23 +160,37 @@ __global__ __launch_bounds__(kThreads, KV4 ? 3 : 2) void mass_kernel(MassArgs a,
     asm volatile("" ::: "memory");  // these loads go out before those of Q
   }
 
-  u32x4 qx[kMassCols * (D / 8) / kThreads];  // all loads, then all stores
+  auto load_columns = [&](int tid) {
+    u32x4 qx[kMassCols * (D / 8) / kThreads];  // all loads, then all stores
 #pragma unroll
-  for (int e = 0; e < kMassCols * (D / 8) / kThreads; ++e) {
-    const int u = tid + e * kThreads, row = u / (D / 8), ch = u % (D / 8);
-    qx[e] = u32x4{0u, 0u, 0u, 0u};
-    if (row < it.M) qx[e] = *(const u32x4*)(a.q + column_row(a, it, row) * D + 8 * ch);
-  }
+    for (int e = 0; e < kMassCols * (D / 8) / kThreads; ++e) {
+      const int u = tid + e * kThreads, col = c0 + u / (D / 8), ch = u % (D / 8);
+      qx[e] = u32x4{0u, 0u, 0u, 0u};
+      if (col < it.M) qx[e] = *(const u32x4*)(a.q + column_row(a, it, col) * D + 8 * ch);
+    }
 #pragma unroll
-  for (int e = 0; e < kMassCols * (D / 8) / kThreads; ++e) {
-    const int u = tid + e * kThreads, row = u / (D / 8), ch = u % (D / 8);
-    if (row < 32 * tiles) *(u32x4*)(qs + row * QROW + 16 * ch) = qx[e];
-  }
-  // a column that does not count weighs exp2(-inf) = 0
-  if (tid < 32 * tiles) lse2[tid] = tid < it.M ? a.lse[column_row(a, it, tid)] * kLog2e : -kNegInf;
-  lds_barrier();
+    for (int e = 0; e < kMassCols * (D / 8) / kThreads; ++e) {
+      const int u = tid + e * kThreads, row = u / (D / 8), ch = u % (D / 8);
+      if (row < 32 * tiles) *(u32x4*)(qs + row * QROW + 16 * ch) = qx[e];
+    }
+    // a column that does not count weighs exp2(-inf) = 0
+    if (tid < 32 * tiles) lse2[tid] = c0 + tid < it.M ? a.lse[column_row(a, it, c0 + tid)] * kLog2e : -kNegInf;
+    lds_barrier();
+  };
+  load_columns(tid);
+  // The next columns, if there are any.
+  auto next_columns = [&]() {
+    c0 += kMassCols;
+    if (!WIDE || c0 >= it.M) return false;
+    tiles = (min(it.M - c0, kMassCols) + 31) / 32;
+    lds_barrier();  // those before are no longer read
+    int again = tid;
+    asm volatile("" : "+v"(again));  // or places in LDS and q stay in registers all the while
+    load_columns(again);
+    return true;
+  };
 
-  // Adds the weights of N key tiles, 32 * kMassWaves keys apart, over all columns.
+  // Adds the weights of N key tiles, 32 * kMassWaves keys apart, over the columns in LDS.
   auto weigh = [&](const auto& k, int kb, auto& w) {
     constexpr int N = sizeof(w) / sizeof(w[0]);
     for (int t = 0; t < tiles; ++t) {
@@ -195,37 +213,46 @@ __global__ __launch_bounds__(kThreads, KV4 ? 3 : 2) void mass_kernel(MassArgs a,
         ls[4 * i4] = x.x, ls[4 * i4 + 1] = x.y, ls[4 * i4 + 2] = x.z, ls[4 * i4 + 3] = x.w;
       }
 #pragma unroll
-      for (int s = 0; s < N; ++s) add_weights(a, it, sc[s], ls, 32 * t, kb + 32 * kMassWaves * s, w[s]);
+      for (int s = 0; s < N; ++s) add_weights(a, it, sc[s], ls, c0 + 32 * t, kb + 32 * kMassWaves * s, w[s]);
     }
   };
   if constexpr (KV4) {
-    // two key tiles a step: half the reads of Q, two chains of products
-    for (int kb = it.kbeg + 32 * wave; kb < kend; kb += 2 * STEP) {
-      bf16x8 k[2][KSTEPS];
+    do {
+      // two key tiles a step: half the reads of Q, two chains of products
+      for (int kb = it.kbeg + 32 * wave; kb < kend; kb += 2 * STEP) {
+        bf16x8 k[2][KSTEPS];
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-          const float f = scale_of((ksc[s] >> (8 * lh + 16 * i)) & 0xff);
+          for (int i = 0; i < D / 64; ++i) {
+            const float f = scale_of((ksc[s] >> (8 * lh + 16 * i)) & 0xff);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) k[s][4 * i + e] = __builtin_bit_cast(bf16x8, decode8(kc[s][i][e], f));
+            for (int e = 0; e < 4; ++e) k[s][4 * i + e] = __builtin_bit_cast(bf16x8, decode8(kc[s][i][e], f));
+          }
+        // the next step's codes, or the first's for the next columns
+        if (kb + 2 * STEP < kend) load(kb + 2 * STEP);
+        else if (WIDE && c0 + kMassCols < it.M) load(it.kbeg + 32 * wave);
+        float w[2] = {0.f, 0.f};
+        weigh(k, kb, w);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const float sum = w[s] + __shfl_xor(w[s], 32);
+          if (lh == 0 && kb + STEP * s < kend) {
+            float& at = sums[kb + STEP * s - it.kbeg + lc];  // always this lane's
+            at = WIDE && c0 > 0 ? at + sum : sum;
+          }
         }
-      if (kb + 2 * STEP < kend) load(kb + 2 * STEP);
-      float w[2] = {0.f, 0.f};
-      weigh(k, kb, w);
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const float sum = w[s] + __shfl_xor(w[s], 32);
-        if (lh == 0 && kb + STEP * s < kend) sums[kb + STEP * s - it.kbeg + lc] = sum;
       }
-    }
+    } while (next_columns());
     // behind the loop: a load or store of the mass in it would wait for the codes
     lds_barrier();
     for (int key = it.kbeg + tid; key < kend; key += kThreads) write_mass(a, it, key, sums[key - it.kbeg]);
   } else {
     const int kb = it.kbeg + 32 * wave;
     float w[kMassSub] = {};
-    if (kb < it.T) weigh(kf, kb, w);
+    do
+      if (kb < it.T) weigh(kf, kb, w);
+    while (next_columns());
 #pragma unroll
     for (int s = 0; s < kMassSub; ++s) {
       const float sum = w[s] + __shfl_xor(w[s], 32);
@@ -233,6 +260,15 @@ __global__ __launch_bounds__(kThreads, KV4 ? 3 : 2) void mass_kernel(MassArgs a,
       if (lh == 0 && key < it.T) write_mass(a, it, key, sum);
     }
   }
+}
+
+template <int D, bool KV4>
+__global__ __launch_bounds__(kThreads, KV4 ? 3 : 2) void mass_kernel(MassArgs a, AttnPlan p) {
+  mass_run<D, KV4, false>(a, p);
+}
+template <int D, bool KV4>
+__global__ __launch_bounds__(kThreads, KV4 ? 3 : 2) void mass_wide_kernel(MassArgs a, AttnPlan p) {
+  mass_run<D, KV4, true>(a, p);
 }
 
 template <int D, bool KV4>
@@ -344,12 +380,15 @@ __global__ __launch_bounds__(kThreads, 3) void mass_rows_kernel(MassArgs a, Attn
 
 }  // namespace
 
-hipError_t launch_mass(const MassArgs& a, const AttnPlan& p, int head_dim, bool kv4, hipStream_t stream) {
+hipError_t launch_mass(const MassArgs& a, const AttnPlan& p, int head_dim, bool kv4, bool wide, hipStream_t stream) {
   const dim3 grid(p.total_items), block(kThreads);
-  if (head_dim == 128 && kv4) hipLaunchKernelGGL((mass_kernel<128, true>), grid, block, 0, stream, a, p);
-  else if (head_dim == 128) hipLaunchKernelGGL((mass_kernel<128, false>), grid, block, 0, stream, a, p);
-  else if (kv4) hipLaunchKernelGGL((mass_kernel<64, true>), grid, block, 0, stream, a, p);
-  else hipLaunchKernelGGL((mass_kernel<64, false>), grid, block, 0, stream, a, p);
+  auto launch = [&](auto narrow_kernel, auto wide_kernel) {
+    hipLaunchKernelGGL((wide ? wide_kernel : narrow_kernel), grid, block, 0, stream, a, p);
+  };
+  if (head_dim == 128 && kv4) launch(mass_kernel<128, true>, mass_wide_kernel<128, true>);
+  else if (head_dim == 128) launch(mass_kernel<128, false>, mass_wide_kernel<128, false>);
+  else if (kv4) launch(mass_kernel<64, true>, mass_wide_kernel<64, true>);
+  else launch(mass_kernel<64, false>, mass_wide_kernel<64, false>);
   return hipGetLastError();
 }
 

@@ -65,3 +65,11 @@ def test_cache_kernels_do_not_spill(tmp_path, part, count, vgprs):
     for name, k in kernels.items():
         assert int(k["vgpr_spill_count"]) == 0 and int(k["private_segment_fixed_size"]) == 0, name
         assert int(k["vgpr_count"]) <= vgprs, name
+
+
+def test_wide_mass_kernels_do_not_spill(tmp_path):
+    kernels = {k: v for k, v in _kernels(tmp_path).items() if "mass_wide_kernel" in k}
+    assert len(kernels) == 2 * 2  # head sizes x caches
+    for name, k in kernels.items():
+        assert int(k["vgpr_spill_count"]) == 0 and int(k["private_segment_fixed_size"]) == 0, name
+        assert int(k["vgpr_count"]) <= 168, name  # three waves per SIMD
