@@ -545,7 +545,9 @@ rg_status rg_plan_block_sizes(const rg_block_policy* policy, const int32_t* acce
  *             v + j * v_stride (elements, at least Hkv * D, multiples of 8;
  *             pointers 16-byte aligned)
  *   cache     DEVICE pool
- * The layout's n_verify, num_q_heads and sm_scale have no effect.
+ * The layout's n_verify, num_q_heads and sm_scale do not change what is
+ * written, but have to be those of a layout: n_verify[r] in 0 .. n_r, Hq a
+ * multiple of Hkv (RG_ERR_SHAPE otherwise).
  */
 rg_status rg_kv4_append(const rg_attn_layout* layout, const uint16_t* k, int64_t k_stride, const uint16_t* v,
                         int64_t v_stride, uint8_t* cache, void* stream);

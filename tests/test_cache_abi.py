@@ -158,3 +158,12 @@ def test_mass_refuses_before_it_launches():
     assert mass(l) == UNSUPPORTED
     l = L(ctx=(40, 1 << 29), nv=(1, 200), n=(1, 200), hq=n, hkv=n, D=64)
     assert mass(l) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("call", [append, read])
+def test_rows_check_the_whole_layout(call):
+    """Fields that rows do not use have to be valid all the same."""
+    null = ctypes.c_void_p(None)
+    assert call(L(nv=(7, 5), hq=2), cache=null) == NULL and call(L(nv=(0, 0), hq=64), cache=null) == NULL
+    for kw in (dict(nv=(8, 0)), dict(nv=(0, -1)), dict(hq=3), dict(hq=0)):
+        assert call(L(**kw), cache=null) == SHAPE, kw
