@@ -259,6 +259,9 @@ rg_status run_mass(const rg_attn_layout* L, const uint16_t* q, const void* keys,
                    const int32_t* row_count, float decay, float* mass, void* stream) {
   rg_status st = validate_layout(L);
   if (st != RG_OK) return st;
+  // launch_mass_rows addresses a request's rows by 32-bit offsets
+  for (int r = 0; r < L->num_requests; ++r)
+    if ((int64_t)L->n_verify[r] * L->num_q_heads * L->head_dim * 2 > INT32_MAX) return RG_ERR_UNSUPPORTED;
   if (!q || !keys || !lse || !mass) return RG_ERR_NULL;
   if (!(decay >= 0.f) || std::isinf(decay)) return RG_ERR_SHAPE;
   if (!aligned(q, 16) || !aligned(keys, 16) || !aligned(lse, 4) || !aligned(mass, 4) || !aligned(L->page_indices, 4) ||
@@ -311,9 +314,6 @@ rg_status run_mass(const rg_attn_layout* L, const uint16_t* q, const void* keys,
   for (int r = 0; r < L->num_requests; ++r)
     if (!many(r)) all += len(r) * L->num_kv_heads;
   const int64_t run = kv4 ? std::min<int64_t>(kMassRun, std::max<int64_t>(128, all / (4 * cus) / 128 * 128)) : kMassKeys;
-  // rows of a request are addressed by 32-bit offsets
-  for (int r = 0; r < L->num_requests; ++r)
-    if (many(r) && (int64_t)L->n_verify[r] * a.hq * L->head_dim * 2 > INT32_MAX) return RG_ERR_UNSUPPORTED;
   const auto few_items = [&](int r) { return many(r) ? 0 : runs(r, run); };
   const auto many_items = [&](int r) { return many(r) ? runs(r, kMassRowKeys) : 0; };
   const int threads = 64 * kMassWaves;

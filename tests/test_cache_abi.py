@@ -167,3 +167,16 @@ def test_rows_check_the_whole_layout(call):
     assert call(L(nv=(7, 5), hq=2), cache=null) == NULL and call(L(nv=(0, 0), hq=64), cache=null) == NULL
     for kw in (dict(nv=(8, 0)), dict(nv=(0, -1)), dict(hq=3), dict(hq=0)):
         assert call(L(**kw), cache=null) == SHAPE, kw
+
+
+@pytest.mark.parametrize("n, hq, D, fits", [(65535, 128, 128, True), (65535, 129, 128, False), (32767, 256, 128, True),
+                                            (32768, 256, 128, False), (65535, 256, 64, True), (65535, 257, 64, False),
+                                            (100, 8, 128, True)])
+def test_mass_bound_of_query_bytes_from_both_sides(n, hq, D, fits):
+    """Of a layout alone, before any pointer: one that fits goes on to the
+    missing pointer.  The largest byte that fits is 2^31 - 32768."""
+    assert (n * hq * D * 2 < 2 ** 31) == fits
+    for hkv in {1, hq}:
+        assert mass(L(ctx=(0,), nv=(n,), n=(n,), hq=hq, hkv=hkv, D=D), m=None) == (NULL if fits else UNSUPPORTED)
+    # draft rows do not count
+    assert mass(L(ctx=(0,), nv=(1,), n=(65535,), hq=1 << 12, hkv=1, D=D), m=None) == NULL
