@@ -359,8 +359,8 @@ rg_status each_evict_plan(const rg_evict_layout* L, int64_t& words, F f) {
     std::memset(&p, 0, sizeof(p));
     p.num_req = std::min(kMaxEvictReq, L->num_requests - r0);
     int64_t ws = 0, moves = 0;
-    // The longest requests first: a choice takes as long as its request, and one
-    // of more than 8192 tokens fills a compute unit.
+    // The longest requests first: a choice takes as long as its request, and two
+    // work groups at a time share a compute unit.
     int order[kMaxEvictReq];
     std::iota(order, order + p.num_req, r0);
     std::stable_sort(order, order + p.num_req, [&](int x, int y) { return L->ctx_len[x] > L->ctx_len[y]; });

@@ -218,7 +218,10 @@ __global__ __launch_bounds__(kEvictThreads, 8) void evict_select_kernel(EvictArg
     return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
   };
 
-  constexpr int kMasks = KW < 16 ? KW : 16;  // masks held (in scalar registers); the others are made again
+  // Masks held, in scalar registers and, where these are full, in lanes of a vector
+  // register (the compiler's own spills: 10 words with 8 held slots, 60 with 16, 132
+  // with 32, none of them in memory); the others are made again.
+  constexpr int kMasks = KW < 16 ? KW : 16;
   uint64_t kept[kMasks];
   uint32_t tie = tie0, holes = 0, movers = 0, tie_past = 0;  // tie_past: at the first of those
   each([&](int i, uint32_t u, bool in) {

@@ -73,3 +73,22 @@ def test_wide_mass_kernels_do_not_spill(tmp_path):
     for name, k in kernels.items():
         assert int(k["vgpr_spill_count"]) == 0 and int(k["private_segment_fixed_size"]) == 0, name
         assert int(k["vgpr_count"]) <= 168, name  # three waves per SIMD
+
+
+def test_eviction_choices_share_a_compute_unit(tmp_path):
+    """Two work groups of 1024 on a compute unit leave 64 vector registers each;
+    scalar registers past the 102 of a wave go to lanes of those, not to memory."""
+    kernels = {k: v for k, v in _kernels(tmp_path).items() if "evict_select_kernel" in k}
+    spills = {4: 0, 8: 16, 16: 64, 32: 140}  # by the held slots of a thread: their masks are two words each
+    for held, most in spills.items():
+        (k,) = [v for name, v in kernels.items() if f"evict_select_kernelILi{held}E" in name]
+        assert int(k["vgpr_count"]) <= 64 and int(k["private_segment_fixed_size"]) == 0, held
+        assert int(k["sgpr_spill_count"]) <= most, held
+
+
+def test_scalar_spills_of_the_other_cache_kernels(tmp_path):
+    parts = ("kv4_append", "kv4_read", "kv4_attn", "kv4_merge", "mass_kernel", "mass_wide", "mass_rows", "evict_move")
+    for name, k in _kernels(tmp_path).items():
+        if any(part in name for part in parts):
+            # the attention's plan without branches: 20 words in lanes of a vector register
+            assert int(k["sgpr_spill_count"]) <= (24 if "kv4_attn" in name else 0), name
