@@ -114,12 +114,11 @@ Kv4Cols kv4_cols(const rg_attn_layout* L, int r) {
 // Units (kv4_rate) of a work item at most: the least that gives one round of
 // items on the compute units (two work groups each, at head size 64 three), or
 // as many rounds as keep items below kKv4Long units: a long round ends unevenly.
-// Measured (GPU time of the call, merge included): 40 requests of 8k to 32k
-// keys 565 us in one round, 560 in two to four, 585 in six; 16 requests of 1k
-// to 8k keys with branches 85 us in one round, 92 in two, 122 in three.  Equal
-// shares of a request's segments, a work group ending one and beginning the
-// next, took 73 us where these runs take 67: a second start costs more than even
-// lengths give.
+// Measured (a call, merge included): 40 requests of 8k to 32k keys 568 us in one
+// round, 493 in three, 571 in eleven, 695 in 22; 16 requests of 1k to 8k keys with
+// branches 71 us in one round, 84 in two.  Equal shares of a request's segments, a
+// work group ending one and beginning the next, took 73 us where these runs then
+// took 67: a second start costs more than even lengths give.
 // kKv4Least is two steps of a wave on one tile, or one on four: one token over
 // 4097 keys takes 12.5 us with it, 13.3 with three quarters of it, 12.6 with one
 // and a half.
@@ -308,8 +307,8 @@ rg_status run_mass(const rg_attn_layout* L, const uint16_t* q, const void* keys,
   bool wide = false;
   for (int r = 0; r < L->num_requests; ++r) wide = wide || (!many(r) && chunks(r) > 1);
   // 4-bit: the longest run that still gives every compute unit four work
-  // groups, so that a run's start is a small part of it (40 long requests take 150
-  // us so, 151 with eight, 153 with two, 310 with as many as bf16 keys give).
+  // groups, so that a run's start is a small part of it (40 long requests take 146
+  // us so, as with eight or two, 188 with as many as bf16 keys give).
   int64_t all = 0;
   for (int r = 0; r < L->num_requests; ++r)
     if (!many(r)) all += len(r) * L->num_kv_heads;

@@ -14,8 +14,8 @@
 // part of the slots: ties are taken from the lowest slot on, holes and movers get
 // their ranks from wave ballots.  It writes for every kept slot which token it
 // takes, if any.  Bound by latency: a few thousand tokens give one compute unit
-// work that 255 others cannot share.  One request of 4128 tokens 11.0 us, 16 of 1k
-// to 8k 13.5, 40 of 8k to 32k 51 (8 heads each; the start 1.2 us, the first bits 1.8,
+// work that 255 others cannot share.  One request of 4128 tokens 11.4 us, 16 of 1k
+// to 8k 13.3, 40 of 8k to 32k 50 (8 heads each; the start 1.2 us, the first bits 1.8,
 // each later pass 1.1, ranks and lists 4).  Comparing the last few hundred
 // candidates each with all, instead of further bits, took 2.0 us; copies of the
 // bins, so that fewer lanes meet in one, changed nothing.
@@ -26,7 +26,7 @@
 // at head size 64) of every unit: the wave reads its sources' units whole, all
 // at once, and moves the pieces in registers.  Bound by the lines that the pieces
 // lie in, of which a page with any hole has most: 16 requests cut to 3/4, bf16,
-// 320 MB of lines in 68 us; 40 long ones cut to half, 4-bit, 1.2 GB in 342 us.
+// 300 MB of lines in 69 us; 40 long ones cut to half, 4-bit, 1.2 GB in 342 us.
 // Pieces written one by one, without reading the page's units: 67 and 353 us.
 #include <type_traits>
 

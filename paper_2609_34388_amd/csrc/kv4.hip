@@ -13,9 +13,9 @@
 // and blocks go through LDS, where their codes change between the order of rows
 // and that of the block.  A block whose tokens are all new is written with
 // 16-byte stores; of any other only the new tokens' bytes are.  Bound by the
-// bytes, at short calls by the launch.  128 requests' steps 6.6 us in and 5.1 out;
+// bytes, at short calls by the launch.  128 requests' steps 6.6 us in and 4.9 out;
 // 28 thousand rows of 8 heads of 128 36 us in (4.1 TB/s: more reads than writes), 27
-// out (5.4 TB/s); 400 thousand rows out 409 us (5.4 TB/s; 483 with a head a work
+// out (5.4 TB/s); 400 thousand rows out 410 us (5.4 TB/s; 483 with a head a work
 // group, which starts four times as many).  Rows are written past the caches: with
 // ordinary stores the appends and evictions between them took 9 us longer.
 #include "cache_internal.h"

@@ -31,12 +31,13 @@
 // Runs of a request's keys meet in fp32 in the workspace.
 //
 // Measured (query heads / KV heads / head size 32/8/128 unless said):
-// one token over 4097 keys 8.3 us + 4.3 of the merge, bound by the chain of its
+// one token over 4097 keys 8.0 us + 4.2 of the merge, bound by the chain of its
 // start, one key tile a wave, and its end; 16 requests of 1k to 8k keys with
-// branches 67 + 10 us; 48 of up to 6k keys, heads 16/4/64, 30 + 7 us; 40 of 8k to
-// 32k keys 530 + 22 us, 700 TFLOP/s of bf16 products at 2.0 GHz, to which the
-// chip's power limit takes the clock: vector instructions fill 56 % of the
-// cycles, products 41 %.  Codes read straight into registers measured the same
+// branches 61 + 9 us; 48 of up to 6k keys, heads 16/4/64, 29 + 6 us; 40 of 8k to
+// 32k keys 471 + 21 us, 775 TFLOP/s of bf16 products at 2.0 GHz, to which the
+// chip's power limit takes the clock: vector instructions fill 59 % of the
+// cycles, products 40 %.  (After half a second of the same; after idle time calls
+// take up to 20 % longer.)  Codes read straight into registers measured the same
 // within 2 % at head size 128 and leave no registers for a second wave at 64.
 #include "cache_internal.h"
 #include "kv4_device.h"
@@ -589,7 +590,7 @@ hipError_t launch_impl(const Kv4AttnArgs& a, const Plan& p, hipStream_t stream) 
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.total_comb == 0) return e;
   // Many runs, and few enough rows to be bound by latency: one token over 26 runs
-  // takes 4.3 us so, 10.7 with a wave for each row; 40 long requests 75 and 22.
+  // takes 4.2 us so, 10.7 with a wave for each row; 40 long requests 75 and 21.
   if (p.max_chunks > 8 && p.grid_comb <= 1024)
     hipLaunchKernelGGL((kv4_merge_kernel<D, kKv4MergeParts, Plan>), dim3(p.grid_comb),
                        dim3(64 * kKv4MergeParts), 0, stream, a, p);

@@ -18,13 +18,14 @@
 // share the column tiles, whose Q comes through LDS of the wave's own.
 //
 // Measured (heads 32/8/128): 16 requests' steps over 1k to 8k bf16 keys 34 us (144 MB,
-// 4.2 TB/s); 40 over 8k to 32k 4-bit keys 150 us (532 MB, 3.6 TB/s, where a kernel
-// that only reads reaches 4.0); two prompts of 2048 and 1555 rows 106 us, 77 of
+// 4.2 TB/s); 40 over 8k to 32k 4-bit keys 146 us (531 MB, 3.6 TB/s, where a kernel
+// that only reads reaches 5.6: decoding and the columns' exponentials keep the vector
+// units busy for 43 % of the cycles); two prompts of 2048 and 1555 rows 103 us, 68 of
 // products at a large product's rate and 56 of exponentials and sums, which overlap
 // little.  Prompts through mass_kernel, Q read from LDS by each key tile anew, took
 // 406 us; the next tile's products placed between a wave's exponentials, at two
 // waves a SIMD, took 157 where the plain order then took 135; 32, 96 or 128 keys a
-// work group take 146, 106 and 110.
+// work group took 146, 106 and 110 where 64 took 106.
 #include "cache_internal.h"
 #include "kv4_device.h"
 

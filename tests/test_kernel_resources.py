@@ -77,7 +77,7 @@ def test_wide_mass_kernels_do_not_spill(tmp_path):
 
 def test_eviction_choices_share_a_compute_unit(tmp_path):
     """Two work groups of 1024 on a compute unit leave 64 vector registers each;
-    scalar registers past the 102 of a wave go to lanes of those, not to memory."""
+    scalar registers that do not fit go to lanes of those, not to memory."""
     kernels = {k: v for k, v in _kernels(tmp_path).items() if "evict_select_kernel" in k}
     spills = {4: 0, 8: 16, 16: 64, 32: 140}  # by the held slots of a thread: their masks are two words each
     for held, most in spills.items():
