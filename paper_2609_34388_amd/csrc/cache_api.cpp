@@ -296,12 +296,15 @@ rg_status run_mass(const rg_attn_layout* L, const uint16_t* q, const void* keys,
   //                     4-bit   41 / 61      56 / 67      *109 / 106   *224 / 178
   //   one of 4096 keys, bf16    *10 / 11     *13 / 12     *22 / 14     *37 / 20
   //                     4-bit   *13 / 9      *18 / 9      *30 / 11     *57 / 16
-  const int cus = device_cus();
   auto chunks = [&](int r) { return ((int64_t)L->n_verify[r] * a.g + kMassCols - 1) / kMassCols; };
   const int64_t limit = kv4 ? 4 : 8;
   int64_t groups = 0;
-  for (int r = 0; r < L->num_requests; ++r)
+  bool asked = kv4;  // whether the compute units matter: asking for them takes the host a while
+  for (int r = 0; r < L->num_requests; ++r) {
     if (chunks(r) <= limit) groups += runs(r, kMassKeys);
+    asked = asked || chunks(r) > 1;
+  }
+  const int cus = asked ? device_cus() : 1;
   const int64_t most = std::min(limit, std::max<int64_t>(1, groups / (kv4 ? 4 * cus : cus)));
   auto many = [&](int r) { return chunks(r) > most; };
   bool wide = false;

@@ -9,10 +9,11 @@
 // columns stays in the lane.  No atomics: a key's sum has one order.
 //
 // With few query columns (mass_kernel) the bytes of K bound it: up to 128 of them
-// lie in LDS, waves take key tiles; mass_wide_kernel takes more, 128 after 128.  A bf16 wave holds two key tiles, read
-// straight from the pool; four times fewer bytes of a 4-bit key would leave a
-// work group that small waiting for its start, so it takes a longer run of keys,
-// two tiles a step, with the next step's codes in flight.  With many columns
+// lie in LDS, waves take key tiles; mass_wide_kernel takes more, 128 after 128.
+// A bf16 wave holds two key tiles, read straight from the pool; four times fewer
+// bytes of a 4-bit key would leave a work group that small waiting for its start, so
+// it takes a longer run of keys, two tiles a step, with the next step's codes in
+// flight.  With many columns
 // (mass_rows_kernel, prompts) the products and exponentials bound it: a work
 // group takes 64 keys, held in registers by each of its waves, and the waves
 // share the column tiles, whose Q comes through LDS of the wave's own.
@@ -118,7 +119,7 @@ __device__ __forceinline__ void write_mass(const MassArgs& a, const MassItem& it
 
 // A run of keys over up to kMassCols columns, or with WIDE over any number of
 // them, kMassCols at a time: bf16 keys stay in registers, 4-bit ones are read
-// again (from a cache, as a run's codes are 160 KB at most) and their sums stay in LDS.
+// again (from a cache, as a run's codes are 140 KB at most) and their sums stay in LDS.
 template <int D, bool KV4, bool WIDE>
 __device__ __forceinline__ void mass_run(const MassArgs& a, const AttnPlan& p) {
   constexpr int KSTEPS = D / 16, QROW = 2 * D + 16;  // 16 bytes more: a fragment read meets every bank once
