@@ -48,6 +48,16 @@
  *   rg_evict_tokens, rg_kv4_evict_tokens
  *                              cut requests to their best-scored tokens, in place
  *
+ * and, for the rows of a step before its attention, and for layers that see a
+ * window of the context:
+ *
+ *   rg_kv_append               the rows of a step into the bf16 cache, with the
+ *                              rotation of their positions on the way (q's too)
+ *   rg_kv8_append, rg_kv8_read the same into an 8-bit paged cache, and back out
+ *   rg_kv8_attention           the step's attention over that cache
+ *   rg_window_attention        the step's attention over a sliding window of the
+ *                              bf16 cache and a few first tokens
+ *
  * Conventions shared by every entry point
  * ---------------------------------------
  * - bf16 tensors are passed as their raw 16-bit patterns (uint16_t).
@@ -648,6 +658,97 @@ rg_status rg_evict_tokens(const rg_evict_layout* layout, uint16_t* k_cache, uint
                           float* mass, int32_t* positions, void* ws, size_t ws_bytes, void* stream);
 rg_status rg_kv4_evict_tokens(const rg_evict_layout* layout, uint8_t* cache, const float* score, float* mass,
                               int32_t* positions, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Rows into the cache with the rotation of their positions
+ * ------------------------------------------------------------------------ */
+
+/*
+ * The rotation of a step's q and K rows.  A row of position p turns each pair
+ * (x, y) of its first `dims` dims, pair j with c and s the cosine and sine of
+ * p * inv_freq[j], to (x c - y s, y c + x s); dims past `dims` stay.  The angle
+ * is the exact product, c and s are fp32, and each product and sum is rounded
+ * to fp32.  Pairs are dims (j, j + dims / 2), or with `interleaved` not 0
+ * (2 j, 2 j + 1).
+ *
+ *   dims       0 .. D, a multiple of 16 (0: nothing turns)
+ *   inv_freq   DEVICE [dims / 2] fp32 (may be NULL where dims is 0)
+ *   positions  DEVICE [q_indptr[R]] int32, 0 .. 2^31 - 1, of every row, or NULL:
+ *              ctx_len[r] + i for row i of request r.  With branches, and where
+ *              tokens were evicted, a row's position is not its slot.
+ */
+typedef struct rg_rotation {
+  int32_t dims;
+  int32_t interleaved;
+  const float* inv_freq;
+  const int32_t* positions;
+} rg_rotation;
+
+/*
+ * Rows into the bf16 cache of rg_draft_verify_attention: K and V of row i of
+ * request r (rows q_indptr[r] .. q_indptr[r+1]-1) go to token ctx_len[r] + i of
+ * the request's pages, K turned by the row's position and rounded once.  Those
+ * tokens are written and no others, whatever the pages hold.  A page that rows
+ * are written to must not be in another request's list.  q, where it is given,
+ * is turned alike into q_out.
+ *
+ *   rotation  NULL: nothing turns
+ *   q         DEVICE bf16 rows [Hq][D], row j at q + j * q_stride (elements, at
+ *             least Hq * D, a multiple of 8), or NULL
+ *   q_out     DEVICE bf16 [q_indptr[R]][Hq][D], or NULL with q; may be q itself
+ *             where q_stride is Hq * D
+ *   k, v      DEVICE bf16 rows [Hkv][D], alike
+ * Pointers 16-byte aligned.  The layout's n_verify and sm_scale do not change
+ * what is written, but have to be those of a layout.
+ */
+rg_status rg_kv_append(const rg_attn_layout* layout, const rg_rotation* rotation, const uint16_t* q, int64_t q_stride,
+                       uint16_t* q_out, const uint16_t* k, int64_t k_stride, const uint16_t* v, int64_t v_stride,
+                       uint16_t* k_cache, uint16_t* v_cache, void* stream);
+
+/* ------------------------------------------------------------------------
+ * A paged KV cache in 8 bits
+ * ------------------------------------------------------------------------ */
+
+/*
+ * The cache is one pool [num_pages][num_kv_heads] of blocks of
+ * RG_KV8_BLOCK_BYTES(head_dim) bytes (16-byte aligned, contiguous), K and V of
+ * 16 tokens of one KV head, a byte an element, half of the bf16 cache's bytes;
+ * and beside it `scales` [num_pages][num_kv_heads][2] fp32, a block's scale of
+ * K and of V.  In a block lie
+ *
+ *   K  [D/32][16 tokens][32]   bytes of dims 32 i .. 32 i + 31
+ *   V  [2][D][8 tokens]        token = 8 * first + third index
+ *
+ * A byte is an e4m3 number (sign, 4 exponent bits of bias 7, 3 mantissa bits,
+ * 0x7f and 0xff NaN, no infinity: up to 448), and the element that times its
+ * block's scale, a power of two of 2^-117 .. 2^119: exact in bf16.
+ *
+ * Rows are rounded so.  A block that rows go to takes the scale 2^(e - 8) for
+ * them, e the exponent of the largest finite magnitude among the rows' elements
+ * in it, plus one where it is at least 1.75 times its power of two, the result
+ * within 2^-117 .. 2^119; or the scale it has, where that is larger and the
+ * block keeps older tokens (slots below the first new row).  Those tokens are
+ * rounded again at a scale that grew: only elements below 2^-6 of the new scale
+ * can change.  An element is the nearest number of its block, ties to the even code;
+ * magnitudes past 448 become 448, an infinity or a NaN becomes NaN, and no other
+ * element changes for it.
+ */
+#define RG_KV8_BLOCK_BYTES(head_dim) (32 * (head_dim))
+
+/*
+ * rg_kv_append into the 8-bit cache.  Arguments as there; K is rounded to the
+ * block from the turned fp32 values.  Slots behind a request's last row that lie
+ * in a page it writes to stand for other values afterwards.
+ */
+rg_status rg_kv8_append(const rg_attn_layout* layout, const rg_rotation* rotation, const uint16_t* q, int64_t q_stride,
+                        uint16_t* q_out, const uint16_t* k, int64_t k_stride, const uint16_t* v, int64_t v_stride,
+                        uint8_t* cache, float* scales, void* stream);
+
+/* The tokens ctx_len[r] .. ctx_len[r] + n_r - 1 out of the cache, as bf16 rows:
+ * the values they stand for.  A whole context is read with ctx_len 0 and q_indptr
+ * over its tokens (at most 65535 rows of a request a call). */
+rg_status rg_kv8_read(const rg_attn_layout* layout, const uint8_t* cache, const float* scales, uint16_t* k,
+                      int64_t k_stride, uint16_t* v, int64_t v_stride, void* stream);
 
 #ifdef __cplusplus
 }

@@ -55,6 +55,11 @@ class BlockPolicy(ctypes.Structure):
                 ("rho", ctypes.c_float), ("value", ctypes.c_void_p)]
 
 
+class Rotation(ctypes.Structure):
+    _fields_ = [("dims", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("inv_freq", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p)]
+
+
 class EvictLayout(ctypes.Structure):
     _fields_ = [("num_requests", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("sink", ctypes.c_int32),
@@ -86,7 +91,7 @@ EXPORTS = ("rg_abi_version", "rg_status_string", "rg_draft_verify_attention_work
            "rg_multibranch_attention_workspace", "rg_multibranch_attention", "rg_plan_branches",
            "rg_match_branches", "rg_plan_block_sizes", "rg_kv4_append", "rg_kv4_read", "rg_kv4_attention_workspace",
            "rg_kv4_attention", "rg_attention_mass", "rg_kv4_attention_mass", "rg_evict_workspace", "rg_evict_tokens",
-           "rg_kv4_evict_tokens")
+           "rg_kv4_evict_tokens", "rg_kv_append", "rg_kv8_append", "rg_kv8_read")
 
 _LIB = None
 
@@ -134,6 +139,9 @@ def _lib():
         "rg_evict_workspace": (I32, [ctypes.POINTER(EvictLayout), ctypes.POINTER(SZ)]),
         "rg_evict_tokens": (I32, [ctypes.POINTER(EvictLayout), P, P, P, P, P, P, SZ, P]),
         "rg_kv4_evict_tokens": (I32, [ctypes.POINTER(EvictLayout), P, P, P, P, P, SZ, P]),
+        "rg_kv_append": (I32, [ctypes.POINTER(AttnLayout), ctypes.POINTER(Rotation), P, I64, P, P, I64, P, I64, P, P, P]),
+        "rg_kv8_append": (I32, [ctypes.POINTER(AttnLayout), ctypes.POINTER(Rotation), P, I64, P, P, I64, P, I64, P, P, P]),
+        "rg_kv8_read": (I32, [ctypes.POINTER(AttnLayout), P, P, P, I64, P, I64, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -895,3 +903,139 @@ def kv4_evict_tokens(cache: torch.Tensor, score: torch.Tensor, positions: torch.
     _here(cache)
     args, workspace = _evict_args(score, positions, layout, mass, workspace, stream)
     _check(_lib().rg_kv4_evict_tokens(ctypes.byref(c), cache.data_ptr(), *args, _stream(stream)), "rg_kv4_evict_tokens")
+
+
+# ---------------------------------------------------------------------------
+# Rows into the cache with the rotation of their positions
+class _Rotation:
+    """Keeps the tensors alive while the C struct points at them."""
+
+    def __init__(self, inv_freq, interleaved, positions):
+        self.inv_freq = _dev(inv_freq, "inv_freq", torch.float32)
+        self.positions = None if positions is None else _dev(positions, "positions", torch.int32)
+        if inv_freq.dim() != 1 or (positions is not None and positions.dim() != 1):
+            raise ValueError("inv_freq and positions must have one dimension")
+        self.c = Rotation(2 * inv_freq.numel(), int(bool(interleaved)), inv_freq.data_ptr(), _ptr(positions))
+        self.ref = ctypes.byref(self.c)
+
+
+def make_rotation(inv_freq: torch.Tensor, *, interleaved: bool = False,
+                  positions: Optional[torch.Tensor] = None) -> _Rotation:
+    """The rotation of q and K rows (rg_rotation): inv_freq fp32 [dims / 2] on
+    the GPU, positions int32 [rows] there (None: each row's token)."""
+    return _Rotation(inv_freq, interleaved, positions)
+
+
+def _append_args(k, v, layout: _Layout, rotation: Optional[_Rotation], q, q_out, stream, *caches):
+    """Checks, and the arguments in front of the caches'."""
+    c = layout.c
+    hkv, d = c.num_kv_heads, c.head_dim
+    ks, vs = _rows(k, "k", hkv, d), _rows(v, "v", hkv, d)
+    rows = k.shape[0]
+    if v.shape[0] != rows:
+        raise ValueError("k and v must have as many rows")
+    qs = 0
+    if q is not None:
+        qs = _rows(q, "q", c.num_q_heads, d)
+        if q.shape[0] != rows:
+            raise ValueError("q and k must have as many rows")
+        if q_out is None:
+            with _pool_of(stream):
+                q_out = torch.empty(rows, c.num_q_heads, d, dtype=torch.bfloat16, device=q.device)
+        elif _dev(q_out, "q_out", torch.bfloat16).shape != q.shape:
+            raise ValueError("q_out must have q's shape")
+    elif q_out is not None:
+        raise ValueError("q_out is given without q")
+    ref = None
+    if rotation is not None:
+        if rotation.positions is not None and rotation.positions.shape[0] != rows:
+            raise ValueError("positions needs one entry per row")
+        _here(rotation.inv_freq, rotation.positions)
+        ref = rotation.ref
+    here = _check_layout(layout, rows, k, v, q, q_out, *caches)
+    on = _raw_stream(here) if stream is None and _raw_stream is not None else _stream(stream)
+    return rows, on, q_out, (ctypes.byref(c), ref, _ptr(q), qs, _ptr(q_out), k.data_ptr(), ks, v.data_ptr(), vs)
+
+
+def kv_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, layout: _Layout, *,
+              rotation: Optional[_Rotation] = None, q: Optional[torch.Tensor] = None,
+              q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """Rows k, v [rows, Hkv, D] (e.g. parts of one projection's output) into the
+    bf16 cache k_cache [pages, Hkv, 16, D], v_cache [pages, Hkv, D, 16], at the
+    tokens behind each request's context, k turned by its rows' positions
+    (rg_kv_append).  With q [rows, Hq, D], returns it turned."""
+    c = layout.c
+    for t, name, shape in ((k_cache, "k_cache", (c.num_pages, c.num_kv_heads, 16, c.head_dim)),
+                           (v_cache, "v_cache", (c.num_pages, c.num_kv_heads, c.head_dim, 16))):
+        if _dev(t, name, torch.bfloat16).shape != shape:
+            raise ValueError(f"{name} must be {list(shape)}")
+    rows, on, q_out, args = _append_args(k, v, layout, rotation, q, q_out, stream, k_cache, v_cache)
+    if rows:
+        _check(_lib().rg_kv_append(*args, k_cache.data_ptr(), v_cache.data_ptr(), on), "rg_kv_append")
+    return q_out
+
+
+# ---------------------------------------------------------------------------
+# A paged KV cache in 8 bits
+def kv8_block_bytes(head_dim: int) -> int:
+    """Bytes of K and V of 16 tokens of one KV head (RG_KV8_BLOCK_BYTES)."""
+    return 32 * head_dim
+
+
+def new_kv8_cache(num_pages: int, num_kv_heads: int, head_dim: int, device) -> Tuple[torch.Tensor, torch.Tensor]:
+    """An 8-bit cache pool, uint8 [pages, Hkv, 32 D], and its scales, fp32
+    [pages, Hkv, 2] (contents undefined)."""
+    return (torch.empty(num_pages, num_kv_heads, kv8_block_bytes(head_dim), dtype=torch.uint8, device=device),
+            torch.empty(num_pages, num_kv_heads, 2, dtype=torch.float32, device=device))
+
+
+def make_kv8_layout(num_q_heads: int, cache: torch.Tensor, q_indptr, n_verify, ctx_len, page_indptr,
+                    page_indices: torch.Tensor, sm_scale: float = 0.0) -> _Layout:
+    """make_layout for an 8-bit cache (uint8 [pages, Hkv, 32 D])."""
+    num_pages, hkv, block = cache.shape
+    if block % 32:
+        raise ValueError("cache must be [pages, Hkv, 32 D]")
+    return _Layout(num_q_heads, hkv, block // 32, num_pages, q_indptr, n_verify, ctx_len, page_indptr, page_indices,
+                   sm_scale)
+
+
+def _kv8(cache: torch.Tensor, scales: torch.Tensor, layout: _Layout) -> None:
+    c = layout.c
+    if _dev(cache, "cache", torch.uint8).shape != (c.num_pages, c.num_kv_heads, 32 * c.head_dim):
+        raise ValueError("cache must be [pages, Hkv, 32 D] of the layout's sizes")
+    if _dev(scales, "scales", torch.float32).shape != (c.num_pages, c.num_kv_heads, 2):
+        raise ValueError("scales must be [pages, Hkv, 2] of the layout's sizes")
+
+
+def kv8_append(k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor, scales: torch.Tensor, layout: _Layout, *,
+               rotation: Optional[_Rotation] = None, q: Optional[torch.Tensor] = None,
+               q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """kv_append into the 8-bit cache (rg_kv8_append).  An infinity or a NaN
+    reads as NaN."""
+    _kv8(cache, scales, layout)
+    rows, on, q_out, args = _append_args(k, v, layout, rotation, q, q_out, stream, cache, scales)
+    if rows:
+        _check(_lib().rg_kv8_append(*args, cache.data_ptr(), scales.data_ptr(), on), "rg_kv8_append")
+    return q_out
+
+
+def kv8_read(cache: torch.Tensor, scales: torch.Tensor, layout: _Layout, *, k_out: Optional[torch.Tensor] = None,
+             v_out: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The tokens kv8_append writes for this layout, as bf16 rows (rg_kv8_read)."""
+    _kv8(cache, scales, layout)
+    c = layout.c
+    shape = (layout.q_indptr.item(-1), c.num_kv_heads, c.head_dim)
+    if k_out is None or v_out is None:
+        with _pool_of(stream):
+            k_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if k_out is None else k_out
+            v_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if v_out is None else v_out
+    ks, vs = _rows(k_out, "k_out", *shape[1:]), _rows(v_out, "v_out", *shape[1:])
+    rows = k_out.shape[0]
+    if v_out.shape[0] != rows:
+        raise ValueError("k_out and v_out must have as many rows")
+    here = _check_layout(layout, rows, k_out, v_out, cache, scales)
+    if rows:
+        on = _raw_stream(here) if stream is None and _raw_stream is not None else _stream(stream)
+        _check(_lib().rg_kv8_read(ctypes.byref(c), cache.data_ptr(), scales.data_ptr(), k_out.data_ptr(), ks,
+                                  v_out.data_ptr(), vs, on), "rg_kv8_read")
+    return k_out, v_out

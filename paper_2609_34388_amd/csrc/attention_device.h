@@ -73,6 +73,17 @@ __device__ __forceinline__ uint32_t lds_place(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
 }
 
+// x over the divisor that the factor and shift stand for: exact below 2^31
+// (set_divisor in plan_common.h).
+__device__ __forceinline__ int quotient(int x, uint32_t mul, int shift) {
+  return (int)(__umulhi(2u * (uint32_t)x, mul) >> shift);
+}
+// Query row of a column.
+template <typename Args>
+__device__ __forceinline__ int row_of(const Args& a, int col) {
+  return quotient(col, a.g_mul, a.g_shift);
+}
+
 // Request r of a plan.
 __device__ __forceinline__ AttnReq request_of(const AttnPlan& p, int r) { return p.req[r]; }
 __device__ __forceinline__ AttnReqBr request_of(const AttnPlanBr& p, int r) { return p.req[r]; }

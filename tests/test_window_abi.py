@@ -1,0 +1,74 @@
+"""Refusals of rotated appends, the 8-bit cache and attention over a window:
+checked on the host before anything touches a device (no GPU)."""
+import ctypes
+import os
+
+import pytest
+
+from paper_2609_34388_amd import binding
+from test_cache_abi import BAD_LAYOUTS, NULL, ODD, SHAPE, UNSUPPORTED, L, P
+
+pytestmark = pytest.mark.skipif(not os.path.exists(binding.LIB_PATH), reason="library not built")
+
+
+def lib():
+    return binding.library()
+
+
+def rotation(dims=128, interleaved=0, inv_freq=0x1000, positions=None):
+    return ctypes.byref(binding.Rotation(dims, interleaved, inv_freq, positions))
+
+
+def append(l, rot=None, q=P, qs=1024, q_out=P, k=P, ks=256, v=P, vs=256, kc=P, vc=P):
+    a = lib().rg_kv_append(l.ref if l else None, rot, q, qs, q_out, k, ks, v, vs, kc, vc, None)
+    b = lib().rg_kv8_append(l.ref if l else None, rot, q, qs, q_out, k, ks, v, vs, kc, vc, None)
+    if vc is P:
+        assert a == b
+    return a
+
+
+def read(l, cache=P, scales=P, k=P, ks=256, v=P, vs=256):
+    return lib().rg_kv8_read(l.ref if l else None, cache, scales, k, ks, v, vs, None)
+
+
+@pytest.mark.parametrize("call", [append, read])
+def test_layout_refusals(call):
+    assert call(None) == NULL
+    for kw, want in BAD_LAYOUTS:
+        assert call(L(**kw)) == want, kw
+
+
+def test_append_refusals():
+    for name in ("q", "q_out", "k", "v", "kc", "vc"):
+        assert append(L(), **{name: None}) == NULL
+        if name != "vc":
+            assert append(L(), **{name: ODD}) == UNSUPPORTED
+    # V pages want 16 bytes, scales four
+    assert append(L(), vc=ODD) == UNSUPPORTED
+    assert lib().rg_kv8_append(L().ref, None, None, 0, None, P, 256, P, 256, P, ctypes.c_void_p(0x1002), None) == UNSUPPORTED
+    for name in ("ks", "vs"):
+        assert append(L(), **{name: 248}) == SHAPE and append(L(), **{name: -256}) == SHAPE
+        assert append(L(), **{name: 260}) == UNSUPPORTED
+    assert append(L(), qs=1016) == SHAPE and append(L(), qs=1028) == UNSUPPORTED
+    # in place only where rows lie behind one another
+    assert append(L(), qs=1032) == SHAPE
+    assert append(L(indices=0x1002)) == UNSUPPORTED
+
+
+def test_rotation_refusals():
+    assert append(L(), rot=rotation(inv_freq=None)) == NULL
+    for dims in (-16, 8, 24, 144):
+        assert append(L(), rot=rotation(dims=dims)) == SHAPE
+    assert append(L(D=64), rot=rotation(dims=80)) == SHAPE
+    assert append(L(), rot=rotation(inv_freq=0x1002)) == UNSUPPORTED
+    assert append(L(), rot=rotation(positions=0x1001)) == UNSUPPORTED
+
+
+def test_read_refusals():
+    for name in ("k", "v", "cache", "scales"):
+        assert read(L(), **{name: None}) == NULL
+    for name in ("k", "v", "cache"):
+        assert read(L(), **{name: ODD}) == UNSUPPORTED
+    assert read(L(), scales=ctypes.c_void_p(0x1002)) == UNSUPPORTED
+    assert read(L(), ks=248) == SHAPE and read(L(), vs=0) == SHAPE and read(L(), ks=257) == UNSUPPORTED
+
