@@ -750,6 +750,49 @@ rg_status rg_kv8_append(const rg_attn_layout* layout, const rg_rotation* rotatio
 rg_status rg_kv8_read(const rg_attn_layout* layout, const uint8_t* cache, const float* scales, uint16_t* k,
                       int64_t k_stride, uint16_t* v, int64_t v_stride, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Attention over a sliding window with sinks, and over the 8-bit cache
+ * ------------------------------------------------------------------------ */
+
+/*
+ * What a row sees of the keys that Eq. 1 (rg_attn_layout, or with branches
+ * rg_branch_layout) shows it: all rows of its own draft block or branch, and of
+ * the others (cached tokens and verify rows) those of positions t > p - size and
+ * those of t < sink, p its position.  A token's position is its number in the
+ * request's pages; the row i of a request's verify rows and of its draft block
+ * has position ctx_len + i, row t of a branch ctx_len + prefix + t.  (Where
+ * tokens were evicted, positions and the window count what is left.)
+ *
+ *   size  >= 1: 1 is the row itself
+ *   sink  >= 0
+ * Pages that hold no key any row of the request sees are not read: their entries
+ * in page_indices may be anything, so that their pages can go to others.
+ */
+typedef struct rg_window {
+  int32_t size;
+  int32_t sink;
+} rg_window;
+
+/*
+ * rg_draft_verify_attention (branches NULL) or rg_multibranch_attention over a
+ * window: layout, branches, q, caches, out and lse as there.  The workspace
+ * needs no initialisation.  Slots that no row sees may hold anything.
+ * RG_ERR_WORKSPACE also where the host has no memory for the plan.
+ */
+rg_status rg_window_attention_workspace(const rg_attn_layout* layout, const rg_branch_layout* branches,
+                                        const rg_window* window, size_t* bytes);
+rg_status rg_window_attention(const rg_attn_layout* layout, const rg_branch_layout* branches, const rg_window* window,
+                              const uint16_t* q, const uint16_t* k_cache, const uint16_t* v_cache, uint16_t* out, float* lse,
+                              void* ws, size_t ws_bytes, void* stream);
+
+/* The same over an 8-bit cache, K and V the values its bytes stand for; with
+ * window NULL over all keys. */
+rg_status rg_kv8_attention_workspace(const rg_attn_layout* layout, const rg_branch_layout* branches,
+                                     const rg_window* window, size_t* bytes);
+rg_status rg_kv8_attention(const rg_attn_layout* layout, const rg_branch_layout* branches, const rg_window* window,
+                           const uint16_t* q, const uint8_t* cache, const float* scales, uint16_t* out, float* lse, void* ws,
+                           size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

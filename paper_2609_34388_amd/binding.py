@@ -60,6 +60,10 @@ class Rotation(ctypes.Structure):
                 ("positions", ctypes.c_void_p)]
 
 
+class Window(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_int32), ("sink", ctypes.c_int32)]
+
+
 class EvictLayout(ctypes.Structure):
     _fields_ = [("num_requests", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("sink", ctypes.c_int32),
@@ -91,7 +95,8 @@ EXPORTS = ("rg_abi_version", "rg_status_string", "rg_draft_verify_attention_work
            "rg_multibranch_attention_workspace", "rg_multibranch_attention", "rg_plan_branches",
            "rg_match_branches", "rg_plan_block_sizes", "rg_kv4_append", "rg_kv4_read", "rg_kv4_attention_workspace",
            "rg_kv4_attention", "rg_attention_mass", "rg_kv4_attention_mass", "rg_evict_workspace", "rg_evict_tokens",
-           "rg_kv4_evict_tokens", "rg_kv_append", "rg_kv8_append", "rg_kv8_read")
+           "rg_kv4_evict_tokens", "rg_kv_append", "rg_kv8_append", "rg_kv8_read",
+           "rg_window_attention_workspace", "rg_window_attention", "rg_kv8_attention_workspace", "rg_kv8_attention")
 
 _LIB = None
 
@@ -142,6 +147,14 @@ def _lib():
         "rg_kv_append": (I32, [ctypes.POINTER(AttnLayout), ctypes.POINTER(Rotation), P, I64, P, P, I64, P, I64, P, P, P]),
         "rg_kv8_append": (I32, [ctypes.POINTER(AttnLayout), ctypes.POINTER(Rotation), P, I64, P, P, I64, P, I64, P, P, P]),
         "rg_kv8_read": (I32, [ctypes.POINTER(AttnLayout), P, P, P, I64, P, I64, P]),
+        "rg_window_attention_workspace": (I32, [ctypes.POINTER(AttnLayout), ctypes.POINTER(BranchLayout),
+                                                ctypes.POINTER(Window), ctypes.POINTER(SZ)]),
+        "rg_window_attention": (I32, [ctypes.POINTER(AttnLayout), ctypes.POINTER(BranchLayout), ctypes.POINTER(Window),
+                                      P, P, P, P, P, P, SZ, P]),
+        "rg_kv8_attention_workspace": (I32, [ctypes.POINTER(AttnLayout), ctypes.POINTER(BranchLayout),
+                                             ctypes.POINTER(Window), ctypes.POINTER(SZ)]),
+        "rg_kv8_attention": (I32, [ctypes.POINTER(AttnLayout), ctypes.POINTER(BranchLayout), ctypes.POINTER(Window),
+                                   P, P, P, P, P, P, SZ, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -1039,3 +1052,91 @@ def kv8_read(cache: torch.Tensor, scales: torch.Tensor, layout: _Layout, *, k_ou
         _check(_lib().rg_kv8_read(ctypes.byref(c), cache.data_ptr(), scales.data_ptr(), k_out.data_ptr(), ks,
                                   v_out.data_ptr(), vs, on), "rg_kv8_read")
     return k_out, v_out
+
+
+# ---------------------------------------------------------------------------
+# Attention over a sliding window with sinks, and over the 8-bit cache
+def make_window(size: int, sink: int = 0) -> Window:
+    """The latest `size` positions up to a row's own, and the first `sink` (rg_window)."""
+    return Window(int(size), int(sink))
+
+
+def _window_args(layout: _Layout, branches: Optional[_Branches], window: Optional[Window]):
+    if branches is not None and branches.branch_indptr.shape[0] != layout.ctx_len.shape[0] + 1:
+        raise ValueError("branch_indptr must have num_requests + 1 entries")
+    return (ctypes.byref(layout.c), ctypes.byref(branches.c) if branches is not None else None,
+            ctypes.byref(window) if window is not None else None)
+
+
+def _window_workspace_bytes(name: str, layout, branches, window) -> int:
+    n = ctypes.c_size_t(0)
+    _check(getattr(_lib(), name)(*_window_args(layout, branches, window), ctypes.byref(n)), name)
+    return int(n.value)
+
+
+def _window_call(name: str, q, caches, layout: _Layout, branches, window, out, lse, want_lse, workspace, stream):
+    c = layout.c
+    if _dev(q, "q", torch.bfloat16).dim() != 3 or q.shape[1] != c.num_q_heads or q.shape[2] != c.head_dim:
+        raise ValueError("q must be [rows, Hq, D] of the layout's sizes")
+    rows = q.shape[0]
+    if out is None or (lse is None and want_lse):
+        with _pool_of(stream):
+            out = torch.empty_like(q) if out is None else out
+            if lse is None and want_lse:
+                lse = torch.empty(rows, q.shape[1], dtype=torch.float32, device=q.device)
+    if _dev(out, "out", torch.bfloat16).shape != q.shape:
+        raise ValueError("out must have q's shape")
+    if lse is not None and _dev(lse, "lse", torch.float32).shape != q.shape[:2]:
+        raise ValueError("lse must be [rows, Hq]")
+    here = _check_layout(layout, rows, q, out, lse, workspace, *caches)
+    args = _window_args(layout, branches, window)
+    if rows == 0:
+        return out, lse
+    if workspace is None:  # the call itself checks the size of one that is given
+        need = _window_workspace_bytes(name + "_workspace", layout, branches, window)
+        if need:
+            with _pool_of(stream):
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    on = _raw_stream(here) if stream is None and _raw_stream is not None else _stream(stream)
+    _check(getattr(_lib(), name)(*args, q.data_ptr(), *(t.data_ptr() for t in caches), out.data_ptr(), _ptr(lse),
+                                 _ptr(workspace), ws_bytes, on), name)
+    return out, lse
+
+
+def window_attention_workspace_bytes(layout: _Layout, window: Window, branches: Optional[_Branches] = None) -> int:
+    return _window_workspace_bytes("rg_window_attention_workspace", layout, branches, window)
+
+
+def window_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, layout: _Layout, window: Window,
+                     branches: Optional[_Branches] = None, *, out: Optional[torch.Tensor] = None,
+                     lse: Optional[torch.Tensor] = None, want_lse: bool = True,
+                     workspace: Optional[torch.Tensor] = None,
+                     stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """draft_verify_attention, or with branches multibranch_attention, over a
+    sliding window with sinks (rg_window_attention)."""
+    c = layout.c
+    if _dev(k_cache, "k_cache", torch.bfloat16).shape != (c.num_pages, c.num_kv_heads, 16, c.head_dim):
+        raise ValueError("k_cache must be [pages, Hkv, 16, D] of the layout's sizes")
+    if _dev(v_cache, "v_cache", torch.bfloat16).shape != (c.num_pages, c.num_kv_heads, c.head_dim, 16):
+        raise ValueError("v_cache must be [pages, Hkv, D, 16] of the layout's sizes")
+    return _window_call("rg_window_attention", q, (k_cache, v_cache), layout, branches, window, out, lse, want_lse,
+                        workspace, stream)
+
+
+def kv8_attention_workspace_bytes(layout: _Layout, branches: Optional[_Branches] = None, *,
+                                  window: Optional[Window] = None) -> int:
+    return _window_workspace_bytes("rg_kv8_attention_workspace", layout, branches, window)
+
+
+def kv8_attention(q: torch.Tensor, cache: torch.Tensor, scales: torch.Tensor, layout: _Layout,
+                  branches: Optional[_Branches] = None, *, window: Optional[Window] = None,
+                  out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = True,
+                  workspace: Optional[torch.Tensor] = None,
+                  stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """draft_verify_attention, or with branches multibranch_attention, over an
+    8-bit cache, over all keys or a window (rg_kv8_attention); the layout from
+    make_kv8_layout."""
+    _kv8(cache, scales, layout)
+    return _window_call("rg_kv8_attention", q, (cache, scales), layout, branches, window, out, lse, want_lse, workspace,
+                        stream)

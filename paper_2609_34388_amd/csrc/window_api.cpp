@@ -1,6 +1,10 @@
 // C ABI of rotated appends, the 8-bit KV cache and attention over a window:
 // argument validation, planning and launches.  As in api.cpp the plans travel
 // in the kernel arguments; nothing is uploaded or synchronised.
+#include <new>
+#include <numeric>
+#include <vector>
+
 #include "plan_common.h"
 #include "window_internal.h"
 
@@ -92,6 +96,196 @@ rg_status run_append(const rg_attn_layout* L, const rg_rotation* R, const uint16
   });
 }
 
+// ---------------------------------------------------------------------------
+template <typename Plan>
+struct FullPlan {
+  std::vector<Plan> launches;
+  bool narrow = false;
+  size_t ml_offset = 0, ws_bytes = 0;
+};
+
+// Limits of the window; without one, all keys.
+struct Limits {
+  int size, sink;
+};
+constexpr int kAllKeys = 1 << 30;
+Limits limits_of(const rg_window* W) {
+  if (W == nullptr) return {kAllKeys, 0};
+  return {std::min(W->size, kAllKeys), std::min(W->sink, kAllKeys)};
+}
+rg_status validate_window(const rg_window* W) {
+  return W != nullptr && (W->size < 1 || W->sink < 0) ? RG_ERR_SHAPE : RG_OK;
+}
+
+// A request's column groups of up to `waves` tiles, and the keys of the longest.
+struct Groups {
+  int64_t count = 0, tiles = 0, per = 0;  // groups, tiles in all, tiles of a group at most
+  int64_t steps = 0;                      // buffers of the longest
+};
+template <bool BR>
+Groups groups_of(const rg_attn_layout* L, int r, Limits w, int waves) {
+  Groups q;
+  const int n = L->q_indptr[r + 1] - L->q_indptr[r], g = L->num_q_heads / L->num_kv_heads;
+  if (n == 0) return q;
+  const int64_t M = (int64_t)n * g;
+  q.tiles = (M + 31) / 32;
+  q.count = (q.tiles + waves - 1) / waves;
+  q.per = (q.tiles + q.count - 1) / q.count;
+  q.count = (q.tiles + q.per - 1) / q.per;
+  int keys = 0;
+  for (int64_t k = 0; k < q.count; ++k) {
+    const int64_t c0 = k * q.per * 32, c1 = std::min(M, (k + 1) * q.per * 32);
+    const WindowSpan s = window_span<BR>(L->ctx_len[r], L->n_verify[r], n, (int)(c0 / g), (int)((c1 - 1) / g) + 1, w.size, w.sink);
+    keys = std::max(keys, s.keys);
+  }
+  q.steps = (keys + window_keys(waves, L->head_dim) - 1) / window_keys(waves, L->head_dim);
+  return q;
+}
+
+// Time of a buffer of an item with this many tiles, in quarters of that of a
+// buffer at the copy rate.
+int64_t step_cost(int64_t tiles) { return std::max<int64_t>(4, tiles); }
+
+template <typename Plan, int MaxReq>
+rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits w, FullPlan<Plan>& fp) {
+  constexpr bool BR = __is_same(Plan, WindowPlanBr);
+  const int R = L->num_requests, hkv = L->num_kv_heads, cus = device_cus();
+  std::vector<Groups> groups(R);
+  int64_t widest = 0;
+  for (int r = 0; r < R; ++r) {
+    groups[r] = groups_of<BR>(L, r, w, kWindowWaves / 2);
+    widest = std::max(widest, groups[r].tiles);
+  }
+  fp.narrow = widest <= kWindowWaves / 2;
+  const int waves = fp.narrow ? kWindowWaves / 2 : kWindowWaves, keys = window_keys(waves, L->head_dim);
+  if (!fp.narrow)
+    for (int r = 0; r < R; ++r) groups[r] = groups_of<BR>(L, r, w, waves);
+  // Cost of an item at most: the least that gives one round of items.
+  const int64_t slots = (int64_t)cus * (fp.narrow ? 2 : 1);
+  int64_t work = 0, least = 0;
+  for (const Groups& q : groups) {
+    work += q.count * hkv * q.steps * step_cost(q.per);
+    least += q.count * hkv;
+  }
+  auto runs_of = [&](const Groups& q, int64_t target) {
+    const int64_t most = std::max<int64_t>(1, target / step_cost(q.per));  // steps of a run at most
+    const int64_t n = (q.steps + most - 1) / most, each = (q.steps + n - 1) / n;
+    return (q.steps + each - 1) / each;
+  };
+  int64_t target = std::max<int64_t>(8, work / slots);
+  for (;; target += 1 + target / 16) {
+    int64_t items = 0;
+    for (const Groups& q : groups)
+      if (q.count) items += q.count * hkv * runs_of(q, target);
+    if (items <= std::max(least, slots)) break;
+  }
+  // Costliest work items first.
+  std::vector<int> order(R);
+  std::iota(order.begin(), order.end(), 0);
+  std::vector<int64_t> cost(R, 0);
+  for (int r = 0; r < R; ++r) {
+    const Groups& q = groups[r];
+    if (q.count) cost[r] = (q.steps + runs_of(q, target) - 1) / runs_of(q, target) * step_cost(q.per);
+  }
+  std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return cost[x] > cost[y]; });
+  int64_t most_part = 0;
+  for (int r0 = 0; r0 < R; r0 += MaxReq) {
+    Plan p;
+    std::memset(&p, 0, sizeof(p));
+    p.num_req = std::min(MaxReq, R - r0);
+    int64_t items = 0, part = 0, comb = 0;
+    for (int k = 0; k < p.num_req; ++k) {
+      const int r = order[r0 + k];
+      const Groups& q = groups[r];
+      auto& x = p.req[k];
+      if constexpr (BR) pack_branches(B, r, x.br, x.rep);
+      x.q_start = L->q_indptr[r];
+      x.ctx = L->ctx_len[r];
+      x.nv = (int32_t)((uint32_t)(L->q_indptr[r + 1] - L->q_indptr[r]) | ((uint32_t)L->n_verify[r] << 16));
+      x.page_start = L->page_indptr[r];
+      x.item_start = (int32_t)items;
+      x.part_start = (int32_t)part;
+      x.comb_start = (int32_t)comb;
+      if (q.count == 0) continue;
+      const int64_t nch = runs_of(q, target);
+      x.nch = (int32_t)nch;
+      x.run = (int32_t)((q.steps + nch - 1) / nch * keys);
+      items += hkv * q.count * nch;
+      if (nch > 1) {
+        p.max_chunks = std::max(p.max_chunks, x.nch);
+        part += hkv * nch * q.tiles;
+        comb += hkv * q.tiles * (L->head_dim / 8);
+      }
+      if (items > INT32_MAX / 2 || part > INT32_MAX / 64 || comb > INT32_MAX / 2) return RG_ERR_UNSUPPORTED;
+    }
+    p.req[p.num_req].item_start = p.total_items = (int32_t)items;
+    p.req[p.num_req].part_start = (int32_t)part;
+    p.req[p.num_req].comb_start = p.total_comb = (int32_t)comb;
+    p.grid_items = (int32_t)round_up(items, 8);
+    if (!fits_launch(items, 64 * waves) || !fits_launch(comb, 64 * kWindowMergeWaves)) return RG_ERR_UNSUPPORTED;
+    most_part = std::max(most_part, part);
+    if (items > 0) fp.launches.push_back(p);
+  }
+  fp.ml_offset = align256((size_t)most_part * 32 * L->head_dim * sizeof(float));
+  fp.ws_bytes = most_part ? fp.ml_offset + align256((size_t)most_part * 32 * 2 * sizeof(float)) : 0;
+  return RG_OK;
+}
+
+// Calls f(plan) with the plan of a layout and its branches (or NULL).
+template <typename F>
+rg_status with_window_plan(const rg_attn_layout* L, const rg_branch_layout* B, const rg_window* W, F f) try {
+  rg_status st = validate_layout(L);
+  if (st == RG_OK) st = validate_window(W);
+  if (st != RG_OK) return st;
+  if (B == nullptr) {
+    FullPlan<WindowPlan> fp;
+    st = plan_window<WindowPlan, kMaxWindowReq>(L, nullptr, limits_of(W), fp);
+    return st != RG_OK ? st : f(fp);
+  }
+  st = validate_branches(L, B);
+  if (st != RG_OK) return st;
+  FullPlan<WindowPlanBr> fp;
+  st = plan_window<WindowPlanBr, kMaxWindowReqBr>(L, B, limits_of(W), fp);
+  return st != RG_OK ? st : f(fp);
+} catch (const std::bad_alloc&) {  // nothing is launched before a plan is whole
+  return RG_ERR_WORKSPACE;
+}
+
+rg_status run_attention(const rg_attn_layout* L, const rg_branch_layout* B, const rg_window* W, const uint16_t* q,
+                        const void* k_cache, const void* v_cache, const float* scales, bool kv8, uint16_t* out, float* lse,
+                        void* ws, size_t ws_bytes, void* stream) {
+  return with_window_plan(L, B, W, [&](const auto& fp) -> rg_status {
+    if (!q || !k_cache || !out || (kv8 ? !scales : !v_cache)) return RG_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(scales, 4) || !aligned(out, 16) ||
+        !aligned(lse, 4) || !aligned(L->page_indices, 4))
+      return RG_ERR_UNSUPPORTED;
+    if (fp.ws_bytes > 0 && (ws == nullptr || ws_bytes < fp.ws_bytes || !aligned(ws, 16))) return RG_ERR_WORKSPACE;
+    WindowArgs a;
+    a.q = q;
+    a.k_cache = static_cast<const uint8_t*>(k_cache);
+    a.v_cache = static_cast<const uint8_t*>(v_cache);
+    a.scales = scales;
+    a.out = out;
+    a.lse = lse;
+    a.page_indices = L->page_indices;
+    a.part_o = fp.ws_bytes ? static_cast<float*>(ws) : nullptr;
+    a.part_ml = fp.ws_bytes ? reinterpret_cast<float*>(static_cast<char*>(ws) + fp.ml_offset) : nullptr;
+    a.hq = L->num_q_heads;
+    a.hkv = L->num_kv_heads;
+    a.g = a.hq / a.hkv;
+    set_divisor(a.g, a.g_mul, a.g_shift);
+    const Limits w = limits_of(W);
+    a.size = w.size;
+    a.sink = w.sink;
+    a.sm_scale = softmax_scale(L);
+    a.scale_log2 = a.sm_scale * 1.4426950408889634f;
+    for (const auto& p : fp.launches)
+      if (launch_window_attention(a, p, L->head_dim, kv8, fp.narrow, static_cast<hipStream_t>(stream)) != hipSuccess)
+        return RG_ERR_HIP;
+    return RG_OK;
+  });
+}
+
 }  // namespace
 
 extern "C" {
@@ -134,6 +328,34 @@ rg_status rg_kv8_read(const rg_attn_layout* layout, const uint8_t* cache, const 
     p.chunk = heads;
     return launch_kv8_read(a, p, layout->head_dim, static_cast<hipStream_t>(stream));
   });
+}
+
+rg_status rg_kv8_attention_workspace(const rg_attn_layout* layout, const rg_branch_layout* branches,
+                                     const rg_window* window, size_t* bytes) {
+  if (bytes == nullptr) return RG_ERR_NULL;
+  return with_window_plan(layout, branches, window, [&](const auto& fp) {
+    *bytes = fp.ws_bytes;
+    return RG_OK;
+  });
+}
+
+rg_status rg_kv8_attention(const rg_attn_layout* layout, const rg_branch_layout* branches, const rg_window* window,
+                           const uint16_t* q, const uint8_t* cache, const float* scales, uint16_t* out, float* lse, void* ws,
+                           size_t ws_bytes, void* stream) {
+  return run_attention(layout, branches, window, q, cache, nullptr, scales, true, out, lse, ws, ws_bytes, stream);
+}
+
+rg_status rg_window_attention_workspace(const rg_attn_layout* layout, const rg_branch_layout* branches,
+                                        const rg_window* window, size_t* bytes) {
+  if (bytes == nullptr || window == nullptr) return RG_ERR_NULL;
+  return rg_kv8_attention_workspace(layout, branches, window, bytes);
+}
+
+rg_status rg_window_attention(const rg_attn_layout* layout, const rg_branch_layout* branches, const rg_window* window,
+                              const uint16_t* q, const uint16_t* k_cache, const uint16_t* v_cache, uint16_t* out, float* lse,
+                              void* ws, size_t ws_bytes, void* stream) {
+  if (window == nullptr) return RG_ERR_NULL;
+  return run_attention(layout, branches, window, q, k_cache, v_cache, nullptr, false, out, lse, ws, ws_bytes, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,583 @@
+// Hybrid-mask attention over a sliding window with sinks, or over all keys, of
+// a bf16 or an 8-bit paged cache (gfx950).
+//
+// The mathematics is that of attention.hip: S^T = K Q^T, P = exp2 of the scaled
+// scores less a running reference, O^T += V^T P^T, in matrix instructions with
+// columns (query row, query head) of a KV head.  A row of position p sees, of the
+// keys before its own draft block or branch, those of positions > p - size and <
+// sink.  A column group visits only the keys that one of its rows may see
+// (window_span): the sinks' pages, then those from its first row's window on; keys
+// are counted without the gap between, and limits moved alike.  So a group of a
+// prompt reads its window, not the context, and no key behind its last row.
+//
+// Keys pass through LDS, a buffer at a time and two buffers of LDS, as bf16 in the
+// layout of attention.hip: all waves load their share of the next buffers into
+// registers, ahead of the buffer that is computed, and put it into LDS before the
+// one barrier of a buffer.  8-bit codes are decoded on that way, once for all
+// columns (a conversion makes two bf16 and applies the block's scale; the values are
+// exact).  V of slots that no row may see, which can hold anything, is put in as zero.
+//
+// Softmax online in base 2; the product takes P rounded to bf16 (off by at most
+// 2^-8 of each term, as the output's own rounding).  Two sums run in fp32: of P,
+// for the lse, and of the rounded P, by which the product is divided, so that the
+// weights add up to one.  Runs of a request's keys meet in fp32 in the workspace.
+#include "kv8_device.h"
+#include "window_internal.h"
+
+namespace rg {
+namespace {
+
+// How a cache's pages become K and V of a buffer in LDS.  A 16-byte unit of a page
+// and head is `w`, of UNITS<D>.
+struct Bf16Cache {
+  static constexpr bool KV8 = false;
+  static constexpr int DEPTH = 1;  // buffers in flight
+  template <int D>
+  static constexpr int UNITS = 2 * D;
+};
+struct Kv8Cache {
+  static constexpr bool KV8 = true;
+  static constexpr int DEPTH = 2;
+  template <int D>
+  static constexpr int UNITS = D;
+};
+
+// Swizzle of the two 16-byte halves of a dimension row of a V page in LDS.
+__device__ __forceinline__ int vswz(int d) { return ((d >> 2) ^ (d >> 3)) & 1; }
+
+template <int D, int NW>
+struct WindowShape {
+  static constexpr int DT = D / 32;
+  static constexpr int KEYS = window_keys(NW, D);
+  static constexpr int PAGES = KEYS / kPageSize;
+  static constexpr int BUF = KEYS * D * 2;          // bytes of K, or V, of a buffer
+  static constexpr int STATE = 64 * 16 * DT + 192;  // floats of a wave's state
+  static constexpr int LDS = 4 * BUF > NW * STATE * 4 ? 4 * BUF : NW * STATE * 4;
+};
+
+template <typename Cache, int D, int NW, typename Plan>
+__global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, Plan p) {
+  using S = WindowShape<D, NW>;
+  constexpr bool BR = __is_same(Plan, WindowPlanBr);
+  constexpr int DT = S::DT, KSTEPS = D / 16, NCH = D / 8, THREADS = 64 * NW;
+  constexpr int UNITS = Cache::template UNITS<D>;
+  constexpr int PER = S::PAGES * UNITS / THREADS;  // units of K, and of V, of a thread and buffer
+  constexpr int STEP = THREADS / UNITS;            // pages between two of them
+  constexpr int PAGE_LDS = 32 * D;                 // bytes of K, or V, of a page in LDS
+  static_assert(STEP >= 1 && PER * STEP == S::PAGES && UNITS % 64 == 0, "a wave's unit is of one page");
+  __shared__ __attribute__((aligned(16))) char lds[S::LDS];
+
+  const int item = p.num_req == 1 ? xcd_item(p.grid_items) : (int)blockIdx.x;
+  if (item >= p.total_items) return;
+  const int r = find_request(p, item, false);
+  const auto rq = p.req[r];
+  const int n = rq.nv & 0xffff, nver = (int)((uint32_t)rq.nv >> 16), L = rq.ctx;
+  const int g = a.g, M = n * g, tiles = (M + 31) / 32;
+  const int ncg = (tiles + NW - 1) / NW, tpg = (tiles + ncg - 1) / ncg;
+  // Items of a request: runs, then KV heads, then column groups, so that the
+  // groups of a head, which share most keys, follow on one XCD (8 KV heads).
+  int local = item - rq.item_start, c = 0;
+  if (rq.nch > 1) {
+    c = local % rq.nch;
+    local /= rq.nch;
+  }
+  const int cg = local / a.hkv, hk = local - cg * a.hkv;
+  const int tile0 = cg * tpg, nct = min(tpg, tiles - tile0);
+  const int row0 = row_of(a, tile0 * 32), row1 = row_of(a, min(M, (tile0 + nct) * 32) - 1) + 1;
+  const WindowSpan span = window_span<BR>(L, nver, n, row0, row1, a.size, a.sink);
+  const int kbeg = c * rq.run, kend = min(span.keys, kbeg + rq.run);
+
+  const int tid = threadIdx.x, lane = tid & 63, lc = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  // A wave's column tile ct and key group kgi of kg: up to 4 tiles share the waves
+  // evenly, of 5 to 7 the first four have a wave each and the others share four.
+  int ct, kg, kgi, first, apart;  // the tile's waves: first, first + apart, ...
+  if (NW == 4 || nct <= 4) {
+    apart = nct <= 1 ? 1 : nct <= 2 ? 2 : 4;
+    ct = wave % apart;
+    kg = NW / apart;
+    kgi = wave / apart;
+    first = ct;
+  } else if (wave < 4 || nct == 8) {
+    ct = first = wave;
+    kg = apart = 1;
+    kgi = 0;
+  } else if (nct == 7) {
+    ct = min(wave, 6);
+    kg = wave < 6 ? 1 : 2;
+    kgi = wave < 6 ? 0 : wave - 6;
+    first = ct;
+    apart = 1;
+  } else {
+    kg = 4 / (nct - 4);
+    ct = 4 + (wave - 4) / kg;
+    kgi = (wave - 4) % kg;
+    first = wave - kgi;
+    apart = 1;
+  }
+  const int col = (tile0 + ct) * 32 + lc;
+  const bool on = ct < nct, valid = on && col < M;
+  const int tok = valid ? row_of(a, col) : 0, hh = col - tok * g;
+
+  // ---- copies
+  typedef const int32_t __attribute__((address_space(4))) * cpage_ptr;
+  typedef const float __attribute__((address_space(4))) * cscale_ptr;
+  const cpage_ptr pages = (cpage_ptr)(a.page_indices + rq.page_start);
+  const int page0 = kbeg / kPageSize, last_page = max((kend - 1) / kPageSize, 0);
+  const int head_pages = span.head / kPageSize, gap_pages = span.gap / kPageSize;
+  const int my_page = wave * 64 / UNITS, w = tid % UNITS;
+  const size_t page_bytes = (size_t)a.hkv * UNITS * 16 * (Cache::KV8 ? 2 : 1), head_bytes = page_bytes / a.hkv;
+  const uint8_t* kbase = a.k_cache + (size_t)hk * head_bytes + 16 * w;
+  const uint8_t* vbase = (Cache::KV8 ? a.k_cache + 16 * D : a.v_cache) + (size_t)hk * head_bytes + 16 * w;
+  // Places of unit w in a page's K and V in LDS (an 8-bit unit becomes two).
+  int kat[Cache::KV8 ? 2 : 1], vat[Cache::KV8 ? 2 : 1], vkey;  // vkey: first key of V's unit
+  if constexpr (Cache::KV8) {
+    const int slot = w % 32 / 2, ch = 4 * (w / 32) + 2 * (w & 1);
+    kat[0] = slot * 2 * D + 16 * (ch ^ (swap23(slot) & (NCH - 1)));
+    kat[1] = slot * 2 * D + 16 * ((ch + 1) ^ (swap23(slot) & (NCH - 1)));
+    const int d = 2 * (w % (D / 2)), half = w / (D / 2);
+    vat[0] = d * 32 + 16 * (half ^ vswz(d));
+    vat[1] = (d + 1) * 32 + 16 * (half ^ vswz(d + 1));
+    vkey = 8 * half;
+  } else {
+    const int slot = w / NCH, ch = w % NCH;
+    kat[0] = slot * 2 * D + 16 * (ch ^ (swap23(slot) & (NCH - 1)));
+    const int d = w / 2, half = w & 1;
+    vat[0] = d * 32 + 16 * (half ^ vswz(d));
+    vkey = 8 * half;
+  }
+  struct Set {
+    u32x4 k[PER], v[PER];
+    float ks[PER], vs[PER];
+  };
+  // Pages of this wave's units of buffer s; past the run's last page that page again.
+  auto pages_of = [&](int s, int (&pg)[PER]) {
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      const int at = min(page0 + s * S::PAGES + my_page + e * STEP, last_page);
+      pg[e] = pages[at < head_pages ? at : at + gap_pages];
+    }
+  };
+  auto load = [&](const int (&pg)[PER], Set& x) {
+#pragma unroll
+    for (int e = 0; e < PER; ++e) x.k[e] = *(const u32x4*)(kbase + (size_t)pg[e] * page_bytes);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) x.v[e] = *(const u32x4*)(vbase + (size_t)pg[e] * page_bytes);
+    if constexpr (Cache::KV8) {
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        const cscale_ptr at = (cscale_ptr)(a.scales + 2 * ((size_t)pg[e] * a.hkv + hk));
+        x.ks[e] = at[0];
+        x.vs[e] = at[1];
+      }
+    }
+  };
+  auto store = [&](int s, const Set& x) {
+    char* kd = lds + (s & 1) * S::BUF + my_page * PAGE_LDS;
+    char* vd = lds + (2 + (s & 1)) * S::BUF + my_page * PAGE_LDS;
+    const int k0 = kbeg + s * S::KEYS;
+    // V of slots behind the last key, and of those between the sinks and every window, is zero
+    const bool edge = k0 + S::KEYS > kend || (k0 < span.lo && k0 + S::KEYS > a.sink);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      const int to = e * STEP * PAGE_LDS;
+      u32x4 v[2];
+      if constexpr (Cache::KV8) {
+        *(u32x4*)(kd + to + kat[0]) = decode8_8(x.k[e][0], x.k[e][1], x.ks[e]);
+        *(u32x4*)(kd + to + kat[1]) = decode8_8(x.k[e][2], x.k[e][3], x.ks[e]);
+        v[0] = decode8_8(x.v[e][0], x.v[e][1], x.vs[e]);
+        v[1] = decode8_8(x.v[e][2], x.v[e][3], x.vs[e]);
+      } else {
+        *(u32x4*)(kd + to + kat[0]) = x.k[e];
+        v[0] = x.v[e];
+      }
+      if (edge) {
+        const int key = k0 + (my_page + e * STEP) * kPageSize + vkey;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          auto seen = [&](int k) { return k < kend && (k < a.sink || k >= span.lo); };
+          const uint32_t keep = (seen(key + 2 * i) ? 0xffffu : 0u) | (seen(key + 2 * i + 1) ? 0xffff0000u : 0u);
+          v[0][i] &= keep;
+          if (Cache::KV8) v[1][i] &= keep;
+        }
+      }
+      *(u32x4*)(vd + to + vat[0]) = v[0];
+      if constexpr (Cache::KV8) *(u32x4*)(vd + to + vat[1]) = v[1];
+    }
+  };
+
+  // ---- columns
+  bf16x8 qf[KSTEPS];
+  {
+    const uint16_t* qrow = a.q + ((size_t)(rq.q_start + tok) * a.hq + hk * g + hh) * D;
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s) {
+      u32x4 x = {0u, 0u, 0u, 0u};
+      if (valid) x = *(const u32x4*)(qrow + s * 16 + 8 * lh);
+      qf[s] = __builtin_bit_cast(bf16x8, x);
+    }
+  }
+  // Limits of the column: keys lo .. lim - 1 and below the sink, and slo .. shi - 1.
+  int lim, slo, shi, lo;
+  if constexpr (BR) {
+    key_limits(static_cast<const AttnReqBr&>(rq), valid, tok, INT_MAX, lim, slo, shi);
+    // a branch row's position: the kept prefix and its place in the branch
+    lo = tok < nver ? lim - a.size : min(lim, lim + (L + tok - slo) + 1 - a.size);
+    slo -= span.gap;
+    shi -= span.gap;
+  } else {
+    key_limits(static_cast<const AttnReq&>(rq), valid, tok, INT_MAX, lim, slo, shi);
+    lo = tok < nver ? lim - a.size : min(L + nver, L + tok + 1 - a.size);
+  }
+  lim -= span.gap;
+  lo = max(lo - span.gap, 0);
+  if (lo <= a.sink) lo = 0;
+  if (!valid) lim = lo = slo = shi = 0;
+  // Over the wave: below min_lim no column has an upper limit, from max_lo on none a
+  // lower one; nobody sees keys from `end` on, or of sink .. min_lo - 1.
+  int min_lim = valid ? lim : INT_MAX, max_lo = lo, min_lo = valid ? lo : INT_MAX, end = max(lim, shi);
+  for (int off = 32; off >= 1; off >>= 1) {
+    min_lim = min(min_lim, __shfl_xor(min_lim, off));
+    max_lo = max(max_lo, __shfl_xor(max_lo, off));
+    min_lo = min(min_lo, __shfl_xor(min_lo, off));
+    end = max(end, __shfl_xor(end, off));
+  }
+  min_lim = __builtin_amdgcn_readfirstlane(min_lim);
+  max_lo = __builtin_amdgcn_readfirstlane(max_lo);
+  min_lo = __builtin_amdgcn_readfirstlane(min_lo);
+  end = __builtin_amdgcn_readfirstlane(min(end, kend));
+
+  f32x16 acc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+    for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
+  float m_run = kNegInf, l_run = 0.f, r_run = 0.f;  // reference, sum of P, of the rounded P
+  bool open = true;                                 // some column has no reference yet
+  const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+
+  // Byte of this lane's K fragment ks inside a 32-key sub-tile: row swap23(lc),
+  // 16-byte chunk (2 ks + lh) ^ (lc % NCH) = 2 (ks ^ kw) + kb.
+  const int kx = lc & (NCH - 1), kw = kx >> 1;
+  const uint32_t krow = (uint32_t)(swap23(lc) * D * 2 + ((lh ^ (kx & 1)) * 16));
+
+  auto sub_tile = [&](const char* kt, const char* vt, int kbase) {
+    f32x16 sc;
+    {
+      bf16x8 kf[KSTEPS];
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) kf[ks] = *(const bf16x8*)(kt + krow + ((ks ^ kw) << 5));
+      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], sc, 0, 0, 0);
+    }
+    // key - kbase = 8 lh + place, place a constant of i
+    if (kbase + 32 > min_lim) {
+      const int seen = lim - kbase - 8 * lh, from = slo - kbase - 8 * lh, to = shi - kbase - 8 * lh;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int place = 16 * (i >> 3) + 4 * ((i >> 2) & 1) + (i & 3);
+        if (place >= seen && (!BR || place < from || place >= to)) sc[i] = kNegInf;
+      }
+    }
+    if (kbase < max_lo && kbase + 32 > a.sink) {
+      const int hidden = a.sink - kbase - 8 * lh, seen = lo - kbase - 8 * lh;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int place = 16 * (i >> 3) + 4 * ((i >> 2) & 1) + (i & 3);
+        if (place >= hidden && place < seen) sc[i] = kNegInf;
+      }
+    }
+    // P against the running reference, a maximum of earlier scores.  A sum of a
+    // lane's 16 past 2^12 (overflow included), or a column without a reference,
+    // moves the references to the maxima of this tile: P stays below 2^12, and no
+    // maximum is taken where nothing moves.
+    float sum, rsum;
+    u32x4 pk[2];
+    auto weigh = [&]() {
+      const float mc = (m_run == kNegInf) ? 0.f : m_run * a.scale_log2;
+      sum = rsum = 0.f;
+#pragma unroll
+      for (int pp = 0; pp < 2; ++pp)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[8 * pp + 2 * e], a.scale_log2, -mc));
+          const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[8 * pp + 2 * e + 1], a.scale_log2, -mc));
+          sum += x + y;
+          const uint32_t xy = pack_bf16x2(x, y);
+          rsum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, xy), ones, rsum, false);
+          pk[pp][e] = xy;
+        }
+    };
+    weigh();
+    if (open || __any(!(sum <= 4096.f))) {
+      float mx = sc[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      const float m_new = fmaxf(m_run, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
+      const float alpha = m_new == kNegInf ? 1.f : __builtin_amdgcn_exp2f((m_run - m_new) * a.scale_log2);
+      l_run *= alpha;
+      r_run *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
+      m_run = m_new;
+      open = __any(m_new == kNegInf && valid);
+      weigh();
+    }
+    l_run += sum;
+    r_run += rsum;
+#pragma unroll
+    for (int pp = 0; pp < 2; ++pp) {
+      bf16x8 vf[DT];
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const int d = 32 * dt + lc;
+        vf[dt] = *(const bf16x8*)(vt + pp * PAGE_LDS + d * 32 + ((lh ^ vswz(d)) * 16));
+      }
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[dt], __builtin_bit_cast(bf16x8, pk[pp]), acc[dt], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);  // the next sub-tile's loads stay after this one's products
+  };
+  auto compute = [&](int s) {
+    if (!on) return;
+    const char* kt = lds + (s & 1) * S::BUF;
+    const char* vt = lds + (2 + (s & 1)) * S::BUF;
+#pragma unroll 1
+    for (int q = 0; q < S::KEYS / 32; ++q) {
+      const int kbase = kbeg + s * S::KEYS + 32 * q;
+      if (((S::KEYS / 32 * s + q) & (kg - 1)) != kgi || kbase >= end) continue;
+      if (kbase + 32 <= min_lo && kbase >= a.sink) continue;
+      sub_tile(kt + 64 * q * D, vt + 64 * q * D, kbase);
+    }
+  };
+
+  // ---- keys
+  const int nbuf = kend > kbeg ? (kend - kbeg + S::KEYS - 1) / S::KEYS : 0;
+  Set x[Cache::DEPTH];
+  int pg[PER];
+#pragma unroll
+  for (int s = 0; s < Cache::DEPTH; ++s) {
+    if (s >= nbuf) break;
+    pages_of(s, pg);
+    load(pg, x[s]);
+  }
+  if (Cache::DEPTH < nbuf) pages_of(Cache::DEPTH, pg);
+  auto step = [&](int s, Set& y) {
+    store(s, y);  // LDS of buffer s - 2: every wave was done with it before barrier s - 1
+    if (s + Cache::DEPTH < nbuf) {
+      load(pg, y);
+      if (s + Cache::DEPTH + 1 < nbuf) pages_of(s + Cache::DEPTH + 1, pg);
+    }
+    lds_barrier();
+    compute(s);
+  };
+  int s = 0;
+  if constexpr (Cache::DEPTH == 2) {
+    for (; s + 1 < nbuf; s += 2) {
+      step(s, x[0]);
+      step(s + 1, x[1]);
+    }
+    if (s < nbuf) step(s, x[0]);
+  } else {
+    for (; s < nbuf; ++s) step(s, x[0]);
+  }
+
+  // The key groups' states meet in LDS (lane-wise: same columns, same dims), and
+  // each group's wave joins a share of the rows.
+  lds_barrier();
+  float* area = reinterpret_cast<float*>(lds);
+  {
+    float* state = area + wave * S::STATE;
+#pragma unroll
+    for (int v = 0; v < 4 * DT; ++v)
+      *(float4*)(state + (v * 64 + lane) * 4) = make_float4(acc[v / 4][4 * (v % 4)], acc[v / 4][4 * (v % 4) + 1],
+                                                            acc[v / 4][4 * (v % 4) + 2], acc[v / 4][4 * (v % 4) + 3]);
+    state[64 * 16 * DT + lane] = m_run;
+    l_run += __shfl_xor(l_run, 32);
+    r_run += __shfl_xor(r_run, 32);
+    state[64 * 16 * DT + 64 + lane] = l_run;
+    // what makes the products sums of weights l; one where nothing was added
+    state[64 * 16 * DT + 128 + lane] = r_run > 0.f ? l_run / r_run : 1.f;
+  }
+  lds_barrier();
+  if (!valid) return;
+  const float* states = area + first * S::STATE;
+  const int stride = apart * S::STATE, share = 4 * DT / kg;
+  float m = kNegInf, l = 0.f, weight[NW];
+#pragma unroll
+  for (int k = 0; k < NW; ++k) {
+    weight[k] = k < kg ? states[k * stride + 64 * 16 * DT + lane] : kNegInf;
+    m = fmaxf(m, weight[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < NW; ++k) {
+    // a group none of whose keys the column sees weighs nothing
+    weight[k] = weight[k] == kNegInf ? 0.f : __builtin_amdgcn_exp2f((weight[k] - m) * a.scale_log2);
+    if (k < kg) {
+      l += weight[k] * states[k * stride + 64 * 16 * DT + 64 + lane];
+      weight[k] *= states[k * stride + 64 * 16 * DT + 128 + lane];
+    }
+  }
+  const size_t orow = (size_t)(rq.q_start + tok) * a.hq + hk * g + hh;
+  const size_t tile = (size_t)rq.part_start + (size_t)(hk * rq.nch + c) * tiles + (tile0 + ct);
+  const float inv = 1.f / l;
+  // Element e of row v of a lane: dim 32 (v / 4) + 8 (v % 4) + 4 lh + e.
+#pragma unroll 1
+  for (int v = kgi * share; v < kgi * share + share; ++v) {
+    float4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+      if (k >= kg) break;
+      const float4 y = *(const float4*)(states + k * stride + (v * 64 + lane) * 4);
+      o.x += weight[k] * y.x, o.y += weight[k] * y.y, o.z += weight[k] * y.z, o.w += weight[k] * y.w;
+    }
+    if (rq.nch == 1) {
+      const u32x2 y = {pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv)};
+      *(u32x2*)(a.out + orow * D + 8 * v + 4 * lh) = y;
+    } else {
+      *(float4*)(a.part_o + tile * 32 * D + (v * 64 + lane) * 4) = o;
+    }
+  }
+  if (kgi == 0 && lh == 0) {
+    if (rq.nch > 1) *(float2*)(a.part_ml + 2 * (tile * 32 + lc)) = make_float2(m, l);
+    else if (a.lse != nullptr) a.lse[orow] = m * a.sm_scale + __logf(l);
+  }
+}
+
+// Merge of the runs of split requests.  Rows of 16 bytes, 4 dims of a column
+// each, are counted by (request, KV head, 32-column tile, v); a wave has the 32
+// columns of a v, one half of the dims in each half-wave.  PARTS 1: a wave takes
+// kWindowMergeRows of a tile's v.  Else the waves of a work group share a v, wave j
+// taking runs j, j + PARTS, ..., and meet in LDS.
+template <int D, int PARTS, typename Plan>
+__global__ __launch_bounds__(64 * kWindowMergeWaves) void window_merge_kernel(WindowArgs a, Plan p) {
+  constexpr int DT = D / 32, ROWS = PARTS > 1 ? 1 : kWindowMergeRows, N = 8;  // N: runs in flight
+  __shared__ float st[PARTS > 1 ? (PARTS - 1) * 6 * 64 : 1];
+  const int part = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int item = PARTS > 1 ? (int)blockIdx.x : ((int)blockIdx.x * kWindowMergeWaves + part) * ROWS;
+  if (item >= p.total_comb) return;
+  const int r = find_request(p, item, true);
+  const auto rq = p.req[r];
+  const int n = rq.nv & 0xffff, g = a.g, M = n * g, tiles = (M + 31) / 32, nch = rq.nch;
+  int local = item - rq.comb_start;
+  const int v = local % (4 * DT);
+  local /= 4 * DT;
+  const int hk = local / tiles, tile = local - hk * tiles;
+  const size_t base = (size_t)rq.part_start + (size_t)hk * nch * tiles + tile;
+  const int lane = threadIdx.x & 63, lc = lane & 31, lh = lane >> 5;
+  const int col = tile * 32 + lc;
+
+  float m = kNegInf, l = 0.f, o[ROWS][4] = {};
+  auto absorb = [&](const auto& mc, const auto& ls, const auto& oc) {
+    constexpr int C = sizeof(ls) / sizeof(ls[0]);
+    float m_new = m, weight[C];
+#pragma unroll
+    for (int u = 0; u < C; ++u) m_new = fmaxf(m_new, mc[u]);
+    const float a0 = m == kNegInf ? 0.f : __builtin_amdgcn_exp2f((m - m_new) * a.scale_log2);
+    l *= a0;
+#pragma unroll
+    for (int u = 0; u < C; ++u) {
+      weight[u] = mc[u] == kNegInf ? 0.f : __builtin_amdgcn_exp2f((mc[u] - m_new) * a.scale_log2);
+      l += weight[u] * ls[u];
+    }
+#pragma unroll
+    for (int q = 0; q < ROWS; ++q)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        o[q][e] *= a0;
+#pragma unroll
+        for (int u = 0; u < C; ++u) o[q][e] += weight[u] * oc[u][q][e];
+      }
+    m = m_new;
+  };
+  if (col < M) {
+    for (int c0 = PARTS > 1 ? part : 0; c0 < nch; c0 += N * PARTS) {
+      float mc[N], ls[N], x[N][ROWS][4];
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        const int c = min(c0 + u * PARTS, nch - 1);  // past the last: that one again, for nothing
+        const size_t t0 = base + (size_t)c * tiles;
+        const float2 ml = *(const float2*)(a.part_ml + 2 * (t0 * 32 + lc));
+        mc[u] = c0 + u * PARTS < nch ? ml.x : kNegInf;
+        ls[u] = ml.y;
+#pragma unroll
+        for (int q = 0; q < ROWS; ++q) {
+          const float4 y = *(const float4*)(a.part_o + t0 * 32 * D + ((v + q) * 64 + lane) * 4);
+          x[u][q][0] = y.x, x[u][q][1] = y.y, x[u][q][2] = y.z, x[u][q][3] = y.w;
+        }
+      }
+      absorb(mc, ls, x);
+    }
+  }
+  if (PARTS > 1) {
+    if (part > 0) {
+      float* s = st + (part - 1) * 6 * 64 + lane;
+      s[0] = m;
+      s[64] = l;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[(2 + e) * 64] = o[0][e];
+    }
+    __syncthreads();
+    if (part > 0) return;
+#pragma unroll
+    for (int j = 0; j < PARTS - 1; ++j) {
+      const float* s = st + j * 6 * 64 + lane;
+      const float mc[1] = {s[0]}, ls[1] = {s[64]}, x[1][1][4] = {{{s[2 * 64], s[3 * 64], s[4 * 64], s[5 * 64]}}};
+      if constexpr (PARTS > 1) absorb(mc, ls, x);
+    }
+  }
+  if (col >= M) return;
+  const int tok = row_of(a, col), hh = col - tok * g;
+  const size_t orow = (size_t)(rq.q_start + tok) * a.hq + hk * g + hh;
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int q = 0; q < ROWS; ++q) {
+    const u32x2 w = {pack_bf16x2(o[q][0] * inv, o[q][1] * inv), pack_bf16x2(o[q][2] * inv, o[q][3] * inv)};
+    *(u32x2*)(a.out + orow * D + 8 * (v + q) + 4 * lh) = w;
+  }
+  if (a.lse != nullptr && v == 0 && lh == 0) a.lse[orow] = m * a.sm_scale + __logf(l);
+}
+
+template <typename Cache, int D, typename Plan>
+hipError_t launch_impl(const WindowArgs& a, const Plan& p, bool narrow, hipStream_t stream) {
+  if (narrow)
+    hipLaunchKernelGGL((window_attn_kernel<Cache, D, kWindowWaves / 2, Plan>), dim3(p.grid_items),
+                       dim3(64 * kWindowWaves / 2), 0, stream, a, p);
+  else
+    hipLaunchKernelGGL((window_attn_kernel<Cache, D, kWindowWaves, Plan>), dim3(p.grid_items), dim3(64 * kWindowWaves), 0,
+                       stream, a, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.total_comb == 0) return e;
+  const dim3 threads(64 * kWindowMergeWaves);
+  if (p.max_chunks > 8 && p.total_comb <= 1024)  // many runs, and few enough rows to be bound by latency
+    hipLaunchKernelGGL((window_merge_kernel<D, kWindowMergeWaves, Plan>), dim3(p.total_comb), threads, 0, stream, a, p);
+  else
+    hipLaunchKernelGGL((window_merge_kernel<D, 1, Plan>),
+                       dim3((p.total_comb + kWindowMergeRows * kWindowMergeWaves - 1) / (kWindowMergeRows * kWindowMergeWaves)),
+                       threads, 0, stream, a, p);
+  return hipGetLastError();
+}
+template <typename Plan>
+hipError_t launch_any(const WindowArgs& a, const Plan& p, int head_dim, bool kv8, bool narrow, hipStream_t stream) {
+  if (head_dim == 128)
+    return kv8 ? launch_impl<Kv8Cache, 128>(a, p, narrow, stream) : launch_impl<Bf16Cache, 128>(a, p, narrow, stream);
+  return kv8 ? launch_impl<Kv8Cache, 64>(a, p, narrow, stream) : launch_impl<Bf16Cache, 64>(a, p, narrow, stream);
+}
+
+}  // namespace
+
+hipError_t launch_window_attention(const WindowArgs& a, const WindowPlan& p, int head_dim, bool kv8, bool narrow,
+                                   hipStream_t stream) {
+  return launch_any(a, p, head_dim, kv8, narrow, stream);
+}
+hipError_t launch_window_attention(const WindowArgs& a, const WindowPlanBr& p, int head_dim, bool kv8, bool narrow,
+                                   hipStream_t stream) {
+  return launch_any(a, p, head_dim, kv8, narrow, stream);
+}
+
+}  // namespace rg

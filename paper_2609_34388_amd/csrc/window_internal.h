@@ -38,4 +38,78 @@ struct Kv8ReadArgs {
 };
 hipError_t launch_kv8_read(const Kv8ReadArgs& a, const AttnPlan& p, int head_dim, hipStream_t stream);
 
+// Attention over a window, or all, of the keys of a bf16 or an 8-bit cache.
+//
+// A request's 32-column tiles are dealt evenly to column groups of up to `waves`
+// tiles, the waves of a work group: kWindowWaves (one work group a compute unit),
+// or half of them in narrow launches (two).  A group's keys are those that its
+// rows may see: the sinks' pages and those from the first row's window on, counted
+// without the gap between them.  They are cut into `nch` runs of `run` keys, alike
+// for all groups of a request; runs past a group's keys are empty.
+constexpr int kWindowWaves = 8;
+// Keys a buffer of a work group holds.
+__host__ __device__ constexpr int window_keys(int waves, int head_dim) { return 16 * waves * (128 / head_dim); }
+constexpr int kWindowMergeWaves = 4;  // waves of a work group of the merge
+constexpr int kWindowMergeRows = 2;   // rows of one
+template <typename Base>
+struct WindowReqT : Base {
+  int32_t nch, run;
+};
+using WindowReq = WindowReqT<AttnReq>;      // part_start: the first partial tile
+using WindowReqBr = WindowReqT<AttnReqBr>;
+template <typename Req, int MaxReq>
+struct WindowPlanT {
+  int32_t num_req, total_items, grid_items, total_comb, max_chunks;
+  Req req[MaxReq + 1];
+};
+constexpr int kMaxWindowReq = 96, kMaxWindowReqBr = 64;
+using WindowPlan = WindowPlanT<WindowReq, kMaxWindowReq>;
+using WindowPlanBr = WindowPlanT<WindowReqBr, kMaxWindowReqBr>;
+static_assert(sizeof(WindowPlan) <= 3700 && sizeof(WindowPlanBr) <= 3700, "plan must fit the kernel argument block");
+
+struct WindowArgs {
+  const uint16_t* q;
+  const uint8_t* k_cache;  // bf16 K pool, or the 8-bit pool
+  const uint8_t* v_cache;  // bf16 V pool
+  const float* scales;     // of the 8-bit pool
+  uint16_t* out;
+  float* lse;
+  const int32_t* page_indices;
+  float* part_o;   // per 32-column tile: 32 x D fp32 sums, 16-byte rows lane-interleaved
+  float* part_ml;  // [partial columns][2] (reference of raw scores, sum)
+  int32_t hq, hkv, g;
+  uint32_t g_mul;  // quotient by g
+  int32_t g_shift;
+  int32_t size, sink;  // of the window; size 2^30 for all keys
+  float sm_scale, scale_log2;
+};
+// The keys that rows i0 .. i1 - 1 of a request may see.
+struct WindowSpan {
+  int32_t keys;  // their number, with the sinks' pages' other slots
+  int32_t gap;   // key k >= head stands for token k + gap; a multiple of 16
+  int32_t head;  // keys of the sinks' pages where there is a gap
+  int32_t lo;    // the first key of the window
+};
+template <bool BR>
+__host__ __device__ inline WindowSpan window_span(int L, int V, int n, int i0, int i1, int size, int sink) {
+  WindowSpan s;
+  // a branch may keep none of the verify rows
+  const int first = BR && i1 > V ? L : L + i0;
+  int lo = first + 1 - size;
+  if (lo > L + V) lo = L + V;  // draft rows see all of their block
+  if (BR && i1 > V && lo > L) lo = L;
+  if (lo < 0) lo = 0;
+  const int end = i1 <= V ? L + i1 : L + n;
+  s.head = (sink + 15) / 16 * 16;
+  s.gap = lo / 16 * 16 - s.head;
+  if (s.gap < 0) s.gap = 0;
+  s.lo = lo - s.gap;
+  s.keys = end - s.gap;
+  return s;
+}
+hipError_t launch_window_attention(const WindowArgs& a, const WindowPlan& p, int head_dim, bool kv8, bool narrow,
+                                   hipStream_t stream);
+hipError_t launch_window_attention(const WindowArgs& a, const WindowPlanBr& p, int head_dim, bool kv8, bool narrow,
+                                   hipStream_t stream);
+
 }  // namespace rg

@@ -72,3 +72,64 @@ def test_read_refusals():
     assert read(L(), scales=ctypes.c_void_p(0x1002)) == UNSUPPORTED
     assert read(L(), ks=248) == SHAPE and read(L(), vs=0) == SHAPE and read(L(), ks=257) == UNSUPPORTED
 
+
+def window(size=10, sink=2):
+    return ctypes.byref(binding.Window(size, sink))
+
+
+def attend(l, w=None, q=P, cache=P, second=P, out=P, lse=None, ws=None, nbytes=0, br=None):
+    ref, w = l.ref if l else None, window() if w is None else w
+    a = lib().rg_kv8_attention(ref, br, w, q, cache, second, out, lse, ws, nbytes, None)
+    b = lib().rg_window_attention(ref, br, w, q, cache, second, out, lse, ws, nbytes, None)
+    if second is P:
+        assert a == b
+    return a
+
+
+def test_attention_layout_refusals():
+    assert attend(None) == NULL
+    for kw, want in BAD_LAYOUTS:
+        assert attend(L(**kw)) == want, kw
+
+
+def test_attention_refusals():
+    for name in ("q", "cache", "second", "out"):
+        assert attend(L(), **{name: None}) == NULL
+        if name != "second":
+            assert attend(L(), **{name: ODD}) == UNSUPPORTED
+    assert lib().rg_window_attention(L().ref, None, window(), P, P, ODD, P, None, None, 0, None) == UNSUPPORTED
+    assert attend(L(), second=ctypes.c_void_p(0x1002)) == UNSUPPORTED
+    assert attend(L(), lse=ctypes.c_void_p(0x1002)) == UNSUPPORTED
+    assert attend(L(indices=0x1002)) == UNSUPPORTED
+    for size, sink in ((0, 0), (-1, 5), (1, -1)):
+        assert attend(L(), w=window(size, sink)) == SHAPE
+    assert lib().rg_window_attention(L().ref, None, None, P, P, P, P, None, None, 0, None) == NULL
+    long = L(ctx=(9000, 17))
+    need = ctypes.c_size_t()
+    query = lib().rg_kv8_attention_workspace
+    assert query(long.ref, None, None, None) == NULL
+    assert lib().rg_window_attention_workspace(long.ref, None, None, ctypes.byref(need)) == NULL
+    assert query(long.ref, None, window(0), ctypes.byref(need)) == SHAPE
+    assert query(long.ref, None, window(8000), ctypes.byref(need)) == 0 and need.value > 0
+    few = window(8000)
+    assert attend(long, few) == 4 and attend(long, few, ws=P, nbytes=need.value - 1) == 4
+    assert attend(long, few, ws=ODD, nbytes=need.value) == 4
+    all_keys = need.value
+    assert query(long.ref, None, None, ctypes.byref(need)) == 0 and need.value >= all_keys
+    br = binding.make_branches([0, 1, 2], [3, 0], [0, 0], [3, 5])
+    assert attend(L(), br=ctypes.byref(br.c)) == SHAPE
+    br.c.branch_indptr = None
+    assert attend(L(), br=ctypes.byref(br.c)) == NULL
+
+
+def test_windows_bound_the_workspace():
+    """A window's keys, not the context's, are what is split."""
+    need = ctypes.c_size_t()
+    l = L(ctx=(900000, 17), pages=(60000, 2))
+    for size in (1, 100):
+        assert lib().rg_kv8_attention_workspace(l.ref, None, window(size, 4), ctypes.byref(need)) == 0
+        assert need.value <= 4 << 20
+    # the largest layouts and windows plan without overflow
+    for w in (window(2 ** 31 - 1, 2 ** 31 - 1), window(1, 2 ** 31 - 1), None):
+        far = L(ctx=(2 ** 30 - 8, 17), nv=(0, 5), pages=(1 << 26, 2))
+        assert lib().rg_kv8_attention_workspace(far.ref, None, w, ctypes.byref(need)) == 0
