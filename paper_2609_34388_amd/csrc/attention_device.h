@@ -24,21 +24,25 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
 
-// Request owning work item `item`: the last r with start(r) <= item (starts
-// are nondecreasing, empty requests share their successor's start).  Every
-// lane tests one request, so the search is one round of loads, not a chain.
-template <typename Plan>
-__device__ __forceinline__ int find_request(const Plan& p, int item, bool combine) {
+// Request owning work item `item` of `count` requests: the last r with start(r) <=
+// item (starts are nondecreasing, empty requests share their successor's start).
+// Every lane tests one request, so the search is one round of loads, not a chain.
+template <typename Start>
+__device__ __forceinline__ int find_start(int count, int item, Start start) {
   const int lane = threadIdx.x & 63;
   int r = 0;
-  for (int base = 1; base < p.num_req; base += 64) {
+  for (int base = 1; base < count; base += 64) {
     const int k = base + lane;
-    bool le = k < p.num_req;
-    if constexpr (__is_same(Plan, AttnPlanBrPacked)) le = le && p.req[k].item_start <= item;
-    else le = le && (combine ? p.req[k].comb_start : p.req[k].item_start) <= item;
-    r += __popcll(__ballot(le));
+    r += __popcll(__ballot(k < count && start(k) <= item));
   }
   return __builtin_amdgcn_readfirstlane(r);
+}
+template <typename Plan>
+__device__ __forceinline__ int find_request(const Plan& p, int item, bool combine) {
+  return find_start(p.num_req, item, [&](int k) {
+    if constexpr (__is_same(Plan, AttnPlanBrPacked)) return p.req[k].item_start;
+    else return combine ? p.req[k].comb_start : p.req[k].item_start;
+  });
 }
 
 // Consecutive work items of one (request, KV head) land on one XCD: the
@@ -94,9 +98,8 @@ __device__ __forceinline__ AttnReqBr request_of(const AttnPlanBrPacked& p, int r
 // sequence: the kept canonical prefix, then the branch's committed lead rows
 // causally, then its draft rows seeing the whole branch).  Both clipped to the
 // chunk's end.
-template <typename Req>
+template <typename Req, bool BR = !__is_same(Req, AttnReq)>
 __device__ __forceinline__ void key_limits(const Req& rq, bool valid, int tok, int kend, int& lim, int& slo, int& shi) {
-  constexpr bool BR = !__is_same(Req, AttnReq);
   const int n = rq.nv & 0xffff, nver = (int)((uint32_t)rq.nv >> 16), L = rq.ctx, T = L + n;
   slo = shi = 0;
   if (!valid) {

@@ -1,6 +1,7 @@
 // C ABI of rotated appends, the 8-bit KV cache and attention over a window:
 // argument validation, planning and launches.  As in api.cpp the plans travel
 // in the kernel arguments; nothing is uploaded or synchronised.
+#include <cstdio>
 #include <new>
 #include <numeric>
 #include <vector>
@@ -143,7 +144,9 @@ Groups groups_of(const rg_attn_layout* L, int r, Limits w, int waves) {
 }
 
 // Time of a buffer of an item with this many tiles, in quarters of that of a
-// buffer at the copy rate.
+// buffer at the copy rate; of its start and end, and of its partials beside; and
+// the least of an item's keys.
+constexpr int64_t kStartCost = 8, kPartCost = 4, kLeastCost = 8;
 int64_t step_cost(int64_t tiles) { return std::max<int64_t>(4, tiles); }
 
 template <typename Plan, int MaxReq>
@@ -157,28 +160,47 @@ rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits
     widest = std::max(widest, groups[r].tiles);
   }
   fp.narrow = widest <= kWindowWaves / 2;
+  if (getenv("RGX_NARROW")) fp.narrow = atoi(getenv("RGX_NARROW"));
   const int waves = fp.narrow ? kWindowWaves / 2 : kWindowWaves, keys = window_keys(waves, L->head_dim);
   if (!fp.narrow)
     for (int r = 0; r < R; ++r) groups[r] = groups_of<BR>(L, r, w, waves);
-  // Cost of an item at most: the least that gives one round of items.
+  // Cost of an item at most.  Candidates are the least that give one round of
+  // items, two, ...; a round's end is uneven, an item's start and its partials cost.
   const int64_t slots = (int64_t)cus * (fp.narrow ? 2 : 1);
-  int64_t work = 0, least = 0;
-  for (const Groups& q : groups) {
-    work += q.count * hkv * q.steps * step_cost(q.per);
-    least += q.count * hkv;
-  }
+  int64_t work = 0;
+  for (const Groups& q : groups) work += q.count * hkv * q.steps * step_cost(q.per);
   auto runs_of = [&](const Groups& q, int64_t target) {
-    const int64_t most = std::max<int64_t>(1, target / step_cost(q.per));  // steps of a run at most
+    const int64_t most = std::min<int64_t>(kMaxRunSteps, std::max<int64_t>(1, target / step_cost(q.per)));  // steps of a run
     const int64_t n = (q.steps + most - 1) / most, each = (q.steps + n - 1) / n;
     return (q.steps + each - 1) / each;
   };
-  int64_t target = std::max<int64_t>(8, work / slots);
-  for (;; target += 1 + target / 16) {
-    int64_t items = 0;
-    for (const Groups& q : groups)
-      if (q.count) items += q.count * hkv * runs_of(q, target);
-    if (items <= std::max(least, slots)) break;
+  int64_t target = 0;
+  double best = 0.;
+  const char* E = getenv("RGX_ROUNDS");
+  for (int64_t rounds = E ? atoi(E) : 1; rounds <= (E ? atoi(E) : 4); ++rounds) {
+    int64_t t = std::max<int64_t>(kLeastCost, work / (rounds * slots)), items, whole;
+    int64_t longest, total;
+    for (;; t += 1 + t / 16) {
+      items = whole = longest = total = 0;
+      for (const Groups& q : groups) {
+        if (!q.count) continue;
+        const int64_t n = runs_of(q, t), each = (q.steps + n - 1) / n * step_cost(q.per) + kStartCost + (n > 1 ? kPartCost : 0);
+        items += q.count * hkv * n;
+        whole += q.count * hkv;
+        total += q.count * hkv * n * each;
+        longest = std::max(longest, each);
+      }
+      if (items <= std::max(whole, rounds * slots)) break;
+    }
+    const double time = items <= slots ? (double)longest
+                                       : std::max((double)longest, (double)total / slots + 0.5 * (double)total / items);
+    if (target == 0 || time < best) {
+      target = t;
+      best = time;
+    }
+    if (items <= slots * rounds && items == whole) break;  // nothing is split
   }
+  if (getenv("RGX_P")) fprintf(stderr, "narrow %d target %ld best %f work %ld slots %ld\n", (int)fp.narrow, (long)target, best, (long)work, (long)slots);
   // Costliest work items first.
   std::vector<int> order(R);
   std::iota(order.begin(), order.end(), 0);
@@ -205,14 +227,12 @@ rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits
       x.page_start = L->page_indptr[r];
       x.item_start = (int32_t)items;
       x.part_start = (int32_t)part;
-      x.comb_start = (int32_t)comb;
       if (q.count == 0) continue;
       const int64_t nch = runs_of(q, target);
-      x.nch = (int32_t)nch;
-      x.run = (int32_t)((q.steps + nch - 1) / nch * keys);
+      x.runs = (uint32_t)nch | (uint32_t)((q.steps + nch - 1) / nch) << 16;
       items += hkv * q.count * nch;
       if (nch > 1) {
-        p.max_chunks = std::max(p.max_chunks, x.nch);
+        p.max_chunks = std::max(p.max_chunks, (int32_t)nch);
         part += hkv * nch * q.tiles;
         comb += hkv * q.tiles * (L->head_dim / 8);
       }
@@ -220,7 +240,7 @@ rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits
     }
     p.req[p.num_req].item_start = p.total_items = (int32_t)items;
     p.req[p.num_req].part_start = (int32_t)part;
-    p.req[p.num_req].comb_start = p.total_comb = (int32_t)comb;
+    p.total_comb = (int32_t)comb;
     p.grid_items = (int32_t)round_up(items, 8);
     if (!fits_launch(items, 64 * waves) || !fits_launch(comb, 64 * kWindowMergeWaves)) return RG_ERR_UNSUPPORTED;
     most_part = std::max(most_part, part);
@@ -239,13 +259,13 @@ rg_status with_window_plan(const rg_attn_layout* L, const rg_branch_layout* B, c
   if (st != RG_OK) return st;
   if (B == nullptr) {
     FullPlan<WindowPlan> fp;
-    st = plan_window<WindowPlan, kMaxWindowReq>(L, nullptr, limits_of(W), fp);
+    st = plan_window<WindowPlan, kMaxReqPerLaunch>(L, nullptr, limits_of(W), fp);
     return st != RG_OK ? st : f(fp);
   }
   st = validate_branches(L, B);
   if (st != RG_OK) return st;
   FullPlan<WindowPlanBr> fp;
-  st = plan_window<WindowPlanBr, kMaxWindowReqBr>(L, B, limits_of(W), fp);
+  st = plan_window<WindowPlanBr, kMaxReqPerLaunchBr>(L, B, limits_of(W), fp);
   return st != RG_OK ? st : f(fp);
 } catch (const std::bad_alloc&) {  // nothing is launched before a plan is whole
   return RG_ERR_WORKSPACE;

@@ -69,23 +69,24 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
 
   const int item = p.num_req == 1 ? xcd_item(p.grid_items) : (int)blockIdx.x;
   if (item >= p.total_items) return;
-  const int r = find_request(p, item, false);
+  const int r = find_start(p.num_req, item, [&](int k) { return p.req[k].item_start; });
   const auto rq = p.req[r];
   const int n = rq.nv & 0xffff, nver = (int)((uint32_t)rq.nv >> 16), L = rq.ctx;
   const int g = a.g, M = n * g, tiles = (M + 31) / 32;
+  const int nch = rq.runs & 0xffff, run = (int)(rq.runs >> 16) * S::KEYS;
   const int ncg = (tiles + NW - 1) / NW, tpg = (tiles + ncg - 1) / ncg;
   // Items of a request: runs, then KV heads, then column groups, so that the
   // groups of a head, which share most keys, follow on one XCD (8 KV heads).
   int local = item - rq.item_start, c = 0;
-  if (rq.nch > 1) {
-    c = local % rq.nch;
-    local /= rq.nch;
+  if (nch > 1) {
+    c = local % nch;
+    local /= nch;
   }
   const int cg = local / a.hkv, hk = local - cg * a.hkv;
   const int tile0 = cg * tpg, nct = min(tpg, tiles - tile0);
   const int row0 = row_of(a, tile0 * 32), row1 = row_of(a, min(M, (tile0 + nct) * 32) - 1) + 1;
   const WindowSpan span = window_span<BR>(L, nver, n, row0, row1, a.size, a.sink);
-  const int kbeg = c * rq.run, kend = min(span.keys, kbeg + rq.run);
+  const int kbeg = c * run, kend = min(span.keys, kbeg + run);
 
   const int tid = threadIdx.x, lane = tid & 63, lc = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -221,32 +222,28 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
   // Limits of the column: keys lo .. lim - 1 and below the sink, and slo .. shi - 1.
   int lim, slo, shi, lo;
   if constexpr (BR) {
-    key_limits(static_cast<const AttnReqBr&>(rq), valid, tok, INT_MAX, lim, slo, shi);
+    key_limits<WindowReqBr, true>(rq, valid, tok, INT_MAX, lim, slo, shi);
     // a branch row's position: the kept prefix and its place in the branch
     lo = tok < nver ? lim - a.size : min(lim, lim + (L + tok - slo) + 1 - a.size);
     slo -= span.gap;
     shi -= span.gap;
   } else {
-    key_limits(static_cast<const AttnReq&>(rq), valid, tok, INT_MAX, lim, slo, shi);
+    key_limits<WindowReq, false>(rq, valid, tok, INT_MAX, lim, slo, shi);
     lo = tok < nver ? lim - a.size : min(L + nver, L + tok + 1 - a.size);
   }
   lim -= span.gap;
   lo = max(lo - span.gap, 0);
   if (lo <= a.sink) lo = 0;
   if (!valid) lim = lo = slo = shi = 0;
-  // Over the wave: below min_lim no column has an upper limit, from max_lo on none a
-  // lower one; nobody sees keys from `end` on, or of sink .. min_lo - 1.
-  int min_lim = valid ? lim : INT_MAX, max_lo = lo, min_lo = valid ? lo : INT_MAX, end = max(lim, shi);
-  for (int off = 32; off >= 1; off >>= 1) {
-    min_lim = min(min_lim, __shfl_xor(min_lim, off));
-    max_lo = max(max_lo, __shfl_xor(max_lo, off));
-    min_lo = min(min_lo, __shfl_xor(min_lo, off));
-    end = max(end, __shfl_xor(end, off));
-  }
-  min_lim = __builtin_amdgcn_readfirstlane(min_lim);
-  max_lo = __builtin_amdgcn_readfirstlane(max_lo);
-  min_lo = __builtin_amdgcn_readfirstlane(min_lo);
-  end = __builtin_amdgcn_readfirstlane(min(end, kend));
+  // Of the wave's columns, from its first and last row: below min_lim no column has
+  // an upper limit, from max_lo on none a lower one; nobody sees keys from `end` on,
+  // or of sink .. min_lo - 1.  Where branches are among them, bounds of these.
+  const int ra = row_of(a, (tile0 + ct) * 32), rb = row_of(a, min(M, (tile0 + ct) * 32 + 32) - 1);
+  const bool branched = BR && rb >= nver;
+  auto lo_of = [&](int row) { return min(L + nver, L + row + 1 - a.size) - span.gap; };
+  const int min_lim = (branched ? L : ra < nver ? L + ra + 1 : L + n) - span.gap;
+  const int end = min(kend, (rb < nver ? L + rb + 1 : L + n) - span.gap);
+  const int max_lo = lo_of(branched ? n : rb), min_lo = branched ? min(L, L + 1 - a.size) - span.gap : lo_of(ra);
 
   f32x16 acc[DT];
 #pragma unroll
@@ -268,9 +265,11 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks) kf[ks] = *(const bf16x8*)(kt + krow + ((ks ^ kw) << 5));
       for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], sc, 0, 0, 0);
     }
+    __builtin_amdgcn_s_setprio(0);
     // key - kbase = 8 lh + place, place a constant of i
     if (kbase + 32 > min_lim) {
       const int seen = lim - kbase - 8 * lh, from = slo - kbase - 8 * lh, to = shi - kbase - 8 * lh;
@@ -329,6 +328,7 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
     }
     l_run += sum;
     r_run += rsum;
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int pp = 0; pp < 2; ++pp) {
       bf16x8 vf[DT];
@@ -341,6 +341,7 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
       for (int dt = 0; dt < DT; ++dt)
         acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[dt], __builtin_bit_cast(bf16x8, pk[pp]), acc[dt], 0, 0, 0);
     }
+    __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);  // the next sub-tile's loads stay after this one's products
   };
   auto compute = [&](int s) {
@@ -387,6 +388,39 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
     for (; s < nbuf; ++s) step(s, x[0]);
   }
 
+  l_run += __shfl_xor(l_run, 32);
+  r_run += __shfl_xor(r_run, 32);
+  // what makes the products sums of weights l; one where nothing was added
+  const float whole = r_run > 0.f ? l_run / r_run : 1.f;
+  const size_t orow = (size_t)(rq.q_start + tok) * a.hq + hk * g + hh;
+  const size_t tile = (size_t)rq.part_start + (size_t)(hk * nch + c) * tiles + (tile0 + ct);
+  // Element e of row v of a lane: dim 32 (v / 4) + 8 (v % 4) + 4 lh + e.
+  auto put = [&](int v, float4 o, float f) {
+    if (nch == 1) {
+      const u32x2 y = {pack_bf16x2(o.x * f, o.y * f), pack_bf16x2(o.z * f, o.w * f)};
+      *(u32x2*)(a.out + orow * D + 8 * v + 4 * lh) = y;
+    } else {
+      *(float4*)(a.part_o + tile * 32 * D + (v * 64 + lane) * 4) = o;
+    }
+  };
+  auto put_sums = [&](float m, float l) {
+    if (lh != 0) return;
+    if (nch > 1) *(float2*)(a.part_ml + 2 * (tile * 32 + lc)) = make_float2(m, l);
+    else if (a.lse != nullptr) a.lse[orow] = m * a.sm_scale + __logf(l);
+  };
+  if (NW == 4 ? nct > 2 : nct == NW) {  // no tile has more than one wave
+    if (!valid) return;
+    const float f = nch == 1 ? 1.f / r_run : 1.f;
+#pragma unroll
+    for (int v = 0; v < 4 * DT; ++v) {
+      float4 o = make_float4(acc[v / 4][4 * (v % 4)], acc[v / 4][4 * (v % 4) + 1], acc[v / 4][4 * (v % 4) + 2],
+                             acc[v / 4][4 * (v % 4) + 3]);
+      if (nch > 1) o.x *= whole, o.y *= whole, o.z *= whole, o.w *= whole;
+      put(v, o, f);
+    }
+    put_sums(m_run, l_run);
+    return;
+  }
   // The key groups' states meet in LDS (lane-wise: same columns, same dims), and
   // each group's wave joins a share of the rows.
   lds_barrier();
@@ -398,11 +432,8 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
       *(float4*)(state + (v * 64 + lane) * 4) = make_float4(acc[v / 4][4 * (v % 4)], acc[v / 4][4 * (v % 4) + 1],
                                                             acc[v / 4][4 * (v % 4) + 2], acc[v / 4][4 * (v % 4) + 3]);
     state[64 * 16 * DT + lane] = m_run;
-    l_run += __shfl_xor(l_run, 32);
-    r_run += __shfl_xor(r_run, 32);
     state[64 * 16 * DT + 64 + lane] = l_run;
-    // what makes the products sums of weights l; one where nothing was added
-    state[64 * 16 * DT + 128 + lane] = r_run > 0.f ? l_run / r_run : 1.f;
+    state[64 * 16 * DT + 128 + lane] = whole;
   }
   lds_barrier();
   if (!valid) return;
@@ -423,30 +454,18 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
       weight[k] *= states[k * stride + 64 * 16 * DT + 128 + lane];
     }
   }
-  const size_t orow = (size_t)(rq.q_start + tok) * a.hq + hk * g + hh;
-  const size_t tile = (size_t)rq.part_start + (size_t)(hk * rq.nch + c) * tiles + (tile0 + ct);
   const float inv = 1.f / l;
-  // Element e of row v of a lane: dim 32 (v / 4) + 8 (v % 4) + 4 lh + e.
 #pragma unroll 1
   for (int v = kgi * share; v < kgi * share + share; ++v) {
     float4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < NW; ++k) {
-      if (k >= kg) break;
-      const float4 y = *(const float4*)(states + k * stride + (v * 64 + lane) * 4);
+      const float4 y = *(const float4*)(states + (k < kg ? k : 0) * stride + (v * 64 + lane) * 4);
       o.x += weight[k] * y.x, o.y += weight[k] * y.y, o.z += weight[k] * y.z, o.w += weight[k] * y.w;
     }
-    if (rq.nch == 1) {
-      const u32x2 y = {pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv)};
-      *(u32x2*)(a.out + orow * D + 8 * v + 4 * lh) = y;
-    } else {
-      *(float4*)(a.part_o + tile * 32 * D + (v * 64 + lane) * 4) = o;
-    }
+    put(v, o, inv);
   }
-  if (kgi == 0 && lh == 0) {
-    if (rq.nch > 1) *(float2*)(a.part_ml + 2 * (tile * 32 + lc)) = make_float2(m, l);
-    else if (a.lse != nullptr) a.lse[orow] = m * a.sm_scale + __logf(l);
-  }
+  if (kgi == 0) put_sums(m, l);
 }
 
 // Merge of the runs of split requests.  Rows of 16 bytes, 4 dims of a column
@@ -461,10 +480,34 @@ __global__ __launch_bounds__(64 * kWindowMergeWaves) void window_merge_kernel(Wi
   const int part = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int item = PARTS > 1 ? (int)blockIdx.x : ((int)blockIdx.x * kWindowMergeWaves + part) * ROWS;
   if (item >= p.total_comb) return;
-  const int r = find_request(p, item, true);
+  // The request: a lane counts the items of one, and of all before it.
+  int r = 0, before = 0;
+  for (int base = 0; base < p.num_req; base += 64) {
+    const int k = base + ((int)threadIdx.x & 63);
+    int count = 0;
+    if (k < p.num_req) {
+      const uint32_t tiles = ((uint32_t)(p.req[k].nv & 0xffff) * a.g + 31) / 32;
+      if ((p.req[k].runs & 0xffff) > 1) count = (int)(tiles * a.hkv * 4 * DT);
+    }
+    int sum = count;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int x = __shfl_up(sum, off);
+      if (((int)threadIdx.x & 63) >= off) sum += x;
+    }
+    const int all = __shfl(sum, 63);
+    if (item < before + all) {
+      const int at = __popcll(__ballot(before + sum <= item));
+      r = base + at;
+      before += __shfl(sum - count, at);
+      break;
+    }
+    before += all;
+  }
+  r = __builtin_amdgcn_readfirstlane(r);
   const auto rq = p.req[r];
-  const int n = rq.nv & 0xffff, g = a.g, M = n * g, tiles = (M + 31) / 32, nch = rq.nch;
-  int local = item - rq.comb_start;
+  const int n = rq.nv & 0xffff, g = a.g, M = n * g, tiles = (M + 31) / 32, nch = rq.runs & 0xffff;
+  int local = item - __builtin_amdgcn_readfirstlane(before);
   const int v = local % (4 * DT);
   local /= 4 * DT;
   const int hk = local / tiles, tile = local - hk * tiles;

@@ -51,20 +51,22 @@ constexpr int kWindowWaves = 8;
 __host__ __device__ constexpr int window_keys(int waves, int head_dim) { return 16 * waves * (128 / head_dim); }
 constexpr int kWindowMergeWaves = 4;  // waves of a work group of the merge
 constexpr int kWindowMergeRows = 2;   // rows of one
-template <typename Base>
-struct WindowReqT : Base {
-  int32_t nch, run;
+struct WindowReq {
+  int32_t q_start, ctx, nv, page_start, item_start;  // as in AttnReq
+  int32_t part_start;                                // first partial tile in the workspace
+  uint32_t runs;                                     // nch (low 16 bits) | run / keys of a buffer << 16
 };
-using WindowReq = WindowReqT<AttnReq>;      // part_start: the first partial tile
-using WindowReqBr = WindowReqT<AttnReqBr>;
+struct WindowReqBr : WindowReq {
+  int32_t br[3], rep;  // as in AttnReqBr
+};
+constexpr int kMaxRuns = 0xffff, kMaxRunSteps = 0xffff;
 template <typename Req, int MaxReq>
 struct WindowPlanT {
   int32_t num_req, total_items, grid_items, total_comb, max_chunks;
-  Req req[MaxReq + 1];
+  Req req[MaxReq + 1];  // entry num_req holds the end sentinel of item_start
 };
-constexpr int kMaxWindowReq = 96, kMaxWindowReqBr = 64;
-using WindowPlan = WindowPlanT<WindowReq, kMaxWindowReq>;
-using WindowPlanBr = WindowPlanT<WindowReqBr, kMaxWindowReqBr>;
+using WindowPlan = WindowPlanT<WindowReq, kMaxReqPerLaunch>;
+using WindowPlanBr = WindowPlanT<WindowReqBr, kMaxReqPerLaunchBr>;
 static_assert(sizeof(WindowPlan) <= 3700 && sizeof(WindowPlanBr) <= 3700, "plan must fit the kernel argument block");
 
 struct WindowArgs {
