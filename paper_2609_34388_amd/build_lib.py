@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(HERE, "librecguide.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 SOURCES = ("api.cpp", "cache_api.cpp", "attention.hip", "logits.hip", "branches.hip", "blocksize.hip", "kv4.hip",
            "kv4_attention.hip", "mass.hip", "evict.hip", "window_api.cpp", "append.hip",
-           "window_attention.hip")
+           "window_attention.hip", "kv8_attention.hip")
 ARCH = "gfx950"
 
 # Packed fp32 VALU instructions are kept out of the generated code; MFMA

@@ -1,7 +1,6 @@
 // C ABI of rotated appends, the 8-bit KV cache and attention over a window:
 // argument validation, planning and launches.  As in api.cpp the plans travel
 // in the kernel arguments; nothing is uploaded or synchronised.
-#include <cstdio>
 #include <new>
 #include <numeric>
 #include <vector>
@@ -118,20 +117,41 @@ rg_status validate_window(const rg_window* W) {
   return W != nullptr && (W->size < 1 || W->sink < 0) ? RG_ERR_SHAPE : RG_OK;
 }
 
-// A request's column groups of up to `waves` tiles, and the keys of the longest.
+// How a kernel takes a batch: column groups of up to `group` tiles, dealt evenly or
+// full but for the last; steps of `keys` keys; work groups that run at once; the
+// time of a step of so many tiles, of an item's start and end, and of the partials
+// of a split, in hundredths of a microsecond.
+struct Shape {
+  int group, keys, per_cu;
+  bool even;
+  int64_t (*step)(int64_t tiles);
+  int64_t start, parts, least;
+};
+Shape kv8_shape(int head_dim) {
+  return {kKv8Waves, kKv8Step, head_dim == 64 ? 3 : 2, false, [](int64_t tiles) -> int64_t {
+            constexpr int64_t t[] = {0, 6, 9, 15, 16};
+            return 16 * t[tiles];
+          }, 300, 100, 128};
+}
+Shape bf16_shape(bool narrow, int head_dim) {
+  return {narrow ? kWindowWaves / 2 : kWindowWaves, window_keys(narrow ? kWindowWaves / 2 : kWindowWaves, head_dim),
+          narrow ? 2 : 1, true, [](int64_t tiles) { return std::max<int64_t>(270, 130 + 47 * tiles); }, 600, 200, 270};
+}
+
+// A request's column groups and the steps of the longest.
 struct Groups {
   int64_t count = 0, tiles = 0, per = 0;  // groups, tiles in all, tiles of a group at most
-  int64_t steps = 0;                      // buffers of the longest
+  int64_t steps = 0;
 };
 template <bool BR>
-Groups groups_of(const rg_attn_layout* L, int r, Limits w, int waves) {
+Groups groups_of(const rg_attn_layout* L, int r, Limits w, const Shape& shape) {
   Groups q;
   const int n = L->q_indptr[r + 1] - L->q_indptr[r], g = L->num_q_heads / L->num_kv_heads;
   if (n == 0) return q;
   const int64_t M = (int64_t)n * g;
   q.tiles = (M + 31) / 32;
-  q.count = (q.tiles + waves - 1) / waves;
-  q.per = (q.tiles + q.count - 1) / q.count;
+  q.count = (q.tiles + shape.group - 1) / shape.group;
+  q.per = shape.even ? (q.tiles + q.count - 1) / q.count : std::min<int64_t>(q.tiles, shape.group);
   q.count = (q.tiles + q.per - 1) / q.per;
   int keys = 0;
   for (int64_t k = 0; k < q.count; ++k) {
@@ -139,52 +159,41 @@ Groups groups_of(const rg_attn_layout* L, int r, Limits w, int waves) {
     const WindowSpan s = window_span<BR>(L->ctx_len[r], L->n_verify[r], n, (int)(c0 / g), (int)((c1 - 1) / g) + 1, w.size, w.sink);
     keys = std::max(keys, s.keys);
   }
-  q.steps = (keys + window_keys(waves, L->head_dim) - 1) / window_keys(waves, L->head_dim);
+  q.steps = (keys + shape.keys - 1) / shape.keys;
   return q;
 }
 
-// Time of a buffer of an item with this many tiles, in quarters of that of a
-// buffer at the copy rate; of its start and end, and of its partials beside; and
-// the least of an item's keys.
-constexpr int64_t kStartCost = 8, kPartCost = 4, kLeastCost = 8;
-int64_t step_cost(int64_t tiles) { return std::max<int64_t>(4, tiles); }
-
 template <typename Plan, int MaxReq>
-rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits w, FullPlan<Plan>& fp) {
+rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits w, bool kv8, FullPlan<Plan>& fp) {
   constexpr bool BR = __is_same(Plan, WindowPlanBr);
   const int R = L->num_requests, hkv = L->num_kv_heads, cus = device_cus();
-  std::vector<Groups> groups(R);
+  const int64_t g = L->num_q_heads / hkv;
   int64_t widest = 0;
-  for (int r = 0; r < R; ++r) {
-    groups[r] = groups_of<BR>(L, r, w, kWindowWaves / 2);
-    widest = std::max(widest, groups[r].tiles);
-  }
-  fp.narrow = widest <= kWindowWaves / 2;
-  if (getenv("RGX_NARROW")) fp.narrow = atoi(getenv("RGX_NARROW"));
-  const int waves = fp.narrow ? kWindowWaves / 2 : kWindowWaves, keys = window_keys(waves, L->head_dim);
-  if (!fp.narrow)
-    for (int r = 0; r < R; ++r) groups[r] = groups_of<BR>(L, r, w, waves);
+  for (int r = 0; r < R; ++r) widest = std::max<int64_t>(widest, (L->q_indptr[r + 1] - L->q_indptr[r]) * g);
+  fp.narrow = widest <= 32 * kWindowWaves / 2;
+  const Shape shape = kv8 ? kv8_shape(L->head_dim) : bf16_shape(fp.narrow, L->head_dim);
+  std::vector<Groups> groups(R);
+  for (int r = 0; r < R; ++r) groups[r] = groups_of<BR>(L, r, w, shape);
   // Cost of an item at most.  Candidates are the least that give one round of
   // items, two, ...; a round's end is uneven, an item's start and its partials cost.
-  const int64_t slots = (int64_t)cus * (fp.narrow ? 2 : 1);
+  const int64_t slots = (int64_t)cus * shape.per_cu;
   int64_t work = 0;
-  for (const Groups& q : groups) work += q.count * hkv * q.steps * step_cost(q.per);
+  for (const Groups& q : groups) work += q.count * hkv * q.steps * shape.step(q.per);
   auto runs_of = [&](const Groups& q, int64_t target) {
-    const int64_t most = std::min<int64_t>(kMaxRunSteps, std::max<int64_t>(1, target / step_cost(q.per)));  // steps of a run
+    const int64_t most = std::min<int64_t>(kMaxRunSteps, std::max<int64_t>(1, target / shape.step(q.per)));  // steps of a run
     const int64_t n = (q.steps + most - 1) / most, each = (q.steps + n - 1) / n;
     return (q.steps + each - 1) / each;
   };
   int64_t target = 0;
   double best = 0.;
-  const char* E = getenv("RGX_ROUNDS");
-  for (int64_t rounds = E ? atoi(E) : 1; rounds <= (E ? atoi(E) : 4); ++rounds) {
-    int64_t t = std::max<int64_t>(kLeastCost, work / (rounds * slots)), items, whole;
+  for (int64_t rounds = 1; rounds <= 4; ++rounds) {
+    int64_t t = std::max<int64_t>(shape.least, work / (rounds * slots)), items, whole;
     int64_t longest, total;
     for (;; t += 1 + t / 16) {
       items = whole = longest = total = 0;
       for (const Groups& q : groups) {
         if (!q.count) continue;
-        const int64_t n = runs_of(q, t), each = (q.steps + n - 1) / n * step_cost(q.per) + kStartCost + (n > 1 ? kPartCost : 0);
+        const int64_t n = runs_of(q, t), each = (q.steps + n - 1) / n * shape.step(q.per) + shape.start + (n > 1 ? shape.parts : 0);
         items += q.count * hkv * n;
         whole += q.count * hkv;
         total += q.count * hkv * n * each;
@@ -200,14 +209,13 @@ rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits
     }
     if (items <= slots * rounds && items == whole) break;  // nothing is split
   }
-  if (getenv("RGX_P")) fprintf(stderr, "narrow %d target %ld best %f work %ld slots %ld\n", (int)fp.narrow, (long)target, best, (long)work, (long)slots);
   // Costliest work items first.
   std::vector<int> order(R);
   std::iota(order.begin(), order.end(), 0);
   std::vector<int64_t> cost(R, 0);
   for (int r = 0; r < R; ++r) {
     const Groups& q = groups[r];
-    if (q.count) cost[r] = (q.steps + runs_of(q, target) - 1) / runs_of(q, target) * step_cost(q.per);
+    if (q.count) cost[r] = (q.steps + runs_of(q, target) - 1) / runs_of(q, target) * shape.step(q.per);
   }
   std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return cost[x] > cost[y]; });
   int64_t most_part = 0;
@@ -242,7 +250,7 @@ rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits
     p.req[p.num_req].part_start = (int32_t)part;
     p.total_comb = (int32_t)comb;
     p.grid_items = (int32_t)round_up(items, 8);
-    if (!fits_launch(items, 64 * waves) || !fits_launch(comb, 64 * kWindowMergeWaves)) return RG_ERR_UNSUPPORTED;
+    if (!fits_launch(items, 64 * shape.group) || !fits_launch(comb, 64 * kWindowMergeWaves)) return RG_ERR_UNSUPPORTED;
     most_part = std::max(most_part, part);
     if (items > 0) fp.launches.push_back(p);
   }
@@ -253,28 +261,36 @@ rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits
 
 // Calls f(plan) with the plan of a layout and its branches (or NULL).
 template <typename F>
-rg_status with_window_plan(const rg_attn_layout* L, const rg_branch_layout* B, const rg_window* W, F f) try {
+rg_status with_window_plan(const rg_attn_layout* L, const rg_branch_layout* B, const rg_window* W, bool kv8, F f) try {
   rg_status st = validate_layout(L);
   if (st == RG_OK) st = validate_window(W);
   if (st != RG_OK) return st;
   if (B == nullptr) {
     FullPlan<WindowPlan> fp;
-    st = plan_window<WindowPlan, kMaxReqPerLaunch>(L, nullptr, limits_of(W), fp);
+    st = plan_window<WindowPlan, kMaxReqPerLaunch>(L, nullptr, limits_of(W), kv8, fp);
     return st != RG_OK ? st : f(fp);
   }
   st = validate_branches(L, B);
   if (st != RG_OK) return st;
   FullPlan<WindowPlanBr> fp;
-  st = plan_window<WindowPlanBr, kMaxReqPerLaunchBr>(L, B, limits_of(W), fp);
+  st = plan_window<WindowPlanBr, kMaxReqPerLaunchBr>(L, B, limits_of(W), kv8, fp);
   return st != RG_OK ? st : f(fp);
 } catch (const std::bad_alloc&) {  // nothing is launched before a plan is whole
   return RG_ERR_WORKSPACE;
 }
 
+rg_status query_workspace(const rg_attn_layout* L, const rg_branch_layout* B, const rg_window* W, bool kv8, size_t* bytes) {
+  if (bytes == nullptr) return RG_ERR_NULL;
+  return with_window_plan(L, B, W, kv8, [&](const auto& fp) {
+    *bytes = fp.ws_bytes;
+    return RG_OK;
+  });
+}
+
 rg_status run_attention(const rg_attn_layout* L, const rg_branch_layout* B, const rg_window* W, const uint16_t* q,
                         const void* k_cache, const void* v_cache, const float* scales, bool kv8, uint16_t* out, float* lse,
                         void* ws, size_t ws_bytes, void* stream) {
-  return with_window_plan(L, B, W, [&](const auto& fp) -> rg_status {
+  return with_window_plan(L, B, W, kv8, [&](const auto& fp) -> rg_status {
     if (!q || !k_cache || !out || (kv8 ? !scales : !v_cache)) return RG_ERR_NULL;
     if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(scales, 4) || !aligned(out, 16) ||
         !aligned(lse, 4) || !aligned(L->page_indices, 4))
@@ -294,13 +310,16 @@ rg_status run_attention(const rg_attn_layout* L, const rg_branch_layout* B, cons
     a.hkv = L->num_kv_heads;
     a.g = a.hq / a.hkv;
     set_divisor(a.g, a.g_mul, a.g_shift);
+    set_divisor(a.hkv, a.hkv_mul, a.hkv_shift);
     const Limits w = limits_of(W);
     a.size = w.size;
     a.sink = w.sink;
     a.sm_scale = softmax_scale(L);
     a.scale_log2 = a.sm_scale * 1.4426950408889634f;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
     for (const auto& p : fp.launches)
-      if (launch_window_attention(a, p, L->head_dim, kv8, fp.narrow, static_cast<hipStream_t>(stream)) != hipSuccess)
+      if ((kv8 ? launch_kv8_attention(a, p, L->head_dim, s) : launch_window_attention(a, p, L->head_dim, fp.narrow, s)) !=
+          hipSuccess)
         return RG_ERR_HIP;
     return RG_OK;
   });
@@ -352,11 +371,7 @@ rg_status rg_kv8_read(const rg_attn_layout* layout, const uint8_t* cache, const 
 
 rg_status rg_kv8_attention_workspace(const rg_attn_layout* layout, const rg_branch_layout* branches,
                                      const rg_window* window, size_t* bytes) {
-  if (bytes == nullptr) return RG_ERR_NULL;
-  return with_window_plan(layout, branches, window, [&](const auto& fp) {
-    *bytes = fp.ws_bytes;
-    return RG_OK;
-  });
+  return query_workspace(layout, branches, window, true, bytes);
 }
 
 rg_status rg_kv8_attention(const rg_attn_layout* layout, const rg_branch_layout* branches, const rg_window* window,
@@ -368,7 +383,7 @@ rg_status rg_kv8_attention(const rg_attn_layout* layout, const rg_branch_layout*
 rg_status rg_window_attention_workspace(const rg_attn_layout* layout, const rg_branch_layout* branches,
                                         const rg_window* window, size_t* bytes) {
   if (bytes == nullptr || window == nullptr) return RG_ERR_NULL;
-  return rg_kv8_attention_workspace(layout, branches, window, bytes);
+  return query_workspace(layout, branches, window, false, bytes);
 }
 
 rg_status rg_window_attention(const rg_attn_layout* layout, const rg_branch_layout* branches, const rg_window* window,

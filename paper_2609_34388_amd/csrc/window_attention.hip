@@ -1,5 +1,5 @@
-// Hybrid-mask attention over a sliding window with sinks, or over all keys, of
-// a bf16 or an 8-bit paged cache (gfx950).
+// Hybrid-mask attention over a sliding window with sinks of the bf16 paged cache
+// (gfx950), and the merge of it and of attention over the 8-bit cache.
 //
 // The mathematics is that of attention.hip: S^T = K Q^T, P = exp2 of the scaled
 // scores less a running reference, O^T += V^T P^T, in matrix instructions with
@@ -10,37 +10,20 @@
 // are counted without the gap between, and limits moved alike.  So a group of a
 // prompt reads its window, not the context, and no key behind its last row.
 //
-// Keys pass through LDS, a buffer at a time and two buffers of LDS, as bf16 in the
-// layout of attention.hip: all waves load their share of the next buffers into
-// registers, ahead of the buffer that is computed, and put it into LDS before the
-// one barrier of a buffer.  8-bit codes are decoded on that way, once for all
-// columns (a conversion makes two bf16 and applies the block's scale; the values are
-// exact).  V of slots that no row may see, which can hold anything, is put in as zero.
+// Keys pass through LDS, a buffer at a time and two buffers of LDS, in the layout of
+// attention.hip: all waves load their share of the next buffer into registers while
+// one is computed, and put it into LDS before the one barrier of a buffer.  V of
+// slots that no row may see, which can hold anything, is put in as zero.
 //
 // Softmax online in base 2; the product takes P rounded to bf16 (off by at most
 // 2^-8 of each term, as the output's own rounding).  Two sums run in fp32: of P,
 // for the lse, and of the rounded P, by which the product is divided, so that the
 // weights add up to one.  Runs of a request's keys meet in fp32 in the workspace.
-#include "kv8_device.h"
+#include "attention_device.h"
 #include "window_internal.h"
 
 namespace rg {
 namespace {
-
-// How a cache's pages become K and V of a buffer in LDS.  A 16-byte unit of a page
-// and head is `w`, of UNITS<D>.
-struct Bf16Cache {
-  static constexpr bool KV8 = false;
-  static constexpr int DEPTH = 1;  // buffers in flight
-  template <int D>
-  static constexpr int UNITS = 2 * D;
-};
-struct Kv8Cache {
-  static constexpr bool KV8 = true;
-  static constexpr int DEPTH = 2;
-  template <int D>
-  static constexpr int UNITS = D;
-};
 
 // Swizzle of the two 16-byte halves of a dimension row of a V page in LDS.
 __device__ __forceinline__ int vswz(int d) { return ((d >> 2) ^ (d >> 3)) & 1; }
@@ -55,13 +38,13 @@ struct WindowShape {
   static constexpr int LDS = 4 * BUF > NW * STATE * 4 ? 4 * BUF : NW * STATE * 4;
 };
 
-template <typename Cache, int D, int NW, typename Plan>
+template <int D, int NW, typename Plan>
 __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, Plan p) {
   using S = WindowShape<D, NW>;
   constexpr bool BR = __is_same(Plan, WindowPlanBr);
   constexpr int DT = S::DT, KSTEPS = D / 16, NCH = D / 8, THREADS = 64 * NW;
-  constexpr int UNITS = Cache::template UNITS<D>;
-  constexpr int PER = S::PAGES * UNITS / THREADS;  // units of K, and of V, of a thread and buffer
+  constexpr int UNITS = 2 * D;                     // 16-byte units of K, and of V, of a page and head
+  constexpr int PER = S::PAGES * UNITS / THREADS;  // of a thread and buffer
   constexpr int STEP = THREADS / UNITS;            // pages between two of them
   constexpr int PAGE_LDS = 32 * D;                 // bytes of K, or V, of a page in LDS
   static_assert(STEP >= 1 && PER * STEP == S::PAGES && UNITS % 64 == 0, "a wave's unit is of one page");
@@ -75,14 +58,17 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
   const int g = a.g, M = n * g, tiles = (M + 31) / 32;
   const int nch = rq.runs & 0xffff, run = (int)(rq.runs >> 16) * S::KEYS;
   const int ncg = (tiles + NW - 1) / NW, tpg = (tiles + ncg - 1) / ncg;
-  // Items of a request: runs, then KV heads, then column groups, so that the
-  // groups of a head, which share most keys, follow on one XCD (8 KV heads).
-  int local = item - rq.item_start, c = 0;
-  if (nch > 1) {
-    c = local % nch;
-    local /= nch;
+  // Items of a request: KV heads, then column groups, then runs, so that the groups
+  // of a head, which share most keys, follow on one XCD (8 KV heads).  A division by
+  // the groups only where there are several.
+  const int local = item - rq.item_start;
+  int cg = 0, c = quotient(local, a.hkv_mul, a.hkv_shift);
+  const int hk = local - c * a.hkv;
+  if (ncg > 1) {
+    const int of = c;
+    c /= ncg;
+    cg = of - c * ncg;
   }
-  const int cg = local / a.hkv, hk = local - cg * a.hkv;
   const int tile0 = cg * tpg, nct = min(tpg, tiles - tile0);
   const int row0 = row_of(a, tile0 * 32), row1 = row_of(a, min(M, (tile0 + nct) * 32) - 1) + 1;
   const WindowSpan span = window_span<BR>(L, nver, n, row0, row1, a.size, a.sink);
@@ -117,9 +103,10 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
     first = wave - kgi;
     apart = 1;
   }
-  const int col = (tile0 + ct) * 32 + lc;
-  const bool on = ct < nct, valid = on && col < M;
-  const int tok = valid ? row_of(a, col) : 0, hh = col - tok * g;
+  // Columns behind the last are that one again, and not written.
+  const bool on = ct < nct, valid = on && (tile0 + ct) * 32 + lc < M;
+  const int col = min((tile0 + ct) * 32 + lc, M - 1);
+  const int tok = row_of(a, col), hh = col - tok * g;
 
   // ---- copies
   typedef const int32_t __attribute__((address_space(4))) * cpage_ptr;
@@ -128,113 +115,78 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
   const int page0 = kbeg / kPageSize, last_page = max((kend - 1) / kPageSize, 0);
   const int head_pages = span.head / kPageSize, gap_pages = span.gap / kPageSize;
   const int my_page = wave * 64 / UNITS, w = tid % UNITS;
-  const size_t page_bytes = (size_t)a.hkv * UNITS * 16 * (Cache::KV8 ? 2 : 1), head_bytes = page_bytes / a.hkv;
+  const size_t head_bytes = UNITS * 16, page_bytes = a.hkv * head_bytes;
   const uint8_t* kbase = a.k_cache + (size_t)hk * head_bytes + 16 * w;
-  const uint8_t* vbase = (Cache::KV8 ? a.k_cache + 16 * D : a.v_cache) + (size_t)hk * head_bytes + 16 * w;
-  // Places of unit w in a page's K and V in LDS (an 8-bit unit becomes two).
-  int kat[Cache::KV8 ? 2 : 1], vat[Cache::KV8 ? 2 : 1], vkey;  // vkey: first key of V's unit
-  if constexpr (Cache::KV8) {
-    const int slot = w % 32 / 2, ch = 4 * (w / 32) + 2 * (w & 1);
-    kat[0] = slot * 2 * D + 16 * (ch ^ (swap23(slot) & (NCH - 1)));
-    kat[1] = slot * 2 * D + 16 * ((ch + 1) ^ (swap23(slot) & (NCH - 1)));
-    const int d = 2 * (w % (D / 2)), half = w / (D / 2);
-    vat[0] = d * 32 + 16 * (half ^ vswz(d));
-    vat[1] = (d + 1) * 32 + 16 * (half ^ vswz(d + 1));
-    vkey = 8 * half;
-  } else {
-    const int slot = w / NCH, ch = w % NCH;
-    kat[0] = slot * 2 * D + 16 * (ch ^ (swap23(slot) & (NCH - 1)));
-    const int d = w / 2, half = w & 1;
-    vat[0] = d * 32 + 16 * (half ^ vswz(d));
-    vkey = 8 * half;
-  }
-  struct Set {
-    u32x4 k[PER], v[PER];
-    float ks[PER], vs[PER];
-  };
+  const uint8_t* vbase = a.v_cache + (size_t)hk * head_bytes + 16 * w;
+  // Places of unit w in a page's K and V in LDS; the first key of V's unit.
+  const int kslot = w / NCH, vd = w / 2, vhalf = w & 1, vkey = 8 * vhalf;
+  const int kat = kslot * 2 * D + 16 * ((w % NCH) ^ (swap23(kslot) & (NCH - 1))), vat = vd * 32 + 16 * (vhalf ^ vswz(vd));
+  u32x4 kreg[PER], vreg[PER];  // the buffer in flight
+  int pg[PER];                 // pages of the one after it
   // Pages of this wave's units of buffer s; past the run's last page that page again.
-  auto pages_of = [&](int s, int (&pg)[PER]) {
+  auto pages_of = [&](int s) {
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
       const int at = min(page0 + s * S::PAGES + my_page + e * STEP, last_page);
       pg[e] = pages[at < head_pages ? at : at + gap_pages];
     }
   };
-  auto load = [&](const int (&pg)[PER], Set& x) {
+  auto load = [&]() {
 #pragma unroll
-    for (int e = 0; e < PER; ++e) x.k[e] = *(const u32x4*)(kbase + (size_t)pg[e] * page_bytes);
+    for (int e = 0; e < PER; ++e) kreg[e] = *(const u32x4*)(kbase + (size_t)pg[e] * page_bytes);
 #pragma unroll
-    for (int e = 0; e < PER; ++e) x.v[e] = *(const u32x4*)(vbase + (size_t)pg[e] * page_bytes);
-    if constexpr (Cache::KV8) {
-#pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        const cscale_ptr at = (cscale_ptr)(a.scales + 2 * ((size_t)pg[e] * a.hkv + hk));
-        x.ks[e] = at[0];
-        x.vs[e] = at[1];
-      }
-    }
+    for (int e = 0; e < PER; ++e) vreg[e] = *(const u32x4*)(vbase + (size_t)pg[e] * page_bytes);
   };
-  auto store = [&](int s, const Set& x) {
-    char* kd = lds + (s & 1) * S::BUF + my_page * PAGE_LDS;
-    char* vd = lds + (2 + (s & 1)) * S::BUF + my_page * PAGE_LDS;
+  auto store = [&](int s) {
+    char* kd = lds + (s & 1) * S::BUF + my_page * PAGE_LDS + kat;
+    char* vd = lds + (2 + (s & 1)) * S::BUF + my_page * PAGE_LDS + vat;
     const int k0 = kbeg + s * S::KEYS;
     // V of slots behind the last key, and of those between the sinks and every window, is zero
     const bool edge = k0 + S::KEYS > kend || (k0 < span.lo && k0 + S::KEYS > a.sink);
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
-      const int to = e * STEP * PAGE_LDS;
-      u32x4 v[2];
-      if constexpr (Cache::KV8) {
-        *(u32x4*)(kd + to + kat[0]) = decode8_8(x.k[e][0], x.k[e][1], x.ks[e]);
-        *(u32x4*)(kd + to + kat[1]) = decode8_8(x.k[e][2], x.k[e][3], x.ks[e]);
-        v[0] = decode8_8(x.v[e][0], x.v[e][1], x.vs[e]);
-        v[1] = decode8_8(x.v[e][2], x.v[e][3], x.vs[e]);
-      } else {
-        *(u32x4*)(kd + to + kat[0]) = x.k[e];
-        v[0] = x.v[e];
-      }
+      u32x4 v = vreg[e];
       if (edge) {
         const int key = k0 + (my_page + e * STEP) * kPageSize + vkey;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           auto seen = [&](int k) { return k < kend && (k < a.sink || k >= span.lo); };
-          const uint32_t keep = (seen(key + 2 * i) ? 0xffffu : 0u) | (seen(key + 2 * i + 1) ? 0xffff0000u : 0u);
-          v[0][i] &= keep;
-          if (Cache::KV8) v[1][i] &= keep;
+          v[i] &= (seen(key + 2 * i) ? 0xffffu : 0u) | (seen(key + 2 * i + 1) ? 0xffff0000u : 0u);
         }
       }
-      *(u32x4*)(vd + to + vat[0]) = v[0];
-      if constexpr (Cache::KV8) *(u32x4*)(vd + to + vat[1]) = v[1];
+      *(u32x4*)(kd + e * STEP * PAGE_LDS) = kreg[e];
+      *(u32x4*)(vd + e * STEP * PAGE_LDS) = v;
     }
   };
+  const int nbuf = kend > kbeg ? (kend - kbeg + S::KEYS - 1) / S::KEYS : 0;
+  if (nbuf > 0) {
+    pages_of(0);
+    load();
+    if (nbuf > 1) pages_of(1);
+  }
 
   // ---- columns
   bf16x8 qf[KSTEPS];
   {
     const uint16_t* qrow = a.q + ((size_t)(rq.q_start + tok) * a.hq + hk * g + hh) * D;
 #pragma unroll
-    for (int s = 0; s < KSTEPS; ++s) {
-      u32x4 x = {0u, 0u, 0u, 0u};
-      if (valid) x = *(const u32x4*)(qrow + s * 16 + 8 * lh);
-      qf[s] = __builtin_bit_cast(bf16x8, x);
-    }
+    for (int s = 0; s < KSTEPS; ++s) qf[s] = *(const bf16x8*)(qrow + s * 16 + 8 * lh);
   }
   // Limits of the column: keys lo .. lim - 1 and below the sink, and slo .. shi - 1.
   int lim, slo, shi, lo;
   if constexpr (BR) {
-    key_limits<WindowReqBr, true>(rq, valid, tok, INT_MAX, lim, slo, shi);
+    key_limits<WindowReqBr, true>(rq, true, tok, INT_MAX, lim, slo, shi);
     // a branch row's position: the kept prefix and its place in the branch
     lo = tok < nver ? lim - a.size : min(lim, lim + (L + tok - slo) + 1 - a.size);
     slo -= span.gap;
     shi -= span.gap;
   } else {
-    key_limits<WindowReq, false>(rq, valid, tok, INT_MAX, lim, slo, shi);
+    key_limits<WindowReq, false>(rq, true, tok, INT_MAX, lim, slo, shi);
     lo = tok < nver ? lim - a.size : min(L + nver, L + tok + 1 - a.size);
   }
   lim -= span.gap;
   lo = max(lo - span.gap, 0);
   if (lo <= a.sink) lo = 0;
-  if (!valid) lim = lo = slo = shi = 0;
   // Of the wave's columns, from its first and last row: below min_lim no column has
   // an upper limit, from max_lo on none a lower one; nobody sees keys from `end` on,
   // or of sink .. min_lo - 1.  Where branches are among them, bounds of these.
@@ -323,7 +275,7 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
       m_run = m_new;
-      open = __any(m_new == kNegInf && valid);
+      open = __any(m_new == kNegInf);
       weigh();
     }
     l_run += sum;
@@ -358,34 +310,15 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
   };
 
   // ---- keys
-  const int nbuf = kend > kbeg ? (kend - kbeg + S::KEYS - 1) / S::KEYS : 0;
-  Set x[Cache::DEPTH];
-  int pg[PER];
-#pragma unroll
-  for (int s = 0; s < Cache::DEPTH; ++s) {
-    if (s >= nbuf) break;
-    pages_of(s, pg);
-    load(pg, x[s]);
-  }
-  if (Cache::DEPTH < nbuf) pages_of(Cache::DEPTH, pg);
-  auto step = [&](int s, Set& y) {
-    store(s, y);  // LDS of buffer s - 2: every wave was done with it before barrier s - 1
-    if (s + Cache::DEPTH < nbuf) {
-      load(pg, y);
-      if (s + Cache::DEPTH + 1 < nbuf) pages_of(s + Cache::DEPTH + 1, pg);
+#pragma unroll 1
+  for (int s = 0; s < nbuf; ++s) {
+    store(s);  // LDS of buffer s - 2: every wave was done with it before barrier s - 1
+    if (s + 1 < nbuf) {
+      load();
+      if (s + 2 < nbuf) pages_of(s + 2);
     }
     lds_barrier();
     compute(s);
-  };
-  int s = 0;
-  if constexpr (Cache::DEPTH == 2) {
-    for (; s + 1 < nbuf; s += 2) {
-      step(s, x[0]);
-      step(s + 1, x[1]);
-    }
-    if (s < nbuf) step(s, x[0]);
-  } else {
-    for (; s < nbuf; ++s) step(s, x[0]);
   }
 
   l_run += __shfl_xor(l_run, 32);
@@ -400,7 +333,7 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
       const u32x2 y = {pack_bf16x2(o.x * f, o.y * f), pack_bf16x2(o.z * f, o.w * f)};
       *(u32x2*)(a.out + orow * D + 8 * v + 4 * lh) = y;
     } else {
-      *(float4*)(a.part_o + tile * 32 * D + (v * 64 + lane) * 4) = o;
+      *(float4*)(a.part_o + tile * 32 * D + (v * 64 + lane) * 4) = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
     }
   };
   auto put_sums = [&](float m, float l) {
@@ -410,12 +343,11 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
   };
   if (NW == 4 ? nct > 2 : nct == NW) {  // no tile has more than one wave
     if (!valid) return;
-    const float f = nch == 1 ? 1.f / r_run : 1.f;
+    const float f = nch == 1 ? 1.f / r_run : whole;
 #pragma unroll
     for (int v = 0; v < 4 * DT; ++v) {
       float4 o = make_float4(acc[v / 4][4 * (v % 4)], acc[v / 4][4 * (v % 4) + 1], acc[v / 4][4 * (v % 4) + 2],
                              acc[v / 4][4 * (v % 4) + 3]);
-      if (nch > 1) o.x *= whole, o.y *= whole, o.z *= whole, o.w *= whole;
       put(v, o, f);
     }
     put_sums(m_run, l_run);
@@ -454,7 +386,7 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
       weight[k] *= states[k * stride + 64 * 16 * DT + 128 + lane];
     }
   }
-  const float inv = 1.f / l;
+  const float f = nch == 1 ? 1.f / l : 1.f;
 #pragma unroll 1
   for (int v = kgi * share; v < kgi * share + share; ++v) {
     float4 o = {0.f, 0.f, 0.f, 0.f};
@@ -463,7 +395,7 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
       const float4 y = *(const float4*)(states + (k < kg ? k : 0) * stride + (v * 64 + lane) * 4);
       o.x += weight[k] * y.x, o.y += weight[k] * y.y, o.z += weight[k] * y.z, o.w += weight[k] * y.w;
     }
-    put(v, o, inv);
+    put(v, o, f);
   }
   if (kgi == 0) put_sums(m, l);
 }
@@ -581,21 +513,15 @@ __global__ __launch_bounds__(64 * kWindowMergeWaves) void window_merge_kernel(Wi
 #pragma unroll
   for (int q = 0; q < ROWS; ++q) {
     const u32x2 w = {pack_bf16x2(o[q][0] * inv, o[q][1] * inv), pack_bf16x2(o[q][2] * inv, o[q][3] * inv)};
-    *(u32x2*)(a.out + orow * D + 8 * (v + q) + 4 * lh) = w;
+    const int d = a.scales != nullptr ? kv8_dim(DT, v + q, lh) : 8 * (v + q) + 4 * lh;
+    *(u32x2*)(a.out + orow * D + d) = w;
   }
   if (a.lse != nullptr && v == 0 && lh == 0) a.lse[orow] = m * a.sm_scale + __logf(l);
 }
 
-template <typename Cache, int D, typename Plan>
-hipError_t launch_impl(const WindowArgs& a, const Plan& p, bool narrow, hipStream_t stream) {
-  if (narrow)
-    hipLaunchKernelGGL((window_attn_kernel<Cache, D, kWindowWaves / 2, Plan>), dim3(p.grid_items),
-                       dim3(64 * kWindowWaves / 2), 0, stream, a, p);
-  else
-    hipLaunchKernelGGL((window_attn_kernel<Cache, D, kWindowWaves, Plan>), dim3(p.grid_items), dim3(64 * kWindowWaves), 0,
-                       stream, a, p);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.total_comb == 0) return e;
+template <int D, typename Plan>
+hipError_t merge_impl(const WindowArgs& a, const Plan& p, hipStream_t stream) {
+  if (p.total_comb == 0) return hipSuccess;
   const dim3 threads(64 * kWindowMergeWaves);
   if (p.max_chunks > 8 && p.total_comb <= 1024)  // many runs, and few enough rows to be bound by latency
     hipLaunchKernelGGL((window_merge_kernel<D, kWindowMergeWaves, Plan>), dim3(p.total_comb), threads, 0, stream, a, p);
@@ -605,22 +531,31 @@ hipError_t launch_impl(const WindowArgs& a, const Plan& p, bool narrow, hipStrea
                        threads, 0, stream, a, p);
   return hipGetLastError();
 }
-template <typename Plan>
-hipError_t launch_any(const WindowArgs& a, const Plan& p, int head_dim, bool kv8, bool narrow, hipStream_t stream) {
-  if (head_dim == 128)
-    return kv8 ? launch_impl<Kv8Cache, 128>(a, p, narrow, stream) : launch_impl<Bf16Cache, 128>(a, p, narrow, stream);
-  return kv8 ? launch_impl<Kv8Cache, 64>(a, p, narrow, stream) : launch_impl<Bf16Cache, 64>(a, p, narrow, stream);
+template <int D, typename Plan>
+hipError_t launch_impl(const WindowArgs& a, const Plan& p, bool narrow, hipStream_t stream) {
+  if (narrow)
+    hipLaunchKernelGGL((window_attn_kernel<D, kWindowWaves / 2, Plan>), dim3(p.grid_items),
+                       dim3(64 * kWindowWaves / 2), 0, stream, a, p);
+  else
+    hipLaunchKernelGGL((window_attn_kernel<D, kWindowWaves, Plan>), dim3(p.grid_items), dim3(64 * kWindowWaves), 0,
+                       stream, a, p);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : merge_impl<D>(a, p, stream);
 }
 
 }  // namespace
 
-hipError_t launch_window_attention(const WindowArgs& a, const WindowPlan& p, int head_dim, bool kv8, bool narrow,
-                                   hipStream_t stream) {
-  return launch_any(a, p, head_dim, kv8, narrow, stream);
+hipError_t launch_window_attention(const WindowArgs& a, const WindowPlan& p, int head_dim, bool narrow, hipStream_t stream) {
+  return head_dim == 128 ? launch_impl<128>(a, p, narrow, stream) : launch_impl<64>(a, p, narrow, stream);
 }
-hipError_t launch_window_attention(const WindowArgs& a, const WindowPlanBr& p, int head_dim, bool kv8, bool narrow,
-                                   hipStream_t stream) {
-  return launch_any(a, p, head_dim, kv8, narrow, stream);
+hipError_t launch_window_attention(const WindowArgs& a, const WindowPlanBr& p, int head_dim, bool narrow, hipStream_t stream) {
+  return head_dim == 128 ? launch_impl<128>(a, p, narrow, stream) : launch_impl<64>(a, p, narrow, stream);
+}
+hipError_t launch_window_merge(const WindowArgs& a, const WindowPlan& p, int head_dim, hipStream_t stream) {
+  return head_dim == 128 ? merge_impl<128>(a, p, stream) : merge_impl<64>(a, p, stream);
+}
+hipError_t launch_window_merge(const WindowArgs& a, const WindowPlanBr& p, int head_dim, hipStream_t stream) {
+  return head_dim == 128 ? merge_impl<128>(a, p, stream) : merge_impl<64>(a, p, stream);
 }
 
 }  // namespace rg

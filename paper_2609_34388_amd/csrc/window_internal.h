@@ -80,8 +80,8 @@ struct WindowArgs {
   float* part_o;   // per 32-column tile: 32 x D fp32 sums, 16-byte rows lane-interleaved
   float* part_ml;  // [partial columns][2] (reference of raw scores, sum)
   int32_t hq, hkv, g;
-  uint32_t g_mul;  // quotient by g
-  int32_t g_shift;
+  uint32_t g_mul, hkv_mul;  // quotient by g, by hkv
+  int32_t g_shift, hkv_shift;
   int32_t size, sink;  // of the window; size 2^30 for all keys
   float sm_scale, scale_log2;
 };
@@ -109,9 +109,18 @@ __host__ __device__ inline WindowSpan window_span(int L, int V, int n, int i0, i
   s.keys = end - s.gap;
   return s;
 }
-hipError_t launch_window_attention(const WindowArgs& a, const WindowPlan& p, int head_dim, bool kv8, bool narrow,
-                                   hipStream_t stream);
-hipError_t launch_window_attention(const WindowArgs& a, const WindowPlanBr& p, int head_dim, bool kv8, bool narrow,
-                                   hipStream_t stream);
+hipError_t launch_window_attention(const WindowArgs& a, const WindowPlan& p, int head_dim, bool narrow, hipStream_t stream);
+hipError_t launch_window_attention(const WindowArgs& a, const WindowPlanBr& p, int head_dim, bool narrow, hipStream_t stream);
+
+// Over the 8-bit cache: column groups of kKv8Waves tiles and a last one of what
+// remains, steps of kKv8Step keys.
+constexpr int kKv8Waves = 4, kKv8Step = 128;
+// The first of the four dims of row v of a lane in half-wave lh there.
+__host__ __device__ constexpr int kv8_dim(int dt, int v, int lh) { return 8 * dt * (v / dt) + 4 * dt * lh + 4 * (v % dt); }
+hipError_t launch_kv8_attention(const WindowArgs& a, const WindowPlan& p, int head_dim, hipStream_t stream);
+hipError_t launch_kv8_attention(const WindowArgs& a, const WindowPlanBr& p, int head_dim, hipStream_t stream);
+// The merge of both, of split requests' runs (nothing where there are none).
+hipError_t launch_window_merge(const WindowArgs& a, const WindowPlan& p, int head_dim, hipStream_t stream);
+hipError_t launch_window_merge(const WindowArgs& a, const WindowPlanBr& p, int head_dim, hipStream_t stream);
 
 }  // namespace rg
