@@ -100,7 +100,6 @@ rg_status run_append(const rg_attn_layout* L, const rg_rotation* R, const uint16
 template <typename Plan>
 struct FullPlan {
   std::vector<Plan> launches;
-  bool narrow = false;
   size_t ml_offset = 0, ws_bytes = 0;
 };
 
@@ -117,6 +116,7 @@ rg_status validate_window(const rg_window* W) {
   return W != nullptr && (W->size < 1 || W->sink < 0) ? RG_ERR_SHAPE : RG_OK;
 }
 
+constexpr int64_t kLongRound = 8000;  // hundredths of a microsecond, as below
 // How a kernel takes a batch: column groups of up to `group` tiles, dealt evenly or
 // full but for the last; steps of `keys` keys; work groups that run at once; the
 // time of a step of so many tiles, of an item's start and end, and of the partials
@@ -131,11 +131,11 @@ Shape kv8_shape(int head_dim) {
   return {kKv8Waves, kKv8Step, head_dim == 64 ? 3 : 2, false, [](int64_t tiles) -> int64_t {
             constexpr int64_t t[] = {0, 6, 9, 15, 16};
             return 16 * t[tiles];
-          }, 300, 100, 128};
+          }, 600, 600, 128};
 }
-Shape bf16_shape(bool narrow, int head_dim) {
-  return {narrow ? kWindowWaves / 2 : kWindowWaves, window_keys(narrow ? kWindowWaves / 2 : kWindowWaves, head_dim),
-          narrow ? 2 : 1, true, [](int64_t tiles) { return std::max<int64_t>(270, 130 + 47 * tiles); }, 600, 200, 270};
+Shape bf16_shape(int head_dim) {
+  return {kWindowWaves, window_keys(head_dim), 2, true, [](int64_t tiles) { return std::max<int64_t>(270, 130 + 47 * tiles); },
+          600, 200, 270};
 }
 
 // A request's column groups and the steps of the longest.
@@ -144,20 +144,25 @@ struct Groups {
   int64_t steps = 0;
 };
 template <bool BR>
-Groups groups_of(const rg_attn_layout* L, int r, Limits w, const Shape& shape) {
+Groups groups_of(const rg_attn_layout* L, int r, Limits w, const Shape& shape, int g) {
   Groups q;
-  const int n = L->q_indptr[r + 1] - L->q_indptr[r], g = L->num_q_heads / L->num_kv_heads;
+  const int n = L->q_indptr[r + 1] - L->q_indptr[r];
   if (n == 0) return q;
-  const int64_t M = (int64_t)n * g;
-  q.tiles = (M + 31) / 32;
-  q.count = (q.tiles + shape.group - 1) / shape.group;
-  q.per = shape.even ? (q.tiles + q.count - 1) / q.count : std::min<int64_t>(q.tiles, shape.group);
-  q.count = (q.tiles + q.per - 1) / q.per;
+  q.tiles = ((int64_t)n * g + 31) / 32;
+  q.count = 1;
+  q.per = q.tiles;
   int keys = 0;
-  for (int64_t k = 0; k < q.count; ++k) {
-    const int64_t c0 = k * q.per * 32, c1 = std::min(M, (k + 1) * q.per * 32);
-    const WindowSpan s = window_span<BR>(L->ctx_len[r], L->n_verify[r], n, (int)(c0 / g), (int)((c1 - 1) / g) + 1, w.size, w.sink);
-    keys = std::max(keys, s.keys);
+  if (q.tiles <= shape.group) {
+    keys = window_span<BR>(L->ctx_len[r], L->n_verify[r], n, 0, n, w.size, w.sink).keys;
+  } else {
+    q.count = (q.tiles + shape.group - 1) / shape.group;
+    q.per = shape.even ? (q.tiles + q.count - 1) / q.count : shape.group;
+    q.count = (q.tiles + q.per - 1) / q.per;
+    for (int64_t k = 0; k < q.count; ++k) {
+      const int64_t c0 = k * q.per * 32, c1 = std::min((int64_t)n * g, (k + 1) * q.per * 32);
+      const WindowSpan s = window_span<BR>(L->ctx_len[r], L->n_verify[r], n, (int)(c0 / g), (int)((c1 - 1) / g) + 1, w.size, w.sink);
+      keys = std::max(keys, s.keys);
+    }
   }
   q.steps = (keys + shape.keys - 1) / shape.keys;
   return q;
@@ -167,55 +172,85 @@ template <typename Plan, int MaxReq>
 rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits w, bool kv8, FullPlan<Plan>& fp) {
   constexpr bool BR = __is_same(Plan, WindowPlanBr);
   const int R = L->num_requests, hkv = L->num_kv_heads, cus = device_cus();
-  const int64_t g = L->num_q_heads / hkv;
-  int64_t widest = 0;
-  for (int r = 0; r < R; ++r) widest = std::max<int64_t>(widest, (L->q_indptr[r + 1] - L->q_indptr[r]) * g);
-  fp.narrow = widest <= 32 * kWindowWaves / 2;
-  const Shape shape = kv8 ? kv8_shape(L->head_dim) : bf16_shape(fp.narrow, L->head_dim);
+  const Shape shape = kv8 ? kv8_shape(L->head_dim) : bf16_shape(L->head_dim);
   std::vector<Groups> groups(R);
-  for (int r = 0; r < R; ++r) groups[r] = groups_of<BR>(L, r, w, shape);
-  // Cost of an item at most.  Candidates are the least that give one round of
-  // items, two, ...; a round's end is uneven, an item's start and its partials cost.
-  const int64_t slots = (int64_t)cus * shape.per_cu;
-  int64_t work = 0;
-  for (const Groups& q : groups) work += q.count * hkv * q.steps * shape.step(q.per);
+  for (int r = 0; r < R; ++r) groups[r] = groups_of<BR>(L, r, w, shape, L->num_q_heads / hkv);
   auto runs_of = [&](const Groups& q, int64_t target) {
-    const int64_t most = std::min<int64_t>(kMaxRunSteps, std::max<int64_t>(1, target / shape.step(q.per)));  // steps of a run
-    const int64_t n = (q.steps + most - 1) / most, each = (q.steps + n - 1) / n;
-    return (q.steps + each - 1) / each;
+    // in 32 bits, whose divisions are the faster
+    const uint32_t steps = (uint32_t)q.steps, step = (uint32_t)shape.step(q.per);
+    const uint32_t most = std::min<uint32_t>(kMaxRunSteps, std::max(1u, (uint32_t)std::min<int64_t>(target, UINT32_MAX) / step));
+    if (most >= steps) return (int64_t)1;
+    const uint32_t n = (steps + most - 1) / most, each = (steps + n - 1) / n;  // steps of a run
+    return (int64_t)((steps + each - 1) / each);
   };
-  int64_t target = 0;
-  double best = 0.;
-  for (int64_t rounds = 1; rounds <= 4; ++rounds) {
-    int64_t t = std::max<int64_t>(shape.least, work / (rounds * slots)), items, whole;
-    int64_t longest, total;
-    for (;; t += 1 + t / 16) {
-      items = whole = longest = total = 0;
-      for (const Groups& q : groups) {
-        if (!q.count) continue;
-        const int64_t n = runs_of(q, t), each = (q.steps + n - 1) / n * shape.step(q.per) + shape.start + (n > 1 ? shape.parts : 0);
-        items += q.count * hkv * n;
-        whole += q.count * hkv;
-        total += q.count * hkv * n * each;
-        longest = std::max(longest, each);
+  // Cost of an item at most: the least that gives one round of items, or where a
+  // round is long (kLongRound) as many as promise the earliest end: a long round
+  // ends unevenly, an item's start and its partials cost.
+  struct Load {
+    Groups q;
+    int64_t items;  // whole
+  };
+  std::vector<Load> loads;  // those alike together: a batch has few kinds
+  int64_t work = 0, whole = 0, whole_cost = 0;
+  for (const Groups& q : groups) {
+    if (q.count == 0) continue;
+    work += q.count * hkv * q.steps * shape.step(q.per);
+    whole += q.count * hkv;
+    whole_cost = std::max(whole_cost, q.steps * shape.step(q.per));
+    auto same = std::find_if(loads.begin(), loads.end(), [&](const Load& x) { return x.q.steps == q.steps && x.q.per == q.per; });
+    if (same == loads.end()) loads.push_back({q, q.count * hkv});
+    else same->items += q.count * hkv;
+  }
+  const int64_t slots = (int64_t)cus * shape.per_cu;
+  auto items_of = [&](int64_t target) {
+    int64_t items = 0;
+    for (const Load& x : loads) items += x.items * runs_of(x.q, target);
+    return items;
+  };
+  auto fit = [&](int64_t rounds) {  // to 3 %
+    if (whole >= rounds * slots) return whole_cost;
+    int64_t lo = std::max<int64_t>(shape.least, work / (rounds * slots)), hi = std::max(lo, whole_cost);
+    if (items_of(lo) <= rounds * slots) return lo;
+    while (hi - lo > 1 + lo / 32) {
+      const int64_t mid = (lo + hi) / 2;
+      if (items_of(mid) <= rounds * slots) hi = mid;
+      else lo = mid;
+    }
+    return hi;
+  };
+  auto time_of = [&](int64_t target) {
+    int64_t items = 0, longest = 0, total = 0;
+    for (const Load& x : loads) {
+      const int64_t n = runs_of(x.q, target);
+      const int64_t each = (x.q.steps + n - 1) / n * shape.step(x.q.per) + shape.start + (n > 1 ? shape.parts : 0);
+      items += x.items * n;
+      total += x.items * n * each;
+      longest = std::max(longest, each);
+    }
+    return items <= slots ? longest : std::max(longest, total / slots + total / items / 2);
+  };
+  int64_t target = fit(1);
+  if (target > kLongRound) {
+    int64_t best = time_of(target);
+    for (int64_t rounds = 2; rounds <= 4; ++rounds) {
+      const int64_t t = fit(rounds), time = time_of(t);
+      if (time < best) {
+        target = t;
+        best = time;
       }
-      if (items <= std::max(whole, rounds * slots)) break;
     }
-    const double time = items <= slots ? (double)longest
-                                       : std::max((double)longest, (double)total / slots + 0.5 * (double)total / items);
-    if (target == 0 || time < best) {
-      target = t;
-      best = time;
-    }
-    if (items <= slots * rounds && items == whole) break;  // nothing is split
   }
   // Costliest work items first.
   std::vector<int> order(R);
   std::iota(order.begin(), order.end(), 0);
   std::vector<int64_t> cost(R, 0);
+  std::vector<int32_t> runs(R, 0), each(R, 0);  // of a request, and steps of one
   for (int r = 0; r < R; ++r) {
     const Groups& q = groups[r];
-    if (q.count) cost[r] = (q.steps + runs_of(q, target) - 1) / runs_of(q, target) * shape.step(q.per);
+    if (q.count == 0) continue;
+    runs[r] = (int32_t)runs_of(q, target);
+    each[r] = (int32_t)((q.steps + runs[r] - 1) / runs[r]);
+    cost[r] = each[r] * shape.step(q.per);
   }
   std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return cost[x] > cost[y]; });
   int64_t most_part = 0;
@@ -236,8 +271,8 @@ rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits
       x.item_start = (int32_t)items;
       x.part_start = (int32_t)part;
       if (q.count == 0) continue;
-      const int64_t nch = runs_of(q, target);
-      x.runs = (uint32_t)nch | (uint32_t)((q.steps + nch - 1) / nch) << 16;
+      const int64_t nch = runs[r];
+      x.runs = (uint32_t)nch | (uint32_t)each[r] << 16;
       items += hkv * q.count * nch;
       if (nch > 1) {
         p.max_chunks = std::max(p.max_chunks, (int32_t)nch);
@@ -318,7 +353,7 @@ rg_status run_attention(const rg_attn_layout* L, const rg_branch_layout* B, cons
     a.scale_log2 = a.sm_scale * 1.4426950408889634f;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     for (const auto& p : fp.launches)
-      if ((kv8 ? launch_kv8_attention(a, p, L->head_dim, s) : launch_window_attention(a, p, L->head_dim, fp.narrow, s)) !=
+      if ((kv8 ? launch_kv8_attention(a, p, L->head_dim, s) : launch_window_attention(a, p, L->head_dim, s)) !=
           hipSuccess)
         return RG_ERR_HIP;
     return RG_OK;

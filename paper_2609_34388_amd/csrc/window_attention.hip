@@ -28,19 +28,20 @@ namespace {
 // Swizzle of the two 16-byte halves of a dimension row of a V page in LDS.
 __device__ __forceinline__ int vswz(int d) { return ((d >> 2) ^ (d >> 3)) & 1; }
 
-template <int D, int NW>
+template <int D>
 struct WindowShape {
   static constexpr int DT = D / 32;
-  static constexpr int KEYS = window_keys(NW, D);
+  static constexpr int NW = kWindowWaves, KEYS = window_keys(D);
   static constexpr int PAGES = KEYS / kPageSize;
   static constexpr int BUF = KEYS * D * 2;          // bytes of K, or V, of a buffer
   static constexpr int STATE = 64 * 16 * DT + 192;  // floats of a wave's state
   static constexpr int LDS = 4 * BUF > NW * STATE * 4 ? 4 * BUF : NW * STATE * 4;
 };
 
-template <int D, int NW, typename Plan>
-__global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, Plan p) {
-  using S = WindowShape<D, NW>;
+template <int D, typename Plan>
+__global__ __launch_bounds__(64 * kWindowWaves, 2) void window_attn_kernel(WindowArgs a, Plan p) {
+  using S = WindowShape<D>;
+  constexpr int NW = S::NW;
   constexpr bool BR = __is_same(Plan, WindowPlanBr);
   constexpr int DT = S::DT, KSTEPS = D / 16, NCH = D / 8, THREADS = 64 * NW;
   constexpr int UNITS = 2 * D;                     // 16-byte units of K, and of V, of a page and head
@@ -77,32 +78,8 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
   const int tid = threadIdx.x, lane = tid & 63, lc = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  // A wave's column tile ct and key group kgi of kg: up to 4 tiles share the waves
-  // evenly, of 5 to 7 the first four have a wave each and the others share four.
-  int ct, kg, kgi, first, apart;  // the tile's waves: first, first + apart, ...
-  if (NW == 4 || nct <= 4) {
-    apart = nct <= 1 ? 1 : nct <= 2 ? 2 : 4;
-    ct = wave % apart;
-    kg = NW / apart;
-    kgi = wave / apart;
-    first = ct;
-  } else if (wave < 4 || nct == 8) {
-    ct = first = wave;
-    kg = apart = 1;
-    kgi = 0;
-  } else if (nct == 7) {
-    ct = min(wave, 6);
-    kg = wave < 6 ? 1 : 2;
-    kgi = wave < 6 ? 0 : wave - 6;
-    first = ct;
-    apart = 1;
-  } else {
-    kg = 4 / (nct - 4);
-    ct = 4 + (wave - 4) / kg;
-    kgi = (wave - 4) % kg;
-    first = wave - kgi;
-    apart = 1;
-  }
+  // A wave's column tile ct and key group kgi of kg, the tile's waves `apart` apart.
+  const int apart = nct <= 1 ? 1 : nct <= 2 ? 2 : 4, ct = wave % apart, kg = NW / apart, kgi = wave / apart;
   // Columns behind the last are that one again, and not written.
   const bool on = ct < nct, valid = on && (tile0 + ct) * 32 + lc < M;
   const int col = min((tile0 + ct) * 32 + lc, M - 1);
@@ -341,7 +318,7 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
     if (nch > 1) *(float2*)(a.part_ml + 2 * (tile * 32 + lc)) = make_float2(m, l);
     else if (a.lse != nullptr) a.lse[orow] = m * a.sm_scale + __logf(l);
   };
-  if (NW == 4 ? nct > 2 : nct == NW) {  // no tile has more than one wave
+  if (kg == 1) {
     if (!valid) return;
     const float f = nch == 1 ? 1.f / r_run : whole;
 #pragma unroll
@@ -369,7 +346,7 @@ __global__ __launch_bounds__(64 * NW, 2) void window_attn_kernel(WindowArgs a, P
   }
   lds_barrier();
   if (!valid) return;
-  const float* states = area + first * S::STATE;
+  const float* states = area + ct * S::STATE;
   const int stride = apart * S::STATE, share = 4 * DT / kg;
   float m = kNegInf, l = 0.f, weight[NW];
 #pragma unroll
@@ -532,24 +509,19 @@ hipError_t merge_impl(const WindowArgs& a, const Plan& p, hipStream_t stream) {
   return hipGetLastError();
 }
 template <int D, typename Plan>
-hipError_t launch_impl(const WindowArgs& a, const Plan& p, bool narrow, hipStream_t stream) {
-  if (narrow)
-    hipLaunchKernelGGL((window_attn_kernel<D, kWindowWaves / 2, Plan>), dim3(p.grid_items),
-                       dim3(64 * kWindowWaves / 2), 0, stream, a, p);
-  else
-    hipLaunchKernelGGL((window_attn_kernel<D, kWindowWaves, Plan>), dim3(p.grid_items), dim3(64 * kWindowWaves), 0,
-                       stream, a, p);
+hipError_t launch_impl(const WindowArgs& a, const Plan& p, hipStream_t stream) {
+  hipLaunchKernelGGL((window_attn_kernel<D, Plan>), dim3(p.grid_items), dim3(64 * kWindowWaves), 0, stream, a, p);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : merge_impl<D>(a, p, stream);
 }
 
 }  // namespace
 
-hipError_t launch_window_attention(const WindowArgs& a, const WindowPlan& p, int head_dim, bool narrow, hipStream_t stream) {
-  return head_dim == 128 ? launch_impl<128>(a, p, narrow, stream) : launch_impl<64>(a, p, narrow, stream);
+hipError_t launch_window_attention(const WindowArgs& a, const WindowPlan& p, int head_dim, hipStream_t stream) {
+  return head_dim == 128 ? launch_impl<128>(a, p, stream) : launch_impl<64>(a, p, stream);
 }
-hipError_t launch_window_attention(const WindowArgs& a, const WindowPlanBr& p, int head_dim, bool narrow, hipStream_t stream) {
-  return head_dim == 128 ? launch_impl<128>(a, p, narrow, stream) : launch_impl<64>(a, p, narrow, stream);
+hipError_t launch_window_attention(const WindowArgs& a, const WindowPlanBr& p, int head_dim, hipStream_t stream) {
+  return head_dim == 128 ? launch_impl<128>(a, p, stream) : launch_impl<64>(a, p, stream);
 }
 hipError_t launch_window_merge(const WindowArgs& a, const WindowPlan& p, int head_dim, hipStream_t stream) {
   return head_dim == 128 ? merge_impl<128>(a, p, stream) : merge_impl<64>(a, p, stream);

@@ -40,21 +40,20 @@ hipError_t launch_kv8_read(const Kv8ReadArgs& a, const AttnPlan& p, int head_dim
 
 // Attention over a window, or all, of the keys of a bf16 or an 8-bit cache.
 //
-// A request's 32-column tiles are dealt evenly to column groups of up to `waves`
-// tiles, the waves of a work group: kWindowWaves (one work group a compute unit),
-// or half of them in narrow launches (two).  A group's keys are those that its
-// rows may see: the sinks' pages and those from the first row's window on, counted
-// without the gap between them.  They are cut into `nch` runs of `run` keys, alike
-// for all groups of a request; runs past a group's keys are empty.
-constexpr int kWindowWaves = 8;
+// A request's 32-column tiles are dealt evenly to column groups of up to
+// kWindowWaves tiles.  A group's keys are those that its rows may see: the sinks'
+// pages and those from the first row's window on, counted without the gap between
+// them.  They are cut into runs, alike for all groups of a request; runs past a
+// group's keys are empty.
+constexpr int kWindowWaves = 4;  // waves of a work group; two work groups share a compute unit
 // Keys a buffer of a work group holds.
-__host__ __device__ constexpr int window_keys(int waves, int head_dim) { return 16 * waves * (128 / head_dim); }
+__host__ __device__ constexpr int window_keys(int head_dim) { return 16 * kWindowWaves * (128 / head_dim); }
 constexpr int kWindowMergeWaves = 4;  // waves of a work group of the merge
 constexpr int kWindowMergeRows = 2;   // rows of one
 struct WindowReq {
   int32_t q_start, ctx, nv, page_start, item_start;  // as in AttnReq
   int32_t part_start;                                // first partial tile in the workspace
-  uint32_t runs;                                     // nch (low 16 bits) | run / keys of a buffer << 16
+  uint32_t runs;                                     // their number (low 16 bits) | keys of one / keys of a step << 16
 };
 struct WindowReqBr : WindowReq {
   int32_t br[3], rep;  // as in AttnReqBr
@@ -109,8 +108,8 @@ __host__ __device__ inline WindowSpan window_span(int L, int V, int n, int i0, i
   s.keys = end - s.gap;
   return s;
 }
-hipError_t launch_window_attention(const WindowArgs& a, const WindowPlan& p, int head_dim, bool narrow, hipStream_t stream);
-hipError_t launch_window_attention(const WindowArgs& a, const WindowPlanBr& p, int head_dim, bool narrow, hipStream_t stream);
+hipError_t launch_window_attention(const WindowArgs& a, const WindowPlan& p, int head_dim, hipStream_t stream);
+hipError_t launch_window_attention(const WindowArgs& a, const WindowPlanBr& p, int head_dim, hipStream_t stream);
 
 // Over the 8-bit cache: column groups of kKv8Waves tiles and a last one of what
 // remains, steps of kKv8Step keys.
