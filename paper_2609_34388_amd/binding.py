@@ -249,6 +249,11 @@ class _Layout:
                             self.q_indptr.ctypes.data, self.n_verify.ctypes.data,
                             self.ctx_len.ctypes.data, self.page_indptr.ctypes.data,
                             self.page_indices.data_ptr())
+        # what calls ask for every time, without going through the struct
+        self.ref = ctypes.byref(self.c)
+        self.heads = (num_q_heads, num_kv_heads, head_dim)
+        self.pools = {"k": (num_pages, num_kv_heads, 16, head_dim), "v": (num_pages, num_kv_heads, head_dim, 16),
+                      "kv8": (num_pages, num_kv_heads, 32 * head_dim), "scales": (num_pages, num_kv_heads, 2)}
 
 
 def make_layout(q: torch.Tensor, k_cache: torch.Tensor, q_indptr, n_verify, ctx_len, page_indptr,
@@ -939,35 +944,44 @@ def make_rotation(inv_freq: torch.Tensor, *, interleaved: bool = False,
     return _Rotation(inv_freq, interleaved, positions)
 
 
-def _append_args(k, v, layout: _Layout, rotation: Optional[_Rotation], q, q_out, stream, *caches):
-    """Checks, and the arguments in front of the caches'."""
-    c = layout.c
-    hkv, d = c.num_kv_heads, c.head_dim
-    ks, vs = _rows(k, "k", hkv, d), _rows(v, "v", hkv, d)
+def _append(name: str, k, v, caches, layout: _Layout, rotation: Optional[_Rotation], q, q_out, stream):
+    """Checks and calls rg_kv_append or rg_kv8_append."""
+    hq, hkv, d = layout.heads
+    ks, vs, qs, qp, op = _rows(k, "k", hkv, d), _rows(v, "v", hkv, d), 0, None, None
     rows = k.shape[0]
     if v.shape[0] != rows:
         raise ValueError("k and v must have as many rows")
-    qs = 0
     if q is not None:
-        qs = _rows(q, "q", c.num_q_heads, d)
+        qs = _rows(q, "q", hq, d)
         if q.shape[0] != rows:
             raise ValueError("q and k must have as many rows")
         if q_out is None:
             with _pool_of(stream):
-                q_out = torch.empty(rows, c.num_q_heads, d, dtype=torch.bfloat16, device=q.device)
+                q_out = torch.empty(rows, hq, d, dtype=torch.bfloat16, device=q.device)
         elif _dev(q_out, "q_out", torch.bfloat16).shape != q.shape:
             raise ValueError("q_out must have q's shape")
+        qp, op = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out is given without q")
     ref = None
+    here = _check_layout(layout, rows, k, v, q, q_out, *caches)
     if rotation is not None:
         if rotation.positions is not None and rotation.positions.shape[0] != rows:
             raise ValueError("positions needs one entry per row")
         _here(rotation.inv_freq, rotation.positions)
         ref = rotation.ref
-    here = _check_layout(layout, rows, k, v, q, q_out, *caches)
-    on = _raw_stream(here) if stream is None and _raw_stream is not None else _stream(stream)
-    return rows, on, q_out, (ctypes.byref(c), ref, _ptr(q), qs, _ptr(q_out), k.data_ptr(), ks, v.data_ptr(), vs)
+    if rows:
+        on = _raw_stream(here) if stream is None and _raw_stream is not None else _stream(stream)
+        _check(getattr(_lib(), name)(layout.ref, ref, qp, qs, op, k.data_ptr(), ks, v.data_ptr(), vs,
+                                     caches[0].data_ptr(), caches[1].data_ptr(), on), name)
+    return q_out
+
+
+def _bf16_pools(k_cache: torch.Tensor, v_cache: torch.Tensor, layout: _Layout) -> None:
+    if _dev(k_cache, "k_cache", torch.bfloat16).shape != layout.pools["k"]:
+        raise ValueError("k_cache must be [pages, Hkv, 16, D] of the layout's sizes")
+    if _dev(v_cache, "v_cache", torch.bfloat16).shape != layout.pools["v"]:
+        raise ValueError("v_cache must be [pages, Hkv, D, 16] of the layout's sizes")
 
 
 def kv_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, layout: _Layout, *,
@@ -977,15 +991,8 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: 
     bf16 cache k_cache [pages, Hkv, 16, D], v_cache [pages, Hkv, D, 16], at the
     tokens behind each request's context, k turned by its rows' positions
     (rg_kv_append).  With q [rows, Hq, D], returns it turned."""
-    c = layout.c
-    for t, name, shape in ((k_cache, "k_cache", (c.num_pages, c.num_kv_heads, 16, c.head_dim)),
-                           (v_cache, "v_cache", (c.num_pages, c.num_kv_heads, c.head_dim, 16))):
-        if _dev(t, name, torch.bfloat16).shape != shape:
-            raise ValueError(f"{name} must be {list(shape)}")
-    rows, on, q_out, args = _append_args(k, v, layout, rotation, q, q_out, stream, k_cache, v_cache)
-    if rows:
-        _check(_lib().rg_kv_append(*args, k_cache.data_ptr(), v_cache.data_ptr(), on), "rg_kv_append")
-    return q_out
+    _bf16_pools(k_cache, v_cache, layout)
+    return _append("rg_kv_append", k, v, (k_cache, v_cache), layout, rotation, q, q_out, stream)
 
 
 # ---------------------------------------------------------------------------
@@ -1013,10 +1020,9 @@ def make_kv8_layout(num_q_heads: int, cache: torch.Tensor, q_indptr, n_verify, c
 
 
 def _kv8(cache: torch.Tensor, scales: torch.Tensor, layout: _Layout) -> None:
-    c = layout.c
-    if _dev(cache, "cache", torch.uint8).shape != (c.num_pages, c.num_kv_heads, 32 * c.head_dim):
+    if _dev(cache, "cache", torch.uint8).shape != layout.pools["kv8"]:
         raise ValueError("cache must be [pages, Hkv, 32 D] of the layout's sizes")
-    if _dev(scales, "scales", torch.float32).shape != (c.num_pages, c.num_kv_heads, 2):
+    if _dev(scales, "scales", torch.float32).shape != layout.pools["scales"]:
         raise ValueError("scales must be [pages, Hkv, 2] of the layout's sizes")
 
 
@@ -1026,30 +1032,27 @@ def kv8_append(k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor, scales: to
     """kv_append into the 8-bit cache (rg_kv8_append).  An infinity or a NaN
     reads as NaN."""
     _kv8(cache, scales, layout)
-    rows, on, q_out, args = _append_args(k, v, layout, rotation, q, q_out, stream, cache, scales)
-    if rows:
-        _check(_lib().rg_kv8_append(*args, cache.data_ptr(), scales.data_ptr(), on), "rg_kv8_append")
-    return q_out
+    return _append("rg_kv8_append", k, v, (cache, scales), layout, rotation, q, q_out, stream)
 
 
 def kv8_read(cache: torch.Tensor, scales: torch.Tensor, layout: _Layout, *, k_out: Optional[torch.Tensor] = None,
              v_out: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The tokens kv8_append writes for this layout, as bf16 rows (rg_kv8_read)."""
     _kv8(cache, scales, layout)
-    c = layout.c
-    shape = (layout.q_indptr.item(-1), c.num_kv_heads, c.head_dim)
+    _, hkv, d = layout.heads
     if k_out is None or v_out is None:
+        shape = (layout.q_indptr.item(-1), hkv, d)
         with _pool_of(stream):
             k_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if k_out is None else k_out
             v_out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device) if v_out is None else v_out
-    ks, vs = _rows(k_out, "k_out", *shape[1:]), _rows(v_out, "v_out", *shape[1:])
+    ks, vs = _rows(k_out, "k_out", hkv, d), _rows(v_out, "v_out", hkv, d)
     rows = k_out.shape[0]
     if v_out.shape[0] != rows:
         raise ValueError("k_out and v_out must have as many rows")
     here = _check_layout(layout, rows, k_out, v_out, cache, scales)
     if rows:
         on = _raw_stream(here) if stream is None and _raw_stream is not None else _stream(stream)
-        _check(_lib().rg_kv8_read(ctypes.byref(c), cache.data_ptr(), scales.data_ptr(), k_out.data_ptr(), ks,
+        _check(_lib().rg_kv8_read(layout.ref, cache.data_ptr(), scales.data_ptr(), k_out.data_ptr(), ks,
                                   v_out.data_ptr(), vs, on), "rg_kv8_read")
     return k_out, v_out
 
@@ -1064,7 +1067,7 @@ def make_window(size: int, sink: int = 0) -> Window:
 def _window_args(layout: _Layout, branches: Optional[_Branches], window: Optional[Window]):
     if branches is not None and branches.branch_indptr.shape[0] != layout.ctx_len.shape[0] + 1:
         raise ValueError("branch_indptr must have num_requests + 1 entries")
-    return (ctypes.byref(layout.c), ctypes.byref(branches.c) if branches is not None else None,
+    return (layout.ref, ctypes.byref(branches.c) if branches is not None else None,
             ctypes.byref(window) if window is not None else None)
 
 
@@ -1075,18 +1078,18 @@ def _window_workspace_bytes(name: str, layout, branches, window) -> int:
 
 
 def _window_call(name: str, q, caches, layout: _Layout, branches, window, out, lse, want_lse, workspace, stream):
-    c = layout.c
-    if _dev(q, "q", torch.bfloat16).dim() != 3 or q.shape[1] != c.num_q_heads or q.shape[2] != c.head_dim:
+    shape = _dev(q, "q", torch.bfloat16).shape
+    if len(shape) != 3 or shape[1] != layout.heads[0] or shape[2] != layout.heads[2]:
         raise ValueError("q must be [rows, Hq, D] of the layout's sizes")
-    rows = q.shape[0]
+    rows = shape[0]
     if out is None or (lse is None and want_lse):
         with _pool_of(stream):
             out = torch.empty_like(q) if out is None else out
             if lse is None and want_lse:
-                lse = torch.empty(rows, q.shape[1], dtype=torch.float32, device=q.device)
-    if _dev(out, "out", torch.bfloat16).shape != q.shape:
+                lse = torch.empty(rows, shape[1], dtype=torch.float32, device=q.device)
+    if _dev(out, "out", torch.bfloat16).shape != shape:
         raise ValueError("out must have q's shape")
-    if lse is not None and _dev(lse, "lse", torch.float32).shape != q.shape[:2]:
+    if lse is not None and _dev(lse, "lse", torch.float32).shape != shape[:2]:
         raise ValueError("lse must be [rows, Hq]")
     here = _check_layout(layout, rows, q, out, lse, workspace, *caches)
     args = _window_args(layout, branches, window)
@@ -1115,11 +1118,7 @@ def window_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
                      stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """draft_verify_attention, or with branches multibranch_attention, over a
     sliding window with sinks (rg_window_attention)."""
-    c = layout.c
-    if _dev(k_cache, "k_cache", torch.bfloat16).shape != (c.num_pages, c.num_kv_heads, 16, c.head_dim):
-        raise ValueError("k_cache must be [pages, Hkv, 16, D] of the layout's sizes")
-    if _dev(v_cache, "v_cache", torch.bfloat16).shape != (c.num_pages, c.num_kv_heads, c.head_dim, 16):
-        raise ValueError("v_cache must be [pages, Hkv, D, 16] of the layout's sizes")
+    _bf16_pools(k_cache, v_cache, layout)
     return _window_call("rg_window_attention", q, (k_cache, v_cache), layout, branches, window, out, lse, want_lse,
                         workspace, stream)
 

@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, At
   using B = Kv8<D>;
   constexpr int HALF = D / 2;           // angles of a row at most
   constexpr int PAIRS = D / 16;         // pair units of a row
-  constexpr int PER = 4;                // of a thread and pass
+  constexpr int PER = 2;                // of a thread and pass
   constexpr int HEADS = PER * kAppendThreads / (2 * D);  // KV heads of a pass
   constexpr int BLOCK = 32 * D;         // bytes of V of a page and head in bf16, or of an 8-bit block
   __shared__ float2 angle[16 * HALF];

@@ -87,7 +87,7 @@ rg_status run_append(const rg_attn_layout* L, const rg_rotation* R, const uint16
   // Where there are pages enough a work group takes all heads of one, and makes
   // its angles once.
   const bool many = touched_pages(L) > 1024;
-  const int kv_heads = many ? L->num_kv_heads : 1, q_heads = many ? L->num_q_heads : std::min(L->num_q_heads, 8);
+  const int kv_heads = std::min(L->num_kv_heads, 2), q_heads = std::min(L->num_q_heads, many ? 16 : 8);
   const int64_t each = (L->num_kv_heads + kv_heads - 1) / kv_heads + (q ? (L->num_q_heads + q_heads - 1) / q_heads : 0);
   return launch_pages(L, each, [&](AttnPlan& p) {
     p.chunk = kv_heads;
