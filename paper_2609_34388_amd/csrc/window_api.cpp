@@ -129,7 +129,7 @@ struct Shape {
 };
 Shape kv8_shape(int head_dim) {
   return {kKv8Waves, kKv8Step, head_dim == 64 ? 3 : 2, false, [](int64_t tiles) -> int64_t {
-            constexpr int64_t t[] = {0, 6, 9, 15, 16};
+            constexpr int64_t t[] = {0, 6, 9, 16, 16};
             return 16 * t[tiles];
           }, 600, 600, 128};
 }
