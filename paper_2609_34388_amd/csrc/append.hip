@@ -285,41 +285,38 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, At
   }
 }
 
+// Rows out of the 8-bit cache: an item is a page's kv8_read_heads heads, a thread 16
+// elements of a row.  Bound by the bytes, and by the launch where they are few.  Few
+// heads an item, not a page's all: append and read of 32768 rows (8 heads of 128, with
+// 32 of q) 183 us against 194 with 2 heads, 200 with 4 or 8; 21897 rows of 4 heads of
+// 64 55, 53.5 and 58 us with 1, 2 and 4.
 template <int D>
 __global__ __launch_bounds__(kAppendThreads) void kv8_read_kernel(Kv8ReadArgs a, AttnPlan p) {
   using B = Kv8<D>;
-  constexpr int PAIRS = D / 16, PER = 4, HEADS = PER * kAppendThreads / (2 * D);
+  constexpr int PAIRS = D / 16, HEADS = kv8_read_heads(D);
   __shared__ __attribute__((aligned(16))) uint8_t lds[HEADS * B::BLOCK];
-  const PageItem it = page_item(a.page_indices, p, (a.hkv + p.chunk - 1) / p.chunk);
-  const int tid = threadIdx.x, kv = tid / D & 1, slot = tid % D / PAIRS, m = tid % PAIRS;
-  const int h_first = it.local * p.chunk, h_end = min(a.hkv, h_first + p.chunk);
-  for (int h0 = h_first; h0 < h_end; h0 += HEADS) {
-    const int heads = min(HEADS, h_end - h0);
-    const size_t block0 = (size_t)it.pool_page * a.hkv + h0;
-    const uint8_t* from = a.cache + block0 * B::BLOCK;
-    if (h0 > h_first) __syncthreads();
-    for (int i = tid; i < heads * B::BLOCK / 16; i += kAppendThreads) *(u32x4*)(lds + 16 * i) = *(const u32x4*)(from + 16 * i);
-    __syncthreads();
-    if (slot < it.s0 || slot >= it.s1) continue;
+  const PageItem it = page_item(a.page_indices, p, (a.hkv + HEADS - 1) / HEADS);
+  const int tid = threadIdx.x, h = tid / (2 * D), kv = tid / D & 1, slot = tid % D / PAIRS, m = tid % PAIRS;
+  const int h0 = it.local * HEADS, heads = min(HEADS, a.hkv - h0);
+  const size_t block0 = (size_t)it.pool_page * a.hkv + h0;
+  const uint8_t* from = a.cache + block0 * B::BLOCK;
+  for (int i = tid; i < heads * B::BLOCK / 16; i += kAppendThreads) *(u32x4*)(lds + 16 * i) = *(const u32x4*)(from + 16 * i);
+  __syncthreads();
+  if (slot < it.s0 || slot >= it.s1 || h >= heads) return;
+  // after the barrier: before it the D = 64 rows take 4 us longer
+  const float scale = a.scales[2 * (block0 + h) + kv];
+  const uint8_t* blk = lds + h * B::BLOCK;
+  u32x4 w = {0u, 0u, 0u, 0u};
+  if (kv == 0) {
+    w = *(const u32x4*)(blk + B::k_code(slot, 16 * m));
+  } else {
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      const int h = (tid + e * kAppendThreads) / (2 * D);
-      if (h >= heads) continue;
-      const float scale = a.scales[2 * (block0 + h) + kv];
-      const uint8_t* blk = lds + h * B::BLOCK;
-      u32x4 w = {0u, 0u, 0u, 0u};
-      if (kv == 0) {
-        w = *(const u32x4*)(blk + B::k_code(slot, 16 * m));
-      } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) w[i >> 2] |= (uint32_t)blk[B::v_code(slot, 16 * m + i)] << (8 * (i & 3));
-      }
-      const int64_t row = it.row0 + slot;
-      uint16_t* to = (kv ? a.v + row * a.v_stride : a.k + row * a.k_stride) + (size_t)(h0 + h) * D + 16 * m;
-      __builtin_nontemporal_store(decode8_8(w[0], w[1], scale), (u32x4*)to);
-      __builtin_nontemporal_store(decode8_8(w[2], w[3], scale), (u32x4*)(to + 8));
-    }
+    for (int i = 0; i < 16; ++i) w[i >> 2] |= (uint32_t)blk[B::v_code(slot, 16 * m + i)] << (8 * (i & 3));
   }
+  const int64_t row = it.row0 + slot;
+  uint16_t* to = (kv ? a.v + row * a.v_stride : a.k + row * a.k_stride) + (size_t)(h0 + h) * D + 16 * m;
+  __builtin_nontemporal_store(decode8_8(w[0], w[1], scale), (u32x4*)to);
+  __builtin_nontemporal_store(decode8_8(w[2], w[3], scale), (u32x4*)(to + 8));
 }
 
 }  // namespace

@@ -84,8 +84,12 @@ rg_status run_append(const rg_attn_layout* L, const rg_rotation* R, const uint16
   a.hkv = L->num_kv_heads;
   a.dims = R ? R->dims : 0;
   a.interleaved = R && R->interleaved ? 1 : 0;
-  // Where there are pages enough a work group takes all heads of one, and makes
-  // its angles once.
+  // Heads of a work group, which makes a page's angles once: two KV heads (a pass of
+  // the kernel at D = 128; in us, one, two and four of eight: 128 requests' steps 15.7,
+  // 13.5, 14.0, 36862 rows of prompts 179, 175, 184; in 8 bits 64 steps and their read
+  // 19.3, 17.7, 19.9, 21897 rows of D = 64 69, 57, 62), and eight of q, sixteen where
+  // there are pages enough (4, 8, 16 and 32 heads: the steps 15.1, 13.6, 14.0, 17.1,
+  // the prompts 174, 180, 175, 186, in 8 bits 62, 60, 58, 58).
   const bool many = touched_pages(L) > 1024;
   const int kv_heads = std::min(L->num_kv_heads, 2), q_heads = std::min(L->num_q_heads, many ? 16 : 8);
   const int64_t each = (L->num_kv_heads + kv_heads - 1) / kv_heads + (q ? (L->num_q_heads + q_heads - 1) / q_heads : 0);
@@ -272,6 +276,7 @@ rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits
       x.part_start = (int32_t)part;
       if (q.count == 0) continue;
       const int64_t nch = runs[r];
+      if (nch > 0xffff) return RG_ERR_UNSUPPORTED;  // packed in 16 bits
       x.runs = (uint32_t)nch | (uint32_t)each[r] << 16;
       items += hkv * q.count * nch;
       if (nch > 1) {
@@ -397,9 +402,8 @@ rg_status rg_kv8_read(const rg_attn_layout* layout, const uint8_t* cache, const 
   a.v_stride = v_stride;
   a.page_indices = layout->page_indices;
   a.hkv = layout->num_kv_heads;
-  const int heads = touched_pages(layout) > 1024 ? layout->num_kv_heads : 1;
-  return launch_pages(layout, (layout->num_kv_heads + heads - 1) / heads, [&](AttnPlan& p) {
-    p.chunk = heads;
+  const int heads = kv8_read_heads(layout->head_dim);
+  return launch_pages(layout, (layout->num_kv_heads + heads - 1) / heads, [&](const AttnPlan& p) {
     return launch_kv8_read(a, p, layout->head_dim, static_cast<hipStream_t>(stream));
   });
 }

@@ -36,6 +36,8 @@ struct Kv8ReadArgs {
   const int32_t* page_indices;
   int32_t hkv;
 };
+// KV heads of an item of the read.
+__host__ __device__ constexpr int kv8_read_heads(int head_dim) { return kAppendThreads / (2 * head_dim); }
 hipError_t launch_kv8_read(const Kv8ReadArgs& a, const AttnPlan& p, int head_dim, hipStream_t stream);
 
 // Attention over a window, or all, of the keys of a bf16 or an 8-bit cache.
@@ -58,7 +60,7 @@ struct WindowReq {
 struct WindowReqBr : WindowReq {
   int32_t br[3], rep;  // as in AttnReqBr
 };
-constexpr int kMaxRuns = 0xffff, kMaxRunSteps = 0xffff;
+constexpr int kMaxRunSteps = 0xffff;
 template <typename Req, int MaxReq>
 struct WindowPlanT {
   int32_t num_req, total_items, grid_items, total_comb, max_chunks;
