@@ -368,8 +368,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void kv8_attn_kernel(Win
   __shared__ __attribute__((aligned(16))) char lds[Kv8Shape<D>::LDS];
   constexpr bool BR = __is_same(Plan, WindowPlanBr);
 
-  const int item = p.num_req == 1 ? xcd_item(p.grid_items) : (int)blockIdx.x;
-  if (item >= p.total_items) return;
+  const int item = (int)blockIdx.x;
   const int r = find_start(p.num_req, item, [&](int k) { return p.req[k].item_start; });
   const auto rq = p.req[r];
   Kv8Item it;
@@ -380,8 +379,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void kv8_attn_kernel(Win
   it.tiles = (it.M + 31) / 32;
   it.nch = rq.runs & 0xffff;
   const int ncg = (it.tiles + kKv8Waves - 1) / kKv8Waves;
-  // Items of a request: KV heads, then column groups, then runs; a division by the
-  // groups only where there are several.
+  // Items of a request: KV heads, then column groups from the last, which sees most
+  // keys, then runs; a division by the groups only where there are several.
   const int local = item - rq.item_start;
   int cg = 0;
   it.c = quotient(local, a.hkv_mul, a.hkv_shift);
@@ -389,7 +388,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void kv8_attn_kernel(Win
   if (ncg > 1) {
     const int of = it.c;
     it.c /= ncg;
-    cg = of - it.c * ncg;
+    cg = ncg - 1 - (of - it.c * ncg);
   }
   it.tile0 = cg * kKv8Waves;
   it.nct = min(kKv8Waves, it.tiles - it.tile0);
@@ -411,9 +410,9 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void kv8_attn_kernel(Win
 template <typename Plan>
 hipError_t launch_any(const WindowArgs& a, const Plan& p, int head_dim, hipStream_t stream) {
   if (head_dim == 128)
-    hipLaunchKernelGGL((kv8_attn_kernel<128, Plan>), dim3(p.grid_items), dim3(kThreads), 0, stream, a, p);
+    hipLaunchKernelGGL((kv8_attn_kernel<128, Plan>), dim3(p.total_items), dim3(kThreads), 0, stream, a, p);
   else
-    hipLaunchKernelGGL((kv8_attn_kernel<64, Plan>), dim3(p.grid_items), dim3(kThreads), 0, stream, a, p);
+    hipLaunchKernelGGL((kv8_attn_kernel<64, Plan>), dim3(p.total_items), dim3(kThreads), 0, stream, a, p);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : launch_window_merge(a, p, head_dim, stream);
 }

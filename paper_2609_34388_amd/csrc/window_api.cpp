@@ -289,7 +289,6 @@ rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits
     p.req[p.num_req].item_start = p.total_items = (int32_t)items;
     p.req[p.num_req].part_start = (int32_t)part;
     p.total_comb = (int32_t)comb;
-    p.grid_items = (int32_t)round_up(items, 8);
     if (!fits_launch(items, 64 * shape.group) || !fits_launch(comb, 64 * kWindowMergeWaves)) return RG_ERR_UNSUPPORTED;
     most_part = std::max(most_part, part);
     if (items > 0) fp.launches.push_back(p);

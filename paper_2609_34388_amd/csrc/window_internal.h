@@ -63,7 +63,7 @@ struct WindowReqBr : WindowReq {
 constexpr int kMaxRunSteps = 0xffff;
 template <typename Req, int MaxReq>
 struct WindowPlanT {
-  int32_t num_req, total_items, grid_items, total_comb, max_chunks;
+  int32_t num_req, total_items, total_comb, max_chunks;
   Req req[MaxReq + 1];  // entry num_req holds the end sentinel of item_start
 };
 using WindowPlan = WindowPlanT<WindowReq, kMaxReqPerLaunch>;
