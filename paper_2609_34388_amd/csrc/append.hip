@@ -16,6 +16,12 @@
 // A work item is one page that a request's rows touch and some KV heads, or some
 // heads of q: no two work groups write the same block.  V, which lies by dims,
 // and 8-bit blocks go through LDS.
+//
+// Prompts are bound by their bytes: 36862 rows of 32 + 2 x 8 heads of 128, 906 MB
+// read and written, in 175 us (5.2 TB/s, what a copy reaches).  Steps are bound by
+// their one chain of angles, rows, LDS and stores and by the launch: 128 requests of 4
+// to 32 rows, 34 MB, 14 us.  In 8 bits the conversions come to that: VALU 54 % busy at
+// 21897 rows of 16 + 2 x 4 heads of 64, 43 us.
 #include "kv8_device.h"
 #include "window_internal.h"
 
@@ -125,7 +131,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, At
   using B = Kv8<D>;
   constexpr int HALF = D / 2;           // angles of a row at most
   constexpr int PAIRS = D / 16;         // pair units of a row
-  constexpr int PER = 2;                // of a thread and pass
+  constexpr int PER = 2;                // of a thread and pass; 4 take registers and are slower
   constexpr int HEADS = PER * kAppendThreads / (2 * D);  // KV heads of a pass
   constexpr int BLOCK = 32 * D;         // bytes of V of a page and head in bf16, or of an 8-bit block
   __shared__ float2 angle[16 * HALF];
