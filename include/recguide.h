@@ -731,7 +731,8 @@ rg_status rg_kv_append(const rg_attn_layout* layout, const rg_rotation* rotation
  * rounded again at a scale that grew: only elements below 2^-6 of the new scale
  * can change.  An element is the nearest number of its block, ties to the even code;
  * magnitudes past 448 become 448, an infinity or a NaN becomes NaN, and no other
- * element changes for it.
+ * element changes for it.  Attention over a NaN comes out as NaN, from K in the
+ * rows that see the token, from V in any of the request's.
  */
 #define RG_KV8_BLOCK_BYTES(head_dim) (32 * (head_dim))
 
@@ -746,7 +747,8 @@ rg_status rg_kv8_append(const rg_attn_layout* layout, const rg_rotation* rotatio
 
 /* The tokens ctx_len[r] .. ctx_len[r] + n_r - 1 out of the cache, as bf16 rows:
  * the values they stand for.  A whole context is read with ctx_len 0 and q_indptr
- * over its tokens (at most 65535 rows of a request a call). */
+ * over its tokens (at most 65535 rows of a request a call).  q_indptr[R] rows of
+ * k and v are written, at strides and alignments as above. */
 rg_status rg_kv8_read(const rg_attn_layout* layout, const uint8_t* cache, const float* scales, uint16_t* k,
                       int64_t k_stride, uint16_t* v, int64_t v_stride, void* stream);
 
@@ -777,7 +779,8 @@ typedef struct rg_window {
  * rg_draft_verify_attention (branches NULL) or rg_multibranch_attention over a
  * window: layout, branches, q, caches, out and lse as there.  The workspace
  * needs no initialisation.  Slots that no row sees may hold anything.
- * RG_ERR_WORKSPACE also where the host has no memory for the plan.
+ * RG_ERR_WORKSPACE also where the host has no memory for the plan, and
+ * RG_ERR_UNSUPPORTED for a request of 2^30 rows and query heads of a KV head, and more.
  */
 rg_status rg_window_attention_workspace(const rg_attn_layout* layout, const rg_branch_layout* branches,
                                         const rg_window* window, size_t* bytes);

@@ -1061,6 +1061,8 @@ def kv8_read(cache: torch.Tensor, scales: torch.Tensor, layout: _Layout, *, k_ou
 # Attention over a sliding window with sinks, and over the 8-bit cache
 def make_window(size: int, sink: int = 0) -> Window:
     """The latest `size` positions up to a row's own, and the first `sink` (rg_window)."""
+    if max(abs(size), abs(sink)) >= 1 << 31:  # ctypes would cut it to 32 bits
+        raise ValueError("a window's size and sinks are 32-bit numbers")
     return Window(int(size), int(sink))
 
 

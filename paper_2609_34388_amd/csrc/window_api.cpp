@@ -183,6 +183,8 @@ rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits
   constexpr bool BR = __is_same(Plan, WindowPlanBr);
   const int R = L->num_requests, hkv = L->num_kv_heads, cus = device_cus();
   const Shape shape = kv8 ? kv8_shape(L->head_dim) : bf16_shape(L->head_dim);
+  for (int r = 0; r < R; ++r)  // columns of a request: 32 bits
+    if ((int64_t)(L->q_indptr[r + 1] - L->q_indptr[r]) * (L->num_q_heads / hkv) >= int64_t(1) << 30) return RG_ERR_UNSUPPORTED;
   std::vector<Groups> groups(R);
   for (int r = 0; r < R; ++r) groups[r] = groups_of<BR>(L, r, w, shape, L->num_q_heads / hkv);
   auto runs_of = [&](const Groups& q, int64_t target) {

@@ -257,6 +257,33 @@ def test_scale_and_outputs():
         check_attention(out, None, *c.reference(scale=0.25))
 
 
+@pytest.mark.parametrize("window", [None, (60, 5)])
+def test_a_nan_in_the_cache(window):
+    """From K in the rows that see the token, from V there in its dim; no other
+    request changes, and of K no other row."""
+    for kv in (0, 1):
+        c = Case([(100, 6, 5), (257, 3, 0), (70, 5, 4)], kv8=True, window=window)
+        want = c.reference()
+        token = 107  # a draft row of request 0 sees it, no verify row
+        page, slot = c.b.pages(0)[token // PAGE], token % PAGE
+        c.caches[0][int(page), 1, int(ref.place(c.b.d, kv)[slot, 9])] = 0x7f
+        out, lse = c.call()
+        out, lse = out.double().cpu().numpy(), lse.cpu().numpy()
+        rows = np.zeros(c.b.rows, dtype=bool)
+        rows[:int(c.b.n[0])] = c.see[0][:, token]
+        assert 0 < rows.sum() < c.b.n[0]
+        heads = np.arange(c.b.hq) // c.b.g == 1
+        hit = rows[:, None] & heads
+        if kv == 0:
+            assert np.isnan(out[hit]).all() and np.isnan(lse[hit]).all()
+        else:
+            assert np.isnan(out[hit][:, 9]).all() and not np.isnan(lse).any()
+            rows[:int(c.b.n[0])] = True
+            hit = rows[:, None] & heads
+        check_attention(torch.from_numpy(out[~hit][:, None]), torch.from_numpy(lse[~hit][:, None]),
+                        *(x[~hit][:, None] for x in want[:3]), want[3])
+
+
 def test_empty_batches():
     for kv8, window in ((True, None), (False, (30, 3))):
         c = Case([(5, 0, 0), (0, 0, 0)], kv8=kv8, window=window)

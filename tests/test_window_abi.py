@@ -122,6 +122,19 @@ def test_attention_refusals():
     assert attend(L(), br=ctypes.byref(br.c)) == NULL
 
 
+def test_sizes_past_32_bits():
+    for size, sink in ((1 << 31, 0), ((1 << 32) + 5, 0), (5, 1 << 32), (-(1 << 32), 0)):
+        with pytest.raises(ValueError):
+            binding.make_window(size, sink)
+    # a request's columns: rows x query heads of a KV head
+    need = ctypes.c_size_t()
+    for hq, want in ((16384, 0), (16640, UNSUPPORTED)):
+        wide = L(n=(65535, 5), hq=hq, hkv=1)
+        assert lib().rg_kv8_attention_workspace(wide.ref, None, None, ctypes.byref(need)) == want
+        if want:
+            assert attend(wide) == want
+
+
 def test_windows_bound_the_workspace():
     """A window's keys, not the context's, are what is split."""
     need = ctypes.c_size_t()
