@@ -13,15 +13,15 @@
 // scale to the codes they had).  A thread holds 16 elements of a row in
 // registers between the two.
 //
-// A work item is one page that a request's rows touch and some KV heads, or some
+// A work item is one page that a request's rows touch and 256 dims of KV heads, or some
 // heads of q: no two work groups write the same block.  V, which lies by dims,
 // and 8-bit blocks go through LDS.
 //
 // Prompts are bound by their bytes: 36862 rows of 32 + 2 x 8 heads of 128, 906 MB
-// read and written, in 175 us (5.2 TB/s, what a copy reaches).  Steps are bound by
-// their one chain of angles, rows, LDS and stores and by the launch: 128 requests of 4
-// to 32 rows, 34 MB, 14 us.  In 8 bits the conversions come to that: VALU 54 % busy at
-// 21897 rows of 16 + 2 x 4 heads of 64, 43 us.
+// read and written, in 168 us (5.4 TB/s; a copy reaches 5.2).  Steps are bound by their
+// one chain of angles, rows, LDS and stores and by the launch: 128 requests of 4 to 32
+// rows, 34 MB, 11.8 us, of which a launch that does nothing is 10 and the angles 2.  In 8
+// bits vector instructions come to that: 21897 rows of 16 + 2 x 4 heads of 64 36 us.
 #include "kv8_device.h"
 #include "window_internal.h"
 
@@ -71,9 +71,12 @@ __device__ __forceinline__ PageItem page_item(const int32_t* page_indices, const
   const AttnReq rq = p.req[r];
   const int n = rq.nv & 0xffff;
   const uint32_t local = item - rq.item_start;
-  const int page = (rq.ctx >> 4) + (int)(local / (uint32_t)per_page);
+  const uint32_t nth = local / (uint32_t)per_page;
+  const int page = (rq.ctx >> 4) + (int)nth;
   PageItem it;
-  it.local = (int)(local % (uint32_t)per_page);
+  // from page to page another item first: an XCD has all kinds (eight items a page,
+  // the prompts above: 178 us without, 170 with)
+  it.local = (int)((local + nth + (uint32_t)r) % (uint32_t)per_page);
   it.pool_page = page_indices[rq.page_start + page];
   it.s0 = max(rq.ctx - page * 16, 0);
   it.s1 = min(rq.ctx + n - page * 16, 16);
@@ -129,25 +132,30 @@ __device__ __forceinline__ void turn(float (&x)[16], const Units& u, const float
 template <int D, bool KV8, bool NEXT>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, AttnPlan p) {
   using B = Kv8<D>;
-  constexpr int HALF = D / 2;           // angles of a row at most
-  constexpr int PAIRS = D / 16;         // pair units of a row
-  constexpr int PER = 2;                // of a thread and pass; 4 take registers and are slower
-  constexpr int HEADS = PER * kAppendThreads / (2 * D);  // KV heads of a pass
-  constexpr int BLOCK = 32 * D;         // bytes of V of a page and head in bf16, or of an 8-bit block
+  constexpr int HALF = D / 2;                          // angles of a row at most
+  constexpr int PAIRS = D / 16;                        // pair units of a row
+  constexpr int HEADS = append_heads(D);               // KV heads of an item
+  constexpr int PER = HEADS * 2 * D / kAppendThreads;  // units of a thread; 4 take registers and are slower
+  constexpr int BLOCK = 32 * D;                        // bytes of V of a page and head in bf16, or of an 8-bit block
   __shared__ float2 angle[16 * HALF];
   __shared__ __attribute__((aligned(16))) uint8_t lds[HEADS * BLOCK];
   __shared__ float top[PER][kAppendThreads / 64];
-  const int kv_items = (a.hkv + p.chunk - 1) / p.chunk;
+  const int kv_items = (a.hkv + HEADS - 1) / HEADS;
   const int q_items = p.cols_per_group > 0 ? (a.hq + p.cols_per_group - 1) / p.cols_per_group : 0;
   const PageItem it = page_item(a.page_indices, p, kv_items + q_items);
   const int tid = threadIdx.x;
 
+  // Angles: a thread has one frequency and every `apart`-th of the page's new rows.
   const int half = a.dims / 2;
-  for (int i = tid; i < 16 * half; i += kAppendThreads) {
-    const int slot = i / half, j = i - slot * half;
-    if (slot < it.s0 || slot >= it.s1) continue;
-    const int at = a.positions ? a.positions[it.row0 + slot] : it.first_position + slot;
-    angle[slot * HALF + j] = turn_of((double)at * (double)a.inv_freq[j]);
+  if (half > 0) {
+    const int apart = kAppendThreads / half, first = tid / half, j = tid - first * half;
+    if (first < apart) {
+      const double freq = a.inv_freq[j];
+      for (int slot = it.s0 + first; slot < it.s1; slot += apart) {
+        const int at = a.positions ? a.positions[it.row0 + slot] : it.first_position + slot;
+        angle[slot * HALF + j] = turn_of((double)at * freq);
+      }
+    }
   }
   __syncthreads();
 
@@ -171,123 +179,119 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, At
     return;
   }
 
-  const int h_first = it.local * p.chunk, h_end = min(a.hkv, h_first + p.chunk);
-  for (int h0 = h_first; h0 < h_end; h0 += HEADS) {
-    const int heads = min(HEADS, h_end - h0);
-    const size_t block0 = (size_t)it.pool_page * a.hkv + h0;
-    // Pair unit e of this thread: head h0 + head, K (kv 0) or V of slot's row.
-    auto head_of = [&](int e) { return (tid + e * kAppendThreads) / (2 * D); };
-    const int kv = tid / D & 1, slot = tid % D / PAIRS, m = tid % PAIRS;  // alike for every e
-    const Units u = kv ? Units{2 * m, 2 * m + 1, false} : units_of<NEXT>(m, a.dims);
-    const bool fresh = slot >= it.s0 && slot < it.s1;
-    float x[PER][16];
-    {
-      u32x4 w[PER][2];
+  const int h0 = it.local * HEADS, heads = min(HEADS, a.hkv - h0);
+  const size_t block0 = (size_t)it.pool_page * a.hkv + h0;
+  // Pair unit e of this thread: head h0 + head, K (kv 0) or V of slot's row.
+  auto head_of = [&](int e) { return (tid + e * kAppendThreads) / (2 * D); };
+  const int kv = tid / D & 1, slot = tid % D / PAIRS, m = tid % PAIRS;  // alike for every e
+  const Units u = kv ? Units{2 * m, 2 * m + 1, false} : units_of<NEXT>(m, a.dims);
+  const bool fresh = slot >= it.s0 && slot < it.s1;
+  float x[PER][16];
+  {
+    u32x4 w[PER][2];
 #pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        w[e][0] = w[e][1] = u32x4{0u, 0u, 0u, 0u};
-        if (fresh && head_of(e) < heads) {
-          const int64_t row = it.row0 + slot;
-          const uint16_t* from = (kv ? a.v + row * a.v_stride : a.k + row * a.k_stride) + (size_t)(h0 + head_of(e)) * D;
-          w[e][0] = *(const u32x4*)(from + 8 * u.c0);
-          w[e][1] = *(const u32x4*)(from + 8 * u.c1);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        unpack8(w[e][0], x[e]);
-        unpack8(w[e][1], x[e] + 8);
-        if (kv == 0 && fresh) turn<NEXT>(x[e], u, angle + slot * HALF, a.dims);
+    for (int e = 0; e < PER; ++e) {
+      w[e][0] = w[e][1] = u32x4{0u, 0u, 0u, 0u};
+      if (fresh && head_of(e) < heads) {
+        const int64_t row = it.row0 + slot;
+        const uint16_t* from = (kv ? a.v + row * a.v_stride : a.k + row * a.k_stride) + (size_t)(h0 + head_of(e)) * D;
+        w[e][0] = *(const u32x4*)(from + 8 * u.c0);
+        w[e][1] = *(const u32x4*)(from + 8 * u.c1);
       }
     }
-    if constexpr (!KV8) {
 #pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        if (!fresh || head_of(e) >= heads) continue;
-        if (kv == 0) {
-          uint16_t* to = a.k_cache + ((block0 + head_of(e)) * 16 + slot) * D;
-          *(u32x4*)(to + 8 * u.c0) = pack8(x[e]);
-          *(u32x4*)(to + 8 * u.c1) = pack8(x[e] + 8);
-        } else {
-          uint16_t* by_dim = reinterpret_cast<uint16_t*>(lds + head_of(e) * BLOCK) + slot;
+    for (int e = 0; e < PER; ++e) {
+      unpack8(w[e][0], x[e]);
+      unpack8(w[e][1], x[e] + 8);
+      if (kv == 0 && fresh) turn<NEXT>(x[e], u, angle + slot * HALF, a.dims);
+    }
+  }
+  if constexpr (!KV8) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) by_dim[(16 * m + i) * 16] = (uint16_t)(__float_as_uint(x[e][i]) >> 16);  // as it came
-        }
-      }
-      __syncthreads();
-      uint16_t* to = a.v_cache + block0 * 16 * D;
-      if (it.s0 == 0 && it.s1 == 16) {
-        for (int i = tid; i < heads * BLOCK / 16; i += kAppendThreads) *(u32x4*)(to + 8 * i) = *(const u32x4*)(lds + 16 * i);
+    for (int e = 0; e < PER; ++e) {
+      if (!fresh || head_of(e) >= heads) continue;
+      if (kv == 0) {
+        uint16_t* to = a.k_cache + ((block0 + head_of(e)) * 16 + slot) * D;
+        *(u32x4*)(to + 8 * u.c0) = pack8(x[e]);
+        *(u32x4*)(to + 8 * u.c1) = pack8(x[e] + 8);
       } else {
-        const int count = it.s1 - it.s0;
-        for (int i = tid; i < heads * D * count; i += kAppendThreads) {
-          const int row = i / count, s = it.s0 + i - row * count;
-          to[(size_t)row * 16 + s] = reinterpret_cast<const uint16_t*>(lds)[row * 16 + s];
-        }
+        uint16_t* by_dim = reinterpret_cast<uint16_t*>(lds + head_of(e) * BLOCK) + slot;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) by_dim[(16 * m + i) * 16] = (uint16_t)(__float_as_uint(x[e][i]) >> 16);  // as it came
       }
+    }
+    __syncthreads();
+    uint16_t* to = a.v_cache + block0 * 16 * D;
+    if (it.s0 == 0 && it.s1 == 16) {
+      for (int i = tid; i < heads * BLOCK / 16; i += kAppendThreads) *(u32x4*)(to + 8 * i) = *(const u32x4*)(lds + 16 * i);
     } else {
-      // Blocks that are not written whole come in as they are.
-      const bool part = it.s0 > 0 || it.s1 < 16;
-      uint8_t* to = a.cache + block0 * B::BLOCK;
-      if (part)
-        for (int i = tid; i < heads * B::BLOCK / 16; i += kAppendThreads) *(u32x4*)(lds + 16 * i) = *(const u32x4*)(to + 16 * i);
-#pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        float t = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float y = fabsf(x[e][i]);
-          t = y < __builtin_huge_valf() ? fmaxf(t, y) : t;
-        }
-        for (int off = 32; off >= 1; off >>= 1) t = fmaxf(t, __shfl_xor(t, off));
-        if ((tid & 63) == 0) top[e][tid >> 6] = t;
+      const int count = it.s1 - it.s0;
+      for (int i = tid; i < heads * D * count; i += kAppendThreads) {
+        const int row = i / count, s = it.s0 + i - row * count;
+        to[(size_t)row * 16 + s] = reinterpret_cast<const uint16_t*>(lds)[row * 16 + s];
       }
-      __syncthreads();
-      float scales[PER];
+    }
+  } else {
+    // Blocks that are not written whole come in as they are.
+    const bool part = it.s0 > 0 || it.s1 < 16;
+    uint8_t* to = a.cache + block0 * B::BLOCK;
+    if (part)
+      for (int i = tid; i < heads * B::BLOCK / 16; i += kAppendThreads) *(u32x4*)(lds + 16 * i) = *(const u32x4*)(to + 16 * i);
 #pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        if (head_of(e) >= heads) continue;
-        const int wave = tid >> 6;
-        const float t = D == 128 ? fmaxf(top[e][wave], top[e][wave ^ 1]) : top[e][wave];
-        const float old = it.s0 > 0 ? a.scales[2 * (block0 + head_of(e)) + kv] : 0.f;
-        const float scale = fmaxf(__uint_as_float((uint32_t)kv8_exponent(__float_as_uint(t)) << 23), old);
-        scales[e] = scale;
-        if (slot < it.s0) {  // an older token: its codes' values
-          const uint8_t* blk = lds + head_of(e) * B::BLOCK;
-          uint32_t w[4] = {0u, 0u, 0u, 0u};
+    for (int e = 0; e < PER; ++e) {
+      float t = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float y = fabsf(x[e][i]);
+        t = y < __builtin_huge_valf() ? fmaxf(t, y) : t;
+      }
+      for (int off = 32; off >= 1; off >>= 1) t = fmaxf(t, __shfl_xor(t, off));
+      if ((tid & 63) == 0) top[e][tid >> 6] = t;
+    }
+    __syncthreads();
+    float scales[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      if (head_of(e) >= heads) continue;
+      const int wave = tid >> 6;
+      const float t = D == 128 ? fmaxf(top[e][wave], top[e][wave ^ 1]) : top[e][wave];
+      const float old = it.s0 > 0 ? a.scales[2 * (block0 + head_of(e)) + kv] : 0.f;
+      const float scale = fmaxf(__uint_as_float((uint32_t)kv8_exponent(__float_as_uint(t)) << 23), old);
+      scales[e] = scale;
+      if (slot < it.s0) {  // an older token: its codes' values
+        const uint8_t* blk = lds + head_of(e) * B::BLOCK;
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+        if (kv == 0) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) w[k] = *(const uint32_t*)(blk + B::k_code(slot, 8 * (k < 2 ? u.c0 : u.c1) + 4 * (k & 1)));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w[i >> 2] |= (uint32_t)blk[B::v_code(slot, 16 * m + i)] << (8 * (i & 3));
+        }
+        unpack8(decode8_8(w[0], w[1], old), x[e]);
+        unpack8(decode8_8(w[2], w[3], old), x[e] + 8);
+      }
+      if (slot < it.s1) {
+        // its exponent is 254 less the scale's: a power of two again
+        const float inv = __uint_as_float(0x7f000000u - __float_as_uint(scale));
+        uint8_t* blk = lds + head_of(e) * B::BLOCK;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t w = encode4_8(x[e][4 * k], x[e][4 * k + 1], x[e][4 * k + 2], x[e][4 * k + 3], inv);
           if (kv == 0) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = *(const uint32_t*)(blk + B::k_code(slot, 8 * (k < 2 ? u.c0 : u.c1) + 4 * (k & 1)));
+            *(uint32_t*)(blk + B::k_code(slot, 8 * (k < 2 ? u.c0 : u.c1) + 4 * (k & 1))) = w;
           } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i >> 2] |= (uint32_t)blk[B::v_code(slot, 16 * m + i)] << (8 * (i & 3));
-          }
-          unpack8(decode8_8(w[0], w[1], old), x[e]);
-          unpack8(decode8_8(w[2], w[3], old), x[e] + 8);
-        }
-        if (slot < it.s1) {
-          // its exponent is 254 less the scale's: a power of two again
-          const float inv = __uint_as_float(0x7f000000u - __float_as_uint(scale));
-          uint8_t* blk = lds + head_of(e) * B::BLOCK;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t w = encode4_8(x[e][4 * k], x[e][4 * k + 1], x[e][4 * k + 2], x[e][4 * k + 3], inv);
-            if (kv == 0) {
-              *(uint32_t*)(blk + B::k_code(slot, 8 * (k < 2 ? u.c0 : u.c1) + 4 * (k & 1))) = w;
-            } else {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) blk[B::v_code(slot, 16 * m + 4 * k + i)] = (uint8_t)(w >> (8 * i));
-            }
+            for (int i = 0; i < 4; ++i) blk[B::v_code(slot, 16 * m + 4 * k + i)] = (uint8_t)(w >> (8 * i));
           }
         }
       }
-      __syncthreads();  // the old scales are read, the codes are in
-#pragma unroll
-      for (int e = 0; e < PER; ++e)
-        if (head_of(e) < heads && slot == it.s0 && m == 0) a.scales[2 * (block0 + head_of(e)) + kv] = scales[e];
-      for (int i = tid; i < heads * B::BLOCK / 16; i += kAppendThreads) *(u32x4*)(to + 16 * i) = *(const u32x4*)(lds + 16 * i);
     }
-    if (h0 + HEADS < h_end) __syncthreads();  // LDS again
+    __syncthreads();  // the old scales are read, the codes are in
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+      if (head_of(e) < heads && slot == it.s0 && m == 0) a.scales[2 * (block0 + head_of(e)) + kv] = scales[e];
+    for (int i = tid; i < heads * B::BLOCK / 16; i += kAppendThreads) *(u32x4*)(to + 16 * i) = *(const u32x4*)(lds + 16 * i);
   }
 }
 

@@ -84,17 +84,16 @@ rg_status run_append(const rg_attn_layout* L, const rg_rotation* R, const uint16
   a.hkv = L->num_kv_heads;
   a.dims = R ? R->dims : 0;
   a.interleaved = R && R->interleaved ? 1 : 0;
-  // Heads of a work group, which makes a page's angles once: two KV heads (a pass of
-  // the kernel at D = 128; in us, one, two and four of eight: 128 requests' steps 15.7,
-  // 13.5, 14.0, 36862 rows of prompts 179, 175, 184; in 8 bits 64 steps and their read
-  // 19.3, 17.7, 19.9, 21897 rows of D = 64 69, 57, 62), and eight of q, sixteen where
-  // there are pages enough (4, 8, 16 and 32 heads: the steps 15.1, 13.6, 14.0, 17.1,
-  // the prompts 174, 180, 175, 186, in 8 bits 62, 60, 58, 58).
-  const bool many = touched_pages(L) > 1024;
-  const int kv_heads = std::min(L->num_kv_heads, 2), q_heads = std::min(L->num_q_heads, many ? 16 : 8);
+  // Heads of q in an item, whose rows at 4 of D = 128 or 8 of D = 64 weigh what those of
+  // its KV heads do.  At D = 128 eight in few pages, where angles and starts count, and in
+  // 8 bits (us with 4, 8 and 16 heads of 32: 128 requests' steps 12.6, 11.7, 13.2, 256
+  // pages of a prompt 20.5, 18.7, 18.6, 512 pages 40.7, 42.8, 46.4, 2304 168, 172, 180; in
+  // 8 bits 64 steps 17.0, 16.9, 17.2, 2048 pages 173, 176, 184; D = 64 28.7, 29.2, 40.3, in
+  // 8 bits 48.4, 47.3, 59.7).
+  const bool many = touched_pages(L) >= 512;
+  const int q_heads = std::min(L->num_q_heads, L->head_dim == 128 && !kv8 && many ? 4 : 8), kv_heads = append_heads(L->head_dim);
   const int64_t each = (L->num_kv_heads + kv_heads - 1) / kv_heads + (q ? (L->num_q_heads + q_heads - 1) / q_heads : 0);
   return launch_pages(L, each, [&](AttnPlan& p) {
-    p.chunk = kv_heads;
     p.cols_per_group = q ? q_heads : 0;
     return launch_append(a, p, L->head_dim, kv8, static_cast<hipStream_t>(stream));
   });

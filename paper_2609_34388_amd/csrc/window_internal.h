@@ -7,9 +7,10 @@
 namespace rg {
 
 // Rows into, or out of, a cache.  Plans: AttnPlan; a page that a request's rows
-// touch has items of plan.chunk KV heads, then of plan.cols_per_group heads of
-// q (0: no q).
+// touch has items of append_heads KV heads, and of plan.cols_per_group heads of q
+// (0: no q).
 constexpr int kAppendThreads = 256;
+__host__ __device__ constexpr int append_heads(int head_dim) { return 256 / head_dim; }
 struct AppendArgs {
   const uint16_t* q;  // or NULL
   const uint16_t* k;
