@@ -123,6 +123,9 @@ rg_status validate_window(const rg_window* W) {
 // take 718, 566 and 568 us; rounds of less than 80 us are best left one (102, 110, 122;
 // 34, 42, 48), and among longer ones those that fill it evenly (184, 195, 198).
 constexpr int64_t kLongRound = 8000;
+// A merge's launch: not for what a split saves below that.  100 tokens over 500 keys of D =
+// 64 whole 15.9 us, split to fill the chip 21.1; in 8 bits 11.5 and 16.7.
+constexpr int64_t kMerge = 450;
 // How a kernel takes a batch: column groups of up to `group` tiles, dealt evenly or
 // full but for the last; steps of `keys` keys; work groups that run at once; the
 // time of a step of so many tiles, of an item's start and end, and of the partials
@@ -143,7 +146,7 @@ Shape kv8_shape(int head_dim) {
           }, 600, 600, 128};
 }
 Shape bf16_shape(int head_dim) {
-  return {kWindowWaves, window_keys(head_dim), 2, true, [](int64_t tiles) { return std::max<int64_t>(270, 130 + 47 * tiles); },
+  return {kWindowWaves, window_keys(head_dim), head_dim == 64 ? 3 : 2, true, [](int64_t tiles) { return std::max<int64_t>(270, 130 + 47 * tiles); },
           600, 200, 270};
 }
 
@@ -194,9 +197,9 @@ rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits
     const uint32_t n = (steps + most - 1) / most, each = (steps + n - 1) / n;  // steps of a run
     return (int64_t)((steps + each - 1) / each);
   };
-  // Cost of an item at most: the least that gives one round of items, or where a
-  // round is long (kLongRound) as many as promise the earliest end: a long round
-  // ends unevenly, an item's start and its partials cost.
+  // Cost of an item at most: the least that gives one round of items, or no split where
+  // that ends no later, or where a round is long (kLongRound) as many as promise the
+  // earliest end: a long round ends unevenly, an item's start and its partials cost.
   struct Load {
     Groups q;
     int64_t items;  // whole
@@ -238,9 +241,10 @@ rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits
       total += x.items * n * each;
       longest = std::max(longest, each);
     }
-    return items <= slots ? longest : std::max(longest, total / slots + total / items / 2);
+    return (items <= slots ? longest : std::max(longest, total / slots + total / items / 2)) + (items > whole ? kMerge : 0);
   };
   int64_t target = fit(1);
+  if (time_of(whole_cost) <= time_of(target)) target = whole_cost;
   if (target > kLongRound) {
     int64_t best = time_of(target);
     for (int64_t rounds = 2; rounds <= 4; ++rounds) {

@@ -11,9 +11,9 @@
 // prompt reads its window, not the context, and no key behind its last row.
 //
 // Keys pass through LDS, a buffer at a time and two buffers of LDS, in the layout of
-// attention.hip: all waves load their share of the next buffer into registers while
-// one is computed, and put it into LDS before the one barrier of a buffer.  V of
-// slots that no row may see, which can hold anything, is put in as zero.
+// attention.hip: all waves load their share of the next buffer straight into LDS while
+// one is computed, and wait for it before the one barrier of a buffer.  V of slots that
+// no row may see, which can hold anything, is made zero there.
 //
 // Softmax online in base 2; the product takes P rounded to bf16 (off by at most
 // 2^-8 of each term, as the output's own rounding).  Two sums run in fp32: of P,
@@ -21,12 +21,13 @@
 // weights add up to one.  Runs of a request's keys meet in fp32 in the workspace.
 //
 // Tokens are bound by the bytes: 64 requests of one, 4096 keys each of 8 heads of 128,
-// 1.07 GB in 185 us (5.8 TB/s).  Prompts: 13193 rows over windows of 1024 243 us (680
-// TFLOP/s), 8192 rows over all keys 634 (870); products 28 % and vector instructions
-// 35 % of the cycles, the rest waits for LDS, barriers, starts and ends of groups.  Of
-// what hides those nothing gained: K's fragments a sub-tile ahead (4 % slower), two
-// buffers in flight (2.5 %), eight waves a group (2 % faster here, up to 50 % slower in
-// steps), two sub-tiles at once (registers spill).
+// 1.07 GB in 185 us (5.8 TB/s).  Prompts: 13193 rows over windows of 1024 231 us (720
+// TFLOP/s), 8192 rows over all keys 590 (930): products and the softmax of two waves
+// overlap in part, and the rest waits for LDS, barriers, starts and ends of groups.  Keys
+// through registers into LDS took 236 and 612, and V's fragments read after the softmax,
+// with a wave's priority raised for the products, 242 and 629; K's fragments read a
+// sub-tile ahead were 4 % slower, eight waves a group 2 % faster here and up to 50 %
+// slower in steps, two sub-tiles at once do not fit the registers.
 #include "attention_device.h"
 #include "window_internal.h"
 
@@ -47,7 +48,7 @@ struct WindowShape {
 };
 
 template <int D, typename Plan>
-__global__ __launch_bounds__(64 * kWindowWaves, 2) void window_attn_kernel(WindowArgs a, Plan p) {
+__global__ __launch_bounds__(64 * kWindowWaves, D == 64 ? 3 : 2) void window_attn_kernel(WindowArgs a, Plan p) {
   using S = WindowShape<D>;
   constexpr int NW = S::NW;
   constexpr bool BR = __is_same(Plan, WindowPlanBr);
@@ -103,13 +104,12 @@ __global__ __launch_bounds__(64 * kWindowWaves, 2) void window_attn_kernel(Windo
   const int head_pages = span.head / kPageSize, gap_pages = span.gap / kPageSize;
   const int my_page = wave * 64 / UNITS, w = tid % UNITS;
   const size_t head_bytes = UNITS * 16, page_bytes = a.hkv * head_bytes;
-  const uint8_t* kbase = a.k_cache + (size_t)hk * head_bytes + 16 * w;
-  const uint8_t* vbase = a.v_cache + (size_t)hk * head_bytes + 16 * w;
-  // Places of unit w in a page's K and V in LDS; the first key of V's unit.
-  const int kslot = w / NCH, vd = w / 2, vhalf = w & 1, vkey = 8 * vhalf;
-  const int kat = kslot * 2 * D + 16 * ((w % NCH) ^ (swap23(kslot) & (NCH - 1))), vat = vd * 32 + 16 * (vhalf ^ vswz(vd));
-  u32x4 kreg[PER], vreg[PER];  // the buffer in flight
-  int pg[PER];                 // pages of the one after it
+  // Unit w of a page in LDS is unit w of its memory but for the order in a row of K and
+  // of V's pairs; the first key of V's unit.
+  const int kslot = w / NCH, vd = w / 2, vhalf = (w & 1) ^ vswz(vd), vkey = 8 * vhalf;
+  const uint8_t* kbase = a.k_cache + (size_t)hk * head_bytes + 16 * (w ^ (swap23(kslot) & (NCH - 1)));
+  const uint8_t* vbase = a.v_cache + (size_t)hk * head_bytes + 16 * (2 * vd + vhalf);
+  int pg[PER];  // pages of the next buffer to be loaded
   // Pages of this wave's units of buffer s; past the run's last page that page again.
   auto pages_of = [&](int s) {
 #pragma unroll
@@ -118,37 +118,40 @@ __global__ __launch_bounds__(64 * kWindowWaves, 2) void window_attn_kernel(Windo
       pg[e] = pages[at < head_pages ? at : at + gap_pages];
     }
   };
-  auto load = [&]() {
+  // Straight into LDS: a wave's 64 units of 16 bytes lie behind one another there.
+  static_assert(4 * S::BUF <= 65536, "load_to_lds reaches 64 KiB");
+  const uint32_t at0 = lds_place(lds) + my_page * PAGE_LDS + (wave * 64 % UNITS) * 16;
+  auto load = [&](int s) {
+    const uint32_t at = at0 + (s & 1) * S::BUF;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) kreg[e] = *(const u32x4*)(kbase + (size_t)pg[e] * page_bytes);
+    for (int e = 0; e < PER; ++e) load_to_lds(at + e * STEP * PAGE_LDS, kbase + (size_t)pg[e] * page_bytes);
 #pragma unroll
-    for (int e = 0; e < PER; ++e) vreg[e] = *(const u32x4*)(vbase + (size_t)pg[e] * page_bytes);
+    for (int e = 0; e < PER; ++e) load_to_lds(at + 2 * S::BUF + e * STEP * PAGE_LDS, vbase + (size_t)pg[e] * page_bytes);
   };
-  auto store = [&](int s) {
-    char* kd = lds + (s & 1) * S::BUF + my_page * PAGE_LDS + kat;
-    char* vd = lds + (2 + (s & 1)) * S::BUF + my_page * PAGE_LDS + vat;
+  // Waits for buffer s; V of slots behind the last key, and of those between the sinks
+  // and every window, becomes zero.
+  auto arrive = [&](int s) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const int k0 = kbeg + s * S::KEYS;
-    // V of slots behind the last key, and of those between the sinks and every window, is zero
-    const bool edge = k0 + S::KEYS > kend || (k0 < span.lo && k0 + S::KEYS > a.sink);
+    if (k0 + S::KEYS > kend || (k0 < span.lo && k0 + S::KEYS > a.sink)) {
+      char* vto = lds + (2 + (s & 1)) * S::BUF + my_page * PAGE_LDS + 16 * w;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      u32x4 v = vreg[e];
-      if (edge) {
+      for (int e = 0; e < PER; ++e) {
+        u32x4 v = *(const u32x4*)(vto + e * STEP * PAGE_LDS);
         const int key = k0 + (my_page + e * STEP) * kPageSize + vkey;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           auto seen = [&](int k) { return k < kend && (k < a.sink || k >= span.lo); };
           v[i] &= (seen(key + 2 * i) ? 0xffffu : 0u) | (seen(key + 2 * i + 1) ? 0xffff0000u : 0u);
         }
+        *(u32x4*)(vto + e * STEP * PAGE_LDS) = v;
       }
-      *(u32x4*)(kd + e * STEP * PAGE_LDS) = kreg[e];
-      *(u32x4*)(vd + e * STEP * PAGE_LDS) = v;
     }
   };
   const int nbuf = kend > kbeg ? (kend - kbeg + S::KEYS - 1) / S::KEYS : 0;
   if (nbuf > 0) {
     pages_of(0);
-    load();
+    load(0);
     if (nbuf > 1) pages_of(1);
   }
 
@@ -204,11 +207,19 @@ __global__ __launch_bounds__(64 * kWindowWaves, 2) void window_attn_kernel(Windo
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks) kf[ks] = *(const bf16x8*)(kt + krow + ((ks ^ kw) << 5));
       for (int i = 0; i < 16; ++i) sc[i] = 0.f;
-      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], sc, 0, 0, 0);
     }
-    __builtin_amdgcn_s_setprio(0);
+    // V's fragments are on their way during the softmax
+    bf16x8 vf[2][DT];
+#pragma unroll
+    for (int pp = 0; pp < 2; ++pp)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const int d = 32 * dt + lc;
+        vf[pp][dt] = *(const bf16x8*)(vt + pp * PAGE_LDS + d * 32 + ((lh ^ vswz(d)) * 16));
+      }
+    __builtin_amdgcn_sched_barrier(0);
     // key - kbase = 8 lh + place, place a constant of i
     if (kbase + 32 > min_lim) {
       const int seen = lim - kbase - 8 * lh, from = slo - kbase - 8 * lh, to = shi - kbase - 8 * lh;
@@ -267,20 +278,11 @@ __global__ __launch_bounds__(64 * kWindowWaves, 2) void window_attn_kernel(Windo
     }
     l_run += sum;
     r_run += rsum;
-    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int pp = 0; pp < 2; ++pp) {
-      bf16x8 vf[DT];
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const int d = 32 * dt + lc;
-        vf[dt] = *(const bf16x8*)(vt + pp * PAGE_LDS + d * 32 + ((lh ^ vswz(d)) * 16));
-      }
+    for (int pp = 0; pp < 2; ++pp)
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
-        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[dt], __builtin_bit_cast(bf16x8, pk[pp]), acc[dt], 0, 0, 0);
-    }
-    __builtin_amdgcn_s_setprio(0);
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[pp][dt], __builtin_bit_cast(bf16x8, pk[pp]), acc[dt], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);  // the next sub-tile's loads stay after this one's products
   };
   auto compute = [&](int s) {
@@ -299,12 +301,12 @@ __global__ __launch_bounds__(64 * kWindowWaves, 2) void window_attn_kernel(Windo
   // ---- keys
 #pragma unroll 1
   for (int s = 0; s < nbuf; ++s) {
-    store(s);  // LDS of buffer s - 2: every wave was done with it before barrier s - 1
-    if (s + 1 < nbuf) {
-      load();
+    arrive(s);
+    lds_barrier();
+    if (s + 1 < nbuf) {  // into LDS of buffer s - 1, with which every wave was done before the barrier
+      load(s + 1);
       if (s + 2 < nbuf) pages_of(s + 2);
     }
-    lds_barrier();
     compute(s);
   }
 

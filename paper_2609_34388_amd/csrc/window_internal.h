@@ -48,9 +48,12 @@ hipError_t launch_kv8_read(const Kv8ReadArgs& a, const AttnPlan& p, int head_dim
 // pages and those from the first row's window on, counted without the gap between
 // them.  They are cut into runs, alike for all groups of a request; runs past a
 // group's keys are empty.
-constexpr int kWindowWaves = 4;  // waves of a work group; two work groups share a compute unit
-// Keys a buffer of a work group holds.
-__host__ __device__ constexpr int window_keys(int head_dim) { return 16 * kWindowWaves * (128 / head_dim); }
+constexpr int kWindowWaves = 4;  // waves of a work group; two (D = 128) or three share a compute unit
+// Keys a buffer of a work group holds: two of K and two of V leave room for two work
+// groups of D = 128 in a compute unit, three of D = 64 (15 prompts of 555 rows over 3806
+// keys 216 us; with buffers of 128 and two work groups 250, of 64 the same 216, but 100
+// tokens over 500 keys 21 us against 17).
+__host__ __device__ constexpr int window_keys(int head_dim) { return head_dim == 64 ? 96 : 64; }
 constexpr int kWindowMergeWaves = 4;  // waves of a work group of the merge
 constexpr int kWindowMergeRows = 2;   // rows of one
 struct WindowReq {
