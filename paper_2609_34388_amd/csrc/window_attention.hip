@@ -21,11 +21,12 @@
 // weights add up to one.  Runs of a request's keys meet in fp32 in the workspace.
 //
 // Tokens are bound by the bytes: 64 requests of one, 4096 keys each of 8 heads of 128,
-// 1.07 GB in 185 us (5.8 TB/s).  Prompts: 13193 rows over windows of 1024 231 us (720
-// TFLOP/s), 8192 rows over all keys 590 (930): products and the softmax of two waves
+// 1.07 GB in 185 us (5.8 TB/s).  Prompts: 13193 rows over windows of 1024 224 us (740
+// TFLOP/s), 8192 rows over all keys 580 (950): products and the softmax of two waves
 // overlap in part, and the rest waits for LDS, barriers, starts and ends of groups.  Keys
-// through registers into LDS took 236 and 612, and V's fragments read after the softmax,
-// with a wave's priority raised for the products, 242 and 629; K's fragments read a
+// through registers into LDS took 236 and 612, V's fragments read after the softmax,
+// with a wave's priority raised for the products, 242 and 629 then, scalar loads of the
+// page numbers and waits for Q in the loop 228 and 588; K's fragments read a
 // sub-tile ahead were 4 % slower, eight waves a group 2 % faster here and up to 50 %
 // slower in steps, two sub-tiles at once do not fit the registers.
 #include "attention_device.h"
@@ -97,9 +98,8 @@ __global__ __launch_bounds__(64 * kWindowWaves, D == 64 ? 3 : 2) void window_att
   const int tok = row_of(a, col), hh = col - tok * g;
 
   // ---- copies
-  typedef const int32_t __attribute__((address_space(4))) * cpage_ptr;
-  typedef const float __attribute__((address_space(4))) * cscale_ptr;
-  const cpage_ptr pages = (cpage_ptr)(a.page_indices + rq.page_start);
+  // By vector loads: waits for LDS would wait for scalar ones too.
+  const int32_t* pages = a.page_indices + rq.page_start;
   const int page0 = kbeg / kPageSize, last_page = max((kend - 1) / kPageSize, 0);
   const int head_pages = span.head / kPageSize, gap_pages = span.gap / kPageSize;
   const int my_page = wave * 64 / UNITS, w = tid % UNITS;
@@ -131,7 +131,10 @@ __global__ __launch_bounds__(64 * kWindowWaves, D == 64 ? 3 : 2) void window_att
   // Waits for buffer s; V of slots behind the last key, and of those between the sinks
   // and every window, becomes zero.
   auto arrive = [&](int s) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // vmcnt(0), as the compiler understands it: else it waits for Q's loads, and with
+    // them for the buffer in flight, at every product
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    asm volatile("" ::: "memory");
     const int k0 = kbeg + s * S::KEYS;
     if (k0 + S::KEYS > kend || (k0 < span.lo && k0 + S::KEYS > a.sink)) {
       char* vto = lds + (2 + (s & 1)) * S::BUF + my_page * PAGE_LDS + 16 * w;
@@ -207,6 +210,7 @@ __global__ __launch_bounds__(64 * kWindowWaves, D == 64 ? 3 : 2) void window_att
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks) kf[ks] = *(const bf16x8*)(kt + krow + ((ks ^ kw) << 5));
       for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+      __builtin_amdgcn_sched_barrier(0);  // all reads before the products
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], sc, 0, 0, 0);
     }
