@@ -96,7 +96,7 @@
 extern "C" {
 #endif
 
-#define RG_ABI_VERSION 8
+#define RG_ABI_VERSION 9
 
 typedef int32_t rg_status;
 #define RG_OK 0
