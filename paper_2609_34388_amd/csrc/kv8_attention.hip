@@ -206,22 +206,18 @@ __device__ __forceinline__ void kv8_wave(const WindowArgs& a, const Req& rq, con
     const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
 #pragma unroll
     for (int u = 0; u < TILES; ++u) {
-      // key - kbase = 8 lh + place, place a constant of i
-      if (kbase + 32 > min_lim) {
-        const int seen = lim[u] - kbase - 8 * lh, from = slo[u] - kbase - 8 * lh, to = shi[u] - kbase - 8 * lh;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int place = 16 * (i >> 3) + 4 * ((i >> 2) & 1) + (i & 3);
-          if (place >= seen && (!BR || place < from || place >= to)) sc[u][i] = kNegInf;
+      // Keys behind a column's limits, and those before its window.
+      const bool behind = kbase + 32 > min_lim, before = kbase < max_lo && kbase + 32 > a.sink;
+      if (behind || before) {
+        const int base = kbase + 8 * lh;
+        uint32_t hidden = 0;
+        if (behind) {
+          uint32_t seen = places_below(lim[u] - base);
+          if constexpr (BR) seen |= places_below(shi[u] - base) & ~places_below(slo[u] - base);
+          hidden = ~seen;
         }
-      }
-      if (kbase < max_lo && kbase + 32 > a.sink) {
-        const int hidden = a.sink - kbase - 8 * lh, seen = lo[u] - kbase - 8 * lh;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int place = 16 * (i >> 3) + 4 * ((i >> 2) & 1) + (i & 3);
-          if (place >= hidden && place < seen) sc[u][i] = kNegInf;
-        }
+        if (before) hidden |= places_below(lo[u] - base) & ~places_below(a.sink - base);
+        hide_places(sc[u], hidden);
       }
       // P against the running reference, a maximum of earlier scores.  A sum of a
       // lane's 16 past 2^12 (overflow included), or a column without a reference,

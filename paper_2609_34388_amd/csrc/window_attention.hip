@@ -224,22 +224,18 @@ __global__ __launch_bounds__(64 * kWindowWaves, D == 64 ? 3 : 2) void window_att
         vf[pp][dt] = *(const bf16x8*)(vt + pp * PAGE_LDS + d * 32 + ((lh ^ vswz(d)) * 16));
       }
     __builtin_amdgcn_sched_barrier(0);
-    // key - kbase = 8 lh + place, place a constant of i
-    if (kbase + 32 > min_lim) {
-      const int seen = lim - kbase - 8 * lh, from = slo - kbase - 8 * lh, to = shi - kbase - 8 * lh;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int place = 16 * (i >> 3) + 4 * ((i >> 2) & 1) + (i & 3);
-        if (place >= seen && (!BR || place < from || place >= to)) sc[i] = kNegInf;
+    // Keys behind a column's limits, and those before its window.
+    const bool behind = kbase + 32 > min_lim, before = kbase < max_lo && kbase + 32 > a.sink;
+    if (behind || before) {
+      const int base = kbase + 8 * lh;
+      uint32_t hidden = 0;
+      if (behind) {
+        uint32_t seen = places_below(lim - base);
+        if constexpr (BR) seen |= places_below(shi - base) & ~places_below(slo - base);
+        hidden = ~seen;
       }
-    }
-    if (kbase < max_lo && kbase + 32 > a.sink) {
-      const int hidden = a.sink - kbase - 8 * lh, seen = lo - kbase - 8 * lh;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int place = 16 * (i >> 3) + 4 * ((i >> 2) & 1) + (i & 3);
-        if (place >= hidden && place < seen) sc[i] = kNegInf;
-      }
+      if (before) hidden |= places_below(lo - base) & ~places_below(a.sink - base);
+      hide_places(sc, hidden);
     }
     // P against the running reference, a maximum of earlier scores.  A sum of a
     // lane's 16 past 2^12 (overflow included), or a column without a reference,

@@ -114,6 +114,21 @@ __host__ __device__ inline WindowSpan window_span(int L, int V, int n, int i0, i
   s.keys = end - s.gap;
   return s;
 }
+#ifdef __HIPCC__
+// Scores of a 32 x 32 tile: value i of a lane is key 8 lh + place_of(i) of the tile.  A mask
+// is made as bits of the lane's places, and a score hidden in two instructions, without
+// branches or condition registers.
+__device__ __forceinline__ constexpr int place_of(int i) { return 16 * (i >> 3) + 4 * ((i >> 2) & 1) + (i & 3); }
+__device__ __forceinline__ uint32_t places_below(int x) { return (1u << min(max(x, 0), 24)) - 1; }
+template <typename Scores>
+__device__ __forceinline__ void hide_places(Scores& sc, uint32_t hidden) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t all = (uint32_t)__builtin_amdgcn_sbfe((int)hidden, place_of(i), 1);
+    sc[i] = __uint_as_float((all & 0xff800000u) | (~all & __float_as_uint(sc[i])));  // minus infinity
+  }
+}
+#endif
 hipError_t launch_window_attention(const WindowArgs& a, const WindowPlan& p, int head_dim, hipStream_t stream);
 hipError_t launch_window_attention(const WindowArgs& a, const WindowPlanBr& p, int head_dim, hipStream_t stream);
 
