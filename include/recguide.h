@@ -779,8 +779,8 @@ typedef struct rg_window {
  * rg_draft_verify_attention (branches NULL) or rg_multibranch_attention over a
  * window: layout, branches, q, caches, out and lse as there.  The workspace
  * needs no initialisation.  Slots that no row sees may hold anything.
- * RG_ERR_WORKSPACE also where the host has no memory for the plan, and
- * RG_ERR_UNSUPPORTED for a request of 2^30 rows and query heads of a KV head, and more.
+ * RG_ERR_WORKSPACE also where the host has no memory for the plan.  A request's
+ * rows times the query heads of a KV head stay below 2^30 (RG_ERR_UNSUPPORTED).
  */
 rg_status rg_window_attention_workspace(const rg_attn_layout* layout, const rg_branch_layout* branches,
                                         const rg_window* window, size_t* bytes);
