@@ -127,33 +127,40 @@ constexpr int64_t kLongRound = 8000;
 // 64 whole 15.9 us, split to fill the chip 21.1; in 8 bits 11.5 and 16.7.
 constexpr int64_t kMerge = 450;
 // How a kernel takes a batch: column groups of up to `group` tiles, dealt evenly or
-// full but for the last; steps of `keys` keys; work groups that run at once; the
-// time of a step of so many tiles, of an item's start and end, and of the partials
-// of a split, in hundredths of a microsecond.  Measured with every compute unit full: 128
-// keys of D = 128 in 8 bits 1.36, 1.45, 2.34, 2.34 us for 1 to 4 tiles, a step in bf16
-// 2.75, 2.79 and 3.27 for 1, 2 and 4; the 8-bit constants are near those and the best of
-// a sweep over batches of all sizes, where work groups seldom start together.
+// full but for the last; steps of `keys` keys; work groups that run at once; the time of
+// a step of so many tiles, of an item's start and end, and of its partials where it is one
+// of several runs, a part for each and one for each 32 columns of D = 128, in hundredths
+// of a microsecond; and the least that a step takes where few items run, which share bytes
+// and SIMDs with fewer, in percent.
+//
+// Measured with every compute unit full: 128 keys of D = 128 in 8 bits 1.36, 1.45, 2.34,
+// 2.34 us for 1 to 4 tiles, a step in bf16 2.75, 2.79 and 3.27 for 1, 2 and 4; the 8-bit
+// constants are near those and the best of a sweep over batches of all sizes, where work
+// groups seldom start together.  Partials: 90 requests of 5 to 45 rows over 2945 keys 247
+// us; with 2 us for them in all, and so split, 286.  Few items: 48 requests of 4 to 61 rows
+// over 701 keys (D = 64, 8 bits) whole in half of the places 22.1 us, split to fill them,
+// as with 90 or 100 percent, 27.5; with 60 a longer batch takes 102 us against 83.
 struct Shape {
   int group, keys, per_cu;
   bool even;
   int64_t (*step)(int64_t tiles);
-  int64_t start, parts, least;
+  int64_t start, parts, part_tile, least, alone;
 };
 Shape kv8_shape(int head_dim) {
   return {kKv8Waves, kKv8Step, head_dim == 64 ? 3 : 2, false, [](int64_t tiles) -> int64_t {
             constexpr int64_t t[] = {0, 6, 9, 16, 16};
             return 16 * t[tiles];
-          }, 600, 600, 128};
+          }, 600, 300, 100, 128, 80};
 }
 Shape bf16_shape(int head_dim) {
   return {kWindowWaves, window_keys(head_dim), head_dim == 64 ? 3 : 2, true, [](int64_t tiles) { return std::max<int64_t>(270, 130 + 47 * tiles); },
-          600, 200, 270};
+          600, 200, 200, 270, 60};
 }
 
-// A request's column groups and the steps of the longest.
+// A request's column groups.
 struct Groups {
   int64_t count = 0, tiles = 0, per = 0;  // groups, tiles in all, tiles of a group at most
-  int64_t steps = 0;
+  int64_t steps = 0, cols = 0;            // of the longest, and columns of a group at most
 };
 template <bool BR>
 Groups groups_of(const rg_attn_layout* L, int r, Limits w, const Shape& shape, int g) {
@@ -177,6 +184,7 @@ Groups groups_of(const rg_attn_layout* L, int r, Limits w, const Shape& shape, i
     }
   }
   q.steps = (keys + shape.keys - 1) / shape.keys;
+  q.cols = std::min<int64_t>((int64_t)n * g, q.per * 32);
   return q;
 }
 
@@ -197,9 +205,9 @@ rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits
     const uint32_t n = (steps + most - 1) / most, each = (steps + n - 1) / n;  // steps of a run
     return (int64_t)((steps + each - 1) / each);
   };
-  // Cost of an item at most: the least that gives one round of items, or no split where
-  // that ends no later, or where a round is long (kLongRound) as many as promise the
-  // earliest end: a long round ends unevenly, an item's start and its partials cost.
+  // Cost of an item at most: of no split, of one round of items or 0.7 of one, and
+  // where a round is long (kLongRound) of more, what promises the earliest end: a long
+  // round ends unevenly, an item's start, its partials and their merge cost.
   struct Load {
     Groups q;
     int64_t items;  // whole
@@ -211,50 +219,53 @@ rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits
     work += q.count * hkv * q.steps * shape.step(q.per);
     whole += q.count * hkv;
     whole_cost = std::max(whole_cost, q.steps * shape.step(q.per));
-    auto same = std::find_if(loads.begin(), loads.end(), [&](const Load& x) { return x.q.steps == q.steps && x.q.per == q.per; });
+    auto same = std::find_if(loads.begin(), loads.end(), [&](const Load& x) { return x.q.steps == q.steps && x.q.cols == q.cols; });
     if (same == loads.end()) loads.push_back({q, q.count * hkv});
     else same->items += q.count * hkv;
   }
-  const int64_t slots = (int64_t)cus * shape.per_cu;
+  // Places of all launches, which run one after the other.
+  const int64_t slots = (int64_t)cus * shape.per_cu * std::max(R, MaxReq) / MaxReq;
   auto items_of = [&](int64_t target) {
     int64_t items = 0;
     for (const Load& x : loads) items += x.items * runs_of(x.q, target);
     return items;
   };
-  auto fit = [&](int64_t rounds) {  // to 3 %
-    if (whole >= rounds * slots) return whole_cost;
-    int64_t lo = std::max<int64_t>(shape.least, work / (rounds * slots)), hi = std::max(lo, whole_cost);
-    if (items_of(lo) <= rounds * slots) return lo;
+  auto fit = [&](int64_t room) {  // the least for so many items, to 3 %
+    if (whole >= room) return whole_cost;
+    int64_t lo = std::max<int64_t>(shape.least, work / room), hi = std::max(lo, whole_cost);
+    if (items_of(lo) <= room) return lo;
     while (hi - lo > 1 + lo / 32) {
       const int64_t mid = (lo + hi) / 2;
-      if (items_of(mid) <= rounds * slots) hi = mid;
+      if (items_of(mid) <= room) hi = mid;
       else lo = mid;
     }
     return hi;
   };
   auto time_of = [&](int64_t target) {
-    int64_t items = 0, longest = 0, total = 0;
+    const int64_t items = items_of(target), share = std::min<int64_t>(100, std::max(shape.alone, 100 * items / slots));
+    int64_t longest = 0, total = 0;
     for (const Load& x : loads) {
-      const int64_t n = runs_of(x.q, target);
-      const int64_t each = (x.q.steps + n - 1) / n * shape.step(x.q.per) + shape.start + (n > 1 ? shape.parts : 0);
-      items += x.items * n;
+      const int64_t n = runs_of(x.q, target), steps = (x.q.steps + n - 1) / n;
+      int64_t each = steps * shape.step(x.q.per) * share / 100 + shape.start;
+      if (n > 1) each += shape.parts + shape.part_tile * x.q.cols * L->head_dim / (32 * 128);
       total += x.items * n * each;
       longest = std::max(longest, each);
     }
     return (items <= slots ? longest : std::max(longest, total / slots + total / items / 2)) + (items > whole ? kMerge : 0);
   };
-  int64_t target = fit(1);
-  if (time_of(whole_cost) <= time_of(target)) target = whole_cost;
-  if (target > kLongRound) {
-    int64_t best = time_of(target);
-    for (int64_t rounds = 2; rounds <= 4; ++rounds) {
-      const int64_t t = fit(rounds), time = time_of(t);
-      if (time < best) {
-        target = t;
-        best = time;
-      }
+  int64_t target = whole_cost, best = time_of(target);
+  auto consider = [&](int64_t t) {
+    const int64_t time = time_of(t);
+    if (time < best) {
+      target = t;
+      best = time;
     }
-  }
+  };
+  const int64_t one_round = fit(slots);
+  consider(one_round);
+  if (whole < slots) consider(fit(slots * 7 / 10));
+  if (one_round > kLongRound)
+    for (int64_t rounds = 2; rounds <= 4; ++rounds) consider(fit(rounds * slots));
   // Costliest work items first.
   std::vector<int> order(R);
   std::iota(order.begin(), order.end(), 0);
