@@ -123,9 +123,11 @@ rg_status validate_window(const rg_window* W) {
 // take 718, 566 and 568 us; rounds of less than 80 us are best left one (102, 110, 122;
 // 34, 42, 48), and among longer ones those that fill it evenly (184, 195, 198).
 constexpr int64_t kLongRound = 8000;
-// A merge's launch: not for what a split saves below that.  100 tokens over 500 keys of D =
-// 64 whole 15.9 us, split to fill the chip 21.1; in 8 bits 11.5 and 16.7.
-constexpr int64_t kMerge = 450;
+// A merge's launch, and what it takes for each run: not for what a split saves below that.
+// 100 tokens over 500 keys of D = 64 whole 15.9 us, split to fill the chip 21.1; in 8 bits
+// 11.5 and 16.7.  5 requests of 17 to 29 rows over 600 to 4900 keys (D = 64, 8 bits) in 608
+// items of one step 24.7, in half as many 21.6.
+constexpr int64_t kMerge = 450, kMergeRun = 16;
 // How a kernel takes a batch: column groups of up to `group` tiles, dealt evenly or
 // full but for the last; steps of `keys` keys; work groups that run at once; the time of
 // a step of so many tiles, of an item's start and end, and of its partials where it is one
@@ -243,15 +245,17 @@ rg_status plan_window(const rg_attn_layout* L, const rg_branch_layout* B, Limits
   };
   auto time_of = [&](int64_t target) {
     const int64_t items = items_of(target), share = std::min<int64_t>(100, std::max(shape.alone, 100 * items / slots));
-    int64_t longest = 0, total = 0;
+    int64_t longest = 0, total = 0, most_runs = 0;
     for (const Load& x : loads) {
       const int64_t n = runs_of(x.q, target), steps = (x.q.steps + n - 1) / n;
       int64_t each = steps * shape.step(x.q.per) * share / 100 + shape.start;
       if (n > 1) each += shape.parts + shape.part_tile * x.q.cols * L->head_dim / (32 * 128);
       total += x.items * n * each;
       longest = std::max(longest, each);
+      most_runs = std::max(most_runs, n);
     }
-    return (items <= slots ? longest : std::max(longest, total / slots + total / items / 2)) + (items > whole ? kMerge : 0);
+    const int64_t end = items <= slots ? longest : std::max(longest, total / slots + total / items / 2);
+    return end + (items > whole ? kMerge + kMergeRun * most_runs : 0);
   };
   int64_t target = whole_cost, best = time_of(target);
   auto consider = [&](int64_t t) {
