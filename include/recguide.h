@@ -672,7 +672,8 @@ rg_status rg_kv4_evict_tokens(const rg_evict_layout* layout, uint8_t* cache, con
  * (2 j, 2 j + 1).
  *
  *   dims       0 .. D, a multiple of 16 (0: nothing turns)
- *   inv_freq   DEVICE [dims / 2] fp32 (may be NULL where dims is 0)
+ *   inv_freq   DEVICE [dims / 2] fp32 (may be NULL where dims is 0), their angles
+ *              below 2^40
  *   positions  DEVICE [q_indptr[R]] int32, 0 .. 2^31 - 1, of every row, or NULL:
  *              ctx_len[r] + i for row i of request r.  With branches, and where
  *              tokens were evicted, a row's position is not its slot.

@@ -4,7 +4,7 @@ of the library is used."""
 from __future__ import annotations
 
 import math
-from typing import Optional
+from typing import Optional, Tuple
 
 import numpy as np
 
@@ -16,7 +16,8 @@ GRID = np.concatenate([GRID, -GRID])
 
 
 def rotate(x: np.ndarray, position: np.ndarray, inv_freq: np.ndarray, interleaved: bool) -> np.ndarray:
-    """Rows x [rows, heads, D] turned by their positions."""
+    """Rows x [rows, heads, D] turned by their positions.  The angle is the product
+    in 64 bits: exact for fp32 frequencies and positions below 2^29."""
     y = x.copy()
     half = len(inv_freq)
     for j in range(half):
@@ -25,6 +26,14 @@ def rotate(x: np.ndarray, position: np.ndarray, inv_freq: np.ndarray, interleave
         y[..., a] = x[..., a] * np.cos(w) - x[..., b] * np.sin(w)
         y[..., b] = x[..., b] * np.cos(w) + x[..., a] * np.sin(w)
     return y
+
+
+def turns(position: np.ndarray, inv_freq: np.ndarray) -> Tuple[np.ndarray, np.ndarray]:
+    """Cosine and sine [rows, dims / 2] of the exact angles of fp32 frequencies, in
+    80 bits: a position below 2^31 times 24 bits needs 55, of which 64 bits hold 53."""
+    assert inv_freq.dtype == np.float32 and np.finfo(np.longdouble).nmant >= 63
+    w = position.astype(np.longdouble)[:, None] * inv_freq.astype(np.longdouble)
+    return np.cos(w), np.sin(w)
 
 
 def exponent(top: float) -> int:

@@ -3,9 +3,9 @@
 //
 // A row of position p turns the pairs (x, y) of its first dims to (x c - y s,
 // y c + x s), c and s the cosine and sine of p inv_freq.  The angle is the exact
-// product in 64 bits, reduced by multiples of pi / 2 there, so that a far position
-// turns as exactly as a near one; c and s are rounded to fp32 once.  A work group
-// makes the angles of a page's 16 rows once for all of its heads.
+// product, up to 55 bits as the sum of two doubles, reduced by multiples of pi / 2
+// there, so that a far position turns as exactly as a near one; c and s are rounded to
+// fp32 once.  A work group makes the angles of a page's 16 rows once for all of its heads.
 //
 // 8-bit blocks: the largest magnitude of the new rows of a (page, head) gives
 // the block's scale, the one it has is kept where that is larger and older tokens
@@ -28,13 +28,15 @@
 namespace rg {
 namespace {
 
-// Sine and cosine of an angle (to about 2^50 in magnitude), each to about 1e-14 of
-// one: with k = round(x 2 / pi) the remainder is x - k pi / 2, pi / 2 as the sum
-// of two doubles (the first product and difference in one rounding), and Taylor's
-// series on [-pi / 4, pi / 4] end below 3e-14 (r^15 / 15!) and 2e-15 (r^16 / 16!).
-__device__ __forceinline__ float2 turn_of(double x) {
+// Sine and cosine of the angle position x freq (to about 2^40 in magnitude), each to
+// about 1e-14 of one.  The product is x + rest: a position has 31 bits and a frequency
+// 24, a double 53.  With k = round(x 2 / pi) the remainder is x + rest - k pi / 2, pi / 2
+// as the sum of two doubles (the first product and difference in one rounding), and
+// Taylor's series on [-pi / 4, pi / 4] end below 3e-14 (r^15 / 15!) and 2e-15 (r^16 / 16!).
+__device__ __forceinline__ float2 turn_of(double position, double freq) {
+  const double x = position * freq, rest = __builtin_fma(position, freq, -x);
   const double k = __builtin_rint(x * 0.63661977236758134308);
-  double r = __builtin_fma(-k, 1.57079632679489655800, x);
+  double r = __builtin_fma(-k, 1.57079632679489655800, x) + rest;
   r = __builtin_fma(-k, 6.12323399573676603587e-17, r);
   const double z = r * r;
   double s = 1. / 6227020800.;
@@ -153,7 +155,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, At
       const double freq = a.inv_freq[j];
       for (int slot = it.s0 + first; slot < it.s1; slot += apart) {
         const int at = a.positions ? a.positions[it.row0 + slot] : it.first_position + slot;
-        angle[slot * HALF + j] = turn_of((double)at * freq);
+        angle[slot * HALF + j] = turn_of((double)at, freq);
       }
     }
   }
