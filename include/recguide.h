@@ -734,6 +734,9 @@ rg_status rg_kv_append(const rg_attn_layout* layout, const rg_rotation* rotation
  * magnitudes past 448 become 448, an infinity or a NaN becomes NaN, and no other
  * element changes for it.  Attention over a NaN comes out as NaN, from K in the
  * rows that see the token, from V in any of the request's.
+ *
+ * Rows go in and out and attention runs over this cache; attention mass and
+ * eviction are calls of the bf16 and the 4-bit cache.
  */
 #define RG_KV8_BLOCK_BYTES(head_dim) (32 * (head_dim))
 
