@@ -19,9 +19,11 @@
 //
 // Prompts are bound by their bytes: 36862 rows of 32 + 2 x 8 heads of 128, 906 MB
 // read and written, in 168 us (5.4 TB/s; a copy reaches 5.2).  Steps are bound by their
-// one chain of angles, rows, LDS and stores and by the launch: 128 requests of 4 to 32
-// rows, 34 MB, 11.8 us, of which a launch that does nothing is 10 and the angles 2.  In 8
-// bits vector instructions come to that: 21897 rows of 16 + 2 x 4 heads of 64 36 us.
+// one chain of page number, angles, rows, LDS and stores, not by the launch: 128 requests
+// of 4 to 32 rows, 34 MB, 11.7 us in a captured graph, where an empty kernel of the same
+// grid takes 1.8; vector instructions, the angles of every work group among them, fill
+// 63 % of the cycles of a compute unit with work.  In 8 bits they come to that for prompts
+// too (68 %): 33194 rows of 16 + 2 x 4 heads of 64 38 us.
 #include "kv8_device.h"
 #include "window_internal.h"
 
@@ -300,7 +302,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendArgs a, At
 // Rows out of the 8-bit cache: an item is a page's kv8_read_heads heads, a thread 16
 // elements of a row.  Bound by the bytes, and by the launch where they are few.  Few
 // heads an item, not a page's all: append and read of 32768 rows (8 heads of 128, with
-// 32 of q) 183 us against 194 with 2 heads, 200 with 4 or 8; 21897 rows of 4 heads of
+// 32 of q) 183 us against 194 with 2 heads, 200 with 4 or 8; 33194 rows of 4 heads of
 // 64 55, 53.5 and 58 us with 1, 2 and 4.
 template <int D>
 __global__ __launch_bounds__(kAppendThreads) void kv8_read_kernel(Kv8ReadArgs a, AttnPlan p) {
