@@ -17,9 +17,10 @@
 // its keys: 238 us where this takes 199, 127 for 97 and 638 for 565.)
 //
 // Tokens are bound by the bytes: 128 requests of one over 512 to 8192 keys, 8 KV
-// heads of 128, 1.15 GB in 199 us (5.8 TB/s).  Many rows are bound by what a SIMD
-// issues: 40 requests of 8 to 64 rows over 8192 to 32768 keys 546 us (720 TFLOP/s),
-// vector instructions 52 % and products 41 % of the cycles, 8 of the former a product.
+// heads of 128, 1.15 GB in 199 us (5.8 TB/s).  Many rows are bound by what a SIMD's two
+// waves issue, and by the clock under the power limit: 40 requests of 8 to 64 rows over
+// 8192 to 32768 keys 546 us (720 TFLOP/s) at 2.0 GHz, a wave at work 46 % of its time,
+// waiting to issue 34 % and for data 20 %; 8 vector instructions a product.
 //
 // The dims go through the products in another order than in memory: K step s of S^T
 // holds dims 32 (s / 2) + 16 lh + 8 (s % 2) .. + 7 of half-wave lh (Q is read alike),
