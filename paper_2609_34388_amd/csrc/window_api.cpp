@@ -87,7 +87,7 @@ rg_status run_append(const rg_attn_layout* L, const rg_rotation* R, const uint16
   // Heads of q in an item, whose rows at 4 of D = 128 or 8 of D = 64 weigh what those of
   // its KV heads do.  At D = 128 eight in few pages, where angles and starts count, and in
   // 8 bits (us with 4, 8 and 16 heads of 32: 128 requests' steps 12.6, 11.7, 13.2, 256
-  // pages of a prompt 20.5, 18.7, 18.6, 512 pages 40.7, 42.8, 46.4, 2304 168, 172, 180; in
+  // pages of a prompt 20.5, 18.7, 18.6, 512 pages 40.7, 42.8, 46.4, 2307 168, 172, 180; in
   // 8 bits 64 steps 17.0, 16.9, 17.2, 2048 pages 173, 176, 184; D = 64 28.7, 29.2, 40.3, in
   // 8 bits 48.4, 47.3, 59.7).
   const bool many = touched_pages(L) >= 512;
@@ -135,12 +135,14 @@ constexpr int64_t kMerge = 450, kMergeRun = 16;
 // of a microsecond; and the least that a step takes where few items run, which share bytes
 // and SIMDs with fewer, in percent.
 //
-// Measured with every compute unit full: 128 keys of D = 128 in 8 bits 1.36, 1.45, 2.34,
-// 2.34 us for 1 to 4 tiles, a step in bf16 2.75, 2.79 and 3.27 for 1, 2 and 4; the 8-bit
-// constants are near those and the best of a sweep over batches of all sizes, where work
-// groups seldom start together.  Partials: 90 requests of 5 to 45 rows over 2945 keys 247
-// us; with 2 us for them in all, and so split, 286.  Few items: 48 requests of 4 to 61 rows
-// over 701 keys (D = 64, 8 bits) whole in half of the places 22.1 us, split to fill them,
+// A step of a work group with every place taken, for 1 to 4 tiles: in bf16 2.75, 2.77, 2.89
+// and 3.22 us, and of D = 64 (96 keys) 3.14, 3.28, 3.61 and 4.02; in 8 bits 2.78, 2.90,
+// 4.60 and 4.82, and of D = 64 2.11, 2.63, 4.38 and 4.49.  The constants do not know D: in
+// bf16 they are those of D = 128; in 8 bits they are fitted, a third to a half of what was
+// measured, the best of a sweep over batches of all sizes, where work groups seldom start
+// together.  Partials: 90 requests of 5 to 45 rows over 2945 keys 247
+// us; with 2 us for them in all, and so split, 286.  Few items: 48 requests of 8 to 63 rows
+// over 701 keys (D = 64, 8 bits) whole in a third of the places 22.1 us, split to fill them,
 // as with 90 or 100 percent, 27.5; with 60 a longer batch takes 102 us against 83.
 struct Shape {
   int group, keys, per_cu;

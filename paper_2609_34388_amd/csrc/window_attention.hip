@@ -21,8 +21,8 @@
 // weights add up to one.  Runs of a request's keys meet in fp32 in the workspace.
 //
 // Tokens are bound by the bytes: 64 requests of one, 4096 keys each of 8 heads of 128,
-// 1.07 GB in 185 us (5.8 TB/s).  Prompts: 13193 rows over windows of 1024 224 us (740
-// TFLOP/s), 8192 rows over all keys 580 (950): products and the softmax of two waves
+// 1.07 GB in 185 us (5.8 TB/s).  Prompts: 10002 rows over windows of 1024 225 us (740
+// TFLOP/s), 8192 rows over all keys 587 (936): products and the softmax of two waves
 // overlap in part, and the rest waits for LDS, barriers, starts and ends of groups.  Keys
 // through registers into LDS took 236 and 612, V's fragments read after the softmax,
 // with a wave's priority raised for the products, 242 and 629 then, scalar loads of the
